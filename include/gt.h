@@ -420,6 +420,150 @@ gt_status gt_dense_attn_bwd_noalloc(int64_t n, int32_t H, int32_t d, gt_dtype dt
                                     const void* V, const void* O, const void* dO, const float* LSE, float scale,
                                     void* dQ, void* dK, void* dV, hipStream_t stream);
 
+/* ------------------------------------------------------------------------ */
+/* Attention over packed sequences: the full layer of a batch of graphs.     */
+/* ------------------------------------------------------------------------ */
+/* gt_dense_attn_* mixes all n nodes; here the rows of Q and of K and V are a
+ * batch of sequences (the graphs of a batch, prompts, read-out tokens with the
+ * nodes that they read) and each attends to itself only.  Sequence s holds the
+ * queries q_ptr[s] .. q_ptr[s+1]-1 and the keys k_ptr[s] .. k_ptr[s+1]-1; with
+ * lq of the one and lk of the other, its query i attends to its keys j < lk,
+ * and if `causal` to j <= i + lk - lq only (the last query sees every key: new
+ * rows behind keys that were there before).  H query heads share Hkv heads of K
+ * and V: query head h reads kv head h / (H / Hkv).  For the pairs attended to,
+ *   s_ij = scale <Q[i,h], K[j,h']>, LSE_i = log sum_j exp(s_ij),
+ *   O_i = sum_j exp(s_ij - LSE_i) V[j,h'];
+ * a row without any gives O = 0 and LSE = -inf, and no gradient.
+ * Supported: d in {32, 64, 128}; H <= 256, H / Hkv in {1, 2, 4, 8, 16};
+ * GT_F32 (products, sums and softmax in fp32) and GT_BF16 (as above: scores,
+ * statistics and sums in fp32, the weights and score gradients rounded to bf16
+ * where they multiply a bf16 row).
+ * Q is [nq, H, d], K and V [nk, Hkv, d] with ldq, ldk, ldv elements between
+ * consecutive nodes (slices of one wider array, such as a fused projection);
+ * O, dO, dQ [nq, H, d], dK, dV [nk, Hkv, d], LSE [nq, H] fp32, all contiguous.
+ * Feature arrays start at multiples of 16 bytes and their nodes lie at such
+ * (GT_ERR_UNSUPPORTED otherwise).  Rows behind the last sequence are neither
+ * read nor written.  Features are finite: an infinity or NaN in a sequence may
+ * reach any row of that sequence, but never another sequence's.
+ *
+ * The plan (host only; like the tile plan it is built once per batch and kept
+ * for every layer, forward and backward): gt_packed_plan_init checks the
+ * sequences and sizes the work list, gt_packed_plan_fill writes it to a host
+ * buffer of item_bytes, which the caller copies to the device (16-byte aligned)
+ * and enters as plan->items.  q_ptr and k_ptr are host arrays int64[n_seq + 1],
+ * starting at 0 (GT_ERR_OUT_OF_RANGE) and not decreasing (GT_ERR_UNSORTED);
+ * q_ptr[n_seq] and k_ptr[n_seq] < 2^31.  Both calls take the same arguments. */
+typedef struct gt_packed_plan {
+    int64_t n_seq;
+    int64_t nq;          /* q_ptr[n_seq] */
+    int64_t nk;          /* k_ptr[n_seq] */
+    int64_t pair_bytes;  /* size of the bucket ids of the bias calls */
+    int64_t item_bytes;  /* size of `items` */
+    int32_t H, Hkv, causal, reserved;
+    int64_t layout[32];  /* the library's: where the lists in `items` lie */
+    const void* items;   /* device; the caller's copy of the work list */
+} gt_packed_plan;
+gt_status gt_packed_plan_init(int64_t n_seq, const int64_t* q_ptr, const int64_t* k_ptr, int32_t H, int32_t Hkv,
+                              int32_t causal, gt_packed_plan* plan);
+gt_status gt_packed_plan_fill(int64_t n_seq, const int64_t* q_ptr, const int64_t* k_ptr, const gt_packed_plan* plan,
+                              void* host_items, size_t bytes);
+
+size_t gt_packed_attn_fwd_workspace_size(const gt_packed_plan* plan, int32_t d, gt_dtype dtype);
+gt_status gt_packed_attn_fwd(const gt_packed_plan* plan, int32_t d, gt_dtype dtype, const void* Q, int64_t ldq,
+                             const void* K, int64_t ldk, const void* V, int64_t ldv, float scale, void* O, float* LSE,
+                             void* ws, size_t ws_bytes, hipStream_t stream);
+/* Backward from O and LSE of the forward, with the formulas of
+ * gt_dense_attn_bwd (D_i = <dO_i, O_i>); dK and dV sum over the query heads
+ * that share a kv head.  No atomics: results are the same run to run. */
+size_t gt_packed_attn_bwd_workspace_size(const gt_packed_plan* plan, int32_t d, gt_dtype dtype);
+gt_status gt_packed_attn_bwd(const gt_packed_plan* plan, int32_t d, gt_dtype dtype, const void* Q, int64_t ldq,
+                             const void* K, int64_t ldk, const void* V, int64_t ldv, const void* O, const void* dO,
+                             const float* LSE, float scale, void* dQ, void* dK, void* dV, void* ws, size_t ws_bytes,
+                             hipStream_t stream);
+
+/* With a learned bias by buckets (the structural encoding of §2.1 Eq. (3): a
+ * value for each bucketed distance between two nodes and each head),
+ *   s_ij = scale <Q[i,h], K[j,h']> + table[bucket_ij, h],
+ * and its gradient dtable[b, h] = the sum of dS_ij over the pairs in bucket b.
+ *   table, dtable fp32 [n_buckets, H], 1 <= n_buckets <= GT_MAX_BUCKETS
+ *     (GT_ERR_UNSUPPORTED above);
+ *   buckets uint8[plan->pair_bytes]: sequence after sequence, for each query a
+ *     row of lk bytes padded to a multiple of 16 (what the padding holds does
+ *     not matter); the array starts at a multiple of 16 bytes.
+ * A pair whose bucket is n_buckets or more is not attended to.  Table entries
+ * may be -inf (the same) or the type's lowest value (attended to with as little
+ * weight as that gives).  The backward forms D_i from the scores (dtable is
+ * fp32, and a bf16 O would be off by 2^-9), so O is not an input. */
+#define GT_MAX_BUCKETS 64
+size_t gt_packed_attn_fwd_bias_workspace_size(const gt_packed_plan* plan, int32_t d, gt_dtype dtype,
+                                              int32_t n_buckets);
+gt_status gt_packed_attn_fwd_bias(const gt_packed_plan* plan, int32_t d, gt_dtype dtype, const void* Q, int64_t ldq,
+                                  const void* K, int64_t ldk, const void* V, int64_t ldv, const float* table,
+                                  int32_t n_buckets, const uint8_t* buckets, float scale, void* O, float* LSE,
+                                  void* ws, size_t ws_bytes, hipStream_t stream);
+size_t gt_packed_attn_bwd_bias_workspace_size(const gt_packed_plan* plan, int32_t d, gt_dtype dtype,
+                                              int32_t n_buckets);
+gt_status gt_packed_attn_bwd_bias(const gt_packed_plan* plan, int32_t d, gt_dtype dtype, const void* Q, int64_t ldq,
+                                  const void* K, int64_t ldk, const void* V, int64_t ldv, const float* table,
+                                  int32_t n_buckets, const uint8_t* buckets, const void* dO, const float* LSE,
+                                  float scale, void* dQ, void* dK, void* dV, float* dtable, void* ws, size_t ws_bytes,
+                                  hipStream_t stream);
+
+/* The same learned bias on the edges of a sparse layer: the per-edge bias that
+ * gt_sparse_attn_*_bias take, and the table's gradient from their dbias.
+ *   fwd: bias[e, h] = table[bucket[e], h], -inf (the edge is not attended to)
+ *        where bucket[e] >= n_buckets;
+ *   bwd: dtable[b, h] = sum of dbias[e, h] over the edges in bucket b (fixed
+ *        order of additions: the same run to run).
+ * bucket uint8[nnz] and bias, dbias fp32 [nnz, H] in the CSR's edge order;
+ * H in {1, 2, 4, 8, 16}; n_buckets as above; 0 <= nnz < 2^32. */
+gt_status gt_bucket_bias_fwd(int64_t nnz, int32_t H, int32_t n_buckets, const float* table, const uint8_t* bucket,
+                             float* bias, hipStream_t stream);
+size_t gt_bucket_bias_bwd_workspace_size(int64_t nnz, int32_t H, int32_t n_buckets);
+gt_status gt_bucket_bias_bwd(int64_t nnz, int32_t H, int32_t n_buckets, const uint8_t* bucket, const float* dbias,
+                             float* dtable, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Norms between the blocks of a layer.                                      */
+/* ------------------------------------------------------------------------ */
+/* What stands between a block (attention or feed-forward) with output f and the
+ * next one, in one pass: the norm after the block, its gate, the scaled residual
+ * x, and the norm before the next block,
+ *   u = norm(f) * w_post + b_post,  y = res_scale * x + g * u,
+ *   z = norm(y) * w_pre + b_pre.
+ * norm: GT_NORM_LAYER (v - mean) / sqrt(var + eps), GT_NORM_RMS
+ * v / sqrt(mean v^2 + eps), over the D features of a row.
+ * g: GT_GATE_NONE 1; GT_GATE_VECTOR fp32[D] (a learned scale for each feature);
+ * GT_GATE_ROWS [n, D] in dtype; GT_GATE_SIGMOID sigmoid of such.
+ *   x, f, y, z [n, D] contiguous in dtype (no alignment needed beyond the
+ *     element's; rows of whole 16-byte pieces at 16-byte addresses run faster);
+ *   w_post, b_post, w_pre, b_pre fp32[D] or NULL (ones, zeros);
+ *   stats fp32 [n, 4], for the backward: mean and 1/sqrt(var + eps) of f, then
+ *     of y (mean 0 for GT_NORM_RMS).
+ * All arithmetic is fp32 and z is taken from y before y's rounding.
+ * 1 <= D <= 8192, 0 <= n < 2^31, eps > 0. */
+#define GT_NORM_LAYER 0
+#define GT_NORM_RMS 1
+#define GT_GATE_NONE 0
+#define GT_GATE_VECTOR 1
+#define GT_GATE_ROWS 2
+#define GT_GATE_SIGMOID 3
+gt_status gt_block_norm_fwd(int64_t n, int32_t D, gt_dtype dtype, int32_t norm, float eps, const void* x,
+                            float res_scale, const void* f, int32_t gate_kind, const void* gate, const float* w_post,
+                            const float* b_post, const float* w_pre, const float* b_pre, void* y, void* z,
+                            float* stats, hipStream_t stream);
+/* Backward, given dy (the gradient that reaches y past the second norm) and dz:
+ * dx, df [n, D]; dgate fp32[D] (GT_GATE_VECTOR) or [n, D] (GT_GATE_ROWS and
+ * _SIGMOID: of its input), NULL without a gate; dw_post, db_post, dw_pre, db_pre
+ * fp32[D], each may be NULL (not wanted).  y is formed again, so it is not an
+ * input.  Sums over the rows are added in a fixed order. */
+size_t gt_block_norm_bwd_workspace_size(int64_t n, int32_t D, gt_dtype dtype);
+gt_status gt_block_norm_bwd(int64_t n, int32_t D, gt_dtype dtype, int32_t norm, const void* x, float res_scale,
+                            const void* f, int32_t gate_kind, const void* gate, const float* w_post,
+                            const float* b_post, const float* w_pre, const float* stats, const void* dy,
+                            const void* dz, void* dx, void* df, void* dgate, float* dw_post, float* db_post,
+                            float* dw_pre, float* db_pre, void* ws, size_t ws_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

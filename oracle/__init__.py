@@ -20,6 +20,9 @@ Modules:
   and the Auto Tuner that walks its transfer threshold (§3.4).
 * ``interleave`` - the checks of conditions C1-C3 that decide when a dense
   layer is interleaved (§3.2).
+* ``packed`` - softmax attention inside packed sequences, with the learned
+  bias by buckets and its gradient.
+* ``norm`` - the norms, gate and scaled residual between two blocks.
 """
 
-from . import attention, ecr, interleave, plan, reorder  # noqa: F401
+from . import attention, ecr, interleave, norm, packed, plan, reorder  # noqa: F401

@@ -1,0 +1,465 @@
+// The norms between two blocks of a layer, with the gate and the scaled residual
+// that lie between them, in one pass over the rows; forward and backward.
+//
+// Bound by memory: the forward reads x, f (and a gate of rows) and writes y, z;
+// the backward reads x, f, (gate), dy, dz and writes dx, df, (dgate).  A row lies
+// in the registers of LPR lanes (a part of a wavefront, a wavefront or a
+// workgroup), NV 16-byte pieces of each array a lane, so every value is read
+// once; a lane keeps its columns from row to row, and with them the parameters
+// and the columns' sums of the parameters' gradients.  Workgroups walk the rows
+// grid-wide and leave one partial sum per column, which k_norm_sum adds in a
+// fixed order.
+#include "attn_common.h"
+#include "lanes.h"
+
+using namespace gt;
+
+namespace {
+
+constexpr int kMaxD = 8192;
+constexpr int kSums = 5;  // dw_post, db_post, dw_pre, db_pre, dgate (vector)
+
+struct NormArgs {
+    int64_t n;
+    int D, norm, gate_kind;
+    float eps, res_scale;
+    const void *x, *f, *gate, *dy, *dz;
+    const float *w_post, *b_post, *w_pre, *b_pre;
+    void *y, *z, *dx, *df, *dgate;
+    float* stats;
+    float* part;  // [blocks][kSums][D]
+    uint32_t want;  // bit k: sum k is wanted
+};
+
+template <int LPR>
+struct RowSum {
+    static constexpr int kThreads = LPR > 256 ? LPR : 256;
+    static constexpr int kRows = kThreads / LPR;  // rows a workgroup works on together
+    // the sums of a and b over the row's lanes, in every lane
+    __device__ __forceinline__ static void two(float& a, float& b, float* s) {
+        constexpr int W = LPR < kWave ? LPR : kWave;
+        if constexpr (W > 1) step<1, W>(a, b);
+        if constexpr (LPR > kWave) {
+            const int wave = int(threadIdx.x) / kWave;
+            __syncthreads();
+            if (lane_id() == 0) s[2 * wave] = a, s[2 * wave + 1] = b;
+            __syncthreads();
+            a = b = 0.f;
+#pragma unroll
+            for (int w = 0; w < LPR / kWave; ++w) a += s[2 * w], b += s[2 * w + 1];
+        }
+    }
+    template <int O, int W>
+    __device__ __forceinline__ static void step(float& a, float& b) {
+        if constexpr (O < W) {
+            a += __int_as_float(xor_lane<O>(__float_as_int(a)));
+            b += __int_as_float(xor_lane<O>(__float_as_int(b)));
+            step<2 * O, W>(a, b);
+        }
+    }
+};
+
+// A lane's NV pieces of one row: E consecutive features each, LPR pieces apart.
+template <typename T, int LPR, int NV, bool VEC>
+struct Cols {
+    static constexpr int E = 16 / int(sizeof(T));
+    int D, lane;  // lane of the row
+    __device__ __forceinline__ int col(int v) const { return (lane + LPR * v) * E; }
+    __device__ __forceinline__ bool in(int v, int t) const { return VEC ? col(v) < D : col(v) + t < D; }
+    __device__ __forceinline__ void load(float (&o)[NV][E], const void* p, int64_t row) const {
+        const T* r = static_cast<const T*>(p) + row * D;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            if constexpr (VEC) {
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (col(v) < D) x = *reinterpret_cast<const uint4*>(r + col(v));
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    if constexpr (E == 8) o[v][2 * t] = bf16lo(w[t]), o[v][2 * t + 1] = bf16hi(w[t]);
+                    else o[v][t] = __uint_as_float(w[t]);
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < E; ++t) {
+                    o[v][t] = 0.f;
+                    if (col(v) + t < D) {
+                        if constexpr (E == 8) o[v][t] = bf16_to_f32(r[col(v) + t]);
+                        else o[v][t] = r[col(v) + t];
+                    }
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void store(void* p, int64_t row, const float (&o)[NV][E]) const {
+        T* r = static_cast<T*>(p) + row * D;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            if constexpr (VEC) {
+                if (col(v) >= D) continue;
+                uint4 x;
+                if constexpr (E == 8)
+                    x = make_uint4(pack_bf16x2(o[v][0], o[v][1]), pack_bf16x2(o[v][2], o[v][3]),
+                                   pack_bf16x2(o[v][4], o[v][5]), pack_bf16x2(o[v][6], o[v][7]));
+                else
+                    x = make_uint4(__float_as_uint(o[v][0]), __float_as_uint(o[v][1]), __float_as_uint(o[v][2]),
+                                   __float_as_uint(o[v][3]));
+                *reinterpret_cast<uint4*>(r + col(v)) = x;
+            } else {
+#pragma unroll
+                for (int t = 0; t < E; ++t)
+                    if (col(v) + t < D) {
+                        if constexpr (E == 8) r[col(v) + t] = f32_to_bf16(o[v][t]);
+                        else r[col(v) + t] = o[v][t];
+                    }
+            }
+        }
+    }
+    __device__ __forceinline__ void param(float (&o)[NV][E], const float* p, float none) const {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int t = 0; t < E; ++t) o[v][t] = p && col(v) + t < D ? p[col(v) + t] : none;
+    }
+};
+
+// mean and 1 / sqrt(var + eps) of a row (two passes over registers: no
+// cancellation of a large mean); mean 0 without layer.
+template <int LPR, int NV, int E, typename C>
+__device__ __forceinline__ void row_stats(const float (&v)[NV][E], const C& c, bool layer, float eps, float inv_d,
+                                          float* s, float& mean, float& rstd) {
+    float a = 0.f, b = 0.f;
+    mean = 0.f;
+    if (layer) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int t = 0; t < E; ++t) a += v[k][t];
+        RowSum<LPR>::two(a, b, s);
+        mean = a * inv_d;
+    }
+    a = b = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int t = 0; t < E; ++t) {
+            const float x = c.in(k, t) ? v[k][t] - mean : 0.f;
+            a = fmaf(x, x, a);
+        }
+    RowSum<LPR>::two(a, b, s);
+    rstd = 1.f / sqrtf(fmaf(a, inv_d, eps));
+}
+
+__device__ __forceinline__ float sigmoid(float v) { return 1.f / (1.f + __expf(-v)); }
+
+template <typename T, int LPR, int NV, bool VEC>
+__global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_fwd(NormArgs a) {
+    using C = Cols<T, LPR, NV, VEC>;
+    using S = RowSum<LPR>;
+    constexpr int E = C::E;
+    __shared__ float s_sum[2 * S::kThreads / kWave];
+    const int t_row = int(threadIdx.x) / LPR;
+    const C c = {a.D, int(threadIdx.x) % LPR};
+    const bool layer = a.norm == GT_NORM_LAYER;
+    const float inv_d = 1.f / float(a.D);
+    float w1[NV][E], b1[NV][E], w2[NV][E], b2[NV][E], g[NV][E];
+    c.param(w1, a.w_post, 1.f);
+    c.param(b1, a.b_post, 0.f);
+    c.param(w2, a.w_pre, 1.f);
+    c.param(b2, a.b_pre, 0.f);
+    c.param(g, a.gate_kind == GT_GATE_VECTOR ? static_cast<const float*>(a.gate) : nullptr, 1.f);
+    for (int64_t r0 = int64_t(blockIdx.x) * S::kRows; r0 < a.n; r0 += int64_t(gridDim.x) * S::kRows) {
+        // every lane stays in the exchanges; a lane behind the last row works on the last one and writes nothing
+        const int64_t row = r0 + t_row < a.n ? r0 + t_row : a.n - 1;
+        const bool own = r0 + t_row < a.n;
+        float x[NV][E], f[NV][E];
+        c.load(f, a.f, row);
+        c.load(x, a.x, row);
+        if (a.gate_kind >= GT_GATE_ROWS) c.load(g, a.gate, row);
+        float mf, rf, my, ry;
+        row_stats<LPR>(f, c, layer, a.eps, inv_d, s_sum, mf, rf);
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int t = 0; t < E; ++t) {
+                const float u = fmaf((f[v][t] - mf) * rf, w1[v][t], b1[v][t]);
+                const float gv = a.gate_kind == GT_GATE_SIGMOID ? sigmoid(g[v][t]) : g[v][t];
+                x[v][t] = c.in(v, t) ? fmaf(gv, u, a.res_scale * x[v][t]) : 0.f;
+            }
+        row_stats<LPR>(x, c, layer, a.eps, inv_d, s_sum, my, ry);
+        if (own) {
+            c.store(a.y, row, x);
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int t = 0; t < E; ++t) x[v][t] = fmaf((x[v][t] - my) * ry, w2[v][t], b2[v][t]);
+            c.store(a.z, row, x);
+            if (c.lane == 0) *reinterpret_cast<float4*>(a.stats + 4 * row) = make_float4(mf, rf, my, ry);
+        }
+    }
+}
+
+// With fh = (f - mf) rf, yh = (y - my) ry and <v> a row's mean:
+//   t  = dy + ry (dz w2 - <dz w2> - yh <dz w2 yh>)      the gradient of y
+//   dx = res_scale t, dg = u t, du = g t
+//   df = rf (du w1 - <du w1> - fh <du w1 fh>)
+// (without the <dz w2> and <du w1> terms for the root mean square).
+template <typename T, int LPR, int NV, bool VEC>
+__global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_bwd(NormArgs a) {
+    using C = Cols<T, LPR, NV, VEC>;
+    using S = RowSum<LPR>;
+    constexpr int E = C::E;
+    __shared__ float s_sum[2 * S::kThreads / kWave];
+    __shared__ float s_part[S::kRows > 1 ? S::kThreads * NV * E : 1];
+    const int t_row = int(threadIdx.x) / LPR;
+    const C c = {a.D, int(threadIdx.x) % LPR};
+    const bool layer = a.norm == GT_NORM_LAYER;
+    const float inv_d = 1.f / float(a.D);
+    float w1[NV][E], b1[NV][E], w2[NV][E], g[NV][E], sum[kSums][NV][E];
+    c.param(w1, a.w_post, 1.f);
+    c.param(b1, a.b_post, 0.f);
+    c.param(w2, a.w_pre, 1.f);
+    c.param(g, a.gate_kind == GT_GATE_VECTOR ? static_cast<const float*>(a.gate) : nullptr, 1.f);
+#pragma unroll
+    for (int k = 0; k < kSums; ++k)
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int t = 0; t < E; ++t) sum[k][v][t] = 0.f;
+    for (int64_t r0 = int64_t(blockIdx.x) * S::kRows; r0 < a.n; r0 += int64_t(gridDim.x) * S::kRows) {
+        const int64_t row = r0 + t_row < a.n ? r0 + t_row : a.n - 1;
+        const bool own = r0 + t_row < a.n;
+        float x[NV][E], f[NV][E], dy[NV][E], dz[NV][E];
+        const float4 st = *reinterpret_cast<const float4*>(a.stats + 4 * row);
+        c.load(f, a.f, row);
+        c.load(x, a.x, row);
+        if (a.gate_kind >= GT_GATE_ROWS) c.load(g, a.gate, row);
+        c.load(dz, a.dz, row);
+        c.load(dy, a.dy, row);
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int t = 0; t < E; ++t) {
+                f[v][t] = c.in(v, t) ? (f[v][t] - st.x) * st.y : 0.f;  // fh
+                if (a.gate_kind == GT_GATE_SIGMOID) g[v][t] = sigmoid(g[v][t]);
+                const float u = fmaf(f[v][t], w1[v][t], b1[v][t]);
+                x[v][t] = c.in(v, t) ? (fmaf(g[v][t], u, a.res_scale * x[v][t]) - st.z) * st.w : 0.f;  // yh
+                const float d = dz[v][t] * w2[v][t];
+                s1 += d;
+                s2 = fmaf(d, x[v][t], s2);
+                if (own) {
+                    sum[2][v][t] = fmaf(dz[v][t], x[v][t], sum[2][v][t]);
+                    sum[3][v][t] += dz[v][t];
+                }
+            }
+        S::two(s1, s2, s_sum);
+        const float m1 = layer ? s1 * inv_d : 0.f, m2 = s2 * inv_d;
+        s1 = s2 = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int t = 0; t < E; ++t) {
+                const float ty = fmaf(st.w, dz[v][t] * w2[v][t] - m1 - x[v][t] * m2, dy[v][t]);
+                const float u = fmaf(f[v][t], w1[v][t], b1[v][t]);
+                const float du = g[v][t] * ty, dg = u * ty;
+                x[v][t] = a.res_scale * ty;
+                dy[v][t] = a.gate_kind == GT_GATE_SIGMOID ? dg * (g[v][t] * (1.f - g[v][t])) : dg;
+                if (own) {
+                    sum[0][v][t] = fmaf(du, f[v][t], sum[0][v][t]);
+                    sum[1][v][t] += du;
+                    sum[4][v][t] += dg;
+                }
+                dz[v][t] = c.in(v, t) ? du * w1[v][t] : 0.f;
+                s1 += dz[v][t];
+                s2 = fmaf(dz[v][t], f[v][t], s2);
+            }
+        S::two(s1, s2, s_sum);
+        const float n1 = layer ? s1 * inv_d : 0.f, n2 = s2 * inv_d;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int t = 0; t < E; ++t) f[v][t] = st.y * (dz[v][t] - n1 - f[v][t] * n2);
+        if (own) {
+            c.store(a.dx, row, x);
+            c.store(a.df, row, f);
+            if (a.gate_kind >= GT_GATE_ROWS) c.store(a.dgate, row, dy);
+        }
+    }
+    // the columns' sums over the workgroup's rows
+    for (int k = 0; k < kSums; ++k) {
+        if (!(a.want >> k & 1)) continue;
+        float* out = a.part + (int64_t(blockIdx.x) * kSums + k) * a.D;
+        if constexpr (S::kRows > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int t = 0; t < E; ++t) s_part[(t_row * LPR * NV + LPR * v + c.lane) * E + t] = sum[k][v][t];
+            __syncthreads();
+            for (int x = int(threadIdx.x); x < LPR * NV * E && x < a.D; x += S::kThreads) {
+                float t = 0.f;
+                for (int r = 0; r < S::kRows; ++r) t += s_part[r * (LPR * NV * E) + x];
+                out[x] = t;
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int t = 0; t < E; ++t)
+                    if (c.col(v) + t < a.D) out[c.col(v) + t] = sum[k][v][t];
+        }
+    }
+}
+
+// out[k][x] = the sum over the workgroups' partial sums, 64 columns a workgroup.
+struct SumOut {
+    float* p[kSums];
+};
+__global__ __launch_bounds__(1024) void k_norm_sum(int blocks, int D, const float* __restrict__ part, SumOut o) {
+    __shared__ float s[1024];
+    const int k = int(blockIdx.y), x = int(blockIdx.x) * kWave + lane_id();
+    float* out = o.p[k];
+    if (!out) return;  // uniform
+    float t = 0.f;
+    if (x < D)
+        for (int b = int(threadIdx.x) / kWave; b < blocks; b += 1024 / kWave)
+            t += part[(int64_t(b) * kSums + k) * D + x];
+    s[threadIdx.x] = t;
+    __syncthreads();
+    if (threadIdx.x < kWave && x < D) {
+        for (int w = 1; w < 1024 / kWave; ++w) t += s[w * kWave + lane_id()];
+        out[x] = t;
+    }
+}
+
+// Lanes per row and pieces per lane: the fewest lanes that hold a row at one
+// piece each, and two a lane where a row would only just leave a wavefront (or
+// a workgroup).
+#define GT_NORM_SHAPE(pieces, CALL)                 \
+    do {                                            \
+        if ((pieces) <= 8) { CALL(8, 1); }          \
+        else if ((pieces) <= 16) { CALL(16, 1); }   \
+        else if ((pieces) <= 32) { CALL(32, 1); }   \
+        else if ((pieces) <= 64) { CALL(64, 1); }   \
+        else if ((pieces) <= 128) { CALL(64, 2); }  \
+        else if ((pieces) <= 256) { CALL(256, 1); } \
+        else if ((pieces) <= 512) { CALL(256, 2); } \
+        else if ((pieces) <= 1024) { CALL(1024, 1); } \
+        else { CALL(1024, 2); }                     \
+    } while (0)
+
+int norm_rows(int pieces) { return pieces <= 8 ? 32 : pieces <= 16 ? 16 : pieces <= 32 ? 8 : pieces <= 128 ? 4 : 1; }
+
+constexpr int kNormBlocks = 1024;
+
+int norm_blocks(int64_t n, int32_t D, gt_dtype dt) {
+    const int pieces = int(cdiv(D, dt == GT_BF16 ? 8 : 4));
+    const int64_t want = cdiv(n, norm_rows(pieces));
+    return int(want < kNormBlocks ? want : kNormBlocks);
+}
+
+bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
+
+template <typename T, bool VEC>
+void run_fwd(const NormArgs& a, int pieces, int blocks, hipStream_t s) {
+#define GT_CALL(LPR, NV) k_norm_fwd<T, LPR, NV, VEC><<<blocks, RowSum<LPR>::kThreads, 0, s>>>(a)
+    GT_NORM_SHAPE(pieces, GT_CALL);
+#undef GT_CALL
+}
+template <typename T, bool VEC>
+void run_bwd(const NormArgs& a, int pieces, int blocks, hipStream_t s) {
+#define GT_CALL(LPR, NV) k_norm_bwd<T, LPR, NV, VEC><<<blocks, RowSum<LPR>::kThreads, 0, s>>>(a)
+    GT_NORM_SHAPE(pieces, GT_CALL);
+#undef GT_CALL
+}
+
+gt_status norm_check(const char* who, int64_t n, int32_t D, gt_dtype dt, int32_t norm, int32_t gate_kind,
+                     const void* gate, float res_scale) {
+    const std::string w(who);
+    if (n < 0 || n >= (int64_t(1) << 31)) return fail(GT_ERR_INVALID_ARG, w + ": n out of range");
+    if ((dt != GT_BF16 && dt != GT_F32) || D < 1 || D > kMaxD) return fail(GT_ERR_UNSUPPORTED, w + ": unsupported (dtype, D)");
+    if (norm != GT_NORM_LAYER && norm != GT_NORM_RMS) return fail(GT_ERR_UNSUPPORTED, w + ": unknown norm");
+    if (gate_kind < GT_GATE_NONE || gate_kind > GT_GATE_SIGMOID) return fail(GT_ERR_UNSUPPORTED, w + ": unknown gate");
+    if ((gate_kind == GT_GATE_VECTOR || (gate_kind != GT_GATE_NONE && n > 0)) && !gate)
+        return fail(GT_ERR_INVALID_ARG, w + ": null gate");
+    (void)res_scale;
+    return GT_OK;
+}
+
+}  // namespace
+
+extern "C" gt_status gt_block_norm_fwd(int64_t n, int32_t D, gt_dtype dt, int32_t norm, float eps, const void* x,
+                                       float res_scale, const void* f, int32_t gate_kind, const void* gate,
+                                       const float* w_post, const float* b_post, const float* w_pre,
+                                       const float* b_pre, void* y, void* z, float* stats, hipStream_t s) {
+    const char* who = "gt_block_norm_fwd";
+    const gt_status st = norm_check(who, n, D, dt, norm, gate_kind, gate, res_scale);
+    if (st != GT_OK) return st;
+    if (!(eps > 0.f)) return fail(GT_ERR_INVALID_ARG, std::string(who) + ": eps must be positive");
+    if (n == 0) return GT_OK;
+    if (!x || !f || !y || !z || !stats) return fail(GT_ERR_INVALID_ARG, std::string(who) + ": null pointer");
+    if (off16(stats)) return fail(GT_ERR_UNSUPPORTED, std::string(who) + ": stats must start at a multiple of 16 bytes");
+    NormArgs a = {};
+    a.n = n, a.D = D, a.norm = norm, a.gate_kind = gate_kind, a.eps = eps, a.res_scale = res_scale;
+    a.x = x, a.f = f, a.gate = gate;
+    a.w_post = w_post, a.b_post = b_post, a.w_pre = w_pre, a.b_pre = b_pre;
+    a.y = y, a.z = z, a.stats = stats;
+    const int E = dt == GT_BF16 ? 8 : 4, pieces = int(cdiv(D, E)), blocks = norm_blocks(n, D, dt);
+    const bool vec = D % E == 0 && !off16(x) && !off16(f) && !off16(y) && !off16(z) &&
+                     (gate_kind < GT_GATE_ROWS || !off16(gate));
+    if (dt == GT_BF16) vec ? run_fwd<uint16_t, true>(a, pieces, blocks, s) : run_fwd<uint16_t, false>(a, pieces, blocks, s);
+    else vec ? run_fwd<float, true>(a, pieces, blocks, s) : run_fwd<float, false>(a, pieces, blocks, s);
+    GT_LAUNCH_CHECK("block_norm_fwd");
+    return GT_OK;
+}
+
+extern "C" size_t gt_block_norm_bwd_workspace_size(int64_t n, int32_t D, gt_dtype dt) {
+    if (n < 0 || D < 1 || D > kMaxD || (dt != GT_BF16 && dt != GT_F32)) return 0;
+    Ws w(nullptr);
+    w.take<float>(size_t(norm_blocks(n, D, dt)) * kSums * D);
+    return w.size();
+}
+
+extern "C" gt_status gt_block_norm_bwd(int64_t n, int32_t D, gt_dtype dt, int32_t norm, const void* x,
+                                       float res_scale, const void* f, int32_t gate_kind, const void* gate,
+                                       const float* w_post, const float* b_post, const float* w_pre,
+                                       const float* stats, const void* dy, const void* dz, void* dx, void* df,
+                                       void* dgate, float* dw_post, float* db_post, float* dw_pre, float* db_pre,
+                                       void* ws, size_t ws_bytes, hipStream_t s) {
+    const char* who = "gt_block_norm_bwd";
+    const gt_status st = norm_check(who, n, D, dt, norm, gate_kind, gate, res_scale);
+    if (st != GT_OK) return st;
+    if (n > 0 && (!x || !f || !stats || !dy || !dz || !dx || !df || (gate_kind != GT_GATE_NONE && !dgate)))
+        return fail(GT_ERR_INVALID_ARG, std::string(who) + ": null pointer");
+    if (gate_kind == GT_GATE_VECTOR && !dgate) return fail(GT_ERR_INVALID_ARG, std::string(who) + ": null pointer");
+    if (off16(stats)) return fail(GT_ERR_UNSUPPORTED, std::string(who) + ": stats must start at a multiple of 16 bytes");
+    const size_t need = gt_block_norm_bwd_workspace_size(n, D, dt);
+    if (ws_bytes < need) return fail(GT_ERR_WORKSPACE, std::string(who) + ": workspace too small");
+    if (need > 0 && !ws) return fail(GT_ERR_INVALID_ARG, std::string(who) + ": null pointer");
+    Ws w(ws);
+    const int E = dt == GT_BF16 ? 8 : 4, pieces = int(cdiv(D, E)), blocks = norm_blocks(n, D, dt);
+    NormArgs a = {};
+    a.n = n, a.D = D, a.norm = norm, a.gate_kind = gate_kind, a.res_scale = res_scale;
+    a.x = x, a.f = f, a.gate = gate, a.dy = dy, a.dz = dz;
+    a.w_post = w_post, a.b_post = b_post, a.w_pre = w_pre;
+    a.dx = dx, a.df = df, a.dgate = dgate;
+    a.stats = const_cast<float*>(stats);
+    a.part = w.take<float>(size_t(blocks) * kSums * D);
+    SumOut o = {{dw_post, db_post, dw_pre, db_pre,
+                 gate_kind == GT_GATE_VECTOR ? static_cast<float*>(dgate) : nullptr}};
+    for (int k = 0; k < kSums; ++k)
+        if (o.p[k]) a.want |= 1u << k;
+    if (n > 0) {
+        const bool vec = D % E == 0 && !off16(x) && !off16(f) && !off16(dy) && !off16(dz) && !off16(dx) && !off16(df) &&
+                         (gate_kind < GT_GATE_ROWS || (!off16(gate) && !off16(dgate)));
+        if (dt == GT_BF16) vec ? run_bwd<uint16_t, true>(a, pieces, blocks, s) : run_bwd<uint16_t, false>(a, pieces, blocks, s);
+        else vec ? run_bwd<float, true>(a, pieces, blocks, s) : run_bwd<float, false>(a, pieces, blocks, s);
+        GT_LAUNCH_CHECK("block_norm_bwd");
+    }
+    if (a.want) {
+        k_norm_sum<<<dim3(unsigned(cdiv(D, kWave)), kSums), 1024, 0, s>>>(blocks, D, a.part, o);
+        GT_LAUNCH_CHECK("block_norm_bwd sum");
+    }
+    return GT_OK;
+}

@@ -9,6 +9,7 @@ here computes any part of the method.  The library must be built
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -30,6 +31,9 @@ GT_ERR_HIP = -7
 GT_F32 = 0
 GT_BF16 = 1
 GT_LONG_ROW = 256
+GT_MAX_BUCKETS = 64
+GT_NORM_LAYER, GT_NORM_RMS = 0, 1
+GT_GATE_NONE, GT_GATE_VECTOR, GT_GATE_ROWS, GT_GATE_SIGMOID = 0, 1, 2, 3
 
 _i32, _i64, _u32, _u64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint64
 _vp, _sz, _f32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float
@@ -55,6 +59,13 @@ class GtAutotuner(ctypes.Structure):
     _fields_ = [
         ("F", _f64), ("ldr", _f64 * GT_AUTOTUNER_HISTORY), ("t", _i64), ("last_change", _i64), ("level", _i32),
         ("delta", _i32), ("num", _u64 * GT_AUTOTUNER_RUNGS), ("den", _u64 * GT_AUTOTUNER_RUNGS),
+    ]
+
+
+class GtPackedPlan(ctypes.Structure):
+    _fields_ = [
+        ("n_seq", _i64), ("nq", _i64), ("nk", _i64), ("pair_bytes", _i64), ("item_bytes", _i64),
+        ("H", _i32), ("Hkv", _i32), ("causal", _i32), ("reserved", _i32), ("layout", _i64 * 32), ("items", _vp),
     ]
 
 
@@ -120,6 +131,28 @@ SIGNATURES = {
     "gt_dense_attn_bwd_noalloc_max_bytes": (_sz, []),
     "gt_dense_attn_bwd_noalloc": (_i32, [_i64, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _f32, _vp, _vp,
                                          _vp, _vp]),
+    "gt_packed_plan_init": (_i32, [_i64, _vp, _vp, _i32, _i32, _i32, _P(GtPackedPlan)]),
+    "gt_packed_plan_fill": (_i32, [_i64, _vp, _vp, _P(GtPackedPlan), _vp, _sz]),
+    "gt_packed_attn_fwd_workspace_size": (_sz, [_P(GtPackedPlan), _i32, _i32]),
+    "gt_packed_attn_fwd": (_i32, [_P(GtPackedPlan), _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _f32, _vp, _vp,
+                                  _vp, _sz, _vp]),
+    "gt_packed_attn_bwd_workspace_size": (_sz, [_P(GtPackedPlan), _i32, _i32]),
+    "gt_packed_attn_bwd": (_i32, [_P(GtPackedPlan), _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp,
+                                  _f32, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "gt_packed_attn_fwd_bias_workspace_size": (_sz, [_P(GtPackedPlan), _i32, _i32, _i32]),
+    "gt_packed_attn_fwd_bias": (_i32, [_P(GtPackedPlan), _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32, _vp,
+                                       _f32, _vp, _vp, _vp, _sz, _vp]),
+    "gt_packed_attn_bwd_bias_workspace_size": (_sz, [_P(GtPackedPlan), _i32, _i32, _i32]),
+    "gt_packed_attn_bwd_bias": (_i32, [_P(GtPackedPlan), _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32, _vp,
+                                       _vp, _vp, _f32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "gt_bucket_bias_fwd": (_i32, [_i64, _i32, _i32, _vp, _vp, _vp, _vp]),
+    "gt_bucket_bias_bwd_workspace_size": (_sz, [_i64, _i32, _i32]),
+    "gt_bucket_bias_bwd": (_i32, [_i64, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "gt_block_norm_fwd": (_i32, [_i64, _i32, _i32, _i32, _f32, _vp, _f32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp,
+                                 _vp, _vp, _vp]),
+    "gt_block_norm_bwd_workspace_size": (_sz, [_i64, _i32, _i32]),
+    "gt_block_norm_bwd": (_i32, [_i64, _i32, _i32, _i32, _vp, _f32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                 _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
 }
 
 _LIB = None
@@ -640,3 +673,283 @@ def dense_attn_bwd_noalloc(Q, K, V, O, dO, LSE, scale: float | None = None, out=
                                          scale, _ptr(dQ), _ptr(dK), _ptr(dV), _stream(Q.device)),
            "gt_dense_attn_bwd_noalloc")
     return dQ, dK, dV
+
+
+# ------------------------------------------------------------- packed sequences
+
+_SAME_DEVICE = contextlib.nullcontext()
+
+
+def _on(device: torch.device):
+    """Makes `device` the current one around a call (kernels are launched on the current device)."""
+    if device.index is None or device.index == torch.cuda.current_device():
+        return _SAME_DEVICE
+    return torch.cuda.device(device)
+
+
+@dataclass
+class PackedPlan:
+    """The work list of packed-sequence attention: the C struct and the device copy of its items."""
+
+    c: GtPackedPlan
+    items: torch.Tensor
+
+    @property
+    def nq(self):
+        return self.c.nq
+
+    @property
+    def nk(self):
+        return self.c.nk
+
+    @property
+    def pair_bytes(self):
+        return self.c.pair_bytes
+
+
+def _host_ptr(ptr, name: str) -> torch.Tensor:
+    t = torch.as_tensor(ptr)
+    _need(t.dim() == 1 and t.numel() >= 1 and t.dtype in (torch.int32, torch.int64),
+          f"{name} must be 1-D integers, one more than there are sequences")
+    return t.to(device="cpu", dtype=torch.int64).contiguous()
+
+
+def packed_plan(q_ptr, k_ptr=None, *, heads: int, kv_heads: int | None = None, causal: bool = False,
+                device=None) -> PackedPlan:
+    """Plan of attention over packed sequences: sequence s holds the queries q_ptr[s] to q_ptr[s + 1] - 1 and the
+    keys k_ptr[s] to k_ptr[s + 1] - 1 (the same when k_ptr is not given).  The pointers may be lists or tensors
+    (one on the GPU is read back, which waits for it).  Built once per batch and kept for every layer."""
+    lib = load_library()
+    if device is None:
+        device = q_ptr.device if isinstance(q_ptr, torch.Tensor) and q_ptr.is_cuda else "cuda"
+    device = torch.device(device)
+    if device.type == "cuda" and device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    q = _host_ptr(q_ptr, "q_ptr")
+    k = q if k_ptr is None else _host_ptr(k_ptr, "k_ptr")
+    _need(q.numel() == k.numel(), "q_ptr and k_ptr must have the same length")
+    n = q.numel() - 1
+    c = GtPackedPlan()
+    _check(lib.gt_packed_plan_init(n, _ptr(q), _ptr(k), int(heads), int(heads if kv_heads is None else kv_heads),
+                                   int(bool(causal)), ctypes.byref(c)), "gt_packed_plan_init")
+    host = torch.empty(max(c.item_bytes, 1), dtype=torch.uint8)
+    _check(lib.gt_packed_plan_fill(n, _ptr(q), _ptr(k), ctypes.byref(c), _ptr(host), c.item_bytes),
+           "gt_packed_plan_fill")
+    items = host.to(device)
+    c.items = items.data_ptr()
+    return PackedPlan(c=c, items=items)
+
+
+def _check_rows(t: torch.Tensor, n: int, heads: int, d: int, dtype, device, name: str) -> int:
+    """Node stride of a [n or more, heads, d] tensor whose nodes' features are contiguous."""
+    _need(t.is_cuda and t.device == device and t.dtype == dtype and t.dim() == 3 and t.shape[1:] == (heads, d)
+          and t.shape[0] >= n, f"{name} must be a [{n} or more, {heads}, {d}] tensor of the plan's device and one dtype")
+    if t.shape[0] <= 1 and t.is_contiguous():
+        return heads * d
+    s = t.stride()
+    _need((d == 1 or s[2] == 1) and (heads == 1 or s[1] == d) and s[0] >= heads * d,
+          f"{name}: a node's features must be contiguous")
+    return s[0]
+
+
+def _check_packed(plan: PackedPlan, Q, K, V):
+    c = plan.c
+    _need(Q.dim() == 3, "features must be [n, H, d]")
+    d, dev = Q.shape[2], plan.items.device
+    return (d, _dtype_code(Q), _check_rows(Q, c.nq, c.H, d, Q.dtype, dev, "Q"),
+            _check_rows(K, c.nk, c.Hkv, d, Q.dtype, dev, "K"), _check_rows(V, c.nk, c.Hkv, d, Q.dtype, dev, "V"))
+
+
+def _new_rows(like: torch.Tensor, n: int) -> torch.Tensor:
+    """A contiguous tensor of like's shape for a call that writes its first n rows: the others are zeros."""
+    out = torch.empty(like.shape, dtype=like.dtype, device=like.device)
+    if out.shape[0] > n:
+        out[n:].zero_()
+    return out
+
+
+def _new_lse(rows: int, heads: int, n: int, device) -> torch.Tensor:
+    lse = torch.empty((rows, heads), dtype=torch.float32, device=device)
+    if rows > n:
+        lse[n:].fill_(-math.inf)
+    return lse
+
+
+def _check_contiguous(t, shape, dtype, device, name: str):
+    _need(t.shape == shape and t.dtype == dtype and t.device == device and t.is_contiguous(),
+          f"{name} must be a contiguous {list(shape)} tensor of the features' dtype and device")
+
+
+def _check_table(plan: PackedPlan, table, buckets):
+    dev = plan.items.device
+    _need(table.dtype == torch.float32 and table.dim() == 2 and table.shape[1] == plan.c.H and table.is_contiguous()
+          and table.device == dev, "table must be a contiguous fp32 [n_buckets, H] tensor of the plan's device")
+    _need(buckets.dtype == torch.uint8 and buckets.dim() == 1 and buckets.numel() >= plan.c.pair_bytes
+          and buckets.is_contiguous() and buckets.device == dev,
+          "buckets must be a contiguous uint8 tensor of plan.pair_bytes, on the plan's device")
+
+
+def packed_attn_fwd(plan: PackedPlan, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, scale: float | None = None):
+    """(O, LSE) of softmax attention inside each packed sequence.  Q, K and V may be slices of a wider array (any
+    node stride); rows behind the last sequence give zeros and -inf."""
+    lib = load_library()
+    d, dt, ldq, ldk, ldv = _check_packed(plan, Q, K, V)
+    scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
+    with _on(Q.device):
+        O, LSE = _new_rows(Q, plan.c.nq), _new_lse(Q.shape[0], plan.c.H, plan.c.nq, Q.device)
+        ws = _workspace(lib.gt_packed_attn_fwd_workspace_size(ctypes.byref(plan.c), d, dt), Q.device)
+        _check(lib.gt_packed_attn_fwd(ctypes.byref(plan.c), d, dt, _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv, scale,
+                                      _ptr(O), _ptr(LSE), _ptr(ws), ws.numel(), _stream(Q.device)),
+               "gt_packed_attn_fwd")
+    return O, LSE
+
+
+def packed_attn_bwd(plan: PackedPlan, Q, K, V, O, dO, LSE, scale: float | None = None):
+    """(dQ, dK, dV) of softmax attention inside each packed sequence."""
+    lib = load_library()
+    d, dt, ldq, ldk, ldv = _check_packed(plan, Q, K, V)
+    _check_contiguous(O, Q.shape, Q.dtype, Q.device, "O")
+    _check_contiguous(dO, Q.shape, Q.dtype, Q.device, "dO")
+    _check_contiguous(LSE, Q.shape[:2], torch.float32, Q.device, "LSE")
+    scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
+    with _on(Q.device):
+        dQ, dK, dV = _new_rows(Q, plan.c.nq), _new_rows(K, plan.c.nk), _new_rows(V, plan.c.nk)
+        ws = _workspace(lib.gt_packed_attn_bwd_workspace_size(ctypes.byref(plan.c), d, dt), Q.device)
+        _check(lib.gt_packed_attn_bwd(ctypes.byref(plan.c), d, dt, _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv, _ptr(O),
+                                      _ptr(dO), _ptr(LSE), scale, _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(ws), ws.numel(),
+                                      _stream(Q.device)), "gt_packed_attn_bwd")
+    return dQ, dK, dV
+
+
+def packed_attn_fwd_bias(plan: PackedPlan, Q, K, V, table, buckets, scale: float | None = None):
+    """(O, LSE) with the learned bias table[bucket of the pair, head] (fp32 [n_buckets, H]).  buckets: uint8
+    [plan.pair_bytes], sequence after sequence a row of keys for each query, rows padded to 16 bytes; a pair whose
+    bucket is n_buckets or more is not attended to."""
+    lib = load_library()
+    d, dt, ldq, ldk, ldv = _check_packed(plan, Q, K, V)
+    _check_table(plan, table, buckets)
+    scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
+    B = table.shape[0]
+    with _on(Q.device):
+        O, LSE = _new_rows(Q, plan.c.nq), _new_lse(Q.shape[0], plan.c.H, plan.c.nq, Q.device)
+        ws = _workspace(lib.gt_packed_attn_fwd_bias_workspace_size(ctypes.byref(plan.c), d, dt, B), Q.device)
+        _check(lib.gt_packed_attn_fwd_bias(ctypes.byref(plan.c), d, dt, _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv,
+                                           _ptr(table), B, _ptr(buckets), scale, _ptr(O), _ptr(LSE), _ptr(ws),
+                                           ws.numel(), _stream(Q.device)), "gt_packed_attn_fwd_bias")
+    return O, LSE
+
+
+def packed_attn_bwd_bias(plan: PackedPlan, Q, K, V, table, buckets, dO, LSE, scale: float | None = None):
+    """(dQ, dK, dV, dtable) with the learned bias."""
+    lib = load_library()
+    d, dt, ldq, ldk, ldv = _check_packed(plan, Q, K, V)
+    _check_table(plan, table, buckets)
+    _check_contiguous(dO, Q.shape, Q.dtype, Q.device, "dO")
+    _check_contiguous(LSE, Q.shape[:2], torch.float32, Q.device, "LSE")
+    scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
+    B = table.shape[0]
+    with _on(Q.device):
+        dQ, dK, dV = _new_rows(Q, plan.c.nq), _new_rows(K, plan.c.nk), _new_rows(V, plan.c.nk)
+        dtable = torch.empty_like(table)
+        ws = _workspace(lib.gt_packed_attn_bwd_bias_workspace_size(ctypes.byref(plan.c), d, dt, B), Q.device)
+        _check(lib.gt_packed_attn_bwd_bias(ctypes.byref(plan.c), d, dt, _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv,
+                                           _ptr(table), B, _ptr(buckets), _ptr(dO), _ptr(LSE), scale, _ptr(dQ),
+                                           _ptr(dK), _ptr(dV), _ptr(dtable), _ptr(ws), ws.numel(),
+                                           _stream(Q.device)), "gt_packed_attn_bwd_bias")
+    return dQ, dK, dV, dtable
+
+
+def bucket_bias_fwd(table: torch.Tensor, bucket: torch.Tensor) -> torch.Tensor:
+    """The per-edge bias [nnz, H] of a learned table fp32 [n_buckets, H] and the edges' buckets (uint8 [nnz]); -inf
+    where the bucket is n_buckets or more.  For sparse_attn_fwd_bias and sparse_attn_bwd_bias."""
+    lib = load_library()
+    _need(table.is_cuda and table.dtype == torch.float32 and table.dim() == 2 and table.is_contiguous(),
+          "table must be a contiguous fp32 GPU tensor [n_buckets, H]")
+    _need(bucket.dtype == torch.uint8 and bucket.dim() == 1 and bucket.is_contiguous() and bucket.device == table.device,
+          "bucket must be a contiguous uint8 tensor [nnz] on the table's device")
+    nnz, (B, H) = bucket.numel(), table.shape
+    with _on(table.device):
+        bias = torch.empty((nnz, H), dtype=torch.float32, device=table.device)
+        _check(lib.gt_bucket_bias_fwd(nnz, H, B, _ptr(table), _ptr(bucket), _ptr(bias), _stream(table.device)),
+               "gt_bucket_bias_fwd")
+    return bias
+
+
+def bucket_bias_bwd(bucket: torch.Tensor, dbias: torch.Tensor, n_buckets: int) -> torch.Tensor:
+    """The table's gradient [n_buckets, H] from the edges' dbias (fp32 [nnz, H])."""
+    lib = load_library()
+    _need(dbias.is_cuda and dbias.dtype == torch.float32 and dbias.dim() == 2 and dbias.is_contiguous(),
+          "dbias must be a contiguous fp32 GPU tensor [nnz, H]")
+    nnz, H = dbias.shape
+    _need(bucket.dtype == torch.uint8 and bucket.shape == (nnz,) and bucket.is_contiguous()
+          and bucket.device == dbias.device, "bucket must be a contiguous uint8 tensor [nnz] on dbias's device")
+    with _on(dbias.device):
+        dtable = torch.empty((int(n_buckets), H), dtype=torch.float32, device=dbias.device)
+        ws = _workspace(lib.gt_bucket_bias_bwd_workspace_size(nnz, H, int(n_buckets)), dbias.device)
+        _check(lib.gt_bucket_bias_bwd(nnz, H, int(n_buckets), _ptr(bucket), _ptr(dbias), _ptr(dtable), _ptr(ws),
+                                      ws.numel(), _stream(dbias.device)), "gt_bucket_bias_bwd")
+    return dtable
+
+
+# ------------------------------------------------------------- norms between blocks
+
+_NORMS = {"layer": GT_NORM_LAYER, "rms": GT_NORM_RMS}
+
+
+def _check_norm(x, f, gate, sigmoid, kind, params):
+    _need(x.is_cuda and x.dim() == 2 and x.is_contiguous(), "x must be a contiguous GPU tensor [n, D]")
+    _check_contiguous(f, x.shape, x.dtype, x.device, "f")
+    _need(kind in _NORMS, "kind must be 'layer' or 'rms'")
+    n, D = x.shape
+    for name, p in params.items():
+        _need(p is None or (p.dtype == torch.float32 and p.shape == (D,) and p.is_contiguous() and p.device == x.device),
+              f"{name} must be a contiguous fp32 tensor [D] on x's device")
+    if gate is None:
+        _need(not sigmoid, "sigmoid needs a gate")
+        return GT_GATE_NONE
+    if gate.dim() == 1:
+        _need(not sigmoid, "a gate vector is taken as it is")
+        _need(gate.dtype == torch.float32 and gate.shape == (D,) and gate.is_contiguous() and gate.device == x.device,
+              "a gate vector must be a contiguous fp32 tensor [D] on x's device")
+        return GT_GATE_VECTOR
+    _check_contiguous(gate, x.shape, x.dtype, x.device, "gate")
+    return GT_GATE_SIGMOID if sigmoid else GT_GATE_ROWS
+
+
+def block_norm_fwd(x, f, *, w_post=None, b_post=None, w_pre=None, b_pre=None, gate=None, sigmoid: bool = False,
+                   res_scale: float = 1.0, kind: str = "layer", eps: float = 1e-5):
+    """(y, z, stats): y = res_scale x + g (norm(f) w_post + b_post), z = norm(y) w_pre + b_pre over the rows of
+    x and f [n, D].  gate: None, fp32 [D], or [n, D] like x (its sigmoid if asked); stats are for the backward."""
+    lib = load_library()
+    gk = _check_norm(x, f, gate, sigmoid, kind, dict(w_post=w_post, b_post=b_post, w_pre=w_pre, b_pre=b_pre))
+    n, D = x.shape
+    with _on(x.device):
+        y, z = torch.empty_like(x), torch.empty_like(x)
+        stats = torch.empty((n, 4), dtype=torch.float32, device=x.device)
+        _check(lib.gt_block_norm_fwd(n, D, _dtype_code(x), _NORMS[kind], float(eps), _ptr(x), float(res_scale), _ptr(f),
+                                     gk, _ptr(gate), _ptr(w_post), _ptr(b_post), _ptr(w_pre), _ptr(b_pre), _ptr(y),
+                                     _ptr(z), _ptr(stats), _stream(x.device)), "gt_block_norm_fwd")
+    return y, z, stats
+
+
+def block_norm_bwd(x, f, stats, dy, dz, *, w_post=None, b_post=None, w_pre=None, b_pre=None, gate=None,
+                   sigmoid: bool = False, res_scale: float = 1.0, kind: str = "layer", eps: float = 1e-5):
+    """(dx, df, dgate, dw_post, db_post, dw_pre, db_pre) for the same arguments as block_norm_fwd; None for what
+    was not given.  (eps is in stats already.)"""
+    lib = load_library()
+    params = dict(w_post=w_post, b_post=b_post, w_pre=w_pre, b_pre=b_pre)
+    gk = _check_norm(x, f, gate, sigmoid, kind, params)
+    n, D = x.shape
+    _check_contiguous(dy, x.shape, x.dtype, x.device, "dy")
+    _check_contiguous(dz, x.shape, x.dtype, x.device, "dz")
+    _check_contiguous(stats, (n, 4), torch.float32, x.device, "stats")
+    with _on(x.device):
+        dx, df = torch.empty_like(x), torch.empty_like(x)
+        dgate = None if gate is None else torch.empty_like(gate)
+        grads = [None if p is None else torch.empty_like(p) for p in params.values()]
+        ws = _workspace(lib.gt_block_norm_bwd_workspace_size(n, D, _dtype_code(x)), x.device)
+        _check(lib.gt_block_norm_bwd(n, D, _dtype_code(x), _NORMS[kind], _ptr(x), float(res_scale), _ptr(f), gk,
+                                     _ptr(gate), _ptr(w_post), _ptr(b_post), _ptr(w_pre), _ptr(stats), _ptr(dy),
+                                     _ptr(dz), _ptr(dx), _ptr(df), _ptr(dgate), *map(_ptr, grads), _ptr(ws),
+                                     ws.numel(), _stream(x.device)), "gt_block_norm_bwd")
+    return (dx, df, dgate, *grads)

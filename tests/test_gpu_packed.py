@@ -1,0 +1,357 @@
+"""GPU packed-sequence attention and the learned bias by buckets vs the fp64 oracle.
+
+Every result is held to the bound that the oracle derives for it (oracle/packed.py): fp32 dot products and sums in any
+order, weights and score gradients rounded to the features' type where they multiply a row, results rounded once."""
+
+import ctypes
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import attention as OA
+from oracle import packed as OP
+from synth import make_workload
+from synth.tensors import normal_tensor
+from tests.helpers import assert_close, dev_csr, dev_feat, host
+
+pytestmark = pytest.mark.gpu
+
+HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+LOWEST = float(np.finfo(np.float32).min)
+
+
+def say(*a):
+    print(*a, flush=True)
+    sys.stdout.flush()
+
+
+def ptrs(lens):
+    return np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+
+
+def make(lq, lk, H, Hkv, d, dtype, B=0, seed=0, extra=0):
+    """Host inputs (fp32 values of the dtype) and, with B, a table and bytes of buckets (1 in 12 beyond it)."""
+    shapes = ((sum(lq) + extra, H, d), (sum(lk) + extra, Hkv, d), (sum(lk) + extra, Hkv, d), (sum(lq) + extra, H, d))
+    q, k, v, do = (normal_tensor(s, (seed, d, t), dtype) for t, s in enumerate(shapes))
+    if not B:
+        return q, k, v, do, None, None
+    rng = np.random.default_rng(seed)
+    _, n = OP.pair_layout(lq, lk)
+    ids = rng.integers(0, B, size=n).astype(np.uint8)
+    far = rng.random(n) < 1 / 12
+    ids[far] = rng.integers(B, 256, size=int(far.sum()))
+    return q, k, v, do, rng.normal(size=(B, H)).astype(np.float32), ids
+
+
+def check(name, x, r, b):
+    x = np.asarray(x, dtype=np.float64)
+    fin = np.isfinite(r)
+    assert np.array_equal(x[~fin], r[~fin]), f"{name}: infinite values differ"
+    assert np.isfinite(x[fin]).all(), f"{name}: values that are not finite"
+    over = np.abs(x[fin] - r[fin]) - b[fin]
+    assert over.size == 0 or over.max() <= 0, (f"{name}: {int((over > 0).sum())}/{over.size} outside their bound, by "
+                                               f"up to {over.max():.3e} (largest error {np.abs(x[fin] - r[fin]).max():.3e})")
+
+
+def run(gt, lq, lk, H, Hkv, d, dtype, causal, inputs, scale):
+    q, k, v, do, table, ids = inputs
+    plan = gt.packed_plan(ptrs(lq), ptrs(lk), heads=H, kv_heads=Hkv, causal=causal)
+    Q, K, V, dO = (dev_feat(x, dtype) for x in (q, k, v, do))
+    if table is None:
+        O, L = gt.packed_attn_fwd(plan, Q, K, V, scale)
+        out = (O, L) + gt.packed_attn_bwd(plan, Q, K, V, O, dO, L, scale)
+    else:
+        T, I = torch.from_numpy(table).cuda(), torch.from_numpy(ids).cuda()
+        O, L = gt.packed_attn_fwd_bias(plan, Q, K, V, T, I, scale)
+        out = (O, L) + gt.packed_attn_bwd_bias(plan, Q, K, V, T, I, dO, L, scale)
+    torch.cuda.synchronize()
+    return out
+
+
+def compare(gt, lq, lk, H, Hkv, d, dtype, causal, B=0, seed=0, scale=None, inputs=None):
+    say("packed", lq if len(lq) < 12 else len(lq), lk if len(lk) < 12 else "", H, Hkv, d, dtype, causal, B)
+    inputs = make(lq, lk, H, Hkv, d, dtype, B, seed) if inputs is None else inputs
+    scale = 1.0 / np.sqrt(d) if scale is None else scale
+    out = run(gt, lq, lk, H, Hkv, d, dtype, causal, inputs, scale)
+    q, k, v, do, table, ids = inputs
+    r, b = OP.attn(ptrs(lq), ptrs(lk), q, k, v, np.float32(scale).astype(np.float64), causal, table, ids, do,
+                   HALF[dtype], exact_d=table is not None)
+    for name, x in zip(("O", "LSE", "dQ", "dK", "dV", "dtable"), out):
+        check(name, host(x), r[name], b[name])
+    return out, r
+
+
+SIZES = [
+    ([1], [1]), ([5], [3]), ([0, 1, 2, 0], [3, 0, 1, 0]), ([31, 32, 33], [31, 32, 33]),
+    ([63, 64, 65, 127, 128, 129], [129, 128, 127, 65, 64, 63]), ([257], [511]), ([1] * 9, [1, 7, 40, 64, 65, 200, 33, 0, 2]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("B", [0, 7])
+def test_sizes_where_tiles_end(gt, dtype, d, causal, B):
+    for n, (lq, lk) in enumerate(SIZES):
+        compare(gt, lq, lk, 2, 2, d, dtype, causal, B, seed=n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,Hkv", [(1, 1), (3, 3), (4, 2), (4, 1), (8, 1), (16, 1), (32, 2)])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("B", [0, 64])
+def test_grouped_heads(gt, dtype, H, Hkv, causal, B):
+    compare(gt, [1, 2, 17, 40, 3], [70, 2, 17, 45, 1], H, Hkv, 32, dtype, causal, B, seed=H)
+    compare(gt, [130], [150], H, Hkv, 64, dtype, causal, B, seed=H + 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [False, True])
+def test_long_and_many(gt, dtype, causal):
+    compare(gt, [1200, 3, 800], [1200, 2500, 700], 2, 1, 64, dtype, causal)
+    rng = np.random.default_rng(5)
+    n = [int(x) for x in rng.integers(0, 30, size=300)]
+    compare(gt, n, n, 4, 4, 32, dtype, causal, B=21)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_single_queries_over_long_keys(gt, dtype):
+    # read-out tokens and single-token serving: few rows, long walks
+    compare(gt, [1], [9001], 8, 8, 32, dtype, False)
+    compare(gt, [1, 1, 2], [5003, 1, 4096], 16, 2, 128, dtype, True)
+    compare(gt, [3], [6000], 4, 4, 64, dtype, True, B=5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 2.5])
+def test_any_scale(gt, dtype, scale):
+    compare(gt, [70], [90], 2, 2, 32, dtype, True, scale=scale)
+    compare(gt, [70], [90], 2, 2, 32, dtype, True, B=4, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_masks_that_leave_rows_empty(gt, dtype):
+    lq, lk, H, B = [50, 40], [50, 70], 2, 6
+    inputs = list(make(lq, lk, H, H, 32, dtype, B, seed=9))
+    table, ids = inputs[4], inputs[5]
+    at, _ = OP.pair_layout(lq, lk)
+    ids[at[0] + 3 * 64:at[0] + 5 * 64] = 255  # two queries without any pair
+    ids[at[1]:] = np.where(np.arange(len(ids) - at[1]) % 80 < 33, 200, ids[at[1]:])  # the first 33 keys of every row
+    table[2] = -np.inf  # a bucket that masks
+    table[3, 0] = LOWEST  # and one that all but does
+    out, r = compare(gt, lq, lk, H, H, 32, dtype, False, B, inputs=inputs)
+    assert np.isneginf(host(out[1])[3:5]).all() and (host(out[0])[3:5] == 0).all() and (host(out[2])[3:5] == 0).all()
+    assert (host(out[5])[2] == 0).all()
+    # every pair masked, of every sequence
+    ids[:] = B
+    out, _ = compare(gt, lq, lk, H, H, 32, dtype, True, B, inputs=inputs)
+    assert all((host(x) == 0).all() for n, x in enumerate(out) if n != 1) and np.isneginf(host(out[1])).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("level", [LOWEST, -1e30, -1e9, 1e6])
+def test_a_bias_that_swamps_the_scores_still_averages(gt, dtype, level):
+    # beside a bias this large an fp32 score holds nothing of <q, k> (or of log n): every pair weighs 1 / n
+    lq, lk, H = [37], [90], 2
+    q, k, v, do, _, _ = make(lq, lk, H, H, 32, dtype)
+    q, k = q * 0, k * 0
+    table = np.full((1, H), level, dtype=np.float32)
+    ids = np.zeros(OP.pair_layout(lq, lk)[1], dtype=np.uint8)
+    out = run(gt, lq, lk, H, H, 32, dtype, False, (q, k, v, do, table, ids), 0.2)
+    mean = v.astype(np.float64).mean(axis=0)
+    tol = 2 * HALF[dtype] + 128 * 2.0 ** -24
+    np.testing.assert_allclose(host(out[0]), np.broadcast_to(mean, out[0].shape), atol=tol * np.abs(v).max())
+    # dV_j = sum_i dO_i / n: half a step of each rounded weight and of the result, on the sum of |dO|
+    dv = np.broadcast_to(do.astype(np.float64).sum(axis=0) / 90, out[4].shape)
+    np.testing.assert_allclose(host(out[4]), dv, atol=2 * tol * np.abs(do).sum(axis=0).max() / 90)
+
+
+def test_a_query_of_nan_stays_in_its_sequence_and_ends_do_not_leak(gt):
+    # sequences 0 and 2 hold infinities and NaN everywhere: sequence 1, ragged against every tile, does not see them
+    for dtype in ("bf16", "f32"):
+        for lens in ([33, 45, 70], [200, 135, 9]):
+            for B in (0, 5):
+                say("neighbours", dtype, lens, B)
+                inputs = list(make(lens, lens, 2, 2, 64, dtype, B, seed=3))
+                p = ptrs(lens)
+                clean = [x if x is None else x.copy() for x in inputs]
+                for x in inputs[:4]:
+                    x[:p[1]], x[p[2]:] = np.nan, np.inf
+                a = run(gt, lens, lens, 2, 2, 64, dtype, True, inputs, 0.125)
+                b = run(gt, lens, lens, 2, 2, 64, dtype, True, clean, 0.125)
+                for x, y in zip(a[:5], b[:5]):
+                    assert torch.equal(x[p[1]:p[2]], y[p[1]:p[2]])
+
+
+@pytest.mark.parametrize("B", [0, 9])
+def test_slices_of_a_fused_projection(gt, B):
+    lq = [70, 3, 129]
+    for dtype in ("bf16", "f32"):
+        H, Hkv, d = 4, 2, 32
+        q, k, v, do, table, ids = inputs = make(lq, lq, H, Hkv, d, dtype, B)
+        want = run(gt, lq, lq, H, Hkv, d, dtype, True, inputs, 0.2)
+        wide = torch.full((sum(lq), H + 2 * Hkv + 1, d), float("nan"), dtype=want[0].dtype, device="cuda")
+        wide[:, :H], wide[:, H:H + Hkv], wide[:, H + Hkv:-1] = (dev_feat(x, dtype) for x in (q, k, v))
+        Q, K, V = wide[:, :H], wide[:, H:H + Hkv], wide[:, H + Hkv:-1]
+        plan, dO = gt.packed_plan(ptrs(lq), heads=H, kv_heads=Hkv, causal=True), dev_feat(do, dtype)
+        if B:
+            T, I = torch.from_numpy(table).cuda(), torch.from_numpy(ids).cuda()
+            O, L = gt.packed_attn_fwd_bias(plan, Q, K, V, T, I, 0.2)
+            got = (O, L) + gt.packed_attn_bwd_bias(plan, Q, K, V, T, I, dO, L, 0.2)
+        else:
+            O, L = gt.packed_attn_fwd(plan, Q, K, V, 0.2)
+            got = (O, L) + gt.packed_attn_bwd(plan, Q, K, V, O, dO, L, 0.2)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("B", [0, 9])
+def test_rows_behind_the_last_sequence(gt, B):
+    lq, lk, H, d = [40, 33], [60, 5], 2, 32
+    q, k, v, do, table, ids = make(lq, lk, H, H, d, "bf16", B, extra=7)
+    for x in (q, k, v, do):
+        x[-7:] = np.nan  # not read
+    plan = gt.packed_plan(ptrs(lq), ptrs(lk), heads=H)
+    Q, K, V, dO = (dev_feat(x, "bf16") for x in (q, k, v, do))
+    if B:
+        T, I = torch.from_numpy(table).cuda(), torch.from_numpy(ids).cuda()
+        O, L = gt.packed_attn_fwd_bias(plan, Q, K, V, T, I)
+        out = (O, L) + gt.packed_attn_bwd_bias(plan, Q, K, V, T, I, dO, L)
+    else:
+        O, L = gt.packed_attn_fwd(plan, Q, K, V)
+        out = (O, L) + gt.packed_attn_bwd(plan, Q, K, V, O, dO, L)
+    torch.cuda.synchronize()
+    for n, x in enumerate(out[:5]):
+        assert torch.isfinite(x[:-7].float()).all()
+        assert (x[-7:] == (-np.inf if n == 1 else 0)).all()
+    # the C call leaves such rows as they were
+    lib, code = gt.load_library(), gt.GT_BF16
+    O, L = torch.full_like(Q, 5.0), torch.full_like(out[1], 5.0)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    assert lib.gt_packed_attn_fwd(ctypes.byref(plan.c), d, code, Q.data_ptr(), H * d, K.data_ptr(), H * d, V.data_ptr(),
+                                  H * d, 0.1, O.data_ptr(), L.data_ptr(), ws.data_ptr(), ws.numel(),
+                                  torch.cuda.current_stream().cuda_stream) == gt.GT_OK
+    dQ, dK, dV = torch.full_like(Q, 5.0), torch.full_like(K, 5.0), torch.full_like(V, 5.0)
+    assert lib.gt_packed_attn_bwd(ctypes.byref(plan.c), d, code, Q.data_ptr(), H * d, K.data_ptr(), H * d, V.data_ptr(),
+                                  H * d, O.data_ptr(), dO.data_ptr(), L.data_ptr(), 0.1, dQ.data_ptr(), dK.data_ptr(),
+                                  dV.data_ptr(), ws.data_ptr(), ws.numel(),
+                                  torch.cuda.current_stream().cuda_stream) == gt.GT_OK
+    torch.cuda.synchronize()
+    for x in (O, L, dQ, dK, dV):
+        assert (x[-7:] == 5).all() and torch.isfinite(x.float()).all()
+
+
+def test_no_sequences(gt):
+    f = torch.zeros(0, 2, 32, dtype=torch.bfloat16, device="cuda")
+    plan = gt.packed_plan([0], heads=2)
+    O, L = gt.packed_attn_fwd(plan, f, f, f)
+    out = gt.packed_attn_bwd(plan, f, f, f, O, f, L)
+    T, I = torch.ones(3, 2, device="cuda"), torch.zeros(0, dtype=torch.uint8, device="cuda")
+    O, L = gt.packed_attn_fwd_bias(plan, f, f, f, T, I)
+    out = gt.packed_attn_bwd_bias(plan, f, f, f, T, I, f, L)
+    torch.cuda.synchronize()
+    assert O.shape == f.shape and (out[3] == 0).all()
+    # keys that no query reads: their gradients are zeros, not left over
+    k = torch.ones(5, 2, 32, dtype=torch.bfloat16, device="cuda")
+    plan = gt.packed_plan([0, 0], [0, 5], heads=2)
+    _, dk, dv = gt.packed_attn_bwd(plan, f, k, k, f, f, L[:0])
+    torch.cuda.synchronize()
+    assert (dk == 0).all() and (dv == 0).all()
+
+
+def test_same_results_again_and_on_another_stream(gt):
+    lq = [300, 20, 1, 77]
+    for dtype in ("bf16", "f32"):
+        for B in (0, 11):
+            inputs = make(lq, lq, 4, 2, 64, dtype, B)
+            a = run(gt, lq, lq, 4, 2, 64, dtype, True, inputs, 0.1)
+            side = torch.cuda.Stream()
+            with torch.cuda.stream(side):
+                b = run(gt, lq, lq, 4, 2, 64, dtype, True, inputs, 0.1)
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_captured_step_replays(gt):
+    lq, H, d, B = [150, 30, 33], 4, 32, 6
+    q, k, v, do, table, ids = make(lq, lq, H, 2, d, "bf16", B)
+    plan = gt.packed_plan(ptrs(lq), heads=H, kv_heads=2)
+    Q, K, V, dO = (dev_feat(x, "bf16") for x in (q, k, v, do))
+    T, I = torch.from_numpy(table).cuda(), torch.from_numpy(ids).cuda()
+
+    def step():
+        O, L = gt.packed_attn_fwd_bias(plan, Q, K, V, T, I)
+        return (O, L) + gt.packed_attn_bwd_bias(plan, Q, K, V, T, I, dO, L)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for turn in range(4):
+        Q.copy_(dev_feat(normal_tensor(q.shape, (turn, 1), "bf16"), "bf16"))
+        graph.replay()
+        got = [x.clone() for x in out]
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want)), turn
+
+
+@pytest.mark.parametrize("H", [1, 2, 4, 8, 16])
+@pytest.mark.parametrize("nnz,B", [(0, 3), (1, 1), (37, 5), (1000, 64), (70001, 21)])
+def test_edge_bias_and_its_gradient(gt, H, nnz, B):
+    say("edges", nnz, H, B)
+    rng = np.random.default_rng(nnz + H)
+    table, ids = rng.normal(size=(B, H)).astype(np.float32), rng.integers(0, B + 1, size=nnz).astype(np.uint8)
+    grad = rng.normal(size=(nnz, H)).astype(np.float32)
+    ids[rng.random(nnz) < 0.02] = 255
+    T, I, G = torch.from_numpy(table).cuda(), torch.from_numpy(ids).cuda(), torch.from_numpy(grad).cuda()
+    bias, dt = gt.bucket_bias_fwd(T, I), gt.bucket_bias_bwd(I, G, B)
+    again = gt.bucket_bias_bwd(I, G, B)
+    torch.cuda.synchronize()
+    assert np.array_equal(bias.cpu().numpy(), OP.bucket_bias(table, ids))
+    ref = OP.bucket_bias_grad(ids, grad, B)
+    # chains of at most 4,096 additions
+    bound = (min(nnz, 4096) + 4) * 2.0 ** -24 * OP.bucket_bias_grad(ids, np.abs(grad), B)
+    check("dtable", dt.cpu().numpy(), ref, bound)
+    assert torch.equal(dt, again)
+
+
+def test_edge_bias_on_views_that_start_anywhere(gt):
+    rng = np.random.default_rng(1)
+    ids = torch.from_numpy(rng.integers(0, 5, size=1003).astype(np.uint8)).cuda()[3:]
+    table = torch.randn(5, 4, device="cuda")
+    grad = torch.randn(4 * 1000 + 1, device="cuda")[1:].view(1000, 4)
+    bias, dt = gt.bucket_bias_fwd(table, ids), gt.bucket_bias_bwd(ids, grad, 5)
+    torch.cuda.synchronize()
+    assert torch.equal(bias, table[ids.long()])
+    ref = OP.bucket_bias_grad(ids.cpu().numpy(), grad.cpu().numpy(), 5)
+    np.testing.assert_allclose(dt.cpu().numpy(), ref, atol=1004 * 2.0 ** -24 * float(grad.abs().sum(0).max()))
+
+
+def test_sparse_layer_with_a_learned_bias(gt):
+    # the learned bias feeding the sparse layer's bias calls, on a plan with dense tiles, forward and backward
+    w = make_workload("c5", 0.02)
+    g, B = w.graph, 21
+    q, k, v, do = w.tensors()
+    scale = 1.0 / np.sqrt(w.dim)
+    rng = np.random.default_rng(4)
+    table, ids = rng.normal(size=(B, w.heads)).astype(np.float32), rng.integers(0, B, size=g.nnz).astype(np.uint8)
+    rp, cl = dev_csr(g.rowptr, g.col)
+    plan = gt.build_tiles(rp, cl, 128, 10000, edge_positions=True)
+    Q, K, V, dO = (dev_feat(x, "bf16") for x in (q, k, v, do))
+    T, I = torch.from_numpy(table).cuda(), torch.from_numpy(ids).cuda()
+    bias = gt.bucket_bias_fwd(T, I)
+    O, L = gt.sparse_attn_fwd_bias(plan, Q, K, V, bias, scale)
+    dQ, dK, dV, dB = gt.sparse_attn_bwd_bias(plan, gt.edge_map(plan), Q, K, V, bias, dO, L, scale)
+    dT = gt.bucket_bias_bwd(I, dB, B)
+    torch.cuda.synchronize()
+    b64 = OP.bucket_bias(table, ids)
+    O_ref, _ = OA.sparse_attn_fwd(g.rowptr, g.col, q, k, v, scale, bias=b64)
+    ref = OA.sparse_attn_bwd(g.rowptr, g.col, q, k, v, do, scale, bias=b64)
+    for name, x, r in zip(("O", "dQ", "dK", "dV"), (O, dQ, dK, dV), (O_ref, *ref[:3])):
+        assert_close(host(x), r, "bf16", name)
+    # the edges' own tolerance (bf16, 2e-2 + 1e-2 |r|), summed over each bucket's edges
+    bound = OP.bucket_bias_grad(ids, 2e-2 + 1e-2 * np.abs(ref[3]), B)
+    check("dtable", dT.cpu().numpy(), OP.bucket_bias_grad(ids, ref[3], B), bound)

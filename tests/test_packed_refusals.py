@@ -1,0 +1,219 @@
+"""Packed attention, the learned bias and the block norms refuse what they do not take, on the host (no GPU)."""
+
+import ctypes
+import os
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import packed as OP
+from paper_2407_14106_amd import gt
+
+FAKE = ctypes.c_void_p(0x1000)  # never dereferenced
+ODD = ctypes.c_void_p(0x1004)
+BIG = 1 << 40
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(gt.LIB_PATH):
+        from paper_2407_14106_amd import build
+
+        build.build()
+    return gt.load_library()
+
+
+def ptrs(*lens):
+    return np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+
+
+def init(lib, q, k, H=4, Hkv=4, causal=0, n=None):
+    c = gt.GtPackedPlan()
+    q, k = np.ascontiguousarray(q, dtype=np.int64), np.ascontiguousarray(k, dtype=np.int64)
+    st = lib.gt_packed_plan_init(len(q) - 1 if n is None else n, q.ctypes.data, k.ctypes.data, H, Hkv, causal,
+                                 ctypes.byref(c))
+    return st, c
+
+
+@pytest.mark.parametrize("q,k,H,Hkv,want", [
+    ([1, 4], [0, 4], 4, 4, gt.GT_ERR_OUT_OF_RANGE), ([0, 4], [2, 4], 4, 4, gt.GT_ERR_OUT_OF_RANGE),
+    ([0, 4, 3], [0, 4, 8], 4, 4, gt.GT_ERR_UNSORTED), ([0, 4, 8], [0, 4, 2], 4, 4, gt.GT_ERR_UNSORTED),
+    ([0, 1 << 31], [0, 4], 4, 4, gt.GT_ERR_INVALID_ARG), ([0, 4], [0, 1 << 33], 4, 4, gt.GT_ERR_INVALID_ARG),
+    ([0, 4], [0, 4], 6, 4, gt.GT_ERR_UNSUPPORTED), ([0, 4], [0, 4], 6, 2, gt.GT_ERR_UNSUPPORTED),
+    ([0, 4], [0, 4], 32, 1, gt.GT_ERR_UNSUPPORTED), ([0, 4], [0, 4], 0, 1, gt.GT_ERR_UNSUPPORTED),
+    ([0, 4], [0, 4], 4, 0, gt.GT_ERR_UNSUPPORTED), ([0, 4], [0, 4], 512, 512, gt.GT_ERR_UNSUPPORTED),
+    ([0, (1 << 30)], [0, 4], 16, 1, gt.GT_ERR_UNSUPPORTED), ([0, 4], [0, 4], -4, -4, gt.GT_ERR_UNSUPPORTED)])
+def test_plan_refusals(lib, q, k, H, Hkv, want):
+    st, c = init(lib, q, k, H, Hkv)
+    assert st == want, lib.gt_last_error()
+    assert c.item_bytes == 0 and c.layout[31] == 0  # no call takes what init refused
+
+
+def test_plan_null_and_changed_arguments(lib):
+    q = ptrs(5, 40, 300)
+    assert lib.gt_packed_plan_init(3, None, q.ctypes.data, 4, 4, 0, ctypes.byref(gt.GtPackedPlan())) == gt.GT_ERR_INVALID_ARG
+    assert lib.gt_packed_plan_init(3, q.ctypes.data, q.ctypes.data, 4, 4, 0, None) == gt.GT_ERR_INVALID_ARG
+    st, c = init(lib, q, q)
+    assert st == gt.GT_OK and c.nq == c.nk == 345
+    host = np.zeros(c.item_bytes, dtype=np.uint8)
+    fill = lambda p, n=3, b=c.item_bytes: lib.gt_packed_plan_fill(n, p.ctypes.data, q.ctypes.data, ctypes.byref(c),  # noqa: E731
+                                                                   host.ctypes.data, b)
+    assert fill(q) == gt.GT_OK
+    assert fill(q, b=c.item_bytes - 1) == gt.GT_ERR_WORKSPACE
+    assert fill(q, n=2) == gt.GT_ERR_INVALID_ARG
+    assert fill(ptrs(5, 200, 140)) == gt.GT_ERR_INVALID_ARG  # other tiles
+    assert lib.gt_packed_plan_fill(3, q.ctypes.data, q.ctypes.data, ctypes.byref(gt.GtPackedPlan()), host.ctypes.data,
+                                   BIG) == gt.GT_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("causal", [0, 1])
+@pytest.mark.parametrize("group", [1, 4])
+def test_plan_covers_every_row_and_key_once(lib, causal, group):
+    lq = [0, 1, 7, 32, 33, 129, 0, 300, 5, 1, 700]
+    lk = [4, 0, 9, 40, 31, 129, 0, 100, 2000, 4097, 701]
+    q, k = ptrs(*lq), ptrs(*lk)
+    st, c = init(lib, q, k, 2 * group, 2, causal)
+    assert st == gt.GT_OK
+    host = np.zeros(c.item_bytes, dtype=np.uint8)
+    assert lib.gt_packed_plan_fill(len(lq), q.ctypes.data, k.ctypes.data, ctypes.byref(c), host.ctypes.data,
+                                   c.item_bytes) == gt.GT_OK
+    assert c.pair_bytes == OP.pair_layout(lq, lk)[1]
+    at, _ = OP.pair_layout(lq, lk)
+    lists = [(c.layout[2 * i], c.layout[2 * i + 1]) for i in range(4)]
+    items = [host[a:a + 40 * n].view(np.int32).reshape(n, 10) for a, n in lists]
+    by_seq = {(int(q[s]), int(k[s]), lq[s], lk[s]): s for s in range(len(lq))}
+
+    def walked(lists, owned, streamed, needs):
+        """Every owned index is in one tile, and its items walk each partner that it needs exactly once."""
+        seen = [np.zeros((owned(s),), dtype=np.int64) for s in range(len(lq))]
+        for tile, rows in lists:
+            for it in rows:
+                q0, l_q, k0, l_k, t, s0, s1, slot = (int(x) for x in it[:8])
+                s = by_seq[(q0, k0, l_q, l_k)]
+                assert int(it[8:10].view(np.int64)[0]) == at[s]
+                assert 0 <= s0 <= max(s0, s1) <= max(streamed(s), s0) and t % 32 == 0 and t < max(1, owned(s))
+                for x in range(t, min(owned(s), t + tile)):
+                    lo, hi = needs(s, x)
+                    seen[s][x] += max(0, min(hi, s1) - max(lo, s0))
+        for s in range(len(lq)):
+            for x in range(owned(s)):
+                lo, hi = needs(s, x)
+                assert seen[s][x] == max(0, hi - lo), (s, x)
+
+    off = [b - a for a, b in zip(lq, lk)]
+    row_needs = lambda s, r: (0, max(0, min(lk[s], off[s] + r // group + 1)) if causal else lk[s])  # noqa: E731
+    key_needs = lambda s, j: (min(lq[s] * group, max(0, j - off[s]) * group) if causal else 0, lq[s] * group)  # noqa: E731
+    walked([(32, items[0]), (128, items[1])], lambda s: lq[s] * group, lambda s: lk[s], row_needs)
+    walked([(32, items[2]), (128, items[3])], lambda s: lk[s], lambda s: lq[s] * group, key_needs)
+
+
+def attn_args(c, **kw):
+    a = dict(plan=ctypes.byref(c), d=32, dtype=gt.GT_BF16, Q=FAKE, ldq=128, K=FAKE, ldk=128, V=FAKE, ldv=128)
+    a.update(kw)
+    return list(a.values())
+
+
+BAD = [(dict(plan=None), gt.GT_ERR_INVALID_ARG), (dict(d=48), gt.GT_ERR_UNSUPPORTED), (dict(d=256), gt.GT_ERR_UNSUPPORTED),
+       (dict(dtype=2), gt.GT_ERR_UNSUPPORTED), (dict(Q=None), gt.GT_ERR_INVALID_ARG), (dict(K=None), gt.GT_ERR_INVALID_ARG),
+       (dict(V=None), gt.GT_ERR_INVALID_ARG), (dict(ldq=127), gt.GT_ERR_INVALID_ARG), (dict(ldk=-128), gt.GT_ERR_INVALID_ARG),
+       (dict(ldv=132), gt.GT_ERR_UNSUPPORTED), (dict(K=ODD), gt.GT_ERR_UNSUPPORTED), (dict(ldk=1 << 31), gt.GT_ERR_INVALID_ARG)]
+
+
+@pytest.mark.parametrize("kw,want", BAD)
+def test_attention_refusals(lib, kw, want):
+    st, c = init(lib, ptrs(5, 40), ptrs(6, 40))
+    c.items = 0x1000
+    a = attn_args(c, **kw)
+    assert lib.gt_packed_attn_fwd(*a, 0.1, FAKE, FAKE, FAKE, BIG, None) == want
+    assert lib.gt_packed_attn_fwd_bias(*a, FAKE, 8, FAKE, 0.1, FAKE, FAKE, FAKE, BIG, None) == want
+    assert lib.gt_packed_attn_bwd(*a, FAKE, FAKE, FAKE, 0.1, FAKE, FAKE, FAKE, FAKE, BIG, None) == want
+    assert lib.gt_packed_attn_bwd_bias(*a, FAKE, 8, FAKE, FAKE, FAKE, 0.1, FAKE, FAKE, FAKE, FAKE, FAKE, BIG,
+                                       None) == want
+
+
+def test_attention_refuses_missing_outputs_tables_and_workspaces(lib):
+    st, c = init(lib, ptrs(5, 40), ptrs(6, 40))
+    a = attn_args(c)
+    E = gt.GT_ERR_INVALID_ARG
+    assert lib.gt_packed_attn_fwd(*a, 0.1, FAKE, FAKE, FAKE, BIG, None) == E  # items not entered
+    assert b"items" in lib.gt_last_error()
+    c.items = 0x1000
+    assert lib.gt_packed_attn_fwd(*a, 0.1, None, FAKE, FAKE, BIG, None) == E
+    assert lib.gt_packed_attn_fwd(*a, 0.1, FAKE, None, FAKE, BIG, None) == E
+    assert lib.gt_packed_attn_fwd(*a, 0.1, ODD, FAKE, FAKE, BIG, None) == gt.GT_ERR_UNSUPPORTED
+    for table, B, ids, want in ((None, 8, FAKE, E), (FAKE, 8, None, E), (FAKE, 0, FAKE, gt.GT_ERR_UNSUPPORTED),
+                                (FAKE, 65, FAKE, gt.GT_ERR_UNSUPPORTED), (FAKE, 8, ODD, gt.GT_ERR_UNSUPPORTED)):
+        assert lib.gt_packed_attn_fwd_bias(*a, table, B, ids, 0.1, FAKE, FAKE, FAKE, BIG, None) == want
+        assert lib.gt_packed_attn_bwd_bias(*a, table, B, ids, FAKE, FAKE, 0.1, FAKE, FAKE, FAKE, FAKE, FAKE, BIG,
+                                           None) == want
+    full = [FAKE] * 3 + [0.1] + [FAKE] * 3  # O, dO, LSE, scale, dQ, dK, dV
+    for x in (0, 1, 2, 4, 5, 6):
+        args = list(full)
+        args[x] = None
+        assert lib.gt_packed_attn_bwd(*a, *args, FAKE, BIG, None) == E
+    need = lib.gt_packed_attn_bwd_workspace_size(ctypes.byref(c), 32, gt.GT_BF16)
+    assert need >= 45 * 4 * 4
+    assert lib.gt_packed_attn_bwd(*a, *full, FAKE, need - 1, None) == gt.GT_ERR_WORKSPACE
+    assert lib.gt_packed_attn_bwd(*a, *full, None, need, None) == E
+    need = lib.gt_packed_attn_bwd_bias_workspace_size(ctypes.byref(c), 32, gt.GT_BF16, 8)
+    bias = [FAKE, 8, FAKE, FAKE, FAKE, 0.1, FAKE, FAKE, FAKE]
+    assert lib.gt_packed_attn_bwd_bias(*a, *bias, FAKE, FAKE, need - 1, None) == gt.GT_ERR_WORKSPACE
+    assert lib.gt_packed_attn_bwd_bias(*a, *bias, None, FAKE, need, None) == E
+    assert lib.gt_packed_attn_bwd_bias_workspace_size(ctypes.byref(c), 32, gt.GT_BF16, 65) == 0
+
+
+def test_edge_bias_refusals(lib):
+    E, U = gt.GT_ERR_INVALID_ARG, gt.GT_ERR_UNSUPPORTED
+    for nnz, H, B, t, i, o, want in ((-1, 8, 4, FAKE, FAKE, FAKE, E), (1 << 32, 8, 4, FAKE, FAKE, FAKE, E),
+                                     (9, 3, 4, FAKE, FAKE, FAKE, U), (9, 32, 4, FAKE, FAKE, FAKE, U),
+                                     (9, 8, 0, FAKE, FAKE, FAKE, U), (9, 8, 65, FAKE, FAKE, FAKE, U),
+                                     (9, 8, 4, None, FAKE, FAKE, E), (9, 8, 4, FAKE, None, FAKE, E),
+                                     (9, 8, 4, FAKE, FAKE, None, E)):
+        assert lib.gt_bucket_bias_fwd(nnz, H, B, t, i, o, None) == want
+        if t is not None:
+            assert lib.gt_bucket_bias_bwd(nnz, H, B, i, o, FAKE, FAKE, BIG, None) == want
+    need = lib.gt_bucket_bias_bwd_workspace_size(1000, 8, 4)
+    assert need > 0
+    assert lib.gt_bucket_bias_bwd(1000, 8, 4, FAKE, FAKE, FAKE, FAKE, need - 1, None) == gt.GT_ERR_WORKSPACE
+    assert lib.gt_bucket_bias_bwd(1000, 8, 4, FAKE, FAKE, None, FAKE, need, None) == E
+    assert lib.gt_bucket_bias_bwd(1000, 8, 4, FAKE, FAKE, FAKE, None, need, None) == E
+
+
+def test_block_norm_refusals(lib):
+    E, U = gt.GT_ERR_INVALID_ARG, gt.GT_ERR_UNSUPPORTED
+    base = dict(n=9, D=64, dt=gt.GT_BF16, norm=0, eps=1e-5, x=FAKE, a=1.0, f=FAKE, kind=0, gate=None, w1=None, b1=None,
+                w2=None, b2=None, y=FAKE, z=FAKE, stats=FAKE)
+    for kw, want in ((dict(n=-1), E), (dict(n=1 << 31), E), (dict(D=0), U), (dict(D=8193), U), (dict(dt=2), U),
+                     (dict(norm=2), U), (dict(kind=4), U), (dict(kind=-1), U), (dict(kind=1), E), (dict(kind=2), E),
+                     (dict(eps=0.0), E), (dict(eps=float("nan")), E), (dict(x=None), E), (dict(f=None), E),
+                     (dict(y=None), E), (dict(z=None), E), (dict(stats=None), E), (dict(stats=ODD), U)):
+        assert lib.gt_block_norm_fwd(*{**base, **kw}.values(), None) == want, kw
+    base = dict(n=9, D=64, dt=gt.GT_BF16, norm=0, x=FAKE, a=1.0, f=FAKE, kind=2, gate=FAKE, w1=None, b1=None, w2=None,
+                stats=FAKE, dy=FAKE, dz=FAKE, dx=FAKE, df=FAKE, dgate=FAKE, d1=None, d2=None, d3=None, d4=None, ws=FAKE,
+                bytes=BIG)
+    for kw, want in ((dict(n=-1), E), (dict(D=9000), U), (dict(norm=7), U), (dict(dgate=None), E), (dict(gate=None), E),
+                     (dict(x=None), E), (dict(f=None), E), (dict(stats=None), E), (dict(dy=None), E), (dict(dz=None), E),
+                     (dict(dx=None), E), (dict(df=None), E), (dict(ws=None), E), (dict(bytes=16), gt.GT_ERR_WORKSPACE),
+                     (dict(n=0, kind=1, dgate=None), E)):
+        assert lib.gt_block_norm_bwd(*{**base, **kw}.values(), None) == want, kw
+
+
+def test_binding_refuses_bad_tensors():
+    x = torch.zeros(4, 8)
+    with pytest.raises(ValueError):
+        gt.block_norm_fwd(x, x)  # not on the GPU
+    with pytest.raises(ValueError):
+        gt.bucket_bias_fwd(torch.zeros(4, 8), torch.zeros(5, dtype=torch.uint8))
+    with pytest.raises(ValueError):
+        gt.packed_plan([0, 4], [0, 4, 8], heads=4, device="cpu")
+    with pytest.raises(ValueError):
+        gt.packed_plan([[0, 4]], heads=4, device="cpu")
+    with pytest.raises(ValueError):
+        gt.packed_plan(torch.tensor([0.0, 4.0]), heads=4, device="cpu")
+    with pytest.raises(gt.GtError):
+        gt.packed_plan([0, 4, 2], heads=4, device="cpu")
+    plan = gt.packed_plan([0, 4, 9], heads=4, device="cpu")
+    f = torch.zeros(9, 4, 32)
+    with pytest.raises(ValueError):
+        gt.packed_attn_fwd(plan, f, f, f)  # not on the GPU
