@@ -26,8 +26,8 @@ gt_status check(const char* who, const gt_packed_plan* p, int32_t d, gt_dtype dt
     if ((p->nq > 0 && !Q) || (p->nk > 0 && (!K || !V))) return fail(GT_ERR_INVALID_ARG, w + ": null pointer");
     const int64_t piece = dt == GT_BF16 ? 8 : 4;
     if (ldq < int64_t(p->H) * d || ldk < int64_t(p->Hkv) * d || ldv < int64_t(p->Hkv) * d ||
-        ldq >= (int64_t(1) << 31) || ldk >= (int64_t(1) << 31) || ldv >= (int64_t(1) << 31))
-        return fail(GT_ERR_INVALID_ARG, w + ": a node stride below the node's features, or above 2^31 - 1");
+        ldq >= (int64_t(1) << 23) || ldk >= (int64_t(1) << 23) || ldv >= (int64_t(1) << 23))
+        return fail(GT_ERR_INVALID_ARG, w + ": a node stride below the node's features, or 2^23 or more");
     if (off16(Q) || off16(K) || off16(V) || ldq % piece || ldk % piece || ldv % piece)
         return fail(GT_ERR_UNSUPPORTED, w + ": features must lie at multiples of 16 bytes");
     return GT_OK;
@@ -49,7 +49,7 @@ PackedArgs args(const gt_packed_plan* p, const void* Q, int64_t ldq, const void*
     a.gs = ilog2(p->H / p->Hkv);
     a.causal = p->causal;
     a.Q = Q, a.K = K, a.V = V;
-    a.ldq = ldq, a.ldk = ldk, a.ldv = ldv;
+    a.ldq = uint32_t(ldq), a.ldk = uint32_t(ldk), a.ldv = uint32_t(ldv);
     a.scale = scale;
     return a;
 }
@@ -58,22 +58,45 @@ gt_status run_fwd(const gt_packed_plan* p, int32_t d, gt_dtype dt, PackedArgs a,
     return dt == GT_BF16 ? packed_fwd<uint16_t>(p, d, a, s) : packed_fwd<float>(p, d, a, s);
 }
 
+// The largest slot of each pass times the slots there are.
+int64_t row_slots(const gt_packed_plan* p) { return p->layout[kRowSlotsAt] * p->Hkv; }
+int64_t key_slots(const gt_packed_plan* p) { return p->layout[kKeySlotsAt] * p->Hkv; }
+
 struct BwdWs {
-    float *Dv, *Lg = nullptr, *hist = nullptr;
-    BwdWs(Ws& w, const gt_packed_plan* p, int32_t B) {
+    float *Dv, *Lg = nullptr, *slots, *hist = nullptr;
+    BwdWs(Ws& w, const gt_packed_plan* p, int32_t d, gt_dtype dt, int32_t B) {
         Dv = w.take<float>(size_t(p->nq) * p->H);
-        if (B > 0) {
-            Lg = w.take<float>(size_t(p->nq) * p->H);
-            hist = w.take<float>(size_t(packed_items(p, kRowsSmall) + packed_items(p, kRowsLarge)) * p->H * B);
-        }
+        const int64_t a = row_slots(p) * row_slot_floats(d), b = key_slots(p) * key_slot_floats(d);
+        slots = w.take<float>(size_t(a > b ? a : b));
+        if (B == 0) return;
+        Lg = w.take<float>(size_t(p->nq) * p->H);
+        const int row = d * (dt == GT_BF16 ? 2 : 4);
+        int64_t blocks = packed_items(p, kPairs) > 0 ? pair_blocks(p, row) * pair_waves(row) : 0;
+        for (int l = kRowsFew; l <= kRows256; ++l) blocks += packed_items(p, l) * p->Hkv * (l == kRows256 ? 2 : 1);
+        hist = w.take<float>(size_t(blocks) * (p->H / p->Hkv) * B);
     }
 };
 
-size_t bwd_ws(const gt_packed_plan* p, int32_t B) {
-    if (!packed_plan_ok(p)) return 0;
+size_t bwd_ws(const gt_packed_plan* p, int32_t d, gt_dtype dt, int32_t B) {
+    if (!packed_plan_ok(p) || d < 1 || d > 128) return 0;
     Ws w(nullptr);
-    BwdWs b(w, p, B);
+    BwdWs b(w, p, d, dt, B);
     return w.size();
+}
+
+size_t fwd_ws(const gt_packed_plan* p, int32_t d) {
+    if (!packed_plan_ok(p) || d < 1 || d > 128) return 0;
+    Ws w(nullptr);
+    w.take<float>(size_t(row_slots(p) * fwd_slot_floats(d)));
+    return w.size();
+}
+
+gt_status take_fwd_ws(const char* who, const gt_packed_plan* p, int32_t d, PackedArgs& a, void* ws, size_t ws_bytes) {
+    const size_t need = fwd_ws(p, d);
+    if (ws_bytes < need) return fail(GT_ERR_WORKSPACE, std::string(who) + ": workspace too small");
+    if (need > 0 && !ws) return fail(GT_ERR_INVALID_ARG, std::string(who) + ": null pointer");
+    a.slots = static_cast<float*>(ws);
+    return GT_OK;
 }
 
 gt_status run_bwd(const char* who, const gt_packed_plan* p, int32_t d, gt_dtype dt, PackedArgs a, const void* O,
@@ -84,25 +107,27 @@ gt_status run_bwd(const char* who, const gt_packed_plan* p, int32_t d, gt_dtype 
         return fail(GT_ERR_INVALID_ARG, w + ": null pointer");
     if (off16(O) || off16(dO) || off16(dQ) || off16(dK) || off16(dV))
         return fail(GT_ERR_UNSUPPORTED, w + ": features must lie at multiples of 16 bytes");
-    const size_t need = bwd_ws(p, a.B);
+    const size_t need = bwd_ws(p, d, dt, a.B);
     if (ws_bytes < need) return fail(GT_ERR_WORKSPACE, w + ": workspace too small");
     if (need > 0 && !ws) return fail(GT_ERR_INVALID_ARG, w + ": null pointer");
     Ws wk(ws);
-    const BwdWs b(wk, p, a.B);
+    const BwdWs b(wk, p, d, dt, a.B);
     a.O = O, a.dO = dO;
     a.LSE = const_cast<float*>(LSE);
     a.out0 = dQ, a.out1 = dK, a.out2 = dV;
-    a.Dv = b.Dv, a.Lg = b.Lg, a.hist = b.hist;
+    a.Dv = b.Dv, a.Lg = b.Lg, a.slots = b.slots, a.hist = b.hist;
     return dt == GT_BF16 ? packed_bwd<uint16_t>(p, d, a, dtable, s) : packed_bwd<float>(p, d, a, dtable, s);
 }
 
 }  // namespace
 
-extern "C" size_t gt_packed_attn_fwd_workspace_size(const gt_packed_plan*, int32_t, gt_dtype) { return 0; }
+extern "C" size_t gt_packed_attn_fwd_workspace_size(const gt_packed_plan* p, int32_t d, gt_dtype) {
+    return fwd_ws(p, d);
+}
 
 extern "C" gt_status gt_packed_attn_fwd(const gt_packed_plan* p, int32_t d, gt_dtype dt, const void* Q, int64_t ldq,
                                         const void* K, int64_t ldk, const void* V, int64_t ldv, float scale, void* O,
-                                        float* LSE, void*, size_t, hipStream_t s) {
+                                        float* LSE, void* ws, size_t ws_bytes, hipStream_t s) {
     const char* who = "gt_packed_attn_fwd";
     gt_status st = check(who, p, d, dt, Q, ldq, K, ldk, V, ldv);
     if (st != GT_OK) return st;
@@ -111,15 +136,18 @@ extern "C" gt_status gt_packed_attn_fwd(const gt_packed_plan* p, int32_t d, gt_d
     PackedArgs a = args(p, Q, ldq, K, ldk, V, ldv, scale);
     a.out0 = O;
     a.LSE = LSE;
+    if ((st = take_fwd_ws(who, p, d, a, ws, ws_bytes)) != GT_OK) return st;
     return run_fwd(p, d, dt, a, s);
 }
 
-extern "C" size_t gt_packed_attn_fwd_bias_workspace_size(const gt_packed_plan*, int32_t, gt_dtype, int32_t) { return 0; }
+extern "C" size_t gt_packed_attn_fwd_bias_workspace_size(const gt_packed_plan* p, int32_t d, gt_dtype, int32_t) {
+    return fwd_ws(p, d);
+}
 
 extern "C" gt_status gt_packed_attn_fwd_bias(const gt_packed_plan* p, int32_t d, gt_dtype dt, const void* Q,
                                              int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
                                              const float* table, int32_t B, const uint8_t* ids, float scale, void* O,
-                                             float* LSE, void*, size_t, hipStream_t s) {
+                                             float* LSE, void* ws, size_t ws_bytes, hipStream_t s) {
     const char* who = "gt_packed_attn_fwd_bias";
     gt_status st = check(who, p, d, dt, Q, ldq, K, ldk, V, ldv);
     if (st == GT_OK) st = check_bias(who, p, table, B, ids);
@@ -130,10 +158,13 @@ extern "C" gt_status gt_packed_attn_fwd_bias(const gt_packed_plan* p, int32_t d,
     a.out0 = O;
     a.LSE = LSE;
     a.table = table, a.B = B, a.ids = ids;
+    if ((st = take_fwd_ws(who, p, d, a, ws, ws_bytes)) != GT_OK) return st;
     return run_fwd(p, d, dt, a, s);
 }
 
-extern "C" size_t gt_packed_attn_bwd_workspace_size(const gt_packed_plan* p, int32_t, gt_dtype) { return bwd_ws(p, 0); }
+extern "C" size_t gt_packed_attn_bwd_workspace_size(const gt_packed_plan* p, int32_t d, gt_dtype dt) {
+    return bwd_ws(p, d, dt, 0);
+}
 
 extern "C" gt_status gt_packed_attn_bwd(const gt_packed_plan* p, int32_t d, gt_dtype dt, const void* Q, int64_t ldq,
                                         const void* K, int64_t ldk, const void* V, int64_t ldv, const void* O,
@@ -146,8 +177,8 @@ extern "C" gt_status gt_packed_attn_bwd(const gt_packed_plan* p, int32_t d, gt_d
                    ws_bytes, s);
 }
 
-extern "C" size_t gt_packed_attn_bwd_bias_workspace_size(const gt_packed_plan* p, int32_t, gt_dtype, int32_t B) {
-    return B < 1 || B > GT_MAX_BUCKETS ? 0 : bwd_ws(p, B);
+extern "C" size_t gt_packed_attn_bwd_bias_workspace_size(const gt_packed_plan* p, int32_t d, gt_dtype dt, int32_t B) {
+    return B < 1 || B > GT_MAX_BUCKETS ? 0 : bwd_ws(p, d, dt, B);
 }
 
 extern "C" gt_status gt_packed_attn_bwd_bias(const gt_packed_plan* p, int32_t d, gt_dtype dt, const void* Q,

@@ -8,36 +8,172 @@
 namespace gt {
 namespace {
 
+// Pairs: a sequence of at most 32 rows and 32 keys, all of its backward by one
+// wavefront from one reading of Q, K, V and dO: the weights P and dS of the one
+// block, D from them, dQ; then the block turned round through LDS, dK and dV.
+// With a bias a wavefront keeps to one head and goes through its sequences, its
+// part of the table's gradient in LDS.
+template <typename T, int D, bool BIAS>
+__global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair_bwd(PackedArgs a) {
+    using B = Blk<T, D>;
+    using S = Blk<T, 32>;
+    constexpr int W = pair_waves(D * int(sizeof(T)));
+    __shared__ __attribute__((aligned(16))) T s_q[W][B::kElems], s_k[W][B::kElems], s_v[W][B::kElems], s_g[W][B::kElems];
+    extern __shared__ float s_dyn[];
+    const int lane = lane_id(), wave = uniform(int(threadIdx.x) / kWave);
+    T *sQ = s_q[wave], *sK = s_k[wave], *sV = s_v[wave], *sG = s_g[wave];
+    const int gs = a.gs, gm = (1 << gs) - 1;
+    const uint32_t first = blockIdx.x * W + wave, step = gridDim.x * W, units = uint32_t(a.n_items) * uint32_t(a.Hkv);
+    const int hk = int(first % uint32_t(a.Hkv));  // of every unit: step is a multiple of Hkv
+    float* tab = s_dyn + wave * (kTableStride << gs);
+    float* hist = s_dyn + W * (kTableStride << gs) + wave * (a.B + 1) * kWave;
+    if constexpr (BIAS) {
+        load_table<kWave>(tab, a, hk, lane);
+        for (int b = 0; b <= a.B; ++b) hist[b * kWave + lane] = 0.f;
+    }
+    for (uint32_t unit = first; unit < units; unit += step) {
+        const PackedItem it = a.items[unit / uint32_t(a.Hkv)];
+        const int R = it.lq << gs, off = it.lk - it.lq;
+        const int64_t row_at = int64_t(it.q0) * a.H + (hk << gs), key_at = int64_t(it.k0) * a.Hkv + hk;
+        const bool some = R > 0 && it.lk > 0;
+        const int r = lane & 31, q = r >> gs;
+        float L = 0.f;
+        uint4 ids;
+        if (some) {
+            B::template fetch<1>(sK, static_cast<const T*>(a.K) + int64_t(it.k0) * a.ldk + hk * D, it.lk, 0, lane,
+                                 [&](int x) { return __umul24(x, a.ldk); });
+            B::template fetch<1>(sV, static_cast<const T*>(a.V) + int64_t(it.k0) * a.ldv + hk * D, it.lk, 0, lane,
+                                 [&](int x) { return __umul24(x, a.ldv); });
+            B::template fetch<1>(sQ, static_cast<const T*>(a.Q) + int64_t(it.q0) * a.ldq + (hk << gs) * D, R, 0, lane,
+                                 [&](int x) { return __umul24(x >> gs, a.ldq) + uint32_t((x & gm) * D); });
+            B::template fetch<1>(sG, static_cast<const T*>(a.dO) + row_at * D, R, 0, lane,
+                                 [&](int x) { return uint32_t(((x >> gs) * a.H + (x & gm)) * D); });
+            if (r < R) L = a.LSE[row_at + q * a.H + (r & gm)];
+            if (L == -kInf) L = 0.f;  // an empty row: every score is masked
+            if constexpr (BIAS)
+                ids = load_ids(a.ids + it.pair + (r < R ? q : it.lq - 1) * ids_width(it.lk), 0, it.lk, lane);
+        }
+        wave_done();
+        f32x16_t dq[1][D / 32], dk[1][D / 32], dv[1][D / 32];
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) dq[0][db] = dk[0][db] = dv[0][db] = splat16(0.f);
+        if (some) {
+            f32x16_t s[1] = {splat16(0.f)}, dp[1] = {splat16(0.f)};
+            {
+                typename B::Row own[1];
+                own[0].staged(sQ, lane);
+                B::template rows<1>(sK, 0, own, s, lane);
+                own[0].staged(sG, lane);
+                B::template rows<1>(sV, 0, own, dp, lane);
+            }
+            const int lim = r >= R ? 0 : a.causal && off + q + 1 < it.lk ? off + q + 1 : it.lk;
+            float sum = 0.f, dsum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float u;
+                if constexpr (BIAS) u = fmaf(s[0][i], a.scale, tab[(r & gm) * kTableStride + id_of(ids, i, a.B)]);
+                else u = s[0][i] * a.scale;
+                s[0][i] = ex2((u - L) * kLog2e);
+                if (part(i, lane) >= lim) s[0][i] = 0.f, dp[0][i] = 0.f;
+                sum += s[0][i];
+                dsum = fmaf(s[0][i], dp[0][i], dsum);
+            }
+            sum = pair_sum(sum);
+            const float inv = sum == 0.f ? 0.f : 1.f / sum, Dr = pair_sum(dsum) * inv;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[0][i] *= inv;
+                dp[0][i] = s[0][i] * (dp[0][i] - Dr);
+                if constexpr (BIAS) hist_add(hist + lane, id_of(ids, i, a.B), dp[0][i]);
+            }
+            typename B::Cols x;
+            x.load(sK, 0, lane);
+            x.drop(it.lk, lane);
+            B::template apply<1>(x, dp, dq);
+            wave_done();  // K and V are read: their place takes P and dS
+            lay_block<T>(sK, s[0], lane);
+            lay_block<T>(sV, dp[0], lane);
+            wave_done();
+            typename B::Weights w[1];
+            typename S::Cols t;
+            auto turned = [&](const T* from) {
+                t.load(from, 0, lane);
+#pragma unroll
+                for (int i = 0; i < (B::kHalf ? 2 : 16); ++i) w[0].v[i] = t.v[0][i];
+            };
+            turned(sK);
+            x.load(sG, 0, lane);
+            x.drop(R, lane);
+            B::template apply<1>(x, w, dv);
+            turned(sV);
+            x.load(sQ, 0, lane);
+            x.drop(R, lane);
+            B::template apply<1>(x, w, dk);
+        }
+        if (r < R) B::store(static_cast<T*>(a.out0) + (row_at + q * a.H + (r & gm)) * D, dq[0], a.scale, lane);
+        if (r < it.lk) {
+            B::store(static_cast<T*>(a.out1) + (key_at + r * a.Hkv) * D, dk[0], a.scale, lane);
+            B::store(static_cast<T*>(a.out2) + (key_at + r * a.Hkv) * D, dv[0], 1.f, lane);
+        }
+        wave_done();
+    }
+    if constexpr (BIAS)
+        hist_flush<kWave>(hist, 1, a.B, gs, a.hist + int64_t(first) * (int64_t(a.B) << gs), lane);
+}
+
+// The sum of KS sets' accumulators in the first set (false for the others).
+template <int KS, int W, int N>
+__device__ __forceinline__ bool add_sets(f32x16_t (&acc)[N], int set, int at) {
+    if constexpr (KS > 1) {
+        __shared__ float s_acc[KS - 1][8][W * kWave];
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                if (set > 0)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s_acc[set - 1][i][at] = acc[k][8 * half + i];
+                __syncthreads();
+                if (set == 0)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int p = 0; p < KS - 1; ++p) acc[k][8 * half + i] += s_acc[p][i][at];
+                __syncthreads();
+            }
+    }
+    return set == 0;
+}
+
 enum RowPass { kStat, kGrad };
 
 // kGrad: dQ_i = scale sum_j dS_ij K_j with dS_ij = P_ij (dP_ij - D_i); the dP
 // products start from -D_i, so their sum is dP - D with no subtraction.  Without
 // a bias D_i = <dO_i, O_i> (written here for the key pass).
 // kStat (before it, with a bias): D_i = sum_j P_ij dP_ij from the scores, since a
-// bf16 O is off by 2^-9, which moves the table's gradient (fp32) by as much,
+// bf16 O is off by 2^-8, which moves the table's gradient (fp32) by as much,
 // and the weights' sum under the given LSE: an fp32 LSE beside a large bias
 // holds log(sum) only roughly, so P is normalised again by it.
-// The table's gradient: every lane adds the dS of its row to a column of its own
-// in LDS ([bucket][lane]: no two lanes meet, and the order of additions is the
-// program's), summed over the lanes at the end.
-template <typename T, int D, int WAVES, bool BIAS, RowPass PASS>
-__global__ __launch_bounds__(WAVES * kWave) void k_packed_rows(PackedArgs a) {
-    using B = Blk<T, D>;
-    __shared__ __attribute__((aligned(16))) T sK0[B::kElems], sK1[B::kElems], sV0[B::kElems], sV1[B::kElems];
+template <typename T, int D, int STAGE, int W, int KS, int SUB, bool BIAS, RowPass PASS>
+__global__ __launch_bounds__(W * KS * kWave) void k_packed_rows(PackedArgs a) {
+    using B = Blk<T, D, STAGE>;
+    __shared__ __attribute__((aligned(16))) T sK0[KS * B::kElems], sK1[KS * B::kElems];
+    __shared__ __attribute__((aligned(16))) T sV0[KS * B::kElems], sV1[KS * B::kElems];
     extern __shared__ float s_dyn[];
     PackedItem it;
-    int hk;
-    int64_t block;
-    if (!packed_place<WAVES == 1>(a, it, hk, block)) return;
+    int hk, sub;
+    uint32_t block;
+    if (!packed_place<W == 1, SUB>(a, it, hk, sub, block)) return;
     const int lane = lane_id(), wave = uniform(int(threadIdx.x) / kWave);
+    const int set = KS == 1 ? 0 : wave / W, row_wave = wave - set * W;
     const int gs = a.gs, gm = (1 << gs) - 1, R = it.lq << gs, off = it.lk - it.lq;
-    const int row0 = it.tile + wave * 32;
+    const int row0 = it.tile + (sub * W + row_wave) * 32;
     float* s_tab = s_dyn;
-    float* hist = s_dyn + (kTableStride << gs) + wave * (a.B + 1) * kWave;
+    float* hist = s_dyn + (kTableStride << gs) + wave * (a.B + 1) * kWave + lane;
     if constexpr (BIAS) {
-        load_table(s_tab, a, hk);
+        load_table<W * KS * kWave>(s_tab, a, hk, int(threadIdx.x));
         if constexpr (PASS == kGrad)
-            for (int x = 0; x <= a.B; ++x) hist[x * kWave + lane] = 0.f;
+            for (int x = 0; x <= a.B; ++x) hist[x * kWave] = 0.f;
     }
     auto limit = [&](int q) {
         const int l = a.causal ? off + q + 1 : it.s1;
@@ -46,18 +182,20 @@ __global__ __launch_bounds__(WAVES * kWave) void k_packed_rows(PackedArgs a) {
     const T* K = static_cast<const T*>(a.K) + int64_t(it.k0) * a.ldk + hk * D;
     const T* V = static_cast<const T*>(a.V) + int64_t(it.k0) * a.ldv + hk * D;
     auto fetch = [&](int kbase, T* toK, T* toV) {
-        const int rows = it.s1 - kbase;
-        auto key = [&](int r) { return int64_t(kbase + r < it.lk ? kbase + r : it.lk - 1); };
-        B::template fetch<WAVES>(toK, rows, wave, lane, [&](int r) { return K + key(r) * a.ldk; });
-        B::template fetch<WAVES>(toV, rows, wave, lane, [&](int r) { return V + key(r) * a.ldv; });
+        if (kbase >= it.s1) return;
+        B::template fetch<W>(toK + set * B::kElems, K + int64_t(kbase) * a.ldk, it.s1 - kbase, row_wave, lane,
+                             [&](int r) { return __umul24(r, a.ldk); });
+        B::template fetch<W>(toV + set * B::kElems, V + int64_t(kbase) * a.ldv, it.s1 - kbase, row_wave, lane,
+                             [&](int r) { return __umul24(r, a.ldv); });
     };
-    if (it.s0 < it.s1) fetch(it.s0, sK0, sV0);
+    fetch(it.s0 + set * STAGE, sK0, sV0);
     const int r = row0 + (lane & 31), rc = r < R ? r : R - 1;
     const int q = rc >> gs, hg = rc & gm;
     const int64_t at = int64_t(it.q0 + q) * a.H + (hk << gs) + hg;
     const int lim = r < R ? limit(q) : 0;  // a row past the end takes no part, in the table's gradient either
     const int lo = uniform(row0 + 32 <= R ? limit(row0 >> gs) : 0);
     const int hi = uniform(row0 < R ? limit((row0 + 31 < R ? row0 + 31 : R - 1) >> gs) : 0);
+    const uint8_t* id_row = BIAS ? a.ids + it.pair + q * ids_width(it.lk) : nullptr;
     typename B::Row qf[1], gf[1];
     qf[0].load(static_cast<const T*>(a.Q) + int64_t(it.q0 + q) * a.ldq + ((hk << gs) + hg) * D, lane);
     gf[0].load(static_cast<const T*>(a.dO) + at * D, lane);
@@ -69,7 +207,7 @@ __global__ __launch_bounds__(WAVES * kWave) void k_packed_rows(PackedArgs a) {
         typename B::Row of;
         of.load(static_cast<const T*>(a.O) + at * D, lane);
         Dq = pair_sum(gf[0].dot(of));
-        if (r < R && lane < 32) a.Dv[at] = Dq;
+        if (r < R && lane < 32 && set == 0 && it.s0 == 0) a.Dv[at] = Dq;
     } else if constexpr (PASS == kGrad) {
         lg = a.Lg[at];
         Dq = a.Dv[at];
@@ -78,40 +216,41 @@ __global__ __launch_bounds__(WAVES * kWave) void k_packed_rows(PackedArgs a) {
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) acc[0][db] = splat16(0.f);
     float sum = 0.f, dsum = 0.f;
-    const int64_t wide = (int64_t(it.lk) + 15) & ~int64_t(15);
-    stage_done<WAVES>();
+    stage_done<(W > 1) || BIAS>();
     auto stage = [&](int kbase, const T* cK, const T* cV, T* nK, T* nV) {
-        if (kbase + B::kStage < it.s1) fetch(kbase + B::kStage, nK, nV);
+        fetch(kbase + KS * STAGE, nK, nV);
 #pragma unroll
-        for (int kb = 0; kb < B::kStage / 32; ++kb) {
+        for (int kb = 0; kb < STAGE / 32; ++kb) {
             const int key0 = kbase + 32 * kb;
             if (key0 >= hi) break;  // uniform
-            uint32_t id4[4];
-            if constexpr (BIAS) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int k = key0 + 8 * j + 4 * (lane >> 5);
-                    id4[j] = k < wide ? *reinterpret_cast<const uint32_t*>(a.ids + it.pair + q * wide + k) : ~0u;
-                }
-            }
+            uint4 ids;
+            if constexpr (BIAS) ids = load_ids(id_row, key0, it.lk, lane);
             f32x16_t s[1] = {splat16(0.f)}, dp[1] = {splat16(-Dq)};
-            B::template rows<1>(cK, 32 * kb, qf, s, lane);
-            B::template rows<1>(cV, 32 * kb, gf, dp, lane);
+            B::template rows<1>(cK + set * B::kElems, 32 * kb, qf, s, lane);
+            B::template rows<1>(cV + set * B::kElems, 32 * kb, gf, dp, lane);
+            typename B::Cols kt;
+            if constexpr (PASS == kGrad) {
+                kt.load(cK + set * B::kElems, 32 * kb, lane);
+                if (key0 + 32 > it.s1) {
+                    asm volatile("" ::: "memory");
+                    kt.drop(it.s1 - key0, lane);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 if constexpr (BIAS) {
-                    const uint32_t id = (id4[i >> 2] >> (8 * (i & 3))) & 255u;
-                    const float u = fmaf(s[0][i], a.scale,
-                                         s_tab[hg * kTableStride + (id < kMaxBuckets ? id : kMaxBuckets)]);
+                    const float u = fmaf(s[0][i], a.scale, s_tab[hg * kTableStride + id_of(ids, i, a.B)]);
                     s[0][i] = fmaf(u - L, kLog2e, -lg);
                 } else {
                     s[0][i] = fmaf(s[0][i], sl2, -L);
                 }
             }
             if (key0 + 32 > lo) {
+                asm volatile("" ::: "memory");
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (key0 + crow(i, lane) >= lim) s[0][i] = -kInf, dp[0][i] = 0.f;
+                    if (key0 + part(i, lane) >= lim) s[0][i] = -kInf, dp[0][i] = 0.f;
             }
             if constexpr (PASS == kStat) {
 #pragma unroll
@@ -121,77 +260,88 @@ __global__ __launch_bounds__(WAVES * kWave) void k_packed_rows(PackedArgs a) {
                     dsum = fmaf(p, dp[0][i], dsum);
                 }
             } else {
-                typename B::Cols kt;
-                kt.load(cK, 32 * kb, lane);
-                if (key0 + 32 > it.s1) kt.drop(it.s1 - key0, lane);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     s[0][i] = ex2(s[0][i]) * dp[0][i];
-                    if constexpr (BIAS) {
-                        const int id = int((id4[i >> 2] >> (8 * (i & 3))) & 255u);
-                        hist[(id < a.B ? id : a.B) * kWave + lane] += s[0][i];
-                    }
+                    if constexpr (BIAS) hist_add(hist, id_of(ids, i, a.B), s[0][i]);
                 }
                 B::template apply<1>(kt, s, acc);
             }
         }
-        stage_done<WAVES>();
+        stage_done<(W > 1)>();
     };
-    for (int kbase = it.s0; kbase < it.s1; kbase += 2 * B::kStage) {
-        stage(kbase, sK0, sV0, sK1, sV1);
-        if (kbase + B::kStage < it.s1) stage(kbase + B::kStage, sK1, sV1, sK0, sV0);
+    for (int kbase = it.s0; kbase < it.s1; kbase += 2 * KS * STAGE) {
+        stage(kbase + set * STAGE, sK0, sV0, sK1, sV1);
+        if (kbase + KS * STAGE < it.s1) stage(kbase + (KS + set) * STAGE, sK1, sV1, sK0, sV0);
     }
     if constexpr (PASS == kStat) {
         sum = pair_sum(sum);
         dsum = pair_sum(dsum);
-        if (r < R && lane < 32) {
+        if constexpr (KS > 1) {
+            __shared__ float s_sum[2][KS][W * kWave];
+            s_sum[0][set][row_wave * kWave + lane] = sum;
+            s_sum[1][set][row_wave * kWave + lane] = dsum;
+            __syncthreads();
+            if (set > 0) return;
+#pragma unroll
+            for (int p = 1; p < KS; ++p) {
+                sum += s_sum[0][p][row_wave * kWave + lane];
+                dsum += s_sum[1][p][row_wave * kWave + lane];
+            }
+        }
+        if (lane >= 32) return;
+        if (W == 1 && it.slot >= 0) {
+            float* o = a.slots + (int64_t(it.slot) * a.Hkv + hk) * (2 * kFewRows);
+            o[lane] = sum, o[kFewRows + lane] = dsum;
+        } else if (r < R) {
             a.Dv[at] = sum == 0.f ? 0.f : dsum / sum;
             a.Lg[at] = sum == 0.f ? 0.f : __log2f(sum);
         }
     } else {
-        if (r < R) B::store(static_cast<T*>(a.out0) + at * D, acc[0], a.scale, lane);
         if constexpr (BIAS) {
             __syncthreads();
-            // a lane's rows all belong to head lane % g of the group (tiles start at multiples of 32)
-            for (int x = int(threadIdx.x); x < (a.B << gs); x += int(blockDim.x)) {
-                const int head = x / a.B, b = x % a.B;
-                const float* h0 = s_dyn + (kTableStride << gs) + b * kWave;
-                float t = 0.f;
-                for (int w = 0; w < WAVES; ++w)
-                    for (int k = 0; k < kWave >> gs; ++k)
-                        t += h0[w * (a.B + 1) * kWave + ((((k + x) & ((kWave >> gs) - 1)) << gs) | head)];
-                a.hist[block * (int64_t(a.B) << gs) + x] = t;
-            }
+            // a lane's rows all belong to head lane % g of the group: tiles start at multiples of 32
+            hist_flush<W * KS * kWave>(s_dyn + (kTableStride << gs), W * KS, a.B, gs,
+                                       a.hist + int64_t(block) * (int64_t(a.B) << gs), int(threadIdx.x));
         }
+        if (!add_sets<KS, W>(acc[0], set, row_wave * kWave + lane)) return;
+        if (W == 1 && it.slot >= 0)
+            Blk<float, D>::store(a.slots + ((int64_t(it.slot) * a.Hkv + hk) * kFewRows + (lane & 31)) * D, acc[0], 1.f,
+                                 lane);
+        else if (r < R)
+            B::store(static_cast<T*>(a.out0) + at * D, acc[0], a.scale, lane);
     }
 }
 
 // dK_j = scale sum_i dS_ij Q_i and dV_j = sum_i P_ij dO_i over the rows of the
 // whole group, with the wavefront owning 32 keys and the rows streaming through
 // LDS; the dP products start from the rows' -D_i.
-template <typename T, int D, int WAVES, bool BIAS>
-__global__ __launch_bounds__(WAVES * kWave) void k_packed_keys(PackedArgs a) {
-    using B = Blk<T, D>;
-    __shared__ __attribute__((aligned(16))) T sQ0[B::kElems], sQ1[B::kElems], sG0[B::kElems], sG1[B::kElems];
+template <typename T, int D, int STAGE, int W, int KS, bool BIAS>
+__global__ __launch_bounds__(W * KS * kWave) void k_packed_keys(PackedArgs a) {
+    using B = Blk<T, D, STAGE>;
+    __shared__ __attribute__((aligned(16))) T sQ0[KS * B::kElems], sQ1[KS * B::kElems];
+    __shared__ __attribute__((aligned(16))) T sG0[KS * B::kElems], sG1[KS * B::kElems];
     // per row of a stage: LSE (exp2 domain without a bias), -D, log2 of the weights' sum
-    __shared__ __attribute__((aligned(16))) float sR0[3][B::kStage], sR1[3][B::kStage];
+    typedef float Stats[KS][3][STAGE];
+    __shared__ __attribute__((aligned(16))) Stats sR0, sR1;
     extern __shared__ float s_tab[];
     PackedItem it;
-    int hk;
-    int64_t block;
-    if (!packed_place<WAVES == 1>(a, it, hk, block)) return;
+    int hk, sub;
+    uint32_t block;
+    if (!packed_place<W == 1>(a, it, hk, sub, block)) return;
     const int lane = lane_id(), wave = uniform(int(threadIdx.x) / kWave);
+    const int set = KS == 1 ? 0 : wave / W, key_wave = wave - set * W;
     const int gs = a.gs, gm = (1 << gs) - 1, off = it.lk - it.lq;
-    const int key0 = it.tile + wave * 32;
-    if constexpr (BIAS) load_table(s_tab, a, hk);
+    const int key0 = it.tile + key_wave * 32;
+    if constexpr (BIAS) load_table<W * KS * kWave>(s_tab, a, hk, int(threadIdx.x));
     float rs[3] = {0.f, 0.f, 0.f};
     auto load_stats = [&](int base) {
-        if (wave != 0) return;
+        if (key_wave != 0) return;
         const int r = base + lane;
         rs[0] = BIAS ? 0.f : kInf;  // rows past the end weigh nothing
         rs[1] = 0.f;
         rs[2] = BIAS ? kInf : 0.f;
-        if (lane < B::kStage && r < it.s1) {
+        if (lane < STAGE && r < it.s1) {
             const int64_t at = int64_t(it.q0 + (r >> gs)) * a.H + (hk << gs) + (r & gm);
             const float L = a.LSE[at];
             rs[0] = L == -kInf ? 0.f : BIAS ? L : L * kLog2e;
@@ -199,24 +349,21 @@ __global__ __launch_bounds__(WAVES * kWave) void k_packed_keys(PackedArgs a) {
             if constexpr (BIAS) rs[2] = a.Lg[at];
         }
     };
-    auto store_stats = [&](float(&to)[3][B::kStage]) {
-        if (wave == 0 && lane < B::kStage) to[0][lane] = rs[0], to[1][lane] = rs[1], to[2][lane] = rs[2];
+    auto store_stats = [&](Stats& to) {
+        if (key_wave == 0 && lane < STAGE) to[set][0][lane] = rs[0], to[set][1][lane] = rs[1], to[set][2][lane] = rs[2];
     };
     const T* Q = static_cast<const T*>(a.Q) + int64_t(it.q0) * a.ldq + (hk << gs) * D;
     const T* G = static_cast<const T*>(a.dO) + (int64_t(it.q0) * a.H + (hk << gs)) * D;
-    auto fetch = [&](int base, T* toQ, T* toG) {
-        const int rows = it.s1 - base;
-        auto row = [&](int r) { return base + r < it.s1 ? base + r : it.s1 - 1; };
-        B::template fetch<WAVES>(toQ, rows, wave, lane,
-                                 [&](int r) { return Q + int64_t(row(r) >> gs) * a.ldq + (row(r) & gm) * D; });
-        B::template fetch<WAVES>(toG, rows, wave, lane, [&](int r) {
-            return G + (int64_t(row(r) >> gs) * a.H + (row(r) & gm)) * D;
-        });
+    const uint32_t ldg = uint32_t(a.H) * D;
+    auto fetch = [&](int base, T* toQ, T* toG) {  // base is a multiple of the group
+        if (base >= it.s1) return;
+        B::template fetch<W>(toQ + set * B::kElems, Q + int64_t(base >> gs) * a.ldq, it.s1 - base, key_wave, lane,
+                             [&](int r) { return __umul24(r >> gs, a.ldq) + uint32_t((r & gm) * D); });
+        B::template fetch<W>(toG + set * B::kElems, G + int64_t(base >> gs) * ldg, it.s1 - base, key_wave, lane,
+                             [&](int r) { return __umul24(r >> gs, ldg) + uint32_t((r & gm) * D); });
     };
-    if (it.s0 < it.s1) {
-        load_stats(it.s0);
-        fetch(it.s0, sQ0, sG0);
-    }
+    load_stats(it.s0 + set * STAGE);
+    fetch(it.s0 + set * STAGE, sQ0, sG0);
     const int j = key0 + (lane & 31), jc = j < it.lk ? j : it.lk - 1;
     auto first_row = [&](int key) { return a.causal && key > off ? (key - off) << gs : 0; };
     const int rmin = first_row(jc);
@@ -225,22 +372,19 @@ __global__ __launch_bounds__(WAVES * kWave) void k_packed_keys(PackedArgs a) {
     typename B::Row kf[1], vf[1];
     kf[0].load(static_cast<const T*>(a.K) + int64_t(it.k0 + jc) * a.ldk + hk * D, lane);
     vf[0].load(static_cast<const T*>(a.V) + int64_t(it.k0 + jc) * a.ldv + hk * D, lane);
-    f32x16_t dk[1][D / 32], dv[1][D / 32];
+    f32x16_t dk[D / 32], dv[1][D / 32];
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db) dk[0][db] = dv[0][db] = splat16(0.f);
+    for (int db = 0; db < D / 32; ++db) dk[db] = dv[0][db] = splat16(0.f);
     const float sl2 = a.scale * kLog2e;
-    const int64_t wide = (int64_t(it.lk) + 15) & ~int64_t(15);
+    const uint8_t* id_key = BIAS ? a.ids + it.pair + jc : nullptr;
+    const int64_t wide = ids_width(it.lk);
     store_stats(sR0);
-    stage_done<WAVES>();
-    auto stage = [&](int base, const T* cQ, const T* cG, const float(&cR)[3][B::kStage], T* nQ, T* nG,
-                     float(&nR)[3][B::kStage]) {
-        const bool more = base + B::kStage < it.s1;
-        if (more) {
-            load_stats(base + B::kStage);
-            fetch(base + B::kStage, nQ, nG);
-        }
+    stage_done<(W > 1) || BIAS>();
+    auto stage = [&](int base, const T* cQ, const T* cG, const Stats& cR, T* nQ, T* nG, Stats& nR) {
+        load_stats(base + KS * STAGE);
+        fetch(base + KS * STAGE, nQ, nG);
 #pragma unroll
-        for (int rb = 0; rb < B::kStage / 32; ++rb) {
+        for (int rb = 0; rb < STAGE / 32; ++rb) {
             const int r0 = base + 32 * rb;
             if (r0 >= it.s1 || key0 >= it.lk) break;  // uniform
             if (r0 + 32 <= rlo) continue;             // before every key of this wavefront
@@ -248,47 +392,52 @@ __global__ __launch_bounds__(WAVES * kWave) void k_packed_keys(PackedArgs a) {
             if constexpr (BIAS) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int r = r0 + crow(i, lane);
-                    id[i] = r < it.s1 ? a.ids[it.pair + (r >> gs) * wide + jc] : 255u;
+                    const int r = r0 + part(i, lane);
+                    const uint32_t b = r < it.s1 ? id_key[(r >> gs) * wide] : 255u;
+                    id[i] = b < uint32_t(a.B) ? b : uint32_t(a.B);
                 }
             }
             f32x16_t s[1] = {splat16(0.f)}, dp[1];
             float L[16], lg[16];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const int r = 32 * rb + 8 * x + 4 * (lane >> 5);
-                const float4 l4 = *reinterpret_cast<const float4*>(&cR[0][r]);
-                const float4 d4 = *reinterpret_cast<const float4*>(&cR[1][r]);
+                const int r = 32 * rb + 16 * (lane >> 5) + 4 * x;
+                const float4 l4 = *reinterpret_cast<const float4*>(&cR[set][0][r]);
+                const float4 d4 = *reinterpret_cast<const float4*>(&cR[set][1][r]);
                 L[4 * x] = l4.x, L[4 * x + 1] = l4.y, L[4 * x + 2] = l4.z, L[4 * x + 3] = l4.w;
                 dp[0][4 * x] = d4.x, dp[0][4 * x + 1] = d4.y, dp[0][4 * x + 2] = d4.z, dp[0][4 * x + 3] = d4.w;
                 if constexpr (BIAS) {
-                    const float4 g4 = *reinterpret_cast<const float4*>(&cR[2][r]);
+                    const float4 g4 = *reinterpret_cast<const float4*>(&cR[set][2][r]);
                     lg[4 * x] = g4.x, lg[4 * x + 1] = g4.y, lg[4 * x + 2] = g4.z, lg[4 * x + 3] = g4.w;
                 }
             }
-            B::template rows<1>(cQ, 32 * rb, kf, s, lane);
-            B::template rows<1>(cG, 32 * rb, vf, dp, lane);
+            const T *bQ = cQ + set * B::kElems, *bG = cG + set * B::kElems;
+            B::template rows<1>(bQ, 32 * rb, kf, s, lane);
+            B::template rows<1>(bG, 32 * rb, vf, dp, lane);
             typename B::Cols gt_, qt;
-            gt_.load(cG, 32 * rb, lane);
-            qt.load(cQ, 32 * rb, lane);
+            gt_.load(bG, 32 * rb, lane);
+            qt.load(bQ, 32 * rb, lane);
             if (r0 + 32 > it.s1) {
+                asm volatile("" ::: "memory");
                 gt_.drop(it.s1 - r0, lane);
                 qt.drop(it.s1 - r0, lane);
             }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 if constexpr (BIAS) {
-                    const float u = fmaf(s[0][i], a.scale, s_tab[((r0 + crow(i, lane)) & gm) * kTableStride +
-                                                                 (id[i] < kMaxBuckets ? id[i] : kMaxBuckets)]);
+                    const float u =
+                        fmaf(s[0][i], a.scale, s_tab[((r0 + part(i, lane)) & gm) * kTableStride + id[i]]);
                     s[0][i] = fmaf(u - L[i], kLog2e, -lg[i]);
                 } else {
                     s[0][i] = fmaf(s[0][i], sl2, -L[i]);
                 }
             }
             if (r0 < rhi || r0 + 32 > it.s1) {
+                asm volatile("" ::: "memory");
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int r = r0 + crow(i, lane);
+                    const int r = r0 + part(i, lane);
                     if (r < rmin || r >= it.s1) s[0][i] = -kInf, dp[0][i] = 0.f;
                 }
             }
@@ -297,83 +446,112 @@ __global__ __launch_bounds__(WAVES * kWave) void k_packed_keys(PackedArgs a) {
                 s[0][i] = ex2(s[0][i]);
                 dp[0][i] *= s[0][i];
             }
-            B::template apply<1>(gt_, s, dv);
-            B::template apply<1>(qt, dp, dk);
+            typename B::Weights w[1];
+            w[0].set(s[0]);
+            B::template apply<1>(gt_, w, dv);
+            w[0].set(dp[0]);
+            f32x16_t(&dk1)[1][D / 32] = reinterpret_cast<f32x16_t(&)[1][D / 32]>(dk);
+            B::template apply<1>(qt, w, dk1);
         }
-        if (more) store_stats(nR);
-        stage_done<WAVES>();
+        store_stats(nR);
+        stage_done<(W > 1)>();
     };
-    for (int base = it.s0; base < it.s1; base += 2 * B::kStage) {
-        stage(base, sQ0, sG0, sR0, sQ1, sG1, sR1);
-        if (base + B::kStage < it.s1) stage(base + B::kStage, sQ1, sG1, sR1, sQ0, sG0, sR0);
+    for (int base = it.s0; base < it.s1; base += 2 * KS * STAGE) {
+        stage(base + set * STAGE, sQ0, sG0, sR0, sQ1, sG1, sR1);
+        if (base + KS * STAGE < it.s1) stage(base + (KS + set) * STAGE, sQ1, sG1, sR1, sQ0, sG0, sR0);
     }
-    if (j < it.lk) {
+    const int thread = key_wave * kWave + lane;
+    add_sets<KS, W>(dk, set, thread);
+    if (!add_sets<KS, W>(dv[0], set, thread)) return;
+    if (W == 1 && it.slot >= 0) {
+        float* o = a.slots + ((int64_t(it.slot) * a.Hkv + hk) * (2 * kFewRows) + (lane & 31)) * D;
+        Blk<float, D>::store(o, dk, 1.f, lane);
+        Blk<float, D>::store(o + kFewRows * D, dv[0], 1.f, lane);
+    } else if (j < it.lk) {
         const int64_t at = int64_t(it.k0 + j) * a.Hkv + hk;
-        B::store(static_cast<T*>(a.out1) + at * D, dk[0], a.scale, lane);
+        B::store(static_cast<T*>(a.out1) + at * D, dk, a.scale, lane);
         B::store(static_cast<T*>(a.out2) + at * D, dv[0], 1.f, lane);
     }
 }
 
-// dtable[b, h]: the blocks' partial sums, one workgroup per head; thread t of a
-// bucket adds the blocks t, t + 64, ... of that head, then the 64 are added.
-template <bool SMALL>
-__device__ __forceinline__ int64_t hist_block(int64_t i, int hk, int64_t items, int Hkv) {
-    return SMALL ? i * Hkv + hk : hk * items + i;
-}
-__global__ __launch_bounds__(256) void k_packed_table(int64_t n_small, int64_t n_large, int H, int Hkv, int gs, int B,
-                                                      const float* __restrict__ hist, float* __restrict__ out) {
-    const int h = int(blockIdx.x), b = int(blockIdx.y), hk = h >> gs, hg = h & ((1 << gs) - 1);
-    const int64_t per = int64_t(B) << gs;
-    float t = 0.f;
-    for (int64_t i = threadIdx.x; i < n_small + n_large; i += 256) {
-        const int64_t blk = i < n_small ? hist_block<true>(i, hk, n_small, Hkv)
-                                        : n_small * Hkv + hist_block<false>(i - n_small, hk, n_large, Hkv);
-        t += hist[blk * per + hg * B + b];
-    }
-    __shared__ float s[4];
-    t = wave_sum(t);
-    if (lane_id() == 0) s[threadIdx.x / kWave] = t;
-    __syncthreads();
-    if (threadIdx.x == 0) out[int64_t(b) * H + h] = (s[0] + s[1]) + (s[2] + s[3]);
-}
-
 template <typename T, int D, bool BIAS>
 gt_status packed_bwd_d(const gt_packed_plan* p, PackedArgs a, float* dtable, hipStream_t s) {
+    constexpr int kRow = D * int(sizeof(T)), kStage = sizeof(T) == 2 ? 64 : 32;
+    const gt_dtype dt = sizeof(T) == 2 ? GT_BF16 : GT_F32;
     const size_t tab = BIAS ? size_t(kTableStride << a.gs) * sizeof(float) : 0;
     const size_t col = BIAS ? size_t(a.B + 1) * kWave * sizeof(float) : 0;
-    const int64_t n1 = packed_items(p, kRowsSmall), n4 = packed_items(p, kRowsLarge);
-    float* hist = a.hist;
-    auto rows = [&](auto pass) -> gt_status {
-        constexpr RowPass P = decltype(pass)::value;
-        a.items = packed_list(p, kRowsSmall);
-        a.hist = hist;
-        if ((a.n_items = int(n1)) > 0)
-            k_packed_rows<T, D, 1, BIAS, P><<<packed_grid(n1, a.Hkv), kWave, tab + (P == kGrad ? col : 0), s>>>(a);
-        GT_LAUNCH_CHECK("packed_bwd rows");
-        a.items = packed_list(p, kRowsLarge);
-        a.hist = BIAS ? hist + n1 * a.Hkv * (int64_t(a.B) << a.gs) : nullptr;
-        if ((a.n_items = int(n4)) > 0)
-            k_packed_rows<T, D, 4, BIAS, P><<<packed_grid(n4, a.Hkv), 4 * kWave, tab + (P == kGrad ? 4 * col : 0), s>>>(a);
-        GT_LAUNCH_CHECK("packed_bwd rows");
-        return GT_OK;
+    const int64_t per = int64_t(a.B) << a.gs;
+    float* const hist = a.hist;
+    TableParts parts = {};
+    auto list = [&](int l) {
+        a.items = packed_list(p, l);
+        a.n_items = int(packed_items(p, l));
+        return a.n_items > 0;
     };
+    // where a launch of n blocks (or wavefronts) leaves its partial tables
+    auto part = [&](int64_t n, int64_t items) {
+        const int k = parts.count++;
+        parts.at[k] = k == 0 ? 0 : parts.at[k - 1] + parts.n[k - 1] * per;
+        parts.n[k] = n;
+        parts.items[k] = items;
+        a.hist = BIAS ? hist + parts.at[k] : nullptr;
+    };
+    if (list(kPairs)) {
+        constexpr int W = pair_waves(kRow);
+        const int64_t blocks = BIAS ? pair_blocks(p, kRow) : cdiv(int64_t(a.n_items) * a.Hkv, W * a.Hkv) * a.Hkv;
+        part(blocks * W, 0);
+        k_pair_bwd<T, D, BIAS><<<unsigned(blocks), W * kWave, W * (tab + col), s>>>(a);
+        GT_LAUNCH_CHECK("packed_bwd pairs");
+    }
+#define GT_ROWS(LIST, STAGE, W, KS, SUB, PASS)                                                                  \
+    if (list(LIST)) {                                                                                           \
+        if (PASS == kGrad) part(int64_t(a.n_items) * SUB * a.Hkv, W == 1 ? 0 : int64_t(a.n_items) * SUB);       \
+        k_packed_rows<T, D, STAGE, W, KS, SUB, BIAS, PASS><<<packed_grid(a.n_items, a.Hkv, SUB),                \
+                            W * KS * kWave, tab + (PASS == kGrad ? W * KS * col : 0), s>>>(a);                  \
+        GT_LAUNCH_CHECK("packed_bwd rows");                                                                     \
+    }
     if constexpr (BIAS) {
-        const gt_status st = rows(std::integral_constant<RowPass, kStat>{});
+        GT_ROWS(kRowsFew, 32, 1, few_waves(kRow), 1, kStat)
+        GT_ROWS(kRows64, kStage, 2, 1, 1, kStat)
+        GT_ROWS(kRows128, kStage, 4, 1, 1, kStat)
+        GT_ROWS(kRows256, kStage, 8, 1, 1, kStat)
+        if (list(kRowMerges)) {
+            const gt_status st = packed_merge_stat(p, a, s);
+            if (st != GT_OK) return st;
+        }
+        // the table's gradient takes 16 KB of LDS a wavefront: smaller workgroups
+        GT_ROWS(kRowsFew, 32, 1, few_waves_hist(kRow), 1, kGrad)
+        GT_ROWS(kRows64, kStage, 2, 1, 1, kGrad)
+        GT_ROWS(kRows128, kStage, 4, 1, 1, kGrad)
+        GT_ROWS(kRows256, kStage, 4, 1, 2, kGrad)
+    } else {
+        GT_ROWS(kRowsFew, 32, 1, few_waves(kRow), 1, kGrad)
+        GT_ROWS(kRows64, kStage, 2, 1, 1, kGrad)
+        GT_ROWS(kRows128, kStage, 4, 1, 1, kGrad)
+        GT_ROWS(kRows256, kStage, 8, 1, 1, kGrad)
+    }
+#undef GT_ROWS
+    if (list(kRowMerges)) {
+        const gt_status st = packed_merge_rows(p, D, dt, a, s);
         if (st != GT_OK) return st;
     }
-    const gt_status st = rows(std::integral_constant<RowPass, kGrad>{});
-    if (st != GT_OK) return st;
-    a.items = packed_list(p, kKeysSmall);
-    if ((a.n_items = int(packed_items(p, kKeysSmall))) > 0)
-        k_packed_keys<T, D, 1, BIAS><<<packed_grid(a.n_items, a.Hkv), kWave, tab, s>>>(a);
-    GT_LAUNCH_CHECK("packed_bwd keys");
-    a.items = packed_list(p, kKeysLarge);
-    if ((a.n_items = int(packed_items(p, kKeysLarge))) > 0)
-        k_packed_keys<T, D, 4, BIAS><<<packed_grid(a.n_items, a.Hkv), 4 * kWave, tab, s>>>(a);
-    GT_LAUNCH_CHECK("packed_bwd keys");
+#define GT_KEYS(LIST, STAGE, W, KS)                                                                              \
+    if (list(LIST)) {                                                                                            \
+        k_packed_keys<T, D, STAGE, W, KS, BIAS><<<packed_grid(a.n_items, a.Hkv), W * KS * kWave, tab, s>>>(a);   \
+        GT_LAUNCH_CHECK("packed_bwd keys");                                                                      \
+    }
+    GT_KEYS(kKeysFew, 32, 1, few_waves(kRow))
+    GT_KEYS(kKeys64, kStage, 2, 1)
+    GT_KEYS(kKeys128, kStage, 4, 1)
+    GT_KEYS(kKeys256, kStage, 8, 1)
+#undef GT_KEYS
+    if (list(kKeyMerges)) {
+        const gt_status st = packed_merge_keys(p, D, dt, a, s);
+        if (st != GT_OK) return st;
+    }
     if constexpr (BIAS) {
-        k_packed_table<<<dim3(a.H, a.B), 256, 0, s>>>(n1, n4, a.H, a.Hkv, a.gs, a.B, hist, dtable);
-        GT_LAUNCH_CHECK("packed_bwd table");
+        a.hist = hist;
+        return packed_table_sum(parts, a, dtable, s);
     }
     return GT_OK;
 }

@@ -2,8 +2,9 @@
 // bf16 and fp32 features, and what the forward and backward kernels share.
 //
 // Every product is formed in 32 x 32 blocks with the owned rows as columns, so a
-// lane holds one owned row and 16 of its partners (accumulator element i is
-// partner crow(i, lane)).  Row statistics then need one exchange between the
+// lane holds one owned row and 16 of its partners.  Partner rows are staged in an
+// order that makes those 16 consecutive: accumulator element i of a lane is
+// partner part(i, lane) of the block.  Row statistics then need one exchange between the
 // half-waves, and the weights become the next product's B operand straight from
 // the accumulators.  bf16 blocks are v_mfma_f32_32x32x16_bf16; fp32 blocks
 // v_mfma_f32_32x32x2_f32, whose operands are single fp32 values, so nothing is
@@ -20,7 +21,11 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLowest = -3.402823466e38f;  // a running maximum's start: -inf minus it is -inf, no NaN
 
-__device__ __forceinline__ int crow(int i, int lane) { return 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3); }
+__device__ __forceinline__ int part(int i, int lane) { return 16 * (lane >> 5) + i; }
+// The partner (of a block of 32) that lies in LDS row r of the block, and back:
+// the matrix cores give lane half h the LDS rows 8 a + 4 h + b, a, b < 4.
+__device__ __forceinline__ int row_partner(int r) { return 16 * ((r >> 2) & 1) + 4 * (r >> 3) + (r & 3); }
+__device__ __forceinline__ int partner_row(int p) { return 8 * ((p >> 2) & 3) + 4 * (p >> 4) + (p & 3); }
 
 __device__ __forceinline__ f32x16_t splat16(float x) {
     f32x16_t z;
@@ -45,22 +50,25 @@ __device__ __forceinline__ void load_to_lds(void* lds, const void* src) {
         reinterpret_cast<__attribute__((address_space(3))) uint32_t*>(reinterpret_cast<uintptr_t>(lds)), 16, 0, 0);
 }
 
-// The stage fetched last is in LDS for every wavefront of the workgroup, and
-// every wavefront is done reading the one before.
-template <int WAVES>
-__device__ __forceinline__ void stage_done() {
+// The wavefront's own loads into LDS have landed and its reads of LDS are done.
+__device__ __forceinline__ void wave_done() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    if constexpr (WAVES > 1) __syncthreads();
-    else __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_wave_barrier();
+}
+// The same for a workgroup (or, where no wavefront shares a stage, for each).
+template <bool SHARED>
+__device__ __forceinline__ void stage_done() {
+    wave_done();
+    if constexpr (SHARED) __syncthreads();
 }
 
 // Operands of the block products.  A stage of partner rows lies row-major in
 // LDS, each row's 16-byte pieces permuted by the row number, which spreads the
 // same piece of neighbouring rows over the LDS banks.
-template <typename T, int D>
+template <typename T, int D, int STAGE = 32>
 struct Blk {
     static constexpr bool kHalf = sizeof(T) == 2;
-    static constexpr int kStage = kHalf ? 64 : 32;         // partner rows per stage
+    static constexpr int kStage = STAGE;                   // partner rows per stage
     static constexpr int kElems = kStage * D;              // one staged operand
     static constexpr int kPiece = 16 / int(sizeof(T));     // features per 16-byte piece
     static constexpr int kPieces = D / kPiece;             // pieces per row
@@ -79,6 +87,11 @@ struct Blk {
 #pragma unroll
             for (int c = 0; c < kSteps; ++c)
                 v[c] = *reinterpret_cast<const uint4*>(p + kPiece * (2 * c + (lane >> 5)));
+        }
+        // the lane's row of a staged block
+        __device__ __forceinline__ void staged(const T* s, int lane) {
+#pragma unroll
+            for (int c = 0; c < kSteps; ++c) v[c] = piece(s, partner_row(lane & 31), c, lane);
         }
         __device__ __forceinline__ float dot(const Row& o) const {
             float s = 0.f;
@@ -99,20 +112,24 @@ struct Blk {
         }
     };
 
-    // This wavefront's share of a stage: `rows` partner rows (of kStage) are
-    // wanted; row(r) is the address of row r's features.
+    // This wavefront's share of a stage: the `left` (at least 1) partner rows from
+    // `base` on, up to a stage; off(r) is row r's offset in elements, below 2^30.
+    // Rows behind the last one repeat it where their block of 32 is begun.
     template <int WAVES, typename F>
-    __device__ __forceinline__ static void fetch(T* s, int rows, int wave, int lane, F row) {
+    __device__ __forceinline__ static void fetch(T* s, const T* base, int left, int wave, int lane, F off) {
+        constexpr int kRowsPerLoad = 64 / kPieces;
 #pragma unroll
         for (int q0 = 0; q0 < kLoads; q0 += WAVES) {
             const int q = q0 + wave;
-            if (q >= kLoads || q * 64 / kPieces >= rows) break;  // uniform
-            const int at = q * 64 + lane, r = at / kPieces, c = (at % kPieces) ^ turn(r);
-            load_to_lds(s + q * (1024 / int(sizeof(T))), row(r) + kPiece * c);
+            if (q >= kLoads || ((q * kRowsPerLoad) & ~31) >= left) break;  // uniform
+            const int at = q * kRowsPerLoad + lane / kPieces, c = (lane % kPieces) ^ turn(at);
+            const int p = (at & ~31) + row_partner(at & 31);
+            const uint32_t o = off(p < left ? p : left - 1) + uint32_t(kPiece * c);
+            load_to_lds(s + q * (1024 / int(sizeof(T))), reinterpret_cast<const char*>(base) + o * uint32_t(sizeof(T)));
         }
     }
 
-    // c += (staged rows r0 .. r0 + 31) x (owned rows), over the features.
+    // c += (staged LDS rows r0 .. r0 + 31) x (owned rows), over the features.
     __device__ __forceinline__ static f32x16_t mul_piece(uint4 a, uint4 b, f32x16_t c) {
         if constexpr (kHalf) {
             return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a),
@@ -140,7 +157,7 @@ struct Blk {
     // The staged rows r0 .. r0 + 31 turned round (features x partners), in the
     // partner order of an accumulator used as B operand.
     struct Cols {
-        // bf16: partners 16 half + 4 (lane / 32) + {0..3, 8..11}; fp32: partner crow(i, lane)
+        // element 8 half + t (bf16) or i (fp32) of a lane: partner part(.., lane)
         typename std::conditional<kHalf, bf16x8_t, float>::type v[D / 32][kHalf ? 2 : 16];
 
         __device__ __forceinline__ void load(const T* s, int r0, int lane) {
@@ -167,7 +184,7 @@ struct Blk {
                 for (int db = 0; db < D / 32; ++db)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int r = r0 + crow(i, lane), f = 32 * db + (lane & 31);
+                        const int r = r0 + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3), f = 32 * db + (lane & 31);
                         v[db][i] = s[r * D + 4 * ((f >> 2) ^ turn(r)) + (f & 3)];
                     }
             }
@@ -177,7 +194,7 @@ struct Blk {
         __device__ __forceinline__ void drop(int left, int lane) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if (crow(i, lane) >= left)
+                if (part(i, lane) >= left)
 #pragma unroll
                     for (int db = 0; db < D / 32; ++db) {
                         if constexpr (kHalf) v[db][i / 8][i % 8] = (__bf16)0.f;
@@ -185,34 +202,40 @@ struct Blk {
                     }
         }
     };
-    // acc (features x owned rows) += Cols x w, w an accumulator block (partners x
-    // owned rows); bf16 rounds w to bf16 (half a step, 2^-9 of a weight: the
-    // size of the features' own rounding).
+    // Weights (partners x owned rows) as the B operand of a product with Cols:
+    // bf16 rounds them to bf16 (half a step, 2^-8 of a weight at most: the size of
+    // the features' own rounding), fp32 takes them as they are.
+    struct Weights {
+        typename std::conditional<kHalf, bf16x8_t, float>::type v[kHalf ? 2 : 16];
+        __device__ __forceinline__ void set(const f32x16_t& w) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                if constexpr (kHalf) v[i / 8][i % 8] = (__bf16)w[i];
+                else v[i] = w[i];
+            }
+        }
+    };
+    // acc (features x owned rows) += Cols x weights.
     template <int NB>
-    __device__ __forceinline__ static void apply(const Cols& a, const f32x16_t (&w)[NB], f32x16_t (&acc)[NB][D / 32]) {
-        if constexpr (kHalf) {
-            bf16x8_t p[NB][2];
+    __device__ __forceinline__ static void apply(const Cols& a, const Weights (&w)[NB], f32x16_t (&acc)[NB][D / 32]) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) p[b][i / 8][i % 8] = (__bf16)w[b][i];
+        for (int k = 0; k < (kHalf ? 2 : 16); ++k)
 #pragma unroll
             for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-                for (int half = 0; half < 2; ++half)
+                for (int b = 0; b < NB; ++b) {
+                    if constexpr (kHalf)
+                        acc[b][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v[db][k], w[b].v[k], acc[b][db], 0, 0, 0);
+                    else
+                        acc[b][db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[db][k], w[b].v[k], acc[b][db], 0, 0, 0);
+                }
+    }
+    template <int NB>
+    __device__ __forceinline__ static void apply(const Cols& a, const f32x16_t (&w)[NB], f32x16_t (&acc)[NB][D / 32]) {
+        Weights p[NB];
 #pragma unroll
-                    for (int b = 0; b < NB; ++b)
-                        acc[b][db] =
-                            __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v[db][half], p[b][half], acc[b][db], 0, 0, 0);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-#pragma unroll
-                for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-                    for (int b = 0; b < NB; ++b)
-                        acc[b][db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[db][i], w[b][i], acc[b][db], 0, 0, 0);
-        }
+        for (int b = 0; b < NB; ++b) p[b].set(w[b]);
+        apply<NB>(a, p, acc);
     }
     // One owned row of acc times f, as T.
     __device__ __forceinline__ static void store(T* o, const f32x16_t (&a)[D / 32], float f, int lane) {
@@ -229,28 +252,87 @@ struct Blk {
     }
 };
 
-// A block's place: which item and which kv head; false for the grid's padding.
-// Small items lie head by head, so the heads of one sequence, whose features
-// share cache lines, run together; large ones item by item within a head, so an
-// XCD works on few heads' keys at a time.
-template <bool SMALL>
-__device__ __forceinline__ bool packed_place(const PackedArgs& a, PackedItem& it, int& hk, int64_t& block) {
-    const int64_t b = xcd_block(blockIdx.x, gridDim.x);
-    if (b >= int64_t(a.n_items) * a.Hkv) return false;
+// A block of 32 x 32 values (owned row = lane, partners part(i, lane)) laid down
+// so that Cols of a Blk<T, 32> reads it turned round: partner = lane, the owned
+// rows as its 16 elements.
+template <typename T>
+__device__ __forceinline__ void lay_block(T* s, const f32x16_t& w, int lane) {
+    using B = Blk<T, 32>;
+    const int r = partner_row(lane & 31);
+#pragma unroll
+    for (int c = 0; c < 16 / B::kPiece; ++c) {
+        const int p = (16 / B::kPiece) * (lane >> 5) + c;  // piece of the row
+        uint4 x;
+        if constexpr (B::kHalf)
+            x = make_uint4(pack_bf16x2(w[8 * c], w[8 * c + 1]), pack_bf16x2(w[8 * c + 2], w[8 * c + 3]),
+                           pack_bf16x2(w[8 * c + 4], w[8 * c + 5]), pack_bf16x2(w[8 * c + 6], w[8 * c + 7]));
+        else
+            x = make_uint4(__float_as_uint(w[4 * c]), __float_as_uint(w[4 * c + 1]), __float_as_uint(w[4 * c + 2]),
+                           __float_as_uint(w[4 * c + 3]));
+        *reinterpret_cast<uint4*>(s + r * 32 + B::kPiece * (p ^ B::turn(r))) = x;
+    }
+}
+
+// A workgroup's place: which item and which kv head; false for the grid's
+// padding.  Few rows lie head by head, so the heads of one sequence, whose
+// features share cache lines, run together; tiles of many rows item by item
+// within a head, so an XCD works on few heads' keys at a time.
+// An item's tile may be shared by SUB workgroups (sub: which one).
+template <bool BY_HEAD, int SUB = 1>
+__device__ __forceinline__ bool packed_place(const PackedArgs& a, PackedItem& it, int& hk, int& sub, uint32_t& block) {
+    const uint32_t b = uint32_t(xcd_block(blockIdx.x, gridDim.x)), n = uint32_t(a.n_items) * SUB;
+    if (b >= n * uint32_t(a.Hkv)) return false;
     block = b;
-    const int64_t i = SMALL ? b / a.Hkv : b % a.n_items;
-    hk = int(SMALL ? b % a.Hkv : b / a.n_items);
-    it = a.items[i];
+    const uint32_t i = BY_HEAD ? b / uint32_t(a.Hkv) : b % n;
+    hk = int(BY_HEAD ? b % uint32_t(a.Hkv) : b / n);
+    sub = int(i % SUB);
+    it = a.items[i / SUB];
     return true;
 }
-inline unsigned packed_grid(int64_t items, int Hkv) { return xcd_grid(items * Hkv); }
+inline unsigned packed_grid(int64_t items, int Hkv, int sub = 1) { return xcd_grid(items * sub * Hkv); }
 
 // The learned bias's table of one kv head's group in LDS: [g][kTableStride],
 // -inf from the B-th bucket on.
-__device__ __forceinline__ void load_table(float* s, const PackedArgs& a, int hk) {
-    for (int x = int(threadIdx.x); x < (kTableStride << a.gs); x += int(blockDim.x)) {
+template <int THREADS>
+__device__ __forceinline__ void load_table(float* s, const PackedArgs& a, int hk, int thread) {
+    for (int x = thread; x < (kTableStride << a.gs); x += THREADS) {
         const int hg = x / kTableStride, b = x % kTableStride;
         s[x] = b < a.B ? a.table[int64_t(b) * a.H + (hk << a.gs) + hg] : -kInf;
+    }
+}
+
+// The buckets of a lane's row and 16 partners of a block: 16 bytes, at a multiple
+// of 16 (rows of buckets are padded to that); a block behind the row's end has
+// none to read.
+__device__ __forceinline__ uint4 load_ids(const uint8_t* row, int key0, int lk, int lane) {
+    const int k = key0 + 16 * (lane >> 5);
+    return k < lk ? *reinterpret_cast<const uint4*>(row + k) : make_uint4(~0u, ~0u, ~0u, ~0u);
+}
+// Bucket i of the 16, B for any that the table does not hold.
+__device__ __forceinline__ uint32_t id_of(const uint4& ids, int i, uint32_t B) {
+    const uint32_t w = i < 4 ? ids.x : i < 8 ? ids.y : i < 12 ? ids.z : ids.w;
+    const uint32_t b = (w >> (8 * (i & 3))) & 255u;
+    return b < B ? b : B;
+}
+__device__ __forceinline__ int64_t ids_width(int lk) { return (int64_t(lk) + 15) & ~int64_t(15); }
+
+// A lane's own column of a [bucket][lane] sum in LDS: no two lanes meet, so the
+// order of additions is the program's.
+__device__ __forceinline__ void hist_add(float* col, uint32_t id, float v) {
+    __hip_atomic_fetch_add(col + id * kWave, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+// out[head of the group][bucket] = the sums over the lanes (whose row's head is
+// lane % g) of `waves` such columns, each B + 1 buckets.
+template <int THREADS>
+__device__ __forceinline__ void hist_flush(const float* s, int waves, int B, int gs, float* out, int thread) {
+    const int per = kWave >> gs;
+    for (int x = thread; x < (B << gs); x += THREADS) {
+        const int head = x / B, b = x % B;
+        float t = 0.f;
+        for (int w = 0; w < waves; ++w)
+            for (int k = 0; k < per; ++k)
+                t += s[(w * (B + 1) + b) * kWave + (((k + x) & (per - 1)) << gs | head)];
+        out[x] = t;
     }
 }
 

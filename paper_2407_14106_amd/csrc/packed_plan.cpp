@@ -2,6 +2,7 @@
 // every sequence, the longest first, in lists by the kernel that runs them.
 #include <algorithm>
 #include <cstring>
+#include <utility>
 
 #include "packed.h"
 
@@ -15,39 +16,99 @@ constexpr int kMarkAt = 31;
 struct Seqs {
     int64_t n;
     const int64_t *q, *k;
-    int gs;
+    int gs, Hkv;
     bool causal;
 };
 
+// How the tiles are cut; from the whole batch, so that init and fill agree.
+struct Cut {
+    bool large_rows, large_keys;   // tiles of 256 where a sequence has as many
+    int64_t row_chunk, key_chunk;  // most partners in one walk of a tile of 32
+};
+
+// Large tiles read the partners less often, so they are taken where there are
+// enough of them to fill the chip (2 workgroups on each of 256 CUs).
+constexpr int64_t kLargeBlocks = 512;
+// The walks of few rows (or keys) are split for as many workgroups, but not into
+// shorter parts than this: parts cost a second launch and a merge.
+constexpr int64_t kFewBlocks = 512, kFewChunk = 1024;
+
+int64_t row_walk(const Seqs& s, int64_t lk, int64_t off, int64_t last) {  // keys that rows up to `last` attend to
+    return s.causal ? std::max<int64_t>(0, std::min(lk, off + (last >> s.gs) + 1)) : lk;
+}
+int64_t first_row(const Seqs& s, int64_t rows, int64_t off, int64_t key) {  // first row that attends to `key`
+    return s.causal ? std::min(rows, std::max<int64_t>(0, key - off) << s.gs) : 0;
+}
+
+bool is_pair(int64_t rows, int64_t lk) { return rows <= 32 && lk <= 32; }
+
+Cut cut(const Seqs& s) {
+    int64_t large_rows = 0, large_keys = 0, few_rows = 0, few_keys = 0;
+    for (int64_t i = 0; i < s.n; ++i) {
+        const int64_t lq = s.q[i + 1] - s.q[i], lk = s.k[i + 1] - s.k[i], rows = lq << s.gs, off = lk - lq;
+        if (is_pair(rows, lk)) continue;
+        if (rows > 0 && rows <= 32) few_rows += row_walk(s, lk, off, rows - 1);
+        if (lk > 0 && lk <= 32) few_keys += rows;
+        if (rows >= 256) large_rows += (rows + 255) / 256;
+        if (lk >= 256) large_keys += (lk + 255) / 256;
+    }
+    auto chunk = [&](int64_t total) {
+        return std::max(kFewChunk, (total * s.Hkv + kFewBlocks - 1) / kFewBlocks + 255 & ~int64_t(255));
+    };
+    return {large_rows * s.Hkv >= kLargeBlocks, large_keys * s.Hkv >= kLargeBlocks, chunk(few_rows), chunk(few_keys)};
+}
+
 // Calls f(list, item) for every item of the work list, sequence by sequence.
+// Returns the numbers of slots (row lists, key lists).
 template <typename F>
-void each_item(const Seqs& s, F f) {
-    int64_t pair = 0;
+std::pair<int64_t, int64_t> each_item(const Seqs& s, const Cut& c, F f) {
+    int64_t pair = 0, row_slots = 0, key_slots = 0;
     for (int64_t i = 0; i < s.n; ++i) {
         PackedItem it = {};
         it.q0 = int32_t(s.q[i]);
         it.k0 = int32_t(s.k[i]);
         it.lq = int32_t(s.q[i + 1] - s.q[i]);
         it.lk = int32_t(s.k[i + 1] - s.k[i]);
-        it.slot = -1;
         it.pair = pair;
         pair += int64_t(it.lq) * ((int64_t(it.lk) + 15) / 16 * 16);
-        const int64_t rows = int64_t(it.lq) << s.gs, off = int64_t(it.lk) - it.lq;
-        const bool small_rows = rows <= 32, small_keys = it.lk <= 32;
-        for (int64_t t = 0; t < rows; t += small_rows ? 32 : kRowTile) {
-            const int64_t last = std::min(rows, t + (small_rows ? 32 : kRowTile)) - 1;
-            it.tile = int32_t(t);
-            it.s0 = 0;
-            it.s1 = int32_t(s.causal ? std::max<int64_t>(0, std::min<int64_t>(it.lk, off + (last >> s.gs) + 1)) : it.lk);
-            f(small_rows ? kRowsSmall : kRowsLarge, it);
+        const int64_t rows = int64_t(it.lq) << s.gs, lk = it.lk, off = lk - it.lq;
+        it.slot = -1;
+        if (is_pair(rows, lk)) {
+            if (rows > 0 || lk > 0) f(kPairs, it);
+            continue;
         }
-        for (int64_t t = 0; t < it.lk; t += small_keys ? 32 : kRowTile) {
-            it.tile = int32_t(t);
-            it.s0 = int32_t(s.causal ? std::min(rows, std::max<int64_t>(0, t - off) << s.gs) : 0);
-            it.s1 = int32_t(rows);
-            f(small_keys ? kKeysSmall : kKeysLarge, it);
-        }
+        // one tile's walk, in parts of at most `chunk` where it is split
+        auto walk = [&](int list, int merges, int64_t& slots, int64_t tile, int64_t s0, int64_t s1, int64_t chunk) {
+            it.tile = int32_t(tile);
+            const int64_t parts = chunk > 0 ? std::max<int64_t>(1, (s1 - s0 + chunk - 1) / chunk) : 1;
+            it.slot = parts > 1 ? int32_t(slots) : -1;
+            if (parts > 1) {
+                PackedItem m = it;
+                m.s0 = int32_t(parts);
+                f(merges, m);
+                slots += parts;
+            }
+            // parts of equal length, whole blocks of 32 each
+            const int64_t each = ((s1 - s0 + parts - 1) / parts + 31) & ~int64_t(31);
+            for (int64_t p = 0; p < parts; ++p) {
+                it.s0 = int32_t(std::min(s1, s0 + p * each));
+                it.s1 = int32_t(parts > 1 ? std::min(s1, s0 + (p + 1) * each) : s1);
+                f(list, it);
+                if (parts > 1) ++it.slot;
+            }
+        };
+        const int row_list = rows <= 32 ? kRowsFew : rows <= 64 ? kRows64 : c.large_rows && rows >= 256 ? kRows256 : kRows128;
+        const int64_t row_tile = rows <= 32 ? 32 : rows <= 64 ? 64 : row_list == kRows256 ? 256 : 128;
+        for (int64_t t = 0; t < rows; t += row_tile)
+            walk(row_list, kRowMerges, row_slots, t, 0, row_walk(s, lk, off, std::min(rows, t + row_tile) - 1),
+                 row_list == kRowsFew ? c.row_chunk : 0);
+        const int key_list = lk <= 32 ? kKeysFew : lk <= 64 ? kKeys64 : c.large_keys && lk >= 256 ? kKeys256 : kKeys128;
+        const int64_t key_tile = lk <= 32 ? 32 : lk <= 64 ? 64 : key_list == kKeys256 ? 256 : 128;
+        for (int64_t t = 0; t < lk; t += key_tile)
+            walk(key_list, kKeyMerges, key_slots, t, first_row(s, rows, off, t), rows,
+                 key_list == kKeysFew ? c.key_chunk : 0);
     }
+    return {row_slots, key_slots};
 }
 
 gt_status check_seqs(const char* who, const Seqs& s, int64_t* pair_bytes) {
@@ -62,7 +123,7 @@ gt_status check_seqs(const char* who, const Seqs& s, int64_t* pair_bytes) {
     for (int64_t i = 0; i < s.n; ++i) {
         const int64_t lq = s.q[i + 1] - s.q[i], lk = s.k[i + 1] - s.k[i];
         // row numbers of one kv head, with a tile's slack, are 32-bit in the kernels
-        if ((lq << s.gs) > (int64_t(1) << 31) - 4 * kRowTile || lk > (int64_t(1) << 31) - 4 * kRowTile)
+        if ((lq << s.gs) > (int64_t(1) << 31) - 4096 || lk > (int64_t(1) << 31) - 4096)
             return fail(GT_ERR_UNSUPPORTED, w + ": a sequence of this many rows");
         pair += lq * ((lk + 15) / 16 * 16);
     }
@@ -70,10 +131,9 @@ gt_status check_seqs(const char* who, const Seqs& s, int64_t* pair_bytes) {
     return GT_OK;
 }
 
-gt_status plan_lists(const Seqs& s, int64_t (&count)[kPackedLists]) {
-    for (auto& c : count) c = 0;
-    each_item(s, [&](int list, const PackedItem&) { ++count[list]; });
-    return GT_OK;
+std::pair<int64_t, int64_t> plan_lists(const Seqs& s, const Cut& c, int64_t (&count)[kPackedLists]) {
+    for (auto& x : count) x = 0;
+    return each_item(s, c, [&](int list, const PackedItem&) { ++count[list]; });
 }
 
 }  // namespace
@@ -93,12 +153,12 @@ extern "C" gt_status gt_packed_plan_init(int64_t n_seq, const int64_t* q_ptr, co
         return fail(GT_ERR_UNSUPPORTED, std::string(who) + ": H must be a multiple of Hkv, at most 256");
     const int g = H / Hkv;
     if (g > 16 || (g & (g - 1))) return fail(GT_ERR_UNSUPPORTED, std::string(who) + ": H / Hkv must be 1, 2, 4, 8 or 16");
-    const Seqs s = {n_seq, q_ptr, k_ptr, ilog2(g), causal != 0};
+    const Seqs s = {n_seq, q_ptr, k_ptr, ilog2(g), Hkv, causal != 0};
     int64_t pair = 0;
     gt_status st = check_seqs(who, s, &pair);
     if (st != GT_OK) return st;
     int64_t count[kPackedLists];
-    if ((st = plan_lists(s, count)) != GT_OK) return st;
+    const auto slots = plan_lists(s, cut(s), count);
     int64_t at = 0;
     for (int l = 0; l < kPackedLists; ++l) {
         if (count[l] * Hkv > (int64_t(1) << 31) - 64)  // one block for each item and kv head
@@ -115,6 +175,8 @@ extern "C" gt_status gt_packed_plan_init(int64_t n_seq, const int64_t* q_ptr, co
     plan->H = H;
     plan->Hkv = Hkv;
     plan->causal = causal != 0;
+    plan->layout[kRowSlotsAt] = slots.first;
+    plan->layout[kKeySlotsAt] = slots.second;
     plan->layout[kMarkAt] = kPlanMark;
     return GT_OK;
 }
@@ -127,12 +189,13 @@ extern "C" gt_status gt_packed_plan_fill(int64_t n_seq, const int64_t* q_ptr, co
     if (n_seq != plan->n_seq) return fail(GT_ERR_INVALID_ARG, std::string(who) + ": n_seq differs from init's");
     if (bytes < size_t(plan->item_bytes)) return fail(GT_ERR_WORKSPACE, std::string(who) + ": item buffer too small");
     if (plan->item_bytes > 0 && !host_items) return fail(GT_ERR_INVALID_ARG, std::string(who) + ": null pointer");
-    const Seqs s = {n_seq, q_ptr, k_ptr, ilog2(plan->H / plan->Hkv), plan->causal != 0};
+    const Seqs s = {n_seq, q_ptr, k_ptr, ilog2(plan->H / plan->Hkv), plan->Hkv, plan->causal != 0};
     int64_t pair = 0;
     gt_status st = check_seqs(who, s, &pair);
     if (st != GT_OK) return st;
     int64_t count[kPackedLists];
-    if ((st = plan_lists(s, count)) != GT_OK) return st;
+    const Cut c = cut(s);
+    plan_lists(s, c, count);
     bool same = pair == plan->pair_bytes && q_ptr[n_seq] == plan->nq && k_ptr[n_seq] == plan->nk;
     for (int l = 0; l < kPackedLists; ++l) same = same && count[l] == plan->layout[2 * l + 1];
     if (!same) return fail(GT_ERR_INVALID_ARG, std::string(who) + ": the sequences differ from init's");
@@ -140,12 +203,14 @@ extern "C" gt_status gt_packed_plan_fill(int64_t n_seq, const int64_t* q_ptr, co
     for (int l = 0; l < kPackedLists; ++l)
         list[l] = reinterpret_cast<PackedItem*>(static_cast<char*>(host_items) + plan->layout[2 * l]);
     int64_t fill[kPackedLists] = {};
-    each_item(s, [&](int l, const PackedItem& it) { list[l][fill[l]++] = it; });
-    // the longest walks first, so that no long one starts when the chip runs empty
-    for (int l = 0; l < kPackedLists; ++l)
+    each_item(s, c, [&](int l, const PackedItem& it) { list[l][fill[l]++] = it; });
+    // the longest walks first, so that no long one starts when the chip runs empty (pairs are all alike)
+    for (int l = kPairs + 1; l < kRowMerges; ++l)
         std::sort(list[l], list[l] + count[l], [](const PackedItem& a, const PackedItem& b) {
             const int32_t ca = a.s1 - a.s0, cb = b.s1 - b.s0;
-            return ca != cb ? ca > cb : a.q0 != b.q0 ? a.q0 < b.q0 : a.k0 != b.k0 ? a.k0 < b.k0 : a.tile < b.tile;
+            return ca != cb ? ca > cb : a.q0 != b.q0 ? a.q0 < b.q0 : a.k0 != b.k0 ? a.k0 < b.k0
+                                                                   : a.tile != b.tile ? a.tile < b.tile
+                                                                                      : a.s0 < b.s0;
         });
     return GT_OK;
 }

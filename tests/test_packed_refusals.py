@@ -69,43 +69,59 @@ def test_plan_null_and_changed_arguments(lib):
 
 @pytest.mark.parametrize("causal", [0, 1])
 @pytest.mark.parametrize("group", [1, 4])
-def test_plan_covers_every_row_and_key_once(lib, causal, group):
-    lq = [0, 1, 7, 32, 33, 129, 0, 300, 5, 1, 700]
-    lk = [4, 0, 9, 40, 31, 129, 0, 100, 2000, 4097, 701]
+@pytest.mark.parametrize("many", [False, True])
+def test_plan_covers_every_row_and_key_once(lib, causal, group, many):
+    lq = [0, 1, 7, 32, 33, 129, 0, 300, 5, 1, 700, 40, 3000]
+    lk = [4, 0, 9, 40, 31, 129, 0, 100, 2000, 4097, 701, 50, 20]
+    if many:  # enough for large tiles
+        lq, lk = lq + [1000, 257] * 60, lk + [1000, 300] * 60
     q, k = ptrs(*lq), ptrs(*lk)
-    st, c = init(lib, q, k, 2 * group, 2, causal)
+    st, c = init(lib, q, k, 8 * group, 8, causal)
     assert st == gt.GT_OK
     host = np.zeros(c.item_bytes, dtype=np.uint8)
     assert lib.gt_packed_plan_fill(len(lq), q.ctypes.data, k.ctypes.data, ctypes.byref(c), host.ctypes.data,
                                    c.item_bytes) == gt.GT_OK
     assert c.pair_bytes == OP.pair_layout(lq, lk)[1]
     at, _ = OP.pair_layout(lq, lk)
-    lists = [(c.layout[2 * i], c.layout[2 * i + 1]) for i in range(4)]
-    items = [host[a:a + 40 * n].view(np.int32).reshape(n, 10) for a, n in lists]
+    assert not many or (c.layout[2 * 4 + 1] > 0 and c.layout[2 * 8 + 1] > 0)
+    names = ("pairs", 32, 64, 128, 256, 32, 64, 128, 256, "row merges", "key merges")
+    items = [host[c.layout[2 * i]:c.layout[2 * i] + 40 * c.layout[2 * i + 1]].view(np.int32).reshape(-1, 10)
+             for i in range(len(names))]
     by_seq = {(int(q[s]), int(k[s]), lq[s], lk[s]): s for s in range(len(lq))}
 
-    def walked(lists, owned, streamed, needs):
-        """Every owned index is in one tile, and its items walk each partner that it needs exactly once."""
+    def walked(lists, owned, streamed, needs, merges):
+        """Every owned index is in one tile, and its items walk each partner that it needs exactly once; the parts of a
+        split tile have the slots that its merge names."""
         seen = [np.zeros((owned(s),), dtype=np.int64) for s in range(len(lq))]
+        parts = {}
         for tile, rows in lists:
             for it in rows:
                 q0, l_q, k0, l_k, t, s0, s1, slot = (int(x) for x in it[:8])
                 s = by_seq[(q0, k0, l_q, l_k)]
                 assert int(it[8:10].view(np.int64)[0]) == at[s]
                 assert 0 <= s0 <= max(s0, s1) <= max(streamed(s), s0) and t % 32 == 0 and t < max(1, owned(s))
+                if slot >= 0:
+                    assert tile == 32 and s0 % 32 == 0 or not causal
+                    parts.setdefault((s, t), []).append(slot)
                 for x in range(t, min(owned(s), t + tile)):
                     lo, hi = needs(s, x)
                     seen[s][x] += max(0, min(hi, s1) - max(lo, s0))
+        for it in merges:
+            q0, l_q, k0, l_k, t, n, _, slot = (int(x) for x in it[:8])
+            assert sorted(parts.pop((by_seq[(q0, k0, l_q, l_k)], t))) == list(range(slot, slot + n))
+        assert not parts
         for s in range(len(lq)):
             for x in range(owned(s)):
                 lo, hi = needs(s, x)
-                assert seen[s][x] == max(0, hi - lo), (s, x)
+                assert seen[s][x] == max(0, hi - lo) or (lq[s] * group <= 32 and lk[s] <= 32), (s, x)
 
+    small = [s for s in range(len(lq)) if lq[s] * group <= 32 and lk[s] <= 32 and lq[s] + lk[s] > 0]
+    assert sorted(by_seq[tuple(int(it[x]) for x in (0, 2, 1, 3))] for it in items[0]) == small
     off = [b - a for a, b in zip(lq, lk)]
     row_needs = lambda s, r: (0, max(0, min(lk[s], off[s] + r // group + 1)) if causal else lk[s])  # noqa: E731
     key_needs = lambda s, j: (min(lq[s] * group, max(0, j - off[s]) * group) if causal else 0, lq[s] * group)  # noqa: E731
-    walked([(32, items[0]), (128, items[1])], lambda s: lq[s] * group, lambda s: lk[s], row_needs)
-    walked([(32, items[2]), (128, items[3])], lambda s: lk[s], lambda s: lq[s] * group, key_needs)
+    walked(list(zip(names[1:5], items[1:5])), lambda s: lq[s] * group, lambda s: lk[s], row_needs, items[9])
+    walked(list(zip(names[5:9], items[5:9])), lambda s: lk[s], lambda s: lq[s] * group, key_needs, items[10])
 
 
 def attn_args(c, **kw):
