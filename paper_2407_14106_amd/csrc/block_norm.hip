@@ -312,25 +312,25 @@ __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_bwd(NormArgs a) 
     }
 }
 
-// out[k][x] = the sum over the workgroups' partial sums, 64 columns a workgroup.
+// out[k][x] = the sum over the workgroups' partial sums, 16 columns a workgroup:
+// 64 threads for each, every one a 64th of the partial sums, then those 64.
 struct SumOut {
     float* p[kSums];
 };
 __global__ __launch_bounds__(1024) void k_norm_sum(int blocks, int D, const float* __restrict__ part, SumOut o) {
     __shared__ float s[1024];
-    const int k = int(blockIdx.y), x = int(blockIdx.x) * kWave + lane_id();
+    const int k = int(blockIdx.y), x = int(blockIdx.x) * 16 + int(threadIdx.x & 15);
     float* out = o.p[k];
     if (!out) return;  // uniform
     float t = 0.f;
     if (x < D)
-        for (int b = int(threadIdx.x) / kWave; b < blocks; b += 1024 / kWave)
-            t += part[(int64_t(b) * kSums + k) * D + x];
+#pragma unroll 8
+        for (int b = int(threadIdx.x) / 16; b < blocks; b += 64) t += part[(int64_t(b) * kSums + k) * D + x];
     s[threadIdx.x] = t;
     __syncthreads();
-    if (threadIdx.x < kWave && x < D) {
-        for (int w = 1; w < 1024 / kWave; ++w) t += s[w * kWave + lane_id()];
-        out[x] = t;
-    }
+    if (threadIdx.x >= 16 || x >= D) return;
+    for (int w = 1; w < 64; ++w) t += s[16 * w + threadIdx.x];
+    out[x] = t;
 }
 
 // Lanes per row and pieces per lane: the fewest lanes that hold a row at one
@@ -458,7 +458,7 @@ extern "C" gt_status gt_block_norm_bwd(int64_t n, int32_t D, gt_dtype dt, int32_
         GT_LAUNCH_CHECK("block_norm_bwd");
     }
     if (a.want) {
-        k_norm_sum<<<dim3(unsigned(cdiv(D, kWave)), kSums), 1024, 0, s>>>(blocks, D, a.part, o);
+        k_norm_sum<<<dim3(unsigned(cdiv(D, 16)), kSums), 1024, 0, s>>>(blocks, D, a.part, o);
         GT_LAUNCH_CHECK("block_norm_bwd sum");
     }
     return GT_OK;

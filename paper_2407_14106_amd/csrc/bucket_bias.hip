@@ -12,33 +12,51 @@ typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));
 constexpr int kThreads = 256;
 
 // bias[e, h] = table[bucket[e], h].  Bound by its stores: 4 H bytes an edge
-// against one byte read.  A thread writes 16 bytes at a time, UNROLL of them
-// kThreads apart, from the table in LDS.
+// against one byte read.  A thread writes 16 bytes at a time from the table in
+// LDS; workgroups stay (a short one spends its time on loading the table) and
+// take turns at runs of UNROLL x 4 KB, the next run's buckets loaded ahead.
+constexpr int64_t kFwdBlocks = 2048;
+
 template <int HS, int UNROLL>
 __global__ __launch_bounds__(kThreads) void k_bucket_fwd(int64_t nnz, int B, const float* __restrict__ table,
                                                          const uint8_t* __restrict__ bucket,
                                                          float* __restrict__ bias) {
-    constexpr int H = 1 << HS;
+    constexpr int H = 1 << HS, E = H >= 4 ? 1 : 4 / H;  // edges in 16 bytes
     __shared__ float s_tab[(kMaxBuckets + 1) << HS];
     for (int x = int(threadIdx.x); x < (kMaxBuckets + 1) << HS; x += kThreads)
         s_tab[x] = x < (B << HS) ? table[x] : -__builtin_huge_valf();
     __syncthreads();
-    const int64_t total = nnz << HS;
-    const int64_t base = int64_t(blockIdx.x) * (kThreads * 4 * UNROLL) + 4 * int(threadIdx.x);
+    const int64_t total = nnz << HS, run = int64_t(kThreads) * 4 * UNROLL, step = run * gridDim.x;
+    const int head = int((4 * threadIdx.x) & (H - 1));  // a run is whole edges
+    uint32_t id[UNROLL][E];
+    auto load = [&](int64_t base) {
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const int64_t at = base + int64_t(u) * (kThreads * 4);
-        if (at >= total) break;
-        f32x4u_t v;
+        for (int u = 0; u < UNROLL; ++u)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int64_t e = (at + t) >> HS;
-            const int id = e < nnz ? bucket[e] : 0;
-            v[t] = s_tab[(id < B ? id : kMaxBuckets) * H + int((at + t) & (H - 1))];
+            for (int k = 0; k < E; ++k) {
+                const int64_t e = ((base + u * (kThreads * 4)) >> HS) + k;
+                id[u][k] = e < nnz ? bucket[e] : 0u;
+            }
+    };
+    int64_t base = run * blockIdx.x + 4 * int(threadIdx.x);
+    load(base);
+    for (; base < total; base += step) {
+        f32x4u_t v[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const uint32_t b = id[u][E == 1 ? 0 : t / H];
+                v[u][t] = s_tab[(b < uint32_t(B) ? b : uint32_t(kMaxBuckets)) * H + (E == 1 ? head + t : t & (H - 1))];
+            }
+        load(base + step);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int64_t at = base + u * (kThreads * 4);
+            if (at + 4 <= total) *reinterpret_cast<f32x4u_t*>(bias + at) = v[u];
+            else
+                for (int t = 0; t < 4 && at + t < total; ++t) bias[at + t] = v[u][t];
         }
-        if (at + 4 <= total) *reinterpret_cast<f32x4u_t*>(bias + at) = v;
-        else
-            for (int t = 0; t < 4 && at + t < total; ++t) bias[at + t] = v[t];
     }
 }
 
@@ -47,7 +65,7 @@ __global__ __launch_bounds__(kThreads) void k_bucket_fwd(int64_t nnz, int B, con
 // H); it adds each to a column of its own in LDS ([bucket][lane]), so no two
 // lanes meet and the order of additions is the program's.  A workgroup leaves
 // one partial table, and k_bucket_sum adds those.
-constexpr int kBurst = 16;  // loads in flight per lane
+constexpr int kBurst = 16;  // values a lane loads together
 constexpr int64_t kSumBlocks = 1024;
 
 __global__ __launch_bounds__(kThreads) void k_bucket_bwd(int64_t nnz, int hs, int B,
@@ -59,18 +77,29 @@ __global__ __launch_bounds__(kThreads) void k_bucket_bwd(int64_t nnz, int hs, in
     for (int b = 0; b <= B; ++b) col[b * kWave + lane] = 0.f;
     const int64_t total = nnz << hs, step = int64_t(kBurst) * kWave;
     const int64_t waves = int64_t(gridDim.x) * (kThreads / kWave);
-    for (int64_t base = (int64_t(blockIdx.x) * (kThreads / kWave) + wave) * step; base < total; base += waves * step) {
-        float v[kBurst];
-        int id[kBurst];
+    float v[2][kBurst];
+    uint32_t id[2][kBurst];
+    auto load = [&](int k, int64_t base) {
 #pragma unroll
         for (int u = 0; u < kBurst; ++u) {
             const int64_t at = base + u * kWave + lane;
             const bool in = at < total;
-            v[u] = in ? dbias[at] : 0.f;
-            id[u] = in ? bucket[at >> hs] : B;
+            v[k][u] = in ? dbias[at] : 0.f;
+            id[k][u] = in ? bucket[at >> hs] : uint32_t(B);
         }
+    };
+    auto add = [&](int k) {
 #pragma unroll
-        for (int u = 0; u < kBurst; ++u) col[(id[u] < B ? id[u] : B) * kWave + lane] += v[u];
+        for (int u = 0; u < kBurst; ++u) col[(id[k][u] < uint32_t(B) ? id[k][u] : uint32_t(B)) * kWave + lane] += v[k][u];
+    };
+    // a burst is loaded while the one before is added
+    int64_t base = (int64_t(blockIdx.x) * (kThreads / kWave) + wave) * step;
+    load(0, base);
+    for (; base < total; base += 2 * waves * step) {
+        load(1, base + waves * step);
+        add(0);
+        load(0, base + 2 * waves * step);
+        add(1);
     }
     __syncthreads();
     const int H = 1 << hs, per = kWave >> hs;
@@ -83,17 +112,22 @@ __global__ __launch_bounds__(kThreads) void k_bucket_bwd(int64_t nnz, int hs, in
     }
 }
 
-// out[x] = the sum over the partial tables, one workgroup per 64 entries.
-__global__ __launch_bounds__(kThreads) void k_bucket_sum(int64_t parts, int n, const float* __restrict__ part,
-                                                         float* __restrict__ out) {
-    __shared__ float s[kThreads];
-    const int x = int(blockIdx.x) * kWave + lane_id();
+// out[x] = the sum over the partial tables, 16 entries a workgroup: 64 threads
+// for each, every one a 64th of the tables, then those 64.
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void k_bucket_sum(int64_t parts, int n, const float* __restrict__ part,
+                                                            float* __restrict__ out) {
+    __shared__ float s[kSumThreads];
+    const int x = int(blockIdx.x) * 16 + int(threadIdx.x & 15);
     float t = 0.f;
-    for (int64_t p = threadIdx.x / kWave; p < parts; p += kThreads / kWave) t += x < n ? part[p * n + x] : 0.f;
+    if (x < n)
+#pragma unroll 8
+        for (int64_t p = threadIdx.x / 16; p < parts; p += kSumThreads / 16) t += part[p * n + x];
     s[threadIdx.x] = t;
     __syncthreads();
-    if (threadIdx.x < kWave && x < n)
-        out[x] = (s[lane_id()] + s[lane_id() + 64]) + (s[lane_id() + 128] + s[lane_id() + 192]);
+    if (threadIdx.x >= 16 || x >= n) return;
+    for (int k = 1; k < kSumThreads / 16; ++k) t += s[16 * k + threadIdx.x];
+    out[x] = t;
 }
 
 int64_t sum_blocks(int64_t nnz, int32_t H) {
@@ -120,7 +154,8 @@ extern "C" gt_status gt_bucket_bias_fwd(int64_t nnz, int32_t H, int32_t B, const
     if (!table) return fail(GT_ERR_INVALID_ARG, std::string(who) + ": null pointer");
     if (nnz == 0) return GT_OK;
     constexpr int U = 4;
-    const unsigned grid = unsigned(cdiv(nnz * H, int64_t(kThreads) * 4 * U));
+    const int64_t runs = cdiv(nnz * H, int64_t(kThreads) * 4 * U);
+    const unsigned grid = unsigned(runs < kFwdBlocks ? runs : kFwdBlocks);
     switch (H) {
         case 1: k_bucket_fwd<0, U><<<grid, kThreads, 0, s>>>(nnz, B, table, bucket, bias); break;
         case 2: k_bucket_fwd<1, U><<<grid, kThreads, 0, s>>>(nnz, B, table, bucket, bias); break;
@@ -155,7 +190,7 @@ extern "C" gt_status gt_bucket_bias_bwd(int64_t nnz, int32_t H, int32_t B, const
             nnz, ilog2(H), B, bucket, dbias, part);
         GT_LAUNCH_CHECK("bucket_bias_bwd");
     }
-    k_bucket_sum<<<unsigned(cdiv(B * H, kWave)), kThreads, 0, s>>>(blocks, B * H, part, dtable);
+    k_bucket_sum<<<unsigned(cdiv(B * H, 16)), kSumThreads, 0, s>>>(blocks, B * H, part, dtable);
     GT_LAUNCH_CHECK("bucket_bias_bwd sum");
     return GT_OK;
 }

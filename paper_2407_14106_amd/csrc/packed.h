@@ -81,6 +81,10 @@ constexpr int waves_per_simd(int stage_bytes, int waves) {
     return w < 1 ? 1 : w > 2 ? 2 : w;
 }
 
+// Below this many workgroups of four wavefronts (two for each of 256 CUs) two
+// sets of them share a walk.
+constexpr int64_t kSharedBlocks = 512;
+
 // Floats of one slot of a split tile (32 rows or keys): forward m, l and O;
 // statistics; dQ; dK and dV.
 constexpr int64_t kFewRows = 32;

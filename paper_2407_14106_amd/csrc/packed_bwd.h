@@ -31,6 +31,8 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
         load_table<kWave>(tab, a, hk, lane);
         for (int b = 0; b <= a.B; ++b) hist[b * kWave + lane] = 0.f;
     }
+    const typename B::At at(lane, 0);
+    const typename S::At turned_at(lane, 0);
     for (uint32_t unit = first; unit < units; unit += step) {
         const PackedItem it = a.items[unit / uint32_t(a.Hkv)];
         const int R = it.lq << gs, off = it.lk - it.lq;
@@ -62,9 +64,9 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
             {
                 typename B::Row own[1];
                 own[0].staged(sQ, lane);
-                B::template rows<1>(sK, 0, own, s, lane);
+                B::template rows<1>(sK, at, own, s);
                 own[0].staged(sG, lane);
-                B::template rows<1>(sV, 0, own, dp, lane);
+                B::template rows<1>(sV, at, own, dp);
             }
             const int lim = r >= R ? 0 : a.causal && off + q + 1 < it.lk ? off + q + 1 : it.lk;
             float sum = 0.f, dsum = 0.f;
@@ -74,7 +76,7 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
                 if constexpr (BIAS) u = fmaf(s[0][i], a.scale, tab[(r & gm) * kTableStride + id_of(ids, i, a.B)]);
                 else u = s[0][i] * a.scale;
                 s[0][i] = ex2((u - L) * kLog2e);
-                if (part(i, lane) >= lim) s[0][i] = 0.f, dp[0][i] = 0.f;
+                if (i >= lim - part(0, lane)) s[0][i] = 0.f, dp[0][i] = 0.f;
                 sum += s[0][i];
                 dsum = fmaf(s[0][i], dp[0][i], dsum);
             }
@@ -87,7 +89,7 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
                 if constexpr (BIAS) hist_add(hist + lane, id_of(ids, i, a.B), dp[0][i]);
             }
             typename B::Cols x;
-            x.load(sK, 0, lane);
+            x.load(sK, at);
             x.drop(it.lk, lane);
             B::template apply<1>(x, dp, dq);
             wave_done();  // K and V are read: their place takes P and dS
@@ -97,16 +99,16 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
             typename B::Weights w[1];
             typename S::Cols t;
             auto turned = [&](const T* from) {
-                t.load(from, 0, lane);
+                t.load(from, turned_at);
 #pragma unroll
                 for (int i = 0; i < (B::kHalf ? 2 : 16); ++i) w[0].v[i] = t.v[0][i];
             };
             turned(sK);
-            x.load(sG, 0, lane);
+            x.load(sG, at);
             x.drop(R, lane);
             B::template apply<1>(x, w, dv);
             turned(sV);
-            x.load(sQ, 0, lane);
+            x.load(sQ, at);
             x.drop(R, lane);
             B::template apply<1>(x, w, dk);
         }
@@ -155,7 +157,7 @@ enum RowPass { kStat, kGrad };
 // and the weights' sum under the given LSE: an fp32 LSE beside a large bias
 // holds log(sum) only roughly, so P is normalised again by it.
 template <typename T, int D, int STAGE, int W, int KS, int SUB, bool BIAS, RowPass PASS>
-__global__ __launch_bounds__(W * KS * kWave) void k_packed_rows(PackedArgs a) {
+__global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(D * int(sizeof(T)) <= 128 ? waves_per_simd(KS * 4 * STAGE * D * int(sizeof(T)), W* KS) : 1))) void k_packed_rows(PackedArgs a) {
     using B = Blk<T, D, STAGE>;
     __shared__ __attribute__((aligned(16))) T sK0[KS * B::kElems], sK1[KS * B::kElems];
     __shared__ __attribute__((aligned(16))) T sV0[KS * B::kElems], sV1[KS * B::kElems];
@@ -192,8 +194,7 @@ __global__ __launch_bounds__(W * KS * kWave) void k_packed_rows(PackedArgs a) {
     const int r = row0 + (lane & 31), rc = r < R ? r : R - 1;
     const int q = rc >> gs, hg = rc & gm;
     const int64_t at = int64_t(it.q0 + q) * a.H + (hk << gs) + hg;
-    const int lim = r < R ? limit(q) : 0;  // a row past the end takes no part, in the table's gradient either
-    const int lo = uniform(row0 + 32 <= R ? limit(row0 >> gs) : 0);
+    const int lim = limit(q);
     const int hi = uniform(row0 < R ? limit((row0 + 31 < R ? row0 + 31 : R - 1) >> gs) : 0);
     const uint8_t* id_row = BIAS ? a.ids + it.pair + q * ids_width(it.lk) : nullptr;
     typename B::Row qf[1], gf[1];
@@ -202,6 +203,7 @@ __global__ __launch_bounds__(W * KS * kWave) void k_packed_rows(PackedArgs a) {
     const float sl2 = a.scale * kLog2e;
     float L = a.LSE[at], lg = 0.f, Dq = 0.f;
     if (L == -kInf) L = 0.f;  // an empty row: every score is masked
+    if (r >= R) L = kInf;     // a row past the end weighs nothing, in the table's gradient either
     if constexpr (!BIAS) {
         L *= kLog2e;
         typename B::Row of;
@@ -217,62 +219,73 @@ __global__ __launch_bounds__(W * KS * kWave) void k_packed_rows(PackedArgs a) {
     for (int db = 0; db < D / 32; ++db) acc[0][db] = splat16(0.f);
     float sum = 0.f, dsum = 0.f;
     stage_done<(W > 1) || BIAS>();
-    auto stage = [&](int kbase, const T* cK, const T* cV, T* nK, T* nV) {
-        fetch(kbase + KS * STAGE, nK, nV);
+    const typename B::At lds(lane, set * B::kElems * int(sizeof(T)));
+    auto block32 = [&](auto masked, int key0, const T* bK, const T* bV) {
+        uint4 ids;
+        if constexpr (BIAS) ids = load_ids(id_row, key0, it.lk, lane);
+        const int left = lim - key0 - part(0, lane);  // how many of the lane's 16 keys its row attends to
+        f32x16_t s[1] = {splat16(0.f)}, dp[1] = {splat16(-Dq)};
+        B::template rows<1>(bK, lds, qf, s);
+        B::template rows<1>(bV, lds, gf, dp);
+        typename B::Cols kt;
+        if constexpr (PASS == kGrad) {
+            kt.load(bK, lds);
+            if constexpr (masked.value) kt.drop(it.s1 - key0, lane);
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
-        for (int kb = 0; kb < STAGE / 32; ++kb) {
-            const int key0 = kbase + 32 * kb;
-            if (key0 >= hi) break;  // uniform
-            uint4 ids;
-            if constexpr (BIAS) ids = load_ids(id_row, key0, it.lk, lane);
-            f32x16_t s[1] = {splat16(0.f)}, dp[1] = {splat16(-Dq)};
-            B::template rows<1>(cK + set * B::kElems, 32 * kb, qf, s, lane);
-            B::template rows<1>(cV + set * B::kElems, 32 * kb, gf, dp, lane);
-            typename B::Cols kt;
-            if constexpr (PASS == kGrad) {
-                kt.load(cK + set * B::kElems, 32 * kb, lane);
-                if (key0 + 32 > it.s1) {
-                    asm volatile("" ::: "memory");
-                    kt.drop(it.s1 - key0, lane);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                if constexpr (BIAS) {
-                    const float u = fmaf(s[0][i], a.scale, s_tab[hg * kTableStride + id_of(ids, i, a.B)]);
-                    s[0][i] = fmaf(u - L, kLog2e, -lg);
-                } else {
-                    s[0][i] = fmaf(s[0][i], sl2, -L);
-                }
-            }
-            if (key0 + 32 > lo) {
-                asm volatile("" ::: "memory");
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (key0 + part(i, lane) >= lim) s[0][i] = -kInf, dp[0][i] = 0.f;
-            }
-            if constexpr (PASS == kStat) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float p = ex2(s[0][i]);
-                    sum += p;
-                    dsum = fmaf(p, dp[0][i], dsum);
-                }
+        for (int i = 0; i < 16; ++i) {
+            uint32_t id = 0;
+            float t;
+            if constexpr (BIAS) {
+                id = id_of(ids, i, a.B);
+                t = fmaf(fmaf(s[0][i], a.scale, s_tab[hg * kTableStride + id]) - L, kLog2e, -lg);
             } else {
+                t = fmaf(s[0][i], sl2, -L);
+            }
+            if constexpr (masked.value) {
+                const bool out = i >= left;
+                t = out ? -kInf : t;
+                dp[0][i] = out ? 0.f : dp[0][i];
+            }
+            const float p = ex2(t);
+            s[0][i] = p * dp[0][i];
+            if constexpr (PASS == kStat) {
+                sum += p;
+                dsum += s[0][i];
+            } else if constexpr (BIAS) {
+                hist_add(hist, id, s[0][i]);
+            }
+        }
+        if constexpr (PASS == kGrad) B::template apply<1>(kt, s, acc);
+    };
+    auto stage = [&](auto masked, int kbase, const T* cK, const T* cV, T* nK, T* nV) {
+        fetch(kbase + KS * STAGE, nK, nV);
+        if constexpr (masked.value) {
+#pragma unroll 1
+            for (int kb = 0; kb < STAGE / 32; ++kb)
+                if (kbase + 32 * kb < hi)  // uniform
+                    block32(masked, kbase + 32 * kb, cK + 32 * kb * D, cV + 32 * kb * D);
+        } else {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[0][i] = ex2(s[0][i]) * dp[0][i];
-                    if constexpr (BIAS) hist_add(hist, id_of(ids, i, a.B), s[0][i]);
-                }
-                B::template apply<1>(kt, s, acc);
+            for (int kb = 0; kb < STAGE / 32; ++kb) {
+                __builtin_amdgcn_sched_barrier(0);  // two blocks' operands at once do not fit the registers
+                block32(masked, kbase + 32 * kb, cK + 32 * kb * D, cV + 32 * kb * D);
             }
         }
         stage_done<(W > 1)>();
     };
-    for (int kbase = it.s0; kbase < it.s1; kbase += 2 * KS * STAGE) {
-        stage(kbase + set * STAGE, sK0, sV0, sK1, sV1);
-        if (kbase + KS * STAGE < it.s1) stage(kbase + (KS + set) * STAGE, sK1, sV1, sK0, sV0);
+    // as in the forward
+    constexpr int kRound = KS * STAGE;
+    const int first_row = it.tile + sub * W * 32 < R ? it.tile + sub * W * 32 : R - 1, lo = uniform(limit(first_row >> gs));
+    int kbase = it.s0;
+    for (int n = lo > it.s0 ? (lo - it.s0) / (2 * kRound) : 0; n > 0; --n, kbase += 2 * kRound) {
+        stage(Flag<false>{}, kbase + set * STAGE, sK0, sV0, sK1, sV1);
+        stage(Flag<false>{}, kbase + kRound + set * STAGE, sK1, sV1, sK0, sV0);
+    }
+    for (; kbase < it.s1; kbase += 2 * kRound) {
+        stage(Flag<true>{}, kbase + set * STAGE, sK0, sV0, sK1, sV1);
+        if (kbase + kRound < it.s1) stage(Flag<true>{}, kbase + kRound + set * STAGE, sK1, sV1, sK0, sV0);
     }
     if constexpr (PASS == kStat) {
         sum = pair_sum(sum);
@@ -316,8 +329,8 @@ __global__ __launch_bounds__(W * KS * kWave) void k_packed_rows(PackedArgs a) {
 // dK_j = scale sum_i dS_ij Q_i and dV_j = sum_i P_ij dO_i over the rows of the
 // whole group, with the wavefront owning 32 keys and the rows streaming through
 // LDS; the dP products start from the rows' -D_i.
-template <typename T, int D, int STAGE, int W, int KS, bool BIAS>
-__global__ __launch_bounds__(W * KS * kWave) void k_packed_keys(PackedArgs a) {
+template <typename T, int D, int STAGE, int W, int KS, int SUB, bool BIAS>
+__global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(D * int(sizeof(T)) <= 128 ? waves_per_simd(KS * 4 * STAGE * D * int(sizeof(T)), W* KS) : 1))) void k_packed_keys(PackedArgs a) {
     using B = Blk<T, D, STAGE>;
     __shared__ __attribute__((aligned(16))) T sQ0[KS * B::kElems], sQ1[KS * B::kElems];
     __shared__ __attribute__((aligned(16))) T sG0[KS * B::kElems], sG1[KS * B::kElems];
@@ -328,11 +341,11 @@ __global__ __launch_bounds__(W * KS * kWave) void k_packed_keys(PackedArgs a) {
     PackedItem it;
     int hk, sub;
     uint32_t block;
-    if (!packed_place<W == 1>(a, it, hk, sub, block)) return;
+    if (!packed_place<W == 1, SUB>(a, it, hk, sub, block)) return;
     const int lane = lane_id(), wave = uniform(int(threadIdx.x) / kWave);
     const int set = KS == 1 ? 0 : wave / W, key_wave = wave - set * W;
     const int gs = a.gs, gm = (1 << gs) - 1, off = it.lk - it.lq;
-    const int key0 = it.tile + key_wave * 32;
+    const int key0 = it.tile + (sub * W + key_wave) * 32;
     if constexpr (BIAS) load_table<W * KS * kWave>(s_tab, a, hk, int(threadIdx.x));
     float rs[3] = {0.f, 0.f, 0.f};
     auto load_stats = [&](int base) {
@@ -368,108 +381,129 @@ __global__ __launch_bounds__(W * KS * kWave) void k_packed_keys(PackedArgs a) {
     auto first_row = [&](int key) { return a.causal && key > off ? (key - off) << gs : 0; };
     const int rmin = first_row(jc);
     const int rlo = uniform(first_row(key0 < it.lk ? key0 : it.lk - 1));
-    const int rhi = uniform(first_row(key0 + 31 < it.lk ? key0 + 31 : it.lk - 1));
     typename B::Row kf[1], vf[1];
     kf[0].load(static_cast<const T*>(a.K) + int64_t(it.k0 + jc) * a.ldk + hk * D, lane);
     vf[0].load(static_cast<const T*>(a.V) + int64_t(it.k0 + jc) * a.ldv + hk * D, lane);
-    f32x16_t dk[D / 32], dv[1][D / 32];
+    f32x16_t dk[1][D / 32], dv[1][D / 32];
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db) dk[db] = dv[0][db] = splat16(0.f);
+    for (int db = 0; db < D / 32; ++db) dk[0][db] = dv[0][db] = splat16(0.f);
     const float sl2 = a.scale * kLog2e;
     const uint8_t* id_key = BIAS ? a.ids + it.pair + jc : nullptr;
     const int64_t wide = ids_width(it.lk);
     store_stats(sR0);
     stage_done<(W > 1) || BIAS>();
-    auto stage = [&](int base, const T* cQ, const T* cG, const Stats& cR, T* nQ, T* nG, Stats& nR) {
-        load_stats(base + KS * STAGE);
-        fetch(base + KS * STAGE, nQ, nG);
-#pragma unroll
-        for (int rb = 0; rb < STAGE / 32; ++rb) {
-            const int r0 = base + 32 * rb;
-            if (r0 >= it.s1 || key0 >= it.lk) break;  // uniform
-            if (r0 + 32 <= rlo) continue;             // before every key of this wavefront
-            uint32_t id[16];
-            if constexpr (BIAS) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int r = r0 + part(i, lane);
-                    const uint32_t b = r < it.s1 ? id_key[(r >> gs) * wide] : 255u;
-                    id[i] = b < uint32_t(a.B) ? b : uint32_t(a.B);
-                }
-            }
-            f32x16_t s[1] = {splat16(0.f)}, dp[1];
-            float L[16], lg[16];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int r = 32 * rb + 16 * (lane >> 5) + 4 * x;
-                const float4 l4 = *reinterpret_cast<const float4*>(&cR[set][0][r]);
-                const float4 d4 = *reinterpret_cast<const float4*>(&cR[set][1][r]);
-                L[4 * x] = l4.x, L[4 * x + 1] = l4.y, L[4 * x + 2] = l4.z, L[4 * x + 3] = l4.w;
-                dp[0][4 * x] = d4.x, dp[0][4 * x + 1] = d4.y, dp[0][4 * x + 2] = d4.z, dp[0][4 * x + 3] = d4.w;
-                if constexpr (BIAS) {
-                    const float4 g4 = *reinterpret_cast<const float4*>(&cR[set][2][r]);
-                    lg[4 * x] = g4.x, lg[4 * x + 1] = g4.y, lg[4 * x + 2] = g4.z, lg[4 * x + 3] = g4.w;
-                }
-            }
-            const T *bQ = cQ + set * B::kElems, *bG = cG + set * B::kElems;
-            B::template rows<1>(bQ, 32 * rb, kf, s, lane);
-            B::template rows<1>(bG, 32 * rb, vf, dp, lane);
-            typename B::Cols gt_, qt;
-            gt_.load(bG, 32 * rb, lane);
-            qt.load(bQ, 32 * rb, lane);
-            if (r0 + 32 > it.s1) {
-                asm volatile("" ::: "memory");
-                gt_.drop(it.s1 - r0, lane);
-                qt.drop(it.s1 - r0, lane);
-            }
-            __builtin_amdgcn_sched_barrier(0);
+    const typename B::At lds(lane, set * B::kElems * int(sizeof(T)));
+    auto block32 = [&](auto masked, int r0, const T* bQ, const T* bG, const float(&bR)[3][STAGE], int rb) {
+        uint32_t id[16];
+        if constexpr (BIAS) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
+                const int r = r0 + part(i, lane);
+                uint32_t b = 255u;
+                if (!masked.value || r < it.s1) b = id_key[(r >> gs) * wide];
+                id[i] = b < uint32_t(a.B) ? b : uint32_t(a.B);
+            }
+        }
+        // of the lane's 16 rows the first that its key is attended to by, and the first past the end
+        const int from = rmin - r0 - part(0, lane), to = it.s1 - r0 - part(0, lane);
+        f32x16_t s[1] = {splat16(0.f)}, dp[1];
+        const int rs0 = 32 * rb + part(0, lane);  // the lane's rows in the stage's statistics
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const float4 d4 = *reinterpret_cast<const float4*>(&bR[1][rs0 + 4 * x]);
+            dp[0][4 * x] = d4.x, dp[0][4 * x + 1] = d4.y, dp[0][4 * x + 2] = d4.z, dp[0][4 * x + 3] = d4.w;
+        }
+        B::template rows<1>(bQ, lds, kf, s);
+        B::template rows<1>(bG, lds, vf, dp);
+        // operands and statistics are read where they are used: held together they do not fit the registers
+        __builtin_amdgcn_sched_barrier(0);
+        typename B::Cols x;
+        x.load(bG, lds);
+        if constexpr (masked.value) x.drop(it.s1 - r0, lane);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float4 l4 = *reinterpret_cast<const float4*>(&bR[0][rs0 + 4 * k]);
+            float4 g4;
+            if constexpr (BIAS) g4 = *reinterpret_cast<const float4*>(&bR[2][rs0 + 4 * k]);
+            const float L[4] = {l4.x, l4.y, l4.z, l4.w}, lg[4] = {g4.x, g4.y, g4.z, g4.w};
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const int i = 4 * k + y;
+                float t;
                 if constexpr (BIAS) {
-                    const float u =
-                        fmaf(s[0][i], a.scale, s_tab[((r0 + part(i, lane)) & gm) * kTableStride + id[i]]);
-                    s[0][i] = fmaf(u - L[i], kLog2e, -lg[i]);
+                    const float bias = s_tab[((r0 + part(i, lane)) & gm) * kTableStride + id[i]];
+                    t = fmaf(fmaf(s[0][i], a.scale, bias) - L[y], kLog2e, -lg[y]);
                 } else {
-                    s[0][i] = fmaf(s[0][i], sl2, -L[i]);
+                    t = fmaf(s[0][i], sl2, -L[y]);
                 }
-            }
-            if (r0 < rhi || r0 + 32 > it.s1) {
-                asm volatile("" ::: "memory");
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int r = r0 + part(i, lane);
-                    if (r < rmin || r >= it.s1) s[0][i] = -kInf, dp[0][i] = 0.f;
+                if constexpr (masked.value) {
+                    const bool out = i < from || i >= to;
+                    t = out ? -kInf : t;
+                    dp[0][i] = out ? 0.f : dp[0][i];
                 }
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[0][i] = ex2(s[0][i]);
+                s[0][i] = ex2(t);
                 dp[0][i] *= s[0][i];
             }
-            typename B::Weights w[1];
-            w[0].set(s[0]);
-            B::template apply<1>(gt_, w, dv);
-            w[0].set(dp[0]);
-            f32x16_t(&dk1)[1][D / 32] = reinterpret_cast<f32x16_t(&)[1][D / 32]>(dk);
-            B::template apply<1>(qt, w, dk1);
+        }
+        B::template apply<1>(x, s, dv);
+        __builtin_amdgcn_sched_barrier(0);
+        x.load(bQ, lds);
+        if constexpr (masked.value) x.drop(it.s1 - r0, lane);
+        B::template apply<1>(x, dp, dk);
+    };
+    auto stage = [&](auto masked, int base, const T* cQ, const T* cG, const Stats& cR, T* nQ, T* nG, Stats& nR) {
+        load_stats(base + KS * STAGE);
+        fetch(base + KS * STAGE, nQ, nG);
+        if constexpr (masked.value) {
+#pragma unroll 1
+            for (int rb = 0; rb < STAGE / 32; ++rb) {
+                const int r0 = base + 32 * rb;
+                if (r0 < it.s1 && r0 + 32 > rlo && key0 < it.lk)  // uniform
+                    block32(masked, r0, cQ + 32 * rb * D, cG + 32 * rb * D, cR[set], rb);
+            }
+        } else if (key0 < it.lk) {  // uniform
+#pragma unroll
+            for (int rb = 0; rb < STAGE / 32; ++rb) {
+                __builtin_amdgcn_sched_barrier(0);
+                block32(masked, base + 32 * rb, cQ + 32 * rb * D, cG + 32 * rb * D, cR[set], rb);
+            }
         }
         store_stats(nR);
         stage_done<(W > 1)>();
     };
-    for (int base = it.s0; base < it.s1; base += 2 * KS * STAGE) {
-        stage(base + set * STAGE, sQ0, sG0, sR0, sQ1, sG1, sR1);
-        if (base + KS * STAGE < it.s1) stage(base + (KS + set) * STAGE, sQ1, sG1, sR1, sQ0, sG0, sR0);
+    // the stages whose rows attend to every key of the tile lie between the first ones (causal) and the last (ragged);
+    // an even number of stages before them and of them
+    constexpr int kRound = KS * STAGE;
+    const int end_key = it.tile + (sub + 1) * W * 32, last_key = end_key < it.lk ? end_key - 1 : it.lk - 1;
+    const int all = uniform(first_row(last_key)) - it.s0;  // rows before the first that attends to every key
+    const int before = it.s0 + (all > 0 ? (all + 2 * kRound - 1) / (2 * kRound) * (2 * kRound) : 0);
+    const int after = before + (it.s1 > before ? (it.s1 - before) / (2 * kRound) * (2 * kRound) : 0);
+    int base = it.s0;
+#pragma unroll 1
+    for (int phase = 0; phase < 2; ++phase) {
+        const int end = phase == 0 && before < it.s1 ? before : it.s1;
+#pragma unroll 1
+        for (; base < end; base += 2 * kRound) {
+            stage(Flag<true>{}, base + set * STAGE, sQ0, sG0, sR0, sQ1, sG1, sR1);
+            if (base + kRound < it.s1)
+                stage(Flag<true>{}, base + kRound + set * STAGE, sQ1, sG1, sR1, sQ0, sG0, sR0);
+        }
+        if (phase == 0)
+            for (; base < after; base += 2 * kRound) {
+                stage(Flag<false>{}, base + set * STAGE, sQ0, sG0, sR0, sQ1, sG1, sR1);
+                stage(Flag<false>{}, base + kRound + set * STAGE, sQ1, sG1, sR1, sQ0, sG0, sR0);
+            }
     }
     const int thread = key_wave * kWave + lane;
-    add_sets<KS, W>(dk, set, thread);
+    add_sets<KS, W>(dk[0], set, thread);
     if (!add_sets<KS, W>(dv[0], set, thread)) return;
     if (W == 1 && it.slot >= 0) {
         float* o = a.slots + ((int64_t(it.slot) * a.Hkv + hk) * (2 * kFewRows) + (lane & 31)) * D;
-        Blk<float, D>::store(o, dk, 1.f, lane);
+        Blk<float, D>::store(o, dk[0], 1.f, lane);
         Blk<float, D>::store(o + kFewRows * D, dv[0], 1.f, lane);
     } else if (j < it.lk) {
         const int64_t at = int64_t(it.k0 + j) * a.Hkv + hk;
-        B::store(static_cast<T*>(a.out1) + at * D, dk, a.scale, lane);
+        B::store(static_cast<T*>(a.out1) + at * D, dk[0], a.scale, lane);
         B::store(static_cast<T*>(a.out2) + at * D, dv[0], 1.f, lane);
     }
 }
@@ -514,7 +548,7 @@ gt_status packed_bwd_d(const gt_packed_plan* p, PackedArgs a, float* dtable, hip
         GT_ROWS(kRowsFew, 32, 1, few_waves(kRow), 1, kStat)
         GT_ROWS(kRows64, kStage, 2, 1, 1, kStat)
         GT_ROWS(kRows128, kStage, 4, 1, 1, kStat)
-        GT_ROWS(kRows256, kStage, 8, 1, 1, kStat)
+        GT_ROWS(kRows256, kStage, 4, 1, 2, kStat)
         if (list(kRowMerges)) {
             const gt_status st = packed_merge_stat(p, a, s);
             if (st != GT_OK) return st;
@@ -527,23 +561,40 @@ gt_status packed_bwd_d(const gt_packed_plan* p, PackedArgs a, float* dtable, hip
     } else {
         GT_ROWS(kRowsFew, 32, 1, few_waves(kRow), 1, kGrad)
         GT_ROWS(kRows64, kStage, 2, 1, 1, kGrad)
-        GT_ROWS(kRows128, kStage, 4, 1, 1, kGrad)
-        GT_ROWS(kRows256, kStage, 8, 1, 1, kGrad)
+        if (kRow <= 128 && packed_items(p, kRows128) * a.Hkv < kSharedBlocks) {
+            GT_ROWS(kRows128, kStage, 4, (kRow <= 128 ? 2 : 1), 1, kGrad)
+        } else {
+            GT_ROWS(kRows128, kStage, 4, 1, 1, kGrad)
+        }
+        if constexpr (kRow <= 128) {
+            GT_ROWS(kRows256, kStage, 8, 1, 1, kGrad)
+        } else {
+            GT_ROWS(kRows256, kStage, 4, 1, 2, kGrad)
+        }
     }
 #undef GT_ROWS
     if (list(kRowMerges)) {
         const gt_status st = packed_merge_rows(p, D, dt, a, s);
         if (st != GT_OK) return st;
     }
-#define GT_KEYS(LIST, STAGE, W, KS)                                                                              \
-    if (list(LIST)) {                                                                                            \
-        k_packed_keys<T, D, STAGE, W, KS, BIAS><<<packed_grid(a.n_items, a.Hkv), W * KS * kWave, tab, s>>>(a);   \
-        GT_LAUNCH_CHECK("packed_bwd keys");                                                                      \
+#define GT_KEYS(LIST, STAGE, W, KS, SUB)                                                                        \
+    if (list(LIST)) {                                                                                           \
+        k_packed_keys<T, D, STAGE, W, KS, SUB, BIAS>                                                            \
+            <<<packed_grid(a.n_items, a.Hkv, SUB), W * KS * kWave, tab, s>>>(a);                                \
+        GT_LAUNCH_CHECK("packed_bwd keys");                                                                     \
     }
-    GT_KEYS(kKeysFew, 32, 1, few_waves(kRow))
-    GT_KEYS(kKeys64, kStage, 2, 1)
-    GT_KEYS(kKeys128, kStage, 4, 1)
-    GT_KEYS(kKeys256, kStage, 8, 1)
+    GT_KEYS(kKeysFew, 32, 1, few_waves(kRow), 1)
+    GT_KEYS(kKeys64, kStage, 2, 1, 1)
+    if (kRow <= 128 && packed_items(p, kKeys128) * a.Hkv < kSharedBlocks) {
+        GT_KEYS(kKeys128, kStage, 4, (kRow <= 128 ? 2 : 1), 1)
+    } else {
+        GT_KEYS(kKeys128, kStage, 4, 1, 1)
+    }
+    if constexpr (kRow <= 128) {
+        GT_KEYS(kKeys256, kStage, 8, 1, 1)
+    } else {  // the accumulators of two wavefronts a SIMD do not fit
+        GT_KEYS(kKeys256, kStage, 4, 1, 2)
+    }
 #undef GT_KEYS
     if (list(kKeyMerges)) {
         const gt_status st = packed_merge_keys(p, D, dt, a, s);

@@ -44,7 +44,8 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
     wave_done();
     float m = kLowest, l = 0.f;
     if (it.lk > 0) {
-        B::template rows<1>(sK[wave], 0, qf, s, lane);
+        const typename B::At at(lane, 0);
+        B::template rows<1>(sK[wave], at, qf, s);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             if constexpr (BIAS) {
@@ -52,7 +53,7 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
             } else {
                 s[0][i] *= a.scale;
             }
-            if (part(i, lane) >= lim) s[0][i] = -kInf;
+            if (i >= lim - part(0, lane)) s[0][i] = -kInf;
             m = fmaxf(m, s[0][i]);
         }
         m = pair_max(m);
@@ -63,14 +64,14 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
         }
         l = pair_sum(l);
         typename B::Cols vt;
-        vt.load(sV[wave], 0, lane);
+        vt.load(sV[wave], at);
         vt.drop(it.lk, lane);
         B::template apply<1>(vt, s, acc);
     }
     if (r < R) {
-        const int64_t at = int64_t(it.q0 + q) * a.H + h;
-        if (lane < 32) a.LSE[at] = l == 0.f ? -kInf : fmaf(__log2f(l), kLn2, m);
-        B::store(static_cast<T*>(a.out0) + at * D, acc[0], l == 0.f ? 0.f : 1.f / l, lane);
+        const int64_t out = int64_t(it.q0 + q) * a.H + h;
+        if (lane < 32) a.LSE[out] = l == 0.f ? -kInf : fmaf(__log2f(l), kLn2, m);
+        B::store(static_cast<T*>(a.out0) + out * D, acc[0], l == 0.f ? 0.f : 1.f / l, lane);
     }
 }
 
@@ -127,8 +128,8 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
         if constexpr (BIAS) id_row[b] = a.ids + it.pair + q_of[b] * ids_width(it.lk);
         qf[b].load(static_cast<const T*>(a.Q) + int64_t(it.q0 + q_of[b]) * a.ldq + ((hk << gs) + hg[b]) * D, lane);
     }
-    const int first = row0 < R ? row0 : R - 1, last = row0 + 32 * NB - 1 < R ? row0 + 32 * NB - 1 : R - 1;
-    const int lo = uniform(limit(first >> gs)), hi = uniform(row0 < R ? limit(last >> gs) : 0);
+    const int last = row0 + 32 * NB - 1 < R ? row0 + 32 * NB - 1 : R - 1;
+    const int hi = uniform(row0 < R ? limit(last >> gs) : 0);
     f32x16_t acc[NB][D / 32];
     float m[NB], l[NB];
 #pragma unroll
@@ -140,92 +141,105 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
     }
     const float sl2 = a.scale * kLog2e;
     stage_done<(W > 1) || BIAS>();
-    auto stage = [&](int kbase, const T* cK, const T* cV, T* nK, T* nV) {
-        fetch(kbase + KS * STAGE, nK, nV);
+    const typename B::At lds(lane, set * B::kElems * int(sizeof(T)));
+    // one block of 32 keys; masked: some row does not attend to all of them
+    auto block32 = [&](auto masked, int key0, const T* bK, const T* bV) {
+        uint4 ids[NB];
+        int left[NB];  // how many of the lane's 16 keys its row attends to
 #pragma unroll
-        for (int kb = 0; kb < STAGE / 32; ++kb) {
-            const int key0 = kbase + 32 * kb;
-            if (key0 >= hi) break;  // uniform
-            const bool masked = key0 + 32 > lo;
-            uint4 ids[NB];
+        for (int b = 0; b < NB; ++b) {
+            if constexpr (BIAS) ids[b] = load_ids(id_row[b], key0, it.lk, lane);
+            left[b] = lim[b] - key0 - part(0, lane);
+        }
+        f32x16_t s[NB];
+        auto scores = [&] {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) s[b] = splat16(0.f);
+            B::template rows<NB>(bK, lds, qf, s);
             if constexpr (BIAS)
 #pragma unroll
-                for (int b = 0; b < NB; ++b) ids[b] = load_ids(id_row[b], key0, it.lk, lane);
-            f32x16_t s[NB];
-            auto scores = [&] {
-#pragma unroll
-                for (int b = 0; b < NB; ++b) s[b] = splat16(0.f);
-                B::template rows<NB>(cK + set * B::kElems, 32 * kb, qf, s, lane);
-                if constexpr (BIAS)
-#pragma unroll
-                    for (int b = 0; b < NB; ++b)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            s[b][i] = fmaf(s[b][i], a.scale, s_tab[hg[b] * kTableStride + id_of(ids[b], i, a.B)]);
-            };
-            float ls[NB];
-            auto weights = [&] {  // s becomes the weights, ls this lane's sums of them
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
+                for (int b = 0; b < NB; ++b)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        s[b][i] = BIAS ? (s[b][i] - m[b]) * kLog2e : fmaf(s[b][i], sl2, -m[b]);
-                    if (masked) {
-                        asm volatile("" ::: "memory");  // kept a branch
+                        s[b][i] = fmaf(s[b][i], a.scale, s_tab[hg[b] * kTableStride + id_of(ids[b], i, a.B)]);
+        };
+        float ls[NB];
+        auto weights = [&] {  // s becomes the weights, ls this lane's sums of them
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (key0 + part(i, lane) >= lim[b]) s[b][i] = -kInf;
-                    }
-                    float x[2] = {0.f, 0.f};
+            for (int b = 0; b < NB; ++b) {
+                float x[2] = {0.f, 0.f};
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        s[b][i] = ex2(s[b][i]);
-                        x[i & 1] += s[b][i];
-                    }
-                    ls[b] = x[0] + x[1];
+                for (int i = 0; i < 16; ++i) {
+                    float t = BIAS ? (s[b][i] - m[b]) * kLog2e : fmaf(s[b][i], sl2, -m[b]);
+                    if constexpr (masked.value) t = i >= left[b] ? -kInf : t;
+                    s[b][i] = ex2(t);
+                    x[i & 1] += s[b][i];
                 }
-            };
+                ls[b] = x[0] + x[1];
+            }
+        };
+        scores();
+        typename B::Cols vt;
+        vt.load(bV, lds);
+        if constexpr (masked.value) vt.drop(it.s1 - key0, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        weights();
+        bool high = false;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) high |= !(ls[b] <= 256.f);
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(high) != 0, 0)) {
             scores();
-            typename B::Cols vt;
-            vt.load(cV + set * B::kElems, 32 * kb, lane);
-            if (key0 + 32 > it.s1) {
-                asm volatile("" ::: "memory");
-                vt.drop(it.s1 - key0, lane);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            weights();
-            bool high = false;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) high |= !(ls[b] <= 256.f);
-            if (__builtin_expect(__builtin_amdgcn_ballot_w64(high) != 0, 0)) {
-                scores();
+            for (int b = 0; b < NB; ++b) {
+                float mx = -kInf;
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    float mx = -kInf;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        mx = fmaxf(mx, key0 + part(i, lane) >= lim[b] ? -kInf : BIAS ? s[b][i] : s[b][i] * sl2);
-                    const float mn = fmaxf(m[b], pair_max(mx));
-                    const float alpha = ex2(BIAS ? (m[b] - mn) * kLog2e : m[b] - mn);
-                    l[b] *= alpha;
-#pragma unroll
-                    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[b][db][i] *= alpha;
-                    m[b] = mn;
+                for (int i = 0; i < 16; ++i) {
+                    const float t = BIAS ? s[b][i] : s[b][i] * sl2;
+                    mx = fmaxf(mx, masked.value && i >= left[b] ? -kInf : t);
                 }
-                weights();
-            }
+                const float mn = fmaxf(m[b], pair_max(mx));
+                const float alpha = ex2(BIAS ? (m[b] - mn) * kLog2e : m[b] - mn);
+                l[b] *= alpha;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) l[b] += ls[b];
-            B::template apply<NB>(vt, s, acc);
+                for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[b][db][i] *= alpha;
+                m[b] = mn;
+            }
+            weights();
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) l[b] += ls[b];
+        B::template apply<NB>(vt, s, acc);
+    };
+    auto stage = [&](auto masked, int kbase, const T* cK, const T* cV, T* nK, T* nV) {
+        fetch(kbase + KS * STAGE, nK, nV);
+        if constexpr (masked.value) {
+#pragma unroll 1
+            for (int kb = 0; kb < STAGE / 32; ++kb)
+                if (kbase + 32 * kb < hi)  // uniform
+                    block32(masked, kbase + 32 * kb, cK + 32 * kb * D, cV + 32 * kb * D);
+        } else {
+#pragma unroll
+            for (int kb = 0; kb < STAGE / 32; ++kb) {
+                __builtin_amdgcn_sched_barrier(0);  // two blocks' operands at once do not fit the registers
+                block32(masked, kbase + 32 * kb, cK + 32 * kb * D, cV + 32 * kb * D);
+            }
         }
         stage_done<(W > 1)>();
     };
-    // every set goes through the same number of stages, the last ones of some behind the walk's end
-    for (int kbase = it.s0; kbase < it.s1; kbase += 2 * KS * STAGE) {
-        stage(kbase + set * STAGE, sK0, sV0, sK1, sV1);
-        if (kbase + KS * STAGE < it.s1) stage(kbase + (KS + set) * STAGE, sK1, sV1, sK0, sV0);
+    // every set goes through the same number of stages, the last ones of some behind the walk's end; the stages
+    // that every row of the tile attends to whole come first, an even number of them
+    constexpr int kRound = KS * STAGE;
+    const int first_row = it.tile < R ? it.tile : R - 1, lo = uniform(limit(first_row >> gs));
+    int kbase = it.s0;
+    for (int n = lo > it.s0 ? (lo - it.s0) / (2 * kRound) : 0; n > 0; --n, kbase += 2 * kRound) {
+        stage(Flag<false>{}, kbase + set * STAGE, sK0, sV0, sK1, sV1);
+        stage(Flag<false>{}, kbase + kRound + set * STAGE, sK1, sV1, sK0, sV0);
+    }
+    for (; kbase < it.s1; kbase += 2 * kRound) {
+        stage(Flag<true>{}, kbase + set * STAGE, sK0, sV0, sK1, sV1);
+        if (kbase + kRound < it.s1) stage(Flag<true>{}, kbase + kRound + set * STAGE, sK1, sV1, sK0, sV0);
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b) l[b] = pair_sum(l[b]);
@@ -308,7 +322,11 @@ gt_status packed_fwd_d(const gt_packed_plan* p, PackedArgs a, hipStream_t s) {
     }
     GT_FWD(kRowsFew, 32, 1, 1, few_waves(kRow))
     GT_FWD(kRows64, kStage, 1, 2, 1)
-    GT_FWD(kRows128, kStage, 1, 4, 1)
+    if (packed_items(p, kRows128) * a.Hkv < kSharedBlocks) {
+        GT_FWD(kRows128, (kRow <= 128 ? kStage : 32), 1, 4, (kRow <= 256 ? 2 : 1))
+    } else {
+        GT_FWD(kRows128, kStage, 1, 4, 1)
+    }
     if constexpr (kRow <= 128) {
         GT_FWD(kRows256, kStage, 2, 4, 1)
     } else {

@@ -27,6 +27,12 @@ __device__ __forceinline__ int part(int i, int lane) { return 16 * (lane >> 5) +
 __device__ __forceinline__ int row_partner(int r) { return 16 * ((r >> 2) & 1) + 4 * (r >> 3) + (r & 3); }
 __device__ __forceinline__ int partner_row(int p) { return 8 * ((p >> 2) & 3) + 4 * (p >> 4) + (p & 3); }
 
+// A compile-time flag passed as a value (generic lambdas take it as auto).
+template <bool B>
+struct Flag {
+    static constexpr bool value = B;
+};
+
 __device__ __forceinline__ f32x16_t splat16(float x) {
     f32x16_t z;
 #pragma unroll
@@ -80,6 +86,37 @@ struct Blk {
         return kPieces >= 16 ? r & 15 : kPieces == 8 ? (kHalf ? r & 7 : (r >> 1) & 7) : (r >> 1) & 3;
     }
 
+    // A lane's byte offsets into a staged block, of the row operand's pieces and of
+    // the turned operand; set: offset of the wavefront's stage.  What varies with
+    // the block, the stage's buffer and the element is added as a constant, so the
+    // reads of a whole walk share these few registers.
+    static constexpr int kTurned = kHalf ? D / 32 : D == 32 ? 4 : 8;
+    struct At {
+        uint32_t row[kSteps], col[kTurned];
+        __device__ __forceinline__ At(int lane, int set) {
+            const int r = lane & 31, half = lane >> 5;
+#pragma unroll
+            for (int c = 0; c < kSteps; ++c) row[c] = set + int(sizeof(T)) * (r * D + kPiece * ((2 * c + half) ^ turn(r)));
+            if constexpr (kHalf) {
+                const int k = 4 * half + ((lane & 15) >> 2), c = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+#pragma unroll
+                for (int x = 0; x < kTurned; ++x)
+                    col[x] = set + 2 * (k * D + 8 * ((c ^ turn(k)) ^ (4 * x)) + 4 * (lane & 1));
+            } else {
+#pragma unroll
+                for (int x = 0; x < kTurned; ++x)
+                    col[x] = set + 4 * (4 * half * D + 4 * (((r >> 2) ^ turn(4 * half)) ^ turned_bits(x)) + (r & 3));
+            }
+#pragma unroll
+            for (int c = 0; c < kSteps; ++c) asm("" : "+v"(row[c]));
+#pragma unroll
+            for (int x = 0; x < kTurned; ++x) asm("" : "+v"(col[x]));
+        }
+        __device__ __forceinline__ static constexpr int turned_bits(int x) {
+            return D == 32 ? (x & 1) | (x >> 1) << 2 : (x & 3) | (x >> 2) << 3;
+        }
+    };
+
     // One owned row as a B operand: pieces 2 c + lane / 32.
     struct Row {
         uint4 v[kSteps];
@@ -90,8 +127,10 @@ struct Blk {
         }
         // the lane's row of a staged block
         __device__ __forceinline__ void staged(const T* s, int lane) {
+            const int r = partner_row(lane & 31);
 #pragma unroll
-            for (int c = 0; c < kSteps; ++c) v[c] = piece(s, partner_row(lane & 31), c, lane);
+            for (int c = 0; c < kSteps; ++c)
+                v[c] = *reinterpret_cast<const uint4*>(s + r * D + kPiece * ((2 * c + (lane >> 5)) ^ turn(r)));
         }
         __device__ __forceinline__ float dot(const Row& o) const {
             float s = 0.f;
@@ -129,7 +168,7 @@ struct Blk {
         }
     }
 
-    // c += (staged LDS rows r0 .. r0 + 31) x (owned rows), over the features.
+    // c += (the 32 staged rows at s) x (owned rows), over the features.
     __device__ __forceinline__ static f32x16_t mul_piece(uint4 a, uint4 b, f32x16_t c) {
         if constexpr (kHalf) {
             return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a),
@@ -141,41 +180,39 @@ struct Blk {
             return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
         }
     }
-    __device__ __forceinline__ static uint4 piece(const T* s, int r, int c, int lane) {
-        return *reinterpret_cast<const uint4*>(s + r * D + kPiece * ((2 * c + (lane >> 5)) ^ turn(r)));
-    }
     template <int NB>
-    __device__ __forceinline__ static void rows(const T* s, int r0, const Row (&o)[NB], f32x16_t (&c)[NB], int lane) {
+    __device__ __forceinline__ static void rows(const T* s, const At& at, const Row (&o)[NB], f32x16_t (&c)[NB]) {
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
-            const uint4 a = piece(s, r0 + (lane & 31), k, lane);
+            const uint4 a = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(s) + at.row[k]);
 #pragma unroll
             for (int b = 0; b < NB; ++b) c[b] = mul_piece(a, o[b].v[k], c[b]);
         }
     }
 
-    // The staged rows r0 .. r0 + 31 turned round (features x partners), in the
+    // The 32 staged rows at s turned round (features x partners), in the
     // partner order of an accumulator used as B operand.
     struct Cols {
         // element 8 half + t (bf16) or i (fp32) of a lane: partner part(.., lane)
         typename std::conditional<kHalf, bf16x8_t, float>::type v[D / 32][kHalf ? 2 : 16];
 
-        __device__ __forceinline__ void load(const T* s, int r0, int lane) {
+        __device__ __forceinline__ void load(const T* s, const At& at) {
+            const char* p = reinterpret_cast<const char*>(s);
             if constexpr (kHalf) {
                 typedef short s16x4_t __attribute__((ext_vector_type(4)));
                 typedef short s16x8_t __attribute__((ext_vector_type(8)));
-                const int k = 4 * (lane >> 5) + ((lane & 15) >> 2);
+                typedef __attribute__((address_space(3))) s16x4_t* lds_t;
 #pragma unroll
                 for (int db = 0; db < D / 32; ++db)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        const int c = 4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-                        const T* x = s + (r0 + 16 * half + k) * D + 8 * (c ^ turn(k)) + 4 * (lane & 1);
-                        const T* y = s + (r0 + 16 * half + k + 8) * D + 8 * (c ^ turn(k + 8)) + 4 * (lane & 1);
+                        // eight rows on, rows of 256 bytes are turned by another 8 pieces
+                        const char* x = p + 2 * 16 * half * D + at.col[db];
+                        const char* y = p + 2 * (16 * half + 8) * D + at.col[kPieces >= 16 ? db ^ 2 : db];
                         const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            reinterpret_cast<__attribute__((address_space(3))) s16x4_t*>(reinterpret_cast<uintptr_t>(x)));
+                            reinterpret_cast<lds_t>(reinterpret_cast<uintptr_t>(x)));
                         const s16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            reinterpret_cast<__attribute__((address_space(3))) s16x4_t*>(reinterpret_cast<uintptr_t>(y)));
+                            reinterpret_cast<lds_t>(reinterpret_cast<uintptr_t>(y)));
                         v[db][half] =
                             __builtin_bit_cast(bf16x8_t, s16x8_t{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
                     }
@@ -184,17 +221,19 @@ struct Blk {
                 for (int db = 0; db < D / 32; ++db)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int r = r0 + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3), f = 32 * db + (lane & 31);
-                        v[db][i] = s[r * D + 4 * ((f >> 2) ^ turn(r)) + (f & 3)];
+                        const int x = D == 32 ? ((i >> 1) & 1) + 2 * ((i >> 2) & 1) : (i & 3) + 4 * (((i >> 2) ^ db) & 1);
+                        v[db][i] = *reinterpret_cast<const float*>(p + 4 * (8 * (i >> 2) + (i & 3)) * D +
+                                                                   256 * (db >> 1) + at.col[x]);
                     }
             }
         }
         // Zero the partners from the `left`-th on: rows behind the end hold
         // whatever lies there, and a zero weight times an infinity would be NaN.
         __device__ __forceinline__ void drop(int left, int lane) {
+            const int mine = left - part(0, lane);
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if (part(i, lane) >= left)
+                if (i >= mine)
 #pragma unroll
                     for (int db = 0; db < D / 32; ++db) {
                         if constexpr (kHalf) v[db][i / 8][i % 8] = (__bf16)0.f;
@@ -316,11 +355,10 @@ __device__ __forceinline__ uint32_t id_of(const uint4& ids, int i, uint32_t B) {
 }
 __device__ __forceinline__ int64_t ids_width(int lk) { return (int64_t(lk) + 15) & ~int64_t(15); }
 
-// A lane's own column of a [bucket][lane] sum in LDS: no two lanes meet, so the
-// order of additions is the program's.
-__device__ __forceinline__ void hist_add(float* col, uint32_t id, float v) {
-    __hip_atomic_fetch_add(col + id * kWave, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-}
+// Adds to a lane's own column of a [bucket][lane] sum in LDS: no two lanes meet,
+// so the order of additions is the program's, and a load and a store do (12 cycles
+// a wavefront's addition; ds_add_f32 takes 193, it goes lane by lane).
+__device__ __forceinline__ void hist_add(float* col, uint32_t id, float v) { col[id * kWave] += v; }
 // out[head of the group][bucket] = the sums over the lanes (whose row's head is
 // lane % g) of `waves` such columns, each B + 1 buckets.
 template <int THREADS>
