@@ -12,12 +12,14 @@ constexpr int kTableStride = 65;  // a head's table in LDS; entries from n_bucke
 // One tile of one sequence.  The row lists (forward and dQ): rows tile .. of the
 // sequence's lq * g query rows of one kv head (row r is query r / g, head r % g
 // of the group), walking the keys s0 .. s1 - 1.  The key lists (dK, dV): the keys
-// tile .., walking the rows s0 .. s1 - 1.  The merge lists: a tile whose walk was
-// split, its partial results in the slots slot .. slot + s0 - 1.
+// tile .., walking the rows s0 .. s1 - 1.  A tile whose walk is split has an item
+// for each part; part p leaves its result for the tile's u-th 32 rows (or keys) in
+// slot + u.  The merge lists: 32 rows (or keys) from tile on, whose s0 parts lie in
+// the slots slot, slot + s1, ...
 struct PackedItem {
     int32_t q0, lq, k0, lk;  // the sequence's first query and key, and their numbers
     int32_t tile, s0, s1;
-    int32_t slot;            // partial result's slot, -1: the tile's only item
+    int32_t slot;            // partial result's first slot, -1: the tile's only item
     int64_t pair;            // first byte of the sequence's bucket ids
 };
 
@@ -37,7 +39,8 @@ enum PackedList {
     kKeyMerges,
     kPackedLists
 };
-constexpr int kRowSlotsAt = 28, kKeySlotsAt = 29;  // layout: numbers of slots
+constexpr int kRowSlotsAt = 28, kKeySlotsAt = 29;      // layout: numbers of slots
+constexpr int kRowSharedAt = 26, kKeySharedAt = 27;    // layout: two sets of wavefronts share the walks of tiles of 128
 
 struct PackedArgs {
     const PackedItem* items;
@@ -81,11 +84,7 @@ constexpr int waves_per_simd(int stage_bytes, int waves) {
     return w < 1 ? 1 : w > 2 ? 2 : w;
 }
 
-// Below this many workgroups of four wavefronts (two for each of 256 CUs) two
-// sets of them share a walk.
-constexpr int64_t kSharedBlocks = 512;
-
-// Floats of one slot of a split tile (32 rows or keys): forward m, l and O;
+// Floats of one slot (32 rows or keys): forward m, l and O;
 // statistics; dQ; dK and dV.
 constexpr int64_t kFewRows = 32;
 inline int64_t fwd_slot_floats(int d) { return kFewRows * (d + 2); }

@@ -303,8 +303,9 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
             }
         }
         if (lane >= 32) return;
-        if (W == 1 && it.slot >= 0) {
-            float* o = a.slots + (int64_t(it.slot) * a.Hkv + hk) * (2 * kFewRows);
+        if (it.slot >= 0) {  // a part of a split walk
+            if (row0 >= R) return;
+            float* o = a.slots + (int64_t(it.slot + sub * W + row_wave) * a.Hkv + hk) * (2 * kFewRows);
             o[lane] = sum, o[kFewRows + lane] = dsum;
         } else if (r < R) {
             a.Dv[at] = sum == 0.f ? 0.f : dsum / sum;
@@ -318,10 +319,12 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
                                        a.hist + int64_t(block) * (int64_t(a.B) << gs), int(threadIdx.x));
         }
         if (!add_sets<KS, W>(acc[0], set, row_wave * kWave + lane)) return;
-        if (W == 1 && it.slot >= 0)
-            Blk<float, D>::store(a.slots + ((int64_t(it.slot) * a.Hkv + hk) * kFewRows + (lane & 31)) * D, acc[0], 1.f,
-                                 lane);
-        else if (r < R)
+        if (it.slot >= 0) {
+            if (row0 < R)  // uniform
+                Blk<float, D>::store(
+                    a.slots + ((int64_t(it.slot + sub * W + row_wave) * a.Hkv + hk) * kFewRows + (lane & 31)) * D, acc[0],
+                    1.f, lane);
+        } else if (r < R)
             B::store(static_cast<T*>(a.out0) + at * D, acc[0], a.scale, lane);
     }
 }
@@ -477,7 +480,7 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
     const int end_key = it.tile + (sub + 1) * W * 32, last_key = end_key < it.lk ? end_key - 1 : it.lk - 1;
     const int all = uniform(first_row(last_key)) - it.s0;  // rows before the first that attends to every key
     const int before = it.s0 + (all > 0 ? (all + 2 * kRound - 1) / (2 * kRound) * (2 * kRound) : 0);
-    const int after = before + (it.s1 > before ? (it.s1 - before) / (2 * kRound) * (2 * kRound) : 0);
+    const int after = it.s1 > before ? before + (it.s1 - before) / (2 * kRound) * (2 * kRound) : it.s0;
     int base = it.s0;
 #pragma unroll 1
     for (int phase = 0; phase < 2; ++phase) {
@@ -497,8 +500,9 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
     const int thread = key_wave * kWave + lane;
     add_sets<KS, W>(dk[0], set, thread);
     if (!add_sets<KS, W>(dv[0], set, thread)) return;
-    if (W == 1 && it.slot >= 0) {
-        float* o = a.slots + ((int64_t(it.slot) * a.Hkv + hk) * (2 * kFewRows) + (lane & 31)) * D;
+    if (it.slot >= 0) {
+        if (key0 >= it.lk) return;  // uniform
+        float* o = a.slots + ((int64_t(it.slot + sub * W + key_wave) * a.Hkv + hk) * (2 * kFewRows) + (lane & 31)) * D;
         Blk<float, D>::store(o, dk[0], 1.f, lane);
         Blk<float, D>::store(o + kFewRows * D, dv[0], 1.f, lane);
     } else if (j < it.lk) {
@@ -547,7 +551,11 @@ gt_status packed_bwd_d(const gt_packed_plan* p, PackedArgs a, float* dtable, hip
     if constexpr (BIAS) {
         GT_ROWS(kRowsFew, 32, 1, few_waves(kRow), 1, kStat)
         GT_ROWS(kRows64, kStage, 2, 1, 1, kStat)
-        GT_ROWS(kRows128, kStage, 4, 1, 1, kStat)
+        if (kRow <= 128 && p->layout[kRowSharedAt]) {
+            GT_ROWS(kRows128, kStage, 4, (kRow <= 128 ? 2 : 1), 1, kStat)
+        } else {
+            GT_ROWS(kRows128, kStage, 4, 1, 1, kStat)
+        }
         GT_ROWS(kRows256, kStage, 4, 1, 2, kStat)
         if (list(kRowMerges)) {
             const gt_status st = packed_merge_stat(p, a, s);
@@ -556,12 +564,17 @@ gt_status packed_bwd_d(const gt_packed_plan* p, PackedArgs a, float* dtable, hip
         // the table's gradient takes 16 KB of LDS a wavefront: smaller workgroups
         GT_ROWS(kRowsFew, 32, 1, few_waves_hist(kRow), 1, kGrad)
         GT_ROWS(kRows64, kStage, 2, 1, 1, kGrad)
-        GT_ROWS(kRows128, kStage, 4, 1, 1, kGrad)
+        // two sets where their columns fit beside the stages (and the sums' exchange)
+        if (kRow <= 128 && p->layout[kRowSharedAt] && 8 * (kStage * kRow + col) + tab + (16 << 10) <= (160 << 10)) {
+            GT_ROWS(kRows128, kStage, 4, (kRow <= 128 ? 2 : 1), 1, kGrad)
+        } else {
+            GT_ROWS(kRows128, kStage, 4, 1, 1, kGrad)
+        }
         GT_ROWS(kRows256, kStage, 4, 1, 2, kGrad)
     } else {
         GT_ROWS(kRowsFew, 32, 1, few_waves(kRow), 1, kGrad)
         GT_ROWS(kRows64, kStage, 2, 1, 1, kGrad)
-        if (kRow <= 128 && packed_items(p, kRows128) * a.Hkv < kSharedBlocks) {
+        if (kRow <= 128 && p->layout[kRowSharedAt]) {
             GT_ROWS(kRows128, kStage, 4, (kRow <= 128 ? 2 : 1), 1, kGrad)
         } else {
             GT_ROWS(kRows128, kStage, 4, 1, 1, kGrad)
@@ -585,7 +598,7 @@ gt_status packed_bwd_d(const gt_packed_plan* p, PackedArgs a, float* dtable, hip
     }
     GT_KEYS(kKeysFew, 32, 1, few_waves(kRow), 1)
     GT_KEYS(kKeys64, kStage, 2, 1, 1)
-    if (kRow <= 128 && packed_items(p, kKeys128) * a.Hkv < kSharedBlocks) {
+    if (kRow <= 128 && p->layout[kKeySharedAt]) {
         GT_KEYS(kKeys128, kStage, 4, (kRow <= 128 ? 2 : 1), 1)
     } else {
         GT_KEYS(kKeys128, kStage, 4, 1, 1)

@@ -284,11 +284,15 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
         }
         if (set > 0) return;
     }
-    if (W == 1 && it.slot >= 0) {  // a part of a split walk
-        float* o = a.slots + (int64_t(it.slot) * a.Hkv + hk) * (kFewRows * (D + 2));
-        const int r = lane & 31;
-        if (lane < 32) o[r] = m[0], o[kFewRows + r] = l[0];
-        Blk<float, D>::store(o + 2 * kFewRows + r * D, acc[0], 1.f, lane);
+    if (it.slot >= 0) {  // a part of a split walk
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            if (row0 + 32 * b >= R) break;  // uniform
+            float* o = a.slots + (int64_t(it.slot + row_wave * NB + b) * a.Hkv + hk) * (kFewRows * (D + 2));
+            const int r = lane & 31;
+            if (lane < 32) o[r] = m[b], o[kFewRows + r] = l[b];
+            Blk<float, D>::store(o + 2 * kFewRows + r * D, acc[b], 1.f, lane);
+        }
         return;
     }
 #pragma unroll
@@ -322,7 +326,7 @@ gt_status packed_fwd_d(const gt_packed_plan* p, PackedArgs a, hipStream_t s) {
     }
     GT_FWD(kRowsFew, 32, 1, 1, few_waves(kRow))
     GT_FWD(kRows64, kStage, 1, 2, 1)
-    if (packed_items(p, kRows128) * a.Hkv < kSharedBlocks) {
+    if (p->layout[kRowSharedAt]) {
         GT_FWD(kRows128, (kRow <= 128 ? kStage : 32), 1, 4, (kRow <= 256 ? 2 : 1))
     } else {
         GT_FWD(kRows128, kStage, 1, 4, 1)

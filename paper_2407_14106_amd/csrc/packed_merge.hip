@@ -1,7 +1,7 @@
 // Packed-sequence attention: the parts of split walks put together, and the
-// table's gradient from the blocks' partial tables.  A split tile holds at most
-// 32 rows (or keys); its parts are added in their order, so results do not
-// depend on which finished first.
+// table's gradient from the blocks' partial tables.  An item is 32 rows (or keys);
+// their parts are added in their order, so results do not depend on which finished
+// first.
 #include "packed.h"
 
 namespace gt {
@@ -16,7 +16,7 @@ __device__ __forceinline__ T from_f32(float v) {
     else return v;
 }
 
-// Which split tile, kv head and row of the tile this wavefront has.
+// Which item, kv head and row of the item this wavefront has.
 __device__ __forceinline__ bool merge_place(const PackedArgs& a, PackedItem& it, int& hk, int& r) {
     const uint32_t per = kFewRows / kOut, b = blockIdx.x;
     hk = int(b / per % uint32_t(a.Hkv));
@@ -38,8 +38,8 @@ __global__ __launch_bounds__(kThreads) void k_merge_fwd(PackedArgs a, int D) {
     merge_place(a, it, hk, r);
     if (it.tile + r >= it.lq << a.gs) return;
     const int lane = lane_id();
-    const int64_t step = int64_t(a.Hkv) * (kFewRows * (D + 2));
-    const float* s = a.slots + int64_t(it.slot) * step + int64_t(hk) * (kFewRows * (D + 2));
+    const int64_t slot = kFewRows * (D + 2), step = it.s1 * int64_t(a.Hkv) * slot;
+    const float* s = a.slots + (int64_t(it.slot) * a.Hkv + hk) * slot;
     const float to2 = a.B > 0 ? kLog2e : 1.f;  // m is in the exp2 domain without a bias
     float m = -3.402823466e38f, l = 0.f, o[2] = {0.f, 0.f};
     for (int p = 0; p < it.s0; ++p) m = fmaxf(m, s[p * step + r]);
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(kThreads) void k_merge_stat(PackedArgs a) {
     if (it.tile + r >= it.lq << a.gs) return;
     float sum = 0.f, dsum = 0.f;
     for (int p = 0; p < it.s0; ++p) {
-        const float* s = a.slots + (int64_t(it.slot + p) * a.Hkv + hk) * (2 * kFewRows);
+        const float* s = a.slots + ((it.slot + int64_t(p) * it.s1) * a.Hkv + hk) * (2 * kFewRows);
         sum += s[r];
         dsum += s[kFewRows + r];
     }
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kThreads) void k_merge_rows(PackedArgs a, int D) {
     const int64_t at = row_at(a, it, hk, it.tile + r);
     for (int c = lane_id(); c < D; c += kWave) {
         float t = 0.f;
-        for (int p = 0; p < it.s0; ++p) t += a.slots[((int64_t(it.slot + p) * a.Hkv + hk) * kFewRows + r) * D + c];
+        for (int p = 0; p < it.s0; ++p) t += a.slots[(((it.slot + int64_t(p) * it.s1) * a.Hkv + hk) * kFewRows + r) * D + c];
         static_cast<T*>(a.out0)[at * D + c] = from_f32<T>(t * a.scale);
     }
 }
@@ -99,7 +99,7 @@ __global__ __launch_bounds__(kThreads) void k_merge_keys(PackedArgs a, int D) {
     for (int c = lane_id(); c < D; c += kWave) {
         float k = 0.f, v = 0.f;
         for (int p = 0; p < it.s0; ++p) {
-            const float* s = a.slots + ((int64_t(it.slot + p) * a.Hkv + hk) * (2 * kFewRows) + r) * D + c;
+            const float* s = a.slots + (((it.slot + int64_t(p) * it.s1) * a.Hkv + hk) * (2 * kFewRows) + r) * D + c;
             k += s[0];
             v += s[kFewRows * D];
         }

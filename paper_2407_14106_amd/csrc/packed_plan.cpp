@@ -20,18 +20,24 @@ struct Seqs {
     bool causal;
 };
 
-// How the tiles are cut; from the whole batch, so that init and fill agree.
+// How the tiles of one side (rows or keys) are cut; from the whole batch, so that
+// init and fill agree.
 struct Cut {
-    bool large_rows, large_keys;   // tiles of 256 where a sequence has as many
-    int64_t row_chunk, key_chunk;  // most partners in one walk of a tile of 32
+    bool large;         // tiles of 256 where a sequence has as many
+    bool shared;        // two sets of wavefronts share the walk of a tile of 128
+    int64_t chunk;      // longest walk of one item
+    int64_t few_chunk;  // the same for tiles of 32
+};
+struct Cuts {
+    Cut rows, keys;
 };
 
-// Large tiles read the partners less often, so they are taken where there are
-// enough of them to fill the chip (2 workgroups on each of 256 CUs).
-constexpr int64_t kLargeBlocks = 512;
-// The walks of few rows (or keys) are split for as many workgroups, but not into
-// shorter parts than this: parts cost a second launch and a merge.
-constexpr int64_t kFewBlocks = 512, kFewChunk = 1024;
+// A CU works on one set of eight wavefronts at a time (or two of four), so the
+// chip is in balance when no walk is longer than a CU's share of all of them.
+constexpr int64_t kCus = 256;
+// Walks are not split into shorter parts than this: parts cost a second launch
+// and a merge.
+constexpr int64_t kMinChunk = 1024;
 
 int64_t row_walk(const Seqs& s, int64_t lk, int64_t off, int64_t last) {  // keys that rows up to `last` attend to
     return s.causal ? std::max<int64_t>(0, std::min(lk, off + (last >> s.gs) + 1)) : lk;
@@ -42,26 +48,56 @@ int64_t first_row(const Seqs& s, int64_t rows, int64_t off, int64_t key) {  // f
 
 bool is_pair(int64_t rows, int64_t lk) { return rows <= 32 && lk <= 32; }
 
-Cut cut(const Seqs& s) {
-    int64_t large_rows = 0, large_keys = 0, few_rows = 0, few_keys = 0;
+// Walks of the tiles of one size.
+struct Load {
+    int64_t n = 0, total = 0, most = 0;
+    void add(int64_t walk) {
+        ++n;
+        total += walk;
+        most = std::max(most, walk);
+    }
+};
+Cut cut_side(const Load& few, const Load& t128, const Load& t256, int64_t Hkv) {
+    Cut c;
+    auto share = [&](const Load& l, int64_t blocks) { return (l.total * Hkv + blocks - 1) / blocks; };
+    // Large tiles read the partners less often, but take all of a CU: where no walk is more than half its share.
+    c.large = t256.n * Hkv >= 2 * kCus && t256.most <= share(t256, 2 * kCus);
+    c.shared = t128.n * Hkv < 2 * kCus || t128.most > share(t128, 2 * kCus);
+    auto chunk = [&](int64_t x) { return std::max(kMinChunk, (x + 255) & ~int64_t(255)); };
+    c.chunk = chunk(share(t128, kCus));
+    c.few_chunk = chunk(share(few, 2 * kCus));
+    return c;
+}
+
+// Calls f(tile, walk) for the tiles of `size`.
+template <typename F>
+void row_tiles(const Seqs& s, int64_t rows, int64_t lk, int64_t off, int64_t size, F f) {
+    for (int64_t t = 0; t < rows; t += size) f(t, row_walk(s, lk, off, std::min(rows, t + size) - 1));
+}
+template <typename F>
+void key_tiles(const Seqs& s, int64_t rows, int64_t lk, int64_t off, int64_t size, F f) {
+    for (int64_t t = 0; t < lk; t += size) f(t, rows - first_row(s, rows, off, t));
+}
+
+Cuts cut(const Seqs& s) {
+    Load few[2], t128[2], t256[2];
     for (int64_t i = 0; i < s.n; ++i) {
         const int64_t lq = s.q[i + 1] - s.q[i], lk = s.k[i + 1] - s.k[i], rows = lq << s.gs, off = lk - lq;
         if (is_pair(rows, lk)) continue;
-        if (rows > 0 && rows <= 32) few_rows += row_walk(s, lk, off, rows - 1);
-        if (lk > 0 && lk <= 32) few_keys += rows;
-        if (rows >= 256) large_rows += (rows + 255) / 256;
-        if (lk >= 256) large_keys += (lk + 255) / 256;
+        if (rows > 0 && rows <= 32) few[0].add(row_walk(s, lk, off, rows - 1));
+        else row_tiles(s, rows, lk, off, 128, [&](int64_t, int64_t w) { t128[0].add(w); });
+        if (rows >= 256) row_tiles(s, rows, lk, off, 256, [&](int64_t, int64_t w) { t256[0].add(w); });
+        if (lk > 0 && lk <= 32) few[1].add(rows - first_row(s, rows, off, 0));
+        else key_tiles(s, rows, lk, off, 128, [&](int64_t, int64_t w) { t128[1].add(w); });
+        if (lk >= 256) key_tiles(s, rows, lk, off, 256, [&](int64_t, int64_t w) { t256[1].add(w); });
     }
-    auto chunk = [&](int64_t total) {
-        return std::max(kFewChunk, (total * s.Hkv + kFewBlocks - 1) / kFewBlocks + 255 & ~int64_t(255));
-    };
-    return {large_rows * s.Hkv >= kLargeBlocks, large_keys * s.Hkv >= kLargeBlocks, chunk(few_rows), chunk(few_keys)};
+    return {cut_side(few[0], t128[0], t256[0], s.Hkv), cut_side(few[1], t128[1], t256[1], s.Hkv)};
 }
 
 // Calls f(list, item) for every item of the work list, sequence by sequence.
 // Returns the numbers of slots (row lists, key lists).
 template <typename F>
-std::pair<int64_t, int64_t> each_item(const Seqs& s, const Cut& c, F f) {
+std::pair<int64_t, int64_t> each_item(const Seqs& s, const Cuts& c, F f) {
     int64_t pair = 0, row_slots = 0, key_slots = 0;
     for (int64_t i = 0; i < s.n; ++i) {
         PackedItem it = {};
@@ -77,16 +113,23 @@ std::pair<int64_t, int64_t> each_item(const Seqs& s, const Cut& c, F f) {
             if (rows > 0 || lk > 0) f(kPairs, it);
             continue;
         }
-        // one tile's walk, in parts of at most `chunk` where it is split
-        auto walk = [&](int list, int merges, int64_t& slots, int64_t tile, int64_t s0, int64_t s1, int64_t chunk) {
+        // one tile's walk, in parts of at most `chunk`
+        auto walk = [&](int list, int merges, int64_t& slots, int64_t tile, int64_t units, int64_t s0, int64_t s1,
+                        int64_t chunk) {
             it.tile = int32_t(tile);
-            const int64_t parts = chunk > 0 ? std::max<int64_t>(1, (s1 - s0 + chunk - 1) / chunk) : 1;
-            it.slot = parts > 1 ? int32_t(slots) : -1;
+            const int64_t parts = std::max<int64_t>(1, (s1 - s0 + chunk - 1) / chunk);
+            it.slot = -1;
             if (parts > 1) {
                 PackedItem m = it;
                 m.s0 = int32_t(parts);
-                f(merges, m);
-                slots += parts;
+                m.s1 = int32_t(units);
+                for (int64_t u = 0; u < units; ++u) {
+                    m.tile = int32_t(tile + 32 * u);
+                    m.slot = int32_t(slots + u);
+                    f(merges, m);
+                }
+                it.slot = int32_t(slots);
+                slots += parts * units;
             }
             // parts of equal length, whole blocks of 32 each
             const int64_t each = ((s1 - s0 + parts - 1) / parts + 31) & ~int64_t(31);
@@ -94,19 +137,21 @@ std::pair<int64_t, int64_t> each_item(const Seqs& s, const Cut& c, F f) {
                 it.s0 = int32_t(std::min(s1, s0 + p * each));
                 it.s1 = int32_t(parts > 1 ? std::min(s1, s0 + (p + 1) * each) : s1);
                 f(list, it);
-                if (parts > 1) ++it.slot;
+                if (parts > 1) it.slot += int32_t(units);
             }
         };
-        const int row_list = rows <= 32 ? kRowsFew : rows <= 64 ? kRows64 : c.large_rows && rows >= 256 ? kRows256 : kRows128;
+        const int row_list = rows <= 32 ? kRowsFew : rows <= 64 ? kRows64 : c.rows.large && rows >= 256 ? kRows256 : kRows128;
         const int64_t row_tile = rows <= 32 ? 32 : rows <= 64 ? 64 : row_list == kRows256 ? 256 : 128;
-        for (int64_t t = 0; t < rows; t += row_tile)
-            walk(row_list, kRowMerges, row_slots, t, 0, row_walk(s, lk, off, std::min(rows, t + row_tile) - 1),
-                 row_list == kRowsFew ? c.row_chunk : 0);
-        const int key_list = lk <= 32 ? kKeysFew : lk <= 64 ? kKeys64 : c.large_keys && lk >= 256 ? kKeys256 : kKeys128;
+        row_tiles(s, rows, lk, off, row_tile, [&](int64_t t, int64_t w) {
+            walk(row_list, kRowMerges, row_slots, t, (std::min(rows - t, row_tile) + 31) / 32, 0, w,
+                 row_list == kRowsFew ? c.rows.few_chunk : c.rows.chunk);
+        });
+        const int key_list = lk <= 32 ? kKeysFew : lk <= 64 ? kKeys64 : c.keys.large && lk >= 256 ? kKeys256 : kKeys128;
         const int64_t key_tile = lk <= 32 ? 32 : lk <= 64 ? 64 : key_list == kKeys256 ? 256 : 128;
-        for (int64_t t = 0; t < lk; t += key_tile)
-            walk(key_list, kKeyMerges, key_slots, t, first_row(s, rows, off, t), rows,
-                 key_list == kKeysFew ? c.key_chunk : 0);
+        key_tiles(s, rows, lk, off, key_tile, [&](int64_t t, int64_t w) {
+            walk(key_list, kKeyMerges, key_slots, t, (std::min(lk - t, key_tile) + 31) / 32, rows - w, rows,
+                 key_list == kKeysFew ? c.keys.few_chunk : c.keys.chunk);
+        });
     }
     return {row_slots, key_slots};
 }
@@ -131,7 +176,7 @@ gt_status check_seqs(const char* who, const Seqs& s, int64_t* pair_bytes) {
     return GT_OK;
 }
 
-std::pair<int64_t, int64_t> plan_lists(const Seqs& s, const Cut& c, int64_t (&count)[kPackedLists]) {
+std::pair<int64_t, int64_t> plan_lists(const Seqs& s, const Cuts& c, int64_t (&count)[kPackedLists]) {
     for (auto& x : count) x = 0;
     return each_item(s, c, [&](int list, const PackedItem&) { ++count[list]; });
 }
@@ -158,7 +203,10 @@ extern "C" gt_status gt_packed_plan_init(int64_t n_seq, const int64_t* q_ptr, co
     gt_status st = check_seqs(who, s, &pair);
     if (st != GT_OK) return st;
     int64_t count[kPackedLists];
-    const auto slots = plan_lists(s, cut(s), count);
+    const Cuts c = cut(s);
+    const auto slots = plan_lists(s, c, count);
+    if (slots.first * Hkv >= (int64_t(1) << 26) || slots.second * Hkv >= (int64_t(1) << 26))
+        return fail(GT_ERR_UNSUPPORTED, std::string(who) + ": more than 2^26 partial results");
     int64_t at = 0;
     for (int l = 0; l < kPackedLists; ++l) {
         if (count[l] * Hkv > (int64_t(1) << 31) - 64)  // one block for each item and kv head
@@ -175,6 +223,8 @@ extern "C" gt_status gt_packed_plan_init(int64_t n_seq, const int64_t* q_ptr, co
     plan->H = H;
     plan->Hkv = Hkv;
     plan->causal = causal != 0;
+    plan->layout[kRowSharedAt] = c.rows.shared;
+    plan->layout[kKeySharedAt] = c.keys.shared;
     plan->layout[kRowSlotsAt] = slots.first;
     plan->layout[kKeySlotsAt] = slots.second;
     plan->layout[kMarkAt] = kPlanMark;
@@ -194,7 +244,7 @@ extern "C" gt_status gt_packed_plan_fill(int64_t n_seq, const int64_t* q_ptr, co
     gt_status st = check_seqs(who, s, &pair);
     if (st != GT_OK) return st;
     int64_t count[kPackedLists];
-    const Cut c = cut(s);
+    const Cuts c = cut(s);
     plan_lists(s, c, count);
     bool same = pair == plan->pair_bytes && q_ptr[n_seq] == plan->nq && k_ptr[n_seq] == plan->nk;
     for (int l = 0; l < kPackedLists; ++l) same = same && count[l] == plan->layout[2 * l + 1];

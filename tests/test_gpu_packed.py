@@ -125,6 +125,16 @@ def test_single_queries_over_long_keys(gt, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B", [0, 5])
+def test_long_walks_of_few_tiles_are_split(gt, dtype, B):
+    # few rows beside many keys, few keys beside many rows, and both beside short sequences
+    compare(gt, [100, 7], [4500, 9], 1, 1, 32, dtype, False, B)
+    compare(gt, [4500, 3], [100, 200], 1, 1, 64, dtype, False, B)
+    compare(gt, [60, 5], [3000, 2], 2, 1, 128, dtype, True, B)
+    compare(gt, [2500, 40], [30, 2300], 2, 2, 32, dtype, True, B)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("scale", [-0.3, 0.0, 2.5])
 def test_any_scale(gt, dtype, scale):
     compare(gt, [70], [90], 2, 2, 32, dtype, True, scale=scale)

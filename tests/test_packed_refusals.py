@@ -89,26 +89,30 @@ def test_plan_covers_every_row_and_key_once(lib, causal, group, many):
              for i in range(len(names))]
     by_seq = {(int(q[s]), int(k[s]), lq[s], lk[s]): s for s in range(len(lq))}
 
-    def walked(lists, owned, streamed, needs, merges):
+    def walked(lists, owned, streamed, needs, merges, n_slots):
         """Every owned index is in one tile, and its items walk each partner that it needs exactly once; the parts of a
         split tile have the slots that its merge names."""
         seen = [np.zeros((owned(s),), dtype=np.int64) for s in range(len(lq))]
         parts = {}
         for tile, rows in lists:
-            for it in rows:
+            for it in sorted(rows.tolist(), key=lambda x: (x[0], x[2], x[4], x[5])):
+                it = np.array(it, dtype=np.int32)
                 q0, l_q, k0, l_k, t, s0, s1, slot = (int(x) for x in it[:8])
                 s = by_seq[(q0, k0, l_q, l_k)]
                 assert int(it[8:10].view(np.int64)[0]) == at[s]
                 assert 0 <= s0 <= max(s0, s1) <= max(streamed(s), s0) and t % 32 == 0 and t < max(1, owned(s))
-                if slot >= 0:
-                    assert tile == 32 and s0 % 32 == 0 or not causal
-                    parts.setdefault((s, t), []).append(slot)
+                units = (min(owned(s) - t, tile) + 31) // 32
+                for u in range(units if slot >= 0 else 0):
+                    assert s0 % 32 == 0 or causal
+                    parts.setdefault((s, t + 32 * u), []).append(slot + u)
                 for x in range(t, min(owned(s), t + tile)):
                     lo, hi = needs(s, x)
                     seen[s][x] += max(0, min(hi, s1) - max(lo, s0))
+        taken = sorted(x for v in parts.values() for x in v)
+        assert taken == list(range(len(taken))) and len(taken) == n_slots
         for it in merges:
-            q0, l_q, k0, l_k, t, n, _, slot = (int(x) for x in it[:8])
-            assert sorted(parts.pop((by_seq[(q0, k0, l_q, l_k)], t))) == list(range(slot, slot + n))
+            q0, l_q, k0, l_k, t, n, units, slot = (int(x) for x in it[:8])
+            assert parts.pop((by_seq[(q0, k0, l_q, l_k)], t)) == [slot + p * units for p in range(n)]
         assert not parts
         for s in range(len(lq)):
             for x in range(owned(s)):
@@ -120,8 +124,8 @@ def test_plan_covers_every_row_and_key_once(lib, causal, group, many):
     off = [b - a for a, b in zip(lq, lk)]
     row_needs = lambda s, r: (0, max(0, min(lk[s], off[s] + r // group + 1)) if causal else lk[s])  # noqa: E731
     key_needs = lambda s, j: (min(lq[s] * group, max(0, j - off[s]) * group) if causal else 0, lq[s] * group)  # noqa: E731
-    walked(list(zip(names[1:5], items[1:5])), lambda s: lq[s] * group, lambda s: lk[s], row_needs, items[9])
-    walked(list(zip(names[5:9], items[5:9])), lambda s: lk[s], lambda s: lq[s] * group, key_needs, items[10])
+    walked(list(zip(names[1:5], items[1:5])), lambda s: lq[s] * group, lambda s: lk[s], row_needs, items[9], c.layout[28])
+    walked(list(zip(names[5:9], items[5:9])), lambda s: lk[s], lambda s: lq[s] * group, key_needs, items[10], c.layout[29])
 
 
 def attn_args(c, **kw):
