@@ -678,33 +678,32 @@ def dense_attn_bwd_noalloc(Q, K, V, O, dO, LSE, scale: float | None = None, out=
 # ------------------------------------------------------------- packed sequences
 
 _SAME_DEVICE = contextlib.nullcontext()
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _on(device: torch.device):
     """Makes `device` the current one around a call (kernels are launched on the current device)."""
-    if device.index is None or device.index == torch.cuda.current_device():
+    if device.index is None or device.index == _current_device():
         return _SAME_DEVICE
     return torch.cuda.device(device)
 
 
-@dataclass
 class PackedPlan:
     """The work list of packed-sequence attention: the C struct and the device copy of its items."""
 
-    c: GtPackedPlan
-    items: torch.Tensor
+    def __init__(self, c: GtPackedPlan, items: torch.Tensor):
+        self.c, self.items = c, items
+        # what every call asks for, as plain values: a call over short sequences is bound by this binding
+        self.ref, self.device, self._ws = ctypes.byref(c), items.device, {}
+        self.nq, self.nk, self.heads, self.kv_heads, self.pair_bytes = c.nq, c.nk, c.H, c.Hkv, c.pair_bytes
 
-    @property
-    def nq(self):
-        return self.c.nq
-
-    @property
-    def nk(self):
-        return self.c.nk
-
-    @property
-    def pair_bytes(self):
-        return self.c.pair_bytes
+    def workspace(self, size, *args) -> torch.Tensor:
+        """A workspace for the call whose size query `size` takes (plan, *args)."""
+        key = (size.__name__, args)
+        n = self._ws.get(key)
+        if n is None:
+            n = self._ws[key] = size(self.ref, *args)
+        return _workspace(n, self.device)
 
 
 def _host_ptr(ptr, name: str) -> torch.Tensor:
@@ -742,27 +741,30 @@ def packed_plan(q_ptr, k_ptr=None, *, heads: int, kv_heads: int | None = None, c
 
 def _check_rows(t: torch.Tensor, n: int, heads: int, d: int, dtype, device, name: str) -> int:
     """Node stride of a [n or more, heads, d] tensor whose nodes' features are contiguous."""
-    _need(t.is_cuda and t.device == device and t.dtype == dtype and t.dim() == 3 and t.shape[1:] == (heads, d)
-          and t.shape[0] >= n, f"{name} must be a [{n} or more, {heads}, {d}] tensor of the plan's device and one dtype")
-    if t.shape[0] <= 1 and t.is_contiguous():
+    shape = t.shape
+    if not (t.is_cuda and t.dtype is dtype and len(shape) == 3 and shape[0] >= n and shape[1] == heads
+            and shape[2] == d and t.device == device):
+        raise ValueError(f"{name} must be a [{n} or more, {heads}, {d}] tensor of the plan's device and one dtype")
+    if t.is_contiguous():
         return heads * d
     s = t.stride()
-    _need((d == 1 or s[2] == 1) and (heads == 1 or s[1] == d) and s[0] >= heads * d,
+    _need((d == 1 or s[2] == 1) and (heads == 1 or s[1] == d) and (shape[0] <= 1 or s[0] >= heads * d),
           f"{name}: a node's features must be contiguous")
-    return s[0]
+    return s[0] if shape[0] > 1 else heads * d
 
 
 def _check_packed(plan: PackedPlan, Q, K, V):
-    c = plan.c
-    _need(Q.dim() == 3, "features must be [n, H, d]")
-    d, dev = Q.shape[2], plan.items.device
-    return (d, _dtype_code(Q), _check_rows(Q, c.nq, c.H, d, Q.dtype, dev, "Q"),
-            _check_rows(K, c.nk, c.Hkv, d, Q.dtype, dev, "K"), _check_rows(V, c.nk, c.Hkv, d, Q.dtype, dev, "V"))
+    shape = Q.shape
+    _need(len(shape) == 3, "features must be [n, H, d]")
+    d, dtype, dev = shape[2], Q.dtype, plan.device
+    return (d, _dtype_code(Q), _check_rows(Q, plan.nq, plan.heads, d, dtype, dev, "Q"),
+            _check_rows(K, plan.nk, plan.kv_heads, d, dtype, dev, "K"),
+            _check_rows(V, plan.nk, plan.kv_heads, d, dtype, dev, "V"))
 
 
 def _new_rows(like: torch.Tensor, n: int) -> torch.Tensor:
     """A contiguous tensor of like's shape for a call that writes its first n rows: the others are zeros."""
-    out = torch.empty(like.shape, dtype=like.dtype, device=like.device)
+    out = torch.empty_like(like, memory_format=torch.contiguous_format)
     if out.shape[0] > n:
         out[n:].zero_()
     return out
@@ -776,15 +778,15 @@ def _new_lse(rows: int, heads: int, n: int, device) -> torch.Tensor:
 
 
 def _check_contiguous(t, shape, dtype, device, name: str):
-    _need(t.shape == shape and t.dtype == dtype and t.device == device and t.is_contiguous(),
-          f"{name} must be a contiguous {list(shape)} tensor of the features' dtype and device")
+    if not (t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.device == device):
+        raise ValueError(f"{name} must be a contiguous {list(shape)} tensor of {dtype} on the features' device")
 
 
 def _check_table(plan: PackedPlan, table, buckets):
-    dev = plan.items.device
-    _need(table.dtype == torch.float32 and table.dim() == 2 and table.shape[1] == plan.c.H and table.is_contiguous()
+    dev = plan.device
+    _need(table.dtype == torch.float32 and table.dim() == 2 and table.shape[1] == plan.heads and table.is_contiguous()
           and table.device == dev, "table must be a contiguous fp32 [n_buckets, H] tensor of the plan's device")
-    _need(buckets.dtype == torch.uint8 and buckets.dim() == 1 and buckets.numel() >= plan.c.pair_bytes
+    _need(buckets.dtype == torch.uint8 and buckets.dim() == 1 and buckets.numel() >= plan.pair_bytes
           and buckets.is_contiguous() and buckets.device == dev,
           "buckets must be a contiguous uint8 tensor of plan.pair_bytes, on the plan's device")
 
@@ -795,11 +797,11 @@ def packed_attn_fwd(plan: PackedPlan, Q: torch.Tensor, K: torch.Tensor, V: torch
     lib = load_library()
     d, dt, ldq, ldk, ldv = _check_packed(plan, Q, K, V)
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
-    with _on(Q.device):
-        O, LSE = _new_rows(Q, plan.c.nq), _new_lse(Q.shape[0], plan.c.H, plan.c.nq, Q.device)
-        ws = _workspace(lib.gt_packed_attn_fwd_workspace_size(ctypes.byref(plan.c), d, dt), Q.device)
-        _check(lib.gt_packed_attn_fwd(ctypes.byref(plan.c), d, dt, _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv, scale,
-                                      _ptr(O), _ptr(LSE), _ptr(ws), ws.numel(), _stream(Q.device)),
+    with _on(plan.device):
+        O, LSE = _new_rows(Q, plan.nq), _new_lse(Q.shape[0], plan.heads, plan.nq, plan.device)
+        ws = plan.workspace(lib.gt_packed_attn_fwd_workspace_size, d, dt)
+        _check(lib.gt_packed_attn_fwd(plan.ref, d, dt, _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv, scale,
+                                      _ptr(O), _ptr(LSE), _ptr(ws), ws.numel(), _stream(plan.device)),
                "gt_packed_attn_fwd")
     return O, LSE
 
@@ -812,12 +814,12 @@ def packed_attn_bwd(plan: PackedPlan, Q, K, V, O, dO, LSE, scale: float | None =
     _check_contiguous(dO, Q.shape, Q.dtype, Q.device, "dO")
     _check_contiguous(LSE, Q.shape[:2], torch.float32, Q.device, "LSE")
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
-    with _on(Q.device):
-        dQ, dK, dV = _new_rows(Q, plan.c.nq), _new_rows(K, plan.c.nk), _new_rows(V, plan.c.nk)
-        ws = _workspace(lib.gt_packed_attn_bwd_workspace_size(ctypes.byref(plan.c), d, dt), Q.device)
-        _check(lib.gt_packed_attn_bwd(ctypes.byref(plan.c), d, dt, _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv, _ptr(O),
+    with _on(plan.device):
+        dQ, dK, dV = _new_rows(Q, plan.nq), _new_rows(K, plan.nk), _new_rows(V, plan.nk)
+        ws = plan.workspace(lib.gt_packed_attn_bwd_workspace_size, d, dt)
+        _check(lib.gt_packed_attn_bwd(plan.ref, d, dt, _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv, _ptr(O),
                                       _ptr(dO), _ptr(LSE), scale, _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(ws), ws.numel(),
-                                      _stream(Q.device)), "gt_packed_attn_bwd")
+                                      _stream(plan.device)), "gt_packed_attn_bwd")
     return dQ, dK, dV
 
 
@@ -830,12 +832,12 @@ def packed_attn_fwd_bias(plan: PackedPlan, Q, K, V, table, buckets, scale: float
     _check_table(plan, table, buckets)
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
     B = table.shape[0]
-    with _on(Q.device):
-        O, LSE = _new_rows(Q, plan.c.nq), _new_lse(Q.shape[0], plan.c.H, plan.c.nq, Q.device)
-        ws = _workspace(lib.gt_packed_attn_fwd_bias_workspace_size(ctypes.byref(plan.c), d, dt, B), Q.device)
-        _check(lib.gt_packed_attn_fwd_bias(ctypes.byref(plan.c), d, dt, _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv,
+    with _on(plan.device):
+        O, LSE = _new_rows(Q, plan.nq), _new_lse(Q.shape[0], plan.heads, plan.nq, plan.device)
+        ws = plan.workspace(lib.gt_packed_attn_fwd_bias_workspace_size, d, dt, B)
+        _check(lib.gt_packed_attn_fwd_bias(plan.ref, d, dt, _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv,
                                            _ptr(table), B, _ptr(buckets), scale, _ptr(O), _ptr(LSE), _ptr(ws),
-                                           ws.numel(), _stream(Q.device)), "gt_packed_attn_fwd_bias")
+                                           ws.numel(), _stream(plan.device)), "gt_packed_attn_fwd_bias")
     return O, LSE
 
 
@@ -848,14 +850,14 @@ def packed_attn_bwd_bias(plan: PackedPlan, Q, K, V, table, buckets, dO, LSE, sca
     _check_contiguous(LSE, Q.shape[:2], torch.float32, Q.device, "LSE")
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
     B = table.shape[0]
-    with _on(Q.device):
-        dQ, dK, dV = _new_rows(Q, plan.c.nq), _new_rows(K, plan.c.nk), _new_rows(V, plan.c.nk)
+    with _on(plan.device):
+        dQ, dK, dV = _new_rows(Q, plan.nq), _new_rows(K, plan.nk), _new_rows(V, plan.nk)
         dtable = torch.empty_like(table)
-        ws = _workspace(lib.gt_packed_attn_bwd_bias_workspace_size(ctypes.byref(plan.c), d, dt, B), Q.device)
-        _check(lib.gt_packed_attn_bwd_bias(ctypes.byref(plan.c), d, dt, _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv,
+        ws = plan.workspace(lib.gt_packed_attn_bwd_bias_workspace_size, d, dt, B)
+        _check(lib.gt_packed_attn_bwd_bias(plan.ref, d, dt, _ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv,
                                            _ptr(table), B, _ptr(buckets), _ptr(dO), _ptr(LSE), scale, _ptr(dQ),
                                            _ptr(dK), _ptr(dV), _ptr(dtable), _ptr(ws), ws.numel(),
-                                           _stream(Q.device)), "gt_packed_attn_bwd_bias")
+                                           _stream(plan.device)), "gt_packed_attn_bwd_bias")
     return dQ, dK, dV, dtable
 
 
@@ -901,9 +903,11 @@ def _check_norm(x, f, gate, sigmoid, kind, params):
     _check_contiguous(f, x.shape, x.dtype, x.device, "f")
     _need(kind in _NORMS, "kind must be 'layer' or 'rms'")
     n, D = x.shape
+    dev, f32 = x.device, torch.float32
     for name, p in params.items():
-        _need(p is None or (p.dtype == torch.float32 and p.shape == (D,) and p.is_contiguous() and p.device == x.device),
-              f"{name} must be a contiguous fp32 tensor [D] on x's device")
+        if p is not None and not (p.dtype is f32 and p.dim() == 1 and p.shape[0] == D and p.is_contiguous()
+                                  and p.device == dev):
+            raise ValueError(f"{name} must be a contiguous fp32 tensor [D] on x's device")
     if gate is None:
         _need(not sigmoid, "sigmoid needs a gate")
         return GT_GATE_NONE
