@@ -157,7 +157,8 @@ enum RowPass { kStat, kGrad };
 // and the weights' sum under the given LSE: an fp32 LSE beside a large bias
 // holds log(sum) only roughly, so P is normalised again by it.
 template <typename T, int D, int STAGE, int W, int KS, int SUB, bool BIAS, RowPass PASS>
-__global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(D * int(sizeof(T)) <= 128 ? waves_per_simd(KS * 4 * STAGE * D * int(sizeof(T)), W* KS) : 1))) void k_packed_rows(PackedArgs a) {
+__global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
+    D * int(sizeof(T)) <= 256 ? waves_per_simd(KS * 4 * STAGE * D * int(sizeof(T)), W* KS) : 1))) void k_packed_rows(PackedArgs a) {
     using B = Blk<T, D, STAGE>;
     __shared__ __attribute__((aligned(16))) T sK0[KS * B::kElems], sK1[KS * B::kElems];
     __shared__ __attribute__((aligned(16))) T sV0[KS * B::kElems], sV1[KS * B::kElems];
@@ -329,11 +330,18 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
     }
 }
 
+// kBoth: dK and dV of a block from one forming of its weights.  Wide rows' accumulators
+// for both leave room for one wavefront a SIMD, which waits for everything it reads
+// (D = 128, bf16); there a pass for each (kOnlyV: Q, dO; kOnlyK) forms the scores
+// twice, five products for four, with two wavefronts.
+enum KeyPass { kBoth, kOnlyV, kOnlyK };
+
 // dK_j = scale sum_i dS_ij Q_i and dV_j = sum_i P_ij dO_i over the rows of the
 // whole group, with the wavefront owning 32 keys and the rows streaming through
 // LDS; the dP products start from the rows' -D_i.
-template <typename T, int D, int STAGE, int W, int KS, int SUB, bool BIAS>
-__global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(D * int(sizeof(T)) <= 128 ? waves_per_simd(KS * 4 * STAGE * D * int(sizeof(T)), W* KS) : 1))) void k_packed_keys(PackedArgs a) {
+template <typename T, int D, int STAGE, int W, int KS, int SUB, bool BIAS, KeyPass PASS>
+__global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
+    PASS != kBoth || D * int(sizeof(T)) <= 128 ? waves_per_simd(KS * 4 * STAGE * D * int(sizeof(T)), W* KS) : 1))) void k_packed_keys(PackedArgs a) {
     using B = Blk<T, D, STAGE>;
     __shared__ __attribute__((aligned(16))) T sQ0[KS * B::kElems], sQ1[KS * B::kElems];
     __shared__ __attribute__((aligned(16))) T sG0[KS * B::kElems], sG1[KS * B::kElems];
@@ -411,17 +419,18 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
         const int from = rmin - r0 - part(0, lane), to = it.s1 - r0 - part(0, lane);
         f32x16_t s[1] = {splat16(0.f)}, dp[1];
         const int rs0 = 32 * rb + part(0, lane);  // the lane's rows in the stage's statistics
+        if constexpr (PASS != kOnlyV)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             const float4 d4 = *reinterpret_cast<const float4*>(&bR[1][rs0 + 4 * x]);
             dp[0][4 * x] = d4.x, dp[0][4 * x + 1] = d4.y, dp[0][4 * x + 2] = d4.z, dp[0][4 * x + 3] = d4.w;
         }
         B::template rows<1>(bQ, lds, kf, s);
-        B::template rows<1>(bG, lds, vf, dp);
+        if constexpr (PASS != kOnlyV) B::template rows<1>(bG, lds, vf, dp);
         // operands and statistics are read where they are used: held together they do not fit the registers
         __builtin_amdgcn_sched_barrier(0);
         typename B::Cols x;
-        x.load(bG, lds);
+        x.load(PASS == kOnlyK ? bQ : bG, lds);
         if constexpr (masked.value) x.drop(it.s1 - r0, lane);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -442,17 +451,23 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
                 if constexpr (masked.value) {
                     const bool out = i < from || i >= to;
                     t = out ? -kInf : t;
-                    dp[0][i] = out ? 0.f : dp[0][i];
+                    if constexpr (PASS != kOnlyV) dp[0][i] = out ? 0.f : dp[0][i];
                 }
                 s[0][i] = ex2(t);
-                dp[0][i] *= s[0][i];
+                if constexpr (PASS != kOnlyV) dp[0][i] *= s[0][i];
             }
         }
+        if constexpr (PASS == kOnlyK) {
+            B::template apply<1>(x, dp, dk);
+            return;
+        }
         B::template apply<1>(x, s, dv);
-        __builtin_amdgcn_sched_barrier(0);
-        x.load(bQ, lds);
-        if constexpr (masked.value) x.drop(it.s1 - r0, lane);
-        B::template apply<1>(x, dp, dk);
+        if constexpr (PASS == kBoth) {
+            __builtin_amdgcn_sched_barrier(0);
+            x.load(bQ, lds);
+            if constexpr (masked.value) x.drop(it.s1 - r0, lane);
+            B::template apply<1>(x, dp, dk);
+        }
     };
     auto stage = [&](auto masked, int base, const T* cQ, const T* cG, const Stats& cR, T* nQ, T* nG, Stats& nR) {
         load_stats(base + KS * STAGE);
@@ -498,17 +513,18 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
             }
     }
     const int thread = key_wave * kWave + lane;
-    add_sets<KS, W>(dk[0], set, thread);
-    if (!add_sets<KS, W>(dv[0], set, thread)) return;
+    if constexpr (PASS != kOnlyV) add_sets<KS, W>(dk[0], set, thread);
+    if constexpr (PASS != kOnlyK) add_sets<KS, W>(dv[0], set, thread);
+    if (set > 0) return;
     if (it.slot >= 0) {
         if (key0 >= it.lk) return;  // uniform
         float* o = a.slots + ((int64_t(it.slot + sub * W + key_wave) * a.Hkv + hk) * (2 * kFewRows) + (lane & 31)) * D;
-        Blk<float, D>::store(o, dk[0], 1.f, lane);
-        Blk<float, D>::store(o + kFewRows * D, dv[0], 1.f, lane);
+        if constexpr (PASS != kOnlyV) Blk<float, D>::store(o, dk[0], 1.f, lane);
+        if constexpr (PASS != kOnlyK) Blk<float, D>::store(o + kFewRows * D, dv[0], 1.f, lane);
     } else if (j < it.lk) {
         const int64_t at = int64_t(it.k0 + j) * a.Hkv + hk;
-        B::store(static_cast<T*>(a.out1) + at * D, dk[0], a.scale, lane);
-        B::store(static_cast<T*>(a.out2) + at * D, dv[0], 1.f, lane);
+        if constexpr (PASS != kOnlyV) B::store(static_cast<T*>(a.out1) + at * D, dk[0], a.scale, lane);
+        if constexpr (PASS != kOnlyK) B::store(static_cast<T*>(a.out2) + at * D, dv[0], 1.f, lane);
     }
 }
 
@@ -579,7 +595,7 @@ gt_status packed_bwd_d(const gt_packed_plan* p, PackedArgs a, float* dtable, hip
         } else {
             GT_ROWS(kRows128, kStage, 4, 1, 1, kGrad)
         }
-        if constexpr (kRow <= 128) {
+        if constexpr (kRow <= 128 || sizeof(T) == 2) {
             GT_ROWS(kRows256, kStage, 8, 1, 1, kGrad)
         } else {
             GT_ROWS(kRows256, kStage, 4, 1, 2, kGrad)
@@ -590,23 +606,36 @@ gt_status packed_bwd_d(const gt_packed_plan* p, PackedArgs a, float* dtable, hip
         const gt_status st = packed_merge_rows(p, D, dt, a, s);
         if (st != GT_OK) return st;
     }
-#define GT_KEYS(LIST, STAGE, W, KS, SUB)                                                                        \
+#define GT_KEYS(LIST, STAGE, W, KS, SUB, PASS)                                                                  \
     if (list(LIST)) {                                                                                           \
-        k_packed_keys<T, D, STAGE, W, KS, SUB, BIAS>                                                            \
+        k_packed_keys<T, D, STAGE, W, KS, SUB, BIAS, PASS>                                                      \
             <<<packed_grid(a.n_items, a.Hkv, SUB), W * KS * kWave, tab, s>>>(a);                                \
         GT_LAUNCH_CHECK("packed_bwd keys");                                                                     \
     }
-    GT_KEYS(kKeysFew, 32, 1, few_waves(kRow), 1)
-    GT_KEYS(kKeys64, kStage, 2, 1, 1)
-    if (kRow <= 128 && p->layout[kKeySharedAt]) {
-        GT_KEYS(kKeys128, kStage, 4, (kRow <= 128 ? 2 : 1), 1)
-    } else {
-        GT_KEYS(kKeys128, kStage, 4, 1, 1)
-    }
+    GT_KEYS(kKeysFew, 32, 1, few_waves(kRow), 1, kBoth)
     if constexpr (kRow <= 128) {
-        GT_KEYS(kKeys256, kStage, 8, 1, 1)
-    } else {  // the accumulators of two wavefronts a SIMD do not fit
-        GT_KEYS(kKeys256, kStage, 4, 1, 2)
+        GT_KEYS(kKeys64, kStage, 2, 1, 1, kBoth)
+        if (p->layout[kKeySharedAt]) {
+            GT_KEYS(kKeys128, kStage, 4, 2, 1, kBoth)
+        } else {
+            GT_KEYS(kKeys128, kStage, 4, 1, 1, kBoth)
+        }
+        GT_KEYS(kKeys256, kStage, 8, 1, 1, kBoth)
+    } else if constexpr (sizeof(T) == 2) {
+        GT_KEYS(kKeys64, kStage, 2, 1, 1, kBoth)
+        if (p->layout[kKeySharedAt]) {
+            GT_KEYS(kKeys128, 32, 4, 2, 1, kOnlyV)
+            GT_KEYS(kKeys128, 32, 4, 2, 1, kOnlyK)
+        } else {
+            GT_KEYS(kKeys128, kStage, 4, 1, 1, kOnlyV)
+            GT_KEYS(kKeys128, kStage, 4, 1, 1, kOnlyK)
+        }
+        GT_KEYS(kKeys256, kStage, 8, 1, 1, kOnlyV)
+        GT_KEYS(kKeys256, kStage, 8, 1, 1, kOnlyK)
+    } else {
+        GT_KEYS(kKeys64, kStage, 2, 1, 1, kBoth)
+        GT_KEYS(kKeys128, kStage, 4, 1, 1, kBoth)
+        GT_KEYS(kKeys256, kStage, 4, 1, 2, kBoth)
     }
 #undef GT_KEYS
     if (list(kKeyMerges)) {

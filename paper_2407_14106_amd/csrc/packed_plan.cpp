@@ -32,8 +32,9 @@ struct Cuts {
     Cut rows, keys;
 };
 
-// A CU works on one set of eight wavefronts at a time (or two of four), so the
-// chip is in balance when no walk is longer than a CU's share of all of them.
+// A CU works on eight wavefronts at a time, two workgroups of four or one of two
+// such sets, so the chip is in balance when no walk is longer than a workgroup's
+// share of all of them.
 constexpr int64_t kCus = 256;
 // Walks are not split into shorter parts than this: parts cost a second launch
 // and a merge.
@@ -62,9 +63,10 @@ Cut cut_side(const Load& few, const Load& t128, const Load& t256, int64_t Hkv) {
     auto share = [&](const Load& l, int64_t blocks) { return (l.total * Hkv + blocks - 1) / blocks; };
     // Large tiles read the partners less often, but take all of a CU: where no walk is more than half its share.
     c.large = t256.n * Hkv >= 2 * kCus && t256.most <= share(t256, 2 * kCus);
-    c.shared = t128.n * Hkv < 2 * kCus || t128.most > share(t128, 2 * kCus);
+    // Two sets on one walk where there are fewer workgroups than the chip holds.
+    c.shared = t128.n * Hkv < 2 * kCus;
     auto chunk = [&](int64_t x) { return std::max(kMinChunk, (x + 255) & ~int64_t(255)); };
-    c.chunk = chunk(share(t128, kCus));
+    c.chunk = chunk(share(t128, c.shared ? kCus : 2 * kCus));
     c.few_chunk = chunk(share(few, 2 * kCus));
     return c;
 }
