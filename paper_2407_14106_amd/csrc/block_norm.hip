@@ -60,19 +60,20 @@ struct RowSum {
 };
 
 // A lane's NV pieces of one row: E consecutive features each, LPR pieces apart.
-template <typename T, int LPR, int NV, bool VEC>
+// VEC: whole pieces at 16-byte addresses; FULL besides: the row fills its lanes.
+template <typename T, int LPR, int NV, bool VEC, bool FULL>
 struct Cols {
     static constexpr int E = 16 / int(sizeof(T));
     int D, lane;  // lane of the row
     __device__ __forceinline__ int col(int v) const { return (lane + LPR * v) * E; }
-    __device__ __forceinline__ bool in(int v, int t) const { return VEC ? col(v) < D : col(v) + t < D; }
+    __device__ __forceinline__ bool in(int v, int t) const { return FULL || (VEC ? col(v) < D : col(v) + t < D); }
     __device__ __forceinline__ void load(float (&o)[NV][E], const void* p, int64_t row) const {
         const T* r = static_cast<const T*>(p) + row * D;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             if constexpr (VEC) {
                 uint4 x = make_uint4(0, 0, 0, 0);
-                if (col(v) < D) x = *reinterpret_cast<const uint4*>(r + col(v));
+                if (FULL || col(v) < D) x = *reinterpret_cast<const uint4*>(r + col(v));
                 const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
@@ -96,7 +97,7 @@ struct Cols {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             if constexpr (VEC) {
-                if (col(v) >= D) continue;
+                if (!FULL && col(v) >= D) continue;
                 uint4 x;
                 if constexpr (E == 8)
                     x = make_uint4(pack_bf16x2(o[v][0], o[v][1]), pack_bf16x2(o[v][2], o[v][3]),
@@ -152,9 +153,9 @@ __device__ __forceinline__ void row_stats(const float (&v)[NV][E], const C& c, b
 
 __device__ __forceinline__ float sigmoid(float v) { return 1.f / (1.f + __expf(-v)); }
 
-template <typename T, int LPR, int NV, bool VEC>
+template <typename T, int LPR, int NV, bool VEC, bool FULL>
 __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_fwd(NormArgs a) {
-    using C = Cols<T, LPR, NV, VEC>;
+    using C = Cols<T, LPR, NV, VEC, FULL>;
     using S = RowSum<LPR>;
     constexpr int E = C::E;
     __shared__ float s_sum[2 * S::kThreads / kWave];
@@ -204,9 +205,9 @@ __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_fwd(NormArgs a) 
 //   dx = res_scale t, dg = u t, du = g t
 //   df = rf (du w1 - <du w1> - fh <du w1 fh>)
 // (without the <dz w2> and <du w1> terms for the root mean square).
-template <typename T, int LPR, int NV, bool VEC>
+template <typename T, int LPR, int NV, bool VEC, bool FULL>
 __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_bwd(NormArgs a) {
-    using C = Cols<T, LPR, NV, VEC>;
+    using C = Cols<T, LPR, NV, VEC, FULL>;
     using S = RowSum<LPR>;
     constexpr int E = C::E;
     __shared__ float s_sum[2 * S::kThreads / kWave];
@@ -363,13 +364,21 @@ bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 
 template <typename T, bool VEC>
 void run_fwd(const NormArgs& a, int pieces, int blocks, hipStream_t s) {
-#define GT_CALL(LPR, NV) k_norm_fwd<T, LPR, NV, VEC><<<blocks, RowSum<LPR>::kThreads, 0, s>>>(a)
+#define GT_CALL(LPR, NV)                                                                                        \
+    do {                                                                                                        \
+        if (VEC && pieces == LPR * NV) k_norm_fwd<T, LPR, NV, VEC, VEC><<<blocks, RowSum<LPR>::kThreads, 0, s>>>(a); \
+        else k_norm_fwd<T, LPR, NV, VEC, false><<<blocks, RowSum<LPR>::kThreads, 0, s>>>(a);                     \
+    } while (0)
     GT_NORM_SHAPE(pieces, GT_CALL);
 #undef GT_CALL
 }
 template <typename T, bool VEC>
 void run_bwd(const NormArgs& a, int pieces, int blocks, hipStream_t s) {
-#define GT_CALL(LPR, NV) k_norm_bwd<T, LPR, NV, VEC><<<blocks, RowSum<LPR>::kThreads, 0, s>>>(a)
+#define GT_CALL(LPR, NV)                                                                                        \
+    do {                                                                                                        \
+        if (VEC && pieces == LPR * NV) k_norm_bwd<T, LPR, NV, VEC, VEC><<<blocks, RowSum<LPR>::kThreads, 0, s>>>(a); \
+        else k_norm_bwd<T, LPR, NV, VEC, false><<<blocks, RowSum<LPR>::kThreads, 0, s>>>(a);                     \
+    } while (0)
     GT_NORM_SHAPE(pieces, GT_CALL);
 #undef GT_CALL
 }

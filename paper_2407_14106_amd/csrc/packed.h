@@ -94,12 +94,11 @@ inline int64_t key_slot_floats(int d) { return kFewRows * 2 * d; }
 // Blocks of the pair kernels' and of the row kernels' table gradients.
 constexpr int64_t kPairBlocks = 1024;
 inline int64_t pair_blocks(const gt_packed_plan* p, int row_bytes) {
-    const int64_t units = packed_items(p, kPairs) * p->Hkv;
-    // blocks of whole sets of heads, so that a wavefront's pairs are all of one head
-    const int64_t per = int64_t(p->Hkv) * pair_waves(row_bytes);
-    const int64_t most = cdiv(kPairBlocks * pair_waves(row_bytes), per) * per;
-    const int64_t waves = cdiv(units < most ? units : most, per) * per;
-    return waves / pair_waves(row_bytes);
+    // whole sets of heads on each XCD: a wavefront's pairs are all of one head, and an XCD works on the neighbouring
+    // heads of a run of sequences, whose rows share cache lines
+    const int64_t units = packed_items(p, kPairs) * p->Hkv, set = int64_t(kXcds) * p->Hkv, w = pair_waves(row_bytes);
+    const int64_t want = cdiv(units, w * set) * set, most = cdiv(kPairBlocks, set) * set;
+    return want < most ? want : most;
 }
 
 // Launchers, one set per element type (packed_fwd_*.hip, packed_bwd_*.hip).

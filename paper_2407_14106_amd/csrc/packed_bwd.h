@@ -14,7 +14,8 @@ namespace {
 // With a bias a wavefront keeps to one head and goes through its sequences, its
 // part of the table's gradient in LDS.
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair_bwd(PackedArgs a) {
+__global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave)
+    __attribute__((amdgpu_waves_per_eu(D * int(sizeof(T)) <= 64 ? 3 : 1))) void k_pair_bwd(PackedArgs a) {
     using B = Blk<T, D>;
     using S = Blk<T, 32>;
     constexpr int W = pair_waves(D * int(sizeof(T)));
@@ -23,7 +24,7 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
     const int lane = lane_id(), wave = uniform(int(threadIdx.x) / kWave);
     T *sQ = s_q[wave], *sK = s_k[wave], *sV = s_v[wave], *sG = s_g[wave];
     const int gs = a.gs, gm = (1 << gs) - 1;
-    const uint32_t first = blockIdx.x * W + wave, step = gridDim.x * W, units = uint32_t(a.n_items) * uint32_t(a.Hkv);
+    const uint32_t first = uint32_t(xcd_block(blockIdx.x, gridDim.x)) * W + wave, step = gridDim.x * W, units = uint32_t(a.n_items) * uint32_t(a.Hkv);
     const int hk = int(first % uint32_t(a.Hkv));  // of every unit: step is a multiple of Hkv
     float* tab = s_dyn + wave * (kTableStride << gs);
     float* hist = s_dyn + W * (kTableStride << gs) + wave * (a.B + 1) * kWave;
@@ -33,8 +34,10 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
     }
     const typename B::At at(lane, 0);
     const typename S::At turned_at(lane, 0);
+    PackedItem next = a.items[first < units ? first / uint32_t(a.Hkv) : 0];
     for (uint32_t unit = first; unit < units; unit += step) {
-        const PackedItem it = a.items[unit / uint32_t(a.Hkv)];
+        const PackedItem it = next;
+        next = a.items[(unit + step < units ? unit + step : unit) / uint32_t(a.Hkv)];
         const int R = it.lq << gs, off = it.lk - it.lq;
         const int64_t row_at = int64_t(it.q0) * a.H + (hk << gs), key_at = int64_t(it.k0) * a.Hkv + hk;
         const bool some = R > 0 && it.lk > 0;
@@ -76,7 +79,7 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
                 if constexpr (BIAS) u = fmaf(s[0][i], a.scale, tab[(r & gm) * kTableStride + id_of(ids, i, a.B)]);
                 else u = s[0][i] * a.scale;
                 s[0][i] = ex2((u - L) * kLog2e);
-                if (i >= lim - part(0, lane)) s[0][i] = 0.f, dp[0][i] = 0.f;
+                if (i >= lim - part(0, lane)) s[0][i] = 0.f;
                 sum += s[0][i];
                 dsum = fmaf(s[0][i], dp[0][i], dsum);
             }
@@ -90,7 +93,6 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
             }
             typename B::Cols x;
             x.load(sK, at);
-            x.drop(it.lk, lane);
             B::template apply<1>(x, dp, dq);
             wave_done();  // K and V are read: their place takes P and dS
             lay_block<T>(sK, s[0], lane);
@@ -105,11 +107,9 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
             };
             turned(sK);
             x.load(sG, at);
-            x.drop(R, lane);
             B::template apply<1>(x, w, dv);
             turned(sV);
             x.load(sQ, at);
-            x.drop(R, lane);
             B::template apply<1>(x, w, dk);
         }
         if (r < R) B::store(static_cast<T*>(a.out0) + (row_at + q * a.H + (r & gm)) * D, dq[0], a.scale, lane);
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
             B::store(static_cast<T*>(a.out1) + (key_at + r * a.Hkv) * D, dk[0], a.scale, lane);
             B::store(static_cast<T*>(a.out2) + (key_at + r * a.Hkv) * D, dv[0], 1.f, lane);
         }
-        wave_done();
+        lds_done();  // the next sequence's loads may land
     }
     if constexpr (BIAS)
         hist_flush<kWave>(hist, 1, a.B, gs, a.hist + int64_t(first) * (int64_t(a.B) << gs), lane);
@@ -221,9 +221,7 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
     float sum = 0.f, dsum = 0.f;
     stage_done<(W > 1) || BIAS>();
     const typename B::At lds(lane, set * B::kElems * int(sizeof(T)));
-    auto block32 = [&](auto masked, int key0, const T* bK, const T* bV) {
-        uint4 ids;
-        if constexpr (BIAS) ids = load_ids(id_row, key0, it.lk, lane);
+    auto block32 = [&](auto masked, int key0, const T* bK, const T* bV, const uint4& ids) {
         const int left = lim - key0 - part(0, lane);  // how many of the lane's 16 keys its row attends to
         f32x16_t s[1] = {splat16(0.f)}, dp[1] = {splat16(-Dq)};
         B::template rows<1>(bK, lds, qf, s);
@@ -231,7 +229,6 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
         typename B::Cols kt;
         if constexpr (PASS == kGrad) {
             kt.load(bK, lds);
-            if constexpr (masked.value) kt.drop(it.s1 - key0, lane);
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
@@ -244,11 +241,7 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
             } else {
                 t = fmaf(s[0][i], sl2, -L);
             }
-            if constexpr (masked.value) {
-                const bool out = i >= left;
-                t = out ? -kInf : t;
-                dp[0][i] = out ? 0.f : dp[0][i];
-            }
+            if constexpr (masked.value) t = i >= left ? -kInf : t;
             const float p = ex2(t);
             s[0][i] = p * dp[0][i];
             if constexpr (PASS == kStat) {
@@ -260,18 +253,30 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
         }
         if constexpr (PASS == kGrad) B::template apply<1>(kt, s, acc);
     };
+    uint4 ids[STAGE / 32];  // the buckets of a stage, loaded a stage ahead
+    auto next_ids = [&](int kbase) {
+        if constexpr (BIAS)
+#pragma unroll
+            for (int kb = 0; kb < STAGE / 32; ++kb) ids[kb] = load_ids(id_row, kbase + 32 * kb, it.lk, lane);
+    };
+    next_ids(it.s0 + set * STAGE);
     auto stage = [&](auto masked, int kbase, const T* cK, const T* cV, T* nK, T* nV) {
         fetch(kbase + KS * STAGE, nK, nV);
+        uint4 now[STAGE / 32];
+        if constexpr (BIAS)
+#pragma unroll
+            for (int kb = 0; kb < STAGE / 32; ++kb) now[kb] = ids[kb];
+        next_ids(kbase + KS * STAGE);
         if constexpr (masked.value) {
-#pragma unroll 1
+#pragma unroll
             for (int kb = 0; kb < STAGE / 32; ++kb)
                 if (kbase + 32 * kb < hi)  // uniform
-                    block32(masked, kbase + 32 * kb, cK + 32 * kb * D, cV + 32 * kb * D);
+                    block32(masked, kbase + 32 * kb, cK + 32 * kb * D, cV + 32 * kb * D, now[kb]);
         } else {
 #pragma unroll
             for (int kb = 0; kb < STAGE / 32; ++kb) {
                 __builtin_amdgcn_sched_barrier(0);  // two blocks' operands at once do not fit the registers
-                block32(masked, kbase + 32 * kb, cK + 32 * kb * D, cV + 32 * kb * D);
+                block32(masked, kbase + 32 * kb, cK + 32 * kb * D, cV + 32 * kb * D, now[kb]);
             }
         }
         stage_done<(W > 1)>();
@@ -348,6 +353,9 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
     // per row of a stage: LSE (exp2 domain without a bias), -D, log2 of the weights' sum
     typedef float Stats[KS][3][STAGE];
     __shared__ __attribute__((aligned(16))) Stats sR0, sR1;
+    // with a bias, the buckets of a stage's rows and a wavefront's 32 keys: loaded a row a lane, read a key a lane
+    typedef uint8_t Buckets[BIAS ? W * KS : 1][BIAS ? STAGE : 1][32];
+    __shared__ __attribute__((aligned(16))) Buckets sI0, sI1;
     extern __shared__ float s_tab[];
     PackedItem it;
     int hk, sub;
@@ -373,8 +381,23 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
             if constexpr (BIAS) rs[2] = a.Lg[at];
         }
     };
-    auto store_stats = [&](Stats& to) {
+    uint4 ids[STAGE / 32];
+    const int64_t wide = ids_width(it.lk);
+    auto load_rows = [&](int base) {
+        load_stats(base);
+        if constexpr (BIAS)
+#pragma unroll
+            for (int rb = 0; rb < STAGE / 32; ++rb) {
+                const int r = base + 32 * rb + (lane & 31), rc = r < it.s1 ? r : it.s1 - 1;
+                ids[rb] = load_ids(a.ids + it.pair + (rc >> gs) * wide, key0, it.lk, lane);
+            }
+    };
+    auto store_rows = [&](Stats& to, Buckets& toI) {
         if (key_wave == 0 && lane < STAGE) to[set][0][lane] = rs[0], to[set][1][lane] = rs[1], to[set][2][lane] = rs[2];
+        if constexpr (BIAS)
+#pragma unroll
+            for (int rb = 0; rb < STAGE / 32; ++rb)
+                *reinterpret_cast<uint4*>(&toI[wave][32 * rb + (lane & 31)][16 * (lane >> 5)]) = ids[rb];
     };
     const T* Q = static_cast<const T*>(a.Q) + int64_t(it.q0) * a.ldq + (hk << gs) * D;
     const T* G = static_cast<const T*>(a.dO) + (int64_t(it.q0) * a.H + (hk << gs)) * D;
@@ -386,7 +409,7 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
         B::template fetch<W>(toG + set * B::kElems, G + int64_t(base >> gs) * ldg, it.s1 - base, key_wave, lane,
                              [&](int r) { return __umul24(r >> gs, ldg) + uint32_t((r & gm) * D); });
     };
-    load_stats(it.s0 + set * STAGE);
+    if (it.s0 < it.s1) load_rows(it.s0 + set * STAGE);
     fetch(it.s0 + set * STAGE, sQ0, sG0);
     const int j = key0 + (lane & 31), jc = j < it.lk ? j : it.lk - 1;
     auto first_row = [&](int key) { return a.causal && key > off ? (key - off) << gs : 0; };
@@ -399,24 +422,11 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) dk[0][db] = dv[0][db] = splat16(0.f);
     const float sl2 = a.scale * kLog2e;
-    const uint8_t* id_key = BIAS ? a.ids + it.pair + jc : nullptr;
-    const int64_t wide = ids_width(it.lk);
-    store_stats(sR0);
+    store_rows(sR0, sI0);
     stage_done<(W > 1) || BIAS>();
     const typename B::At lds(lane, set * B::kElems * int(sizeof(T)));
-    auto block32 = [&](auto masked, int r0, const T* bQ, const T* bG, const float(&bR)[3][STAGE], int rb) {
-        uint32_t id[16];
-        if constexpr (BIAS) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = r0 + part(i, lane);
-                uint32_t b = 255u;
-                if (!masked.value || r < it.s1) b = id_key[(r >> gs) * wide];
-                id[i] = b < uint32_t(a.B) ? b : uint32_t(a.B);
-            }
-        }
-        // of the lane's 16 rows the first that its key is attended to by, and the first past the end
-        const int from = rmin - r0 - part(0, lane), to = it.s1 - r0 - part(0, lane);
+    auto block32 = [&](auto masked, int r0, const T* bQ, const T* bG, const float(&bR)[3][STAGE], const uint8_t* bI, int rb) {
+        const int from = rmin - r0 - part(0, lane);  // of the lane's 16 rows the first that attends to its key
         f32x16_t s[1] = {splat16(0.f)}, dp[1];
         const int rs0 = 32 * rb + part(0, lane);  // the lane's rows in the stage's statistics
         if constexpr (PASS != kOnlyV)
@@ -431,7 +441,6 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
         __builtin_amdgcn_sched_barrier(0);
         typename B::Cols x;
         x.load(PASS == kOnlyK ? bQ : bG, lds);
-        if constexpr (masked.value) x.drop(it.s1 - r0, lane);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const float4 l4 = *reinterpret_cast<const float4*>(&bR[0][rs0 + 4 * k]);
@@ -443,15 +452,15 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
                 const int i = 4 * k + y;
                 float t;
                 if constexpr (BIAS) {
-                    const float bias = s_tab[((r0 + part(i, lane)) & gm) * kTableStride + id[i]];
+                    const uint32_t id = bI[(32 * rb + part(i, lane)) * 32 + (lane & 31)];
+                    const float bias =
+                        s_tab[(part(i, lane) & gm) * kTableStride + (id < uint32_t(a.B) ? id : uint32_t(a.B))];
                     t = fmaf(fmaf(s[0][i], a.scale, bias) - L[y], kLog2e, -lg[y]);
                 } else {
                     t = fmaf(s[0][i], sl2, -L[y]);
                 }
                 if constexpr (masked.value) {
-                    const bool out = i < from || i >= to;
-                    t = out ? -kInf : t;
-                    if constexpr (PASS != kOnlyV) dp[0][i] = out ? 0.f : dp[0][i];
+                    t = i < from ? -kInf : t;
                 }
                 s[0][i] = ex2(t);
                 if constexpr (PASS != kOnlyV) dp[0][i] *= s[0][i];
@@ -465,28 +474,28 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
         if constexpr (PASS == kBoth) {
             __builtin_amdgcn_sched_barrier(0);
             x.load(bQ, lds);
-            if constexpr (masked.value) x.drop(it.s1 - r0, lane);
-            B::template apply<1>(x, dp, dk);
+                B::template apply<1>(x, dp, dk);
         }
     };
-    auto stage = [&](auto masked, int base, const T* cQ, const T* cG, const Stats& cR, T* nQ, T* nG, Stats& nR) {
-        load_stats(base + KS * STAGE);
+    auto stage = [&](auto masked, int base, const T* cQ, const T* cG, const Stats& cR, const Buckets& cI, T* nQ, T* nG,
+                     Stats& nR, Buckets& nI) {
+        load_rows(base + KS * STAGE);
         fetch(base + KS * STAGE, nQ, nG);
         if constexpr (masked.value) {
 #pragma unroll 1
             for (int rb = 0; rb < STAGE / 32; ++rb) {
                 const int r0 = base + 32 * rb;
                 if (r0 < it.s1 && r0 + 32 > rlo && key0 < it.lk)  // uniform
-                    block32(masked, r0, cQ + 32 * rb * D, cG + 32 * rb * D, cR[set], rb);
+                    block32(masked, r0, cQ + 32 * rb * D, cG + 32 * rb * D, cR[set], &cI[BIAS ? wave : 0][0][0], rb);
             }
         } else if (key0 < it.lk) {  // uniform
 #pragma unroll
             for (int rb = 0; rb < STAGE / 32; ++rb) {
                 __builtin_amdgcn_sched_barrier(0);
-                block32(masked, base + 32 * rb, cQ + 32 * rb * D, cG + 32 * rb * D, cR[set], rb);
+                block32(masked, base + 32 * rb, cQ + 32 * rb * D, cG + 32 * rb * D, cR[set], &cI[BIAS ? wave : 0][0][0], rb);
             }
         }
-        store_stats(nR);
+        store_rows(nR, nI);
         stage_done<(W > 1)>();
     };
     // the stages whose rows attend to every key of the tile lie between the first ones (causal) and the last (ragged);
@@ -502,14 +511,14 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
         const int end = phase == 0 && before < it.s1 ? before : it.s1;
 #pragma unroll 1
         for (; base < end; base += 2 * kRound) {
-            stage(Flag<true>{}, base + set * STAGE, sQ0, sG0, sR0, sQ1, sG1, sR1);
+            stage(Flag<true>{}, base + set * STAGE, sQ0, sG0, sR0, sI0, sQ1, sG1, sR1, sI1);
             if (base + kRound < it.s1)
-                stage(Flag<true>{}, base + kRound + set * STAGE, sQ1, sG1, sR1, sQ0, sG0, sR0);
+                stage(Flag<true>{}, base + kRound + set * STAGE, sQ1, sG1, sR1, sI1, sQ0, sG0, sR0, sI0);
         }
         if (phase == 0)
             for (; base < after; base += 2 * kRound) {
-                stage(Flag<false>{}, base + set * STAGE, sQ0, sG0, sR0, sQ1, sG1, sR1);
-                stage(Flag<false>{}, base + kRound + set * STAGE, sQ1, sG1, sR1, sQ0, sG0, sR0);
+                stage(Flag<false>{}, base + set * STAGE, sQ0, sG0, sR0, sI0, sQ1, sG1, sR1, sI1);
+                stage(Flag<false>{}, base + kRound + set * STAGE, sQ1, sG1, sR1, sI1, sQ0, sG0, sR0, sI0);
             }
     }
     const int thread = key_wave * kWave + lane;
@@ -552,7 +561,7 @@ gt_status packed_bwd_d(const gt_packed_plan* p, PackedArgs a, float* dtable, hip
     };
     if (list(kPairs)) {
         constexpr int W = pair_waves(kRow);
-        const int64_t blocks = BIAS ? pair_blocks(p, kRow) : cdiv(int64_t(a.n_items) * a.Hkv, W * a.Hkv) * a.Hkv;
+        const int64_t blocks = BIAS ? pair_blocks(p, kRow) : cdiv(int64_t(a.n_items) * a.Hkv, W * kXcds * a.Hkv) * kXcds * a.Hkv;
         part(blocks * W, 0);
         k_pair_bwd<T, D, BIAS><<<unsigned(blocks), W * kWave, W * (tab + col), s>>>(a);
         GT_LAUNCH_CHECK("packed_bwd pairs");

@@ -65,7 +65,6 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
         l = pair_sum(l);
         typename B::Cols vt;
         vt.load(sV[wave], at);
-        vt.drop(it.lk, lane);
         B::template apply<1>(vt, s, acc);
     }
     if (r < R) {
@@ -143,14 +142,10 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
     stage_done<(W > 1) || BIAS>();
     const typename B::At lds(lane, set * B::kElems * int(sizeof(T)));
     // one block of 32 keys; masked: some row does not attend to all of them
-    auto block32 = [&](auto masked, int key0, const T* bK, const T* bV) {
-        uint4 ids[NB];
+    auto block32 = [&](auto masked, int key0, const T* bK, const T* bV, const uint4(&ids)[NB]) {
         int left[NB];  // how many of the lane's 16 keys its row attends to
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            if constexpr (BIAS) ids[b] = load_ids(id_row[b], key0, it.lk, lane);
-            left[b] = lim[b] - key0 - part(0, lane);
-        }
+        for (int b = 0; b < NB; ++b) left[b] = lim[b] - key0 - part(0, lane);
         f32x16_t s[NB];
         auto scores = [&] {
 #pragma unroll
@@ -181,7 +176,6 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
         scores();
         typename B::Cols vt;
         vt.load(bV, lds);
-        if constexpr (masked.value) vt.drop(it.s1 - key0, lane);
         __builtin_amdgcn_sched_barrier(0);
         weights();
         bool high = false;
@@ -212,18 +206,34 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
         for (int b = 0; b < NB; ++b) l[b] += ls[b];
         B::template apply<NB>(vt, s, acc);
     };
+    uint4 ids[STAGE / 32][NB];  // the buckets of a stage, loaded a stage ahead
+    auto next_ids = [&](int kbase) {
+        if constexpr (BIAS)
+#pragma unroll
+            for (int kb = 0; kb < STAGE / 32; ++kb)
+#pragma unroll
+                for (int b = 0; b < NB; ++b) ids[kb][b] = load_ids(id_row[b], kbase + 32 * kb, it.lk, lane);
+    };
+    next_ids(it.s0 + set * STAGE);
     auto stage = [&](auto masked, int kbase, const T* cK, const T* cV, T* nK, T* nV) {
         fetch(kbase + KS * STAGE, nK, nV);
+        uint4 now[STAGE / 32][NB];
+        if constexpr (BIAS)
+#pragma unroll
+            for (int kb = 0; kb < STAGE / 32; ++kb)
+#pragma unroll
+                for (int b = 0; b < NB; ++b) now[kb][b] = ids[kb][b];
+        next_ids(kbase + KS * STAGE);
         if constexpr (masked.value) {
-#pragma unroll 1
+#pragma unroll
             for (int kb = 0; kb < STAGE / 32; ++kb)
                 if (kbase + 32 * kb < hi)  // uniform
-                    block32(masked, kbase + 32 * kb, cK + 32 * kb * D, cV + 32 * kb * D);
+                    block32(masked, kbase + 32 * kb, cK + 32 * kb * D, cV + 32 * kb * D, now[kb]);
         } else {
 #pragma unroll
             for (int kb = 0; kb < STAGE / 32; ++kb) {
                 __builtin_amdgcn_sched_barrier(0);  // two blocks' operands at once do not fit the registers
-                block32(masked, kbase + 32 * kb, cK + 32 * kb * D, cV + 32 * kb * D);
+                block32(masked, kbase + 32 * kb, cK + 32 * kb * D, cV + 32 * kb * D, now[kb]);
             }
         }
         stage_done<(W > 1)>();
@@ -331,7 +341,7 @@ gt_status packed_fwd_d(const gt_packed_plan* p, PackedArgs a, hipStream_t s) {
     } else {
         GT_FWD(kRows128, kStage, 1, 4, 1)
     }
-    if constexpr (kRow <= 128) {
+    if constexpr (kRow <= 128 && !BIAS) {  // two blocks of rows and their buckets do not fit the registers
         GT_FWD(kRows256, kStage, 2, 4, 1)
     } else {
         GT_FWD(kRows256, kStage, 1, 8, 1)

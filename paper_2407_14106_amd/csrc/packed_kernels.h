@@ -61,7 +61,12 @@ __device__ __forceinline__ void wave_done() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_wave_barrier();
 }
-// The same for a workgroup (or, where no wavefront shares a stage, for each).
+// The wavefront's accesses to LDS are done (its stores to memory need not be).
+__device__ __forceinline__ void lds_done() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
+// The first for a workgroup (or, where no wavefront shares a stage, for each).
 template <bool SHARED>
 __device__ __forceinline__ void stage_done() {
     wave_done();
@@ -153,7 +158,9 @@ struct Blk {
 
     // This wavefront's share of a stage: the `left` (at least 1) partner rows from
     // `base` on, up to a stage; off(r) is row r's offset in elements, below 2^30.
-    // Rows behind the last one repeat it where their block of 32 is begun.
+    // Rows behind the last one repeat it where their block of 32 is begun, so a
+    // block never holds values that are not the sequence's own: weights of zero
+    // need nothing else.
     template <int WAVES, typename F>
     __device__ __forceinline__ static void fetch(T* s, const T* base, int left, int wave, int lane, F off) {
         constexpr int kRowsPerLoad = 64 / kPieces;
@@ -226,19 +233,6 @@ struct Blk {
                                                                    256 * (db >> 1) + at.col[x]);
                     }
             }
-        }
-        // Zero the partners from the `left`-th on: rows behind the end hold
-        // whatever lies there, and a zero weight times an infinity would be NaN.
-        __device__ __forceinline__ void drop(int left, int lane) {
-            const int mine = left - part(0, lane);
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (i >= mine)
-#pragma unroll
-                    for (int db = 0; db < D / 32; ++db) {
-                        if constexpr (kHalf) v[db][i / 8][i % 8] = (__bf16)0.f;
-                        else v[db][i] = 0.f;
-                    }
         }
     };
     // Weights (partners x owned rows) as the B operand of a product with Cols:

@@ -32,13 +32,13 @@ struct Cuts {
     Cut rows, keys;
 };
 
-// A CU works on eight wavefronts at a time, two workgroups of four or one of two
-// such sets, so the chip is in balance when no walk is longer than a workgroup's
-// share of all of them.
+// A CU works on eight wavefronts at a time (two workgroups of four): walks that are
+// longer than a CU's share of all of them are cut to half of it.
 constexpr int64_t kCus = 256;
 // Walks are not split into shorter parts than this: parts cost a second launch
 // and a merge.
 constexpr int64_t kMinChunk = 1024;
+constexpr int64_t kLongWalk = 2048;
 
 int64_t row_walk(const Seqs& s, int64_t lk, int64_t off, int64_t last) {  // keys that rows up to `last` attend to
     return s.causal ? std::max<int64_t>(0, std::min(lk, off + (last >> s.gs) + 1)) : lk;
@@ -61,12 +61,14 @@ struct Load {
 Cut cut_side(const Load& few, const Load& t128, const Load& t256, int64_t Hkv) {
     Cut c;
     auto share = [&](const Load& l, int64_t blocks) { return (l.total * Hkv + blocks - 1) / blocks; };
-    // Large tiles read the partners less often, but take all of a CU: where no walk is more than half its share.
-    c.large = t256.n * Hkv >= 2 * kCus && t256.most <= share(t256, 2 * kCus);
+    // Large tiles read the partners less often, but take all of a CU and its other work cannot hide their start: for
+    // long walks, where none is more than half its share (8,192 x 16 x 64: 913 against 990 us backward; 128 sequences
+    // of 512: 427 against 415 for half the work).
+    c.large = t256.n * Hkv >= 2 * kCus && t256.most <= share(t256, 2 * kCus) && t256.total >= kLongWalk * t256.n;
     // Two sets on one walk where there are fewer workgroups than the chip holds.
     c.shared = t128.n * Hkv < 2 * kCus;
     auto chunk = [&](int64_t x) { return std::max(kMinChunk, (x + 255) & ~int64_t(255)); };
-    c.chunk = chunk(share(t128, c.shared ? kCus : 2 * kCus));
+    c.chunk = t128.most <= share(t128, kCus) ? std::max<int64_t>(t128.most, 1) : chunk(share(t128, 2 * kCus));
     c.few_chunk = chunk(share(few, 2 * kCus));
     return c;
 }
