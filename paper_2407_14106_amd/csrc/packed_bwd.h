@@ -10,12 +10,12 @@ namespace {
 
 // Pairs: a sequence of at most 32 rows and 32 keys, all of its backward by one
 // wavefront from one reading of Q, K, V and dO: the weights P and dS of the one
-// block, D from them, dQ; then the block turned round through LDS, dK and dV.
+// block, D from them, dQ; then the two turned round through LDS, dV and dK.
 // With a bias a wavefront keeps to one head and goes through its sequences, its
 // part of the table's gradient in LDS.
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave)
-    __attribute__((amdgpu_waves_per_eu(D * int(sizeof(T)) <= 64 ? 3 : 1))) void k_pair_bwd(PackedArgs a) {
+    __attribute__((amdgpu_waves_per_eu(D * int(sizeof(T)) <= 64 ? 3 : D * int(sizeof(T)) <= 128 ? 2 : 1))) void k_pair_bwd(PackedArgs a) {
     using B = Blk<T, D>;
     using S = Blk<T, 32>;
     constexpr int W = pair_waves(D * int(sizeof(T)));
@@ -64,13 +64,11 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave)
         for (int db = 0; db < D / 32; ++db) dq[0][db] = dk[0][db] = dv[0][db] = splat16(0.f);
         if (some) {
             f32x16_t s[1] = {splat16(0.f)}, dp[1] = {splat16(0.f)};
-            {
-                typename B::Row own[1];
-                own[0].staged(sQ, lane);
-                B::template rows<1>(sK, at, own, s);
-                own[0].staged(sG, lane);
-                B::template rows<1>(sV, at, own, dp);
-            }
+            typename B::Row own[1];
+            own[0].staged(sQ, lane);
+            B::template rows<1>(sK, at, own, s);
+            own[0].staged(sG, lane);
+            B::template rows<1>(sV, at, own, dp);
             const int lim = r >= R ? 0 : a.causal && off + q + 1 < it.lk ? off + q + 1 : it.lk;
             float sum = 0.f, dsum = 0.f;
 #pragma unroll
@@ -94,23 +92,22 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave)
             typename B::Cols x;
             x.load(sK, at);
             B::template apply<1>(x, dp, dq);
-            wave_done();  // K and V are read: their place takes P and dS
+            typename B::Weights w[1];
+            lds_done();  // K and V are read: their places take P and dS
             lay_block<T>(sK, s[0], lane);
             lay_block<T>(sV, dp[0], lane);
-            wave_done();
-            typename B::Weights w[1];
-            typename S::Cols t;
-            auto turned = [&](const T* from) {
-                t.load(from, turned_at);
+            lds_done();
+            // acc += (staged rows) x (block turned round)
+            auto turned = [&](const T* block, const T* rows, f32x16_t(&acc)[1][D / 32]) {
+                typename S::Cols t;
+                t.load(block, turned_at);
 #pragma unroll
                 for (int i = 0; i < (B::kHalf ? 2 : 16); ++i) w[0].v[i] = t.v[0][i];
+                x.load(rows, at);
+                B::template apply<1>(x, w, acc);
             };
-            turned(sK);
-            x.load(sG, at);
-            B::template apply<1>(x, w, dv);
-            turned(sV);
-            x.load(sQ, at);
-            B::template apply<1>(x, w, dk);
+            turned(sK, sG, dv);
+            turned(sV, sQ, dk);
         }
         if (r < R) B::store(static_cast<T*>(a.out0) + (row_at + q * a.H + (r & gm)) * D, dq[0], a.scale, lane);
         if (r < it.lk) {

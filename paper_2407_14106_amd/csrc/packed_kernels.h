@@ -270,18 +270,33 @@ struct Blk {
         for (int b = 0; b < NB; ++b) p[b].set(w[b]);
         apply<NB>(a, p, acc);
     }
-    // One owned row of acc times f, as T.
+    // One owned row of acc times f, as T.  A lane holds every other 4 features of its
+    // row; bf16 lanes exchange with the other half-wave first, so that each writes 16
+    // bytes (8-byte writes are twice the requests).
     __device__ __forceinline__ static void store(T* o, const f32x16_t (&a)[D / 32], float f, int lane) {
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db)
+        for (int db = 0; db < D / 32; ++db) {
+            if constexpr (kHalf) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                T* to = o + 32 * db + 8 * j + 4 * (lane >> 5);
-                const float x = a[db][4 * j] * f, y = a[db][4 * j + 1] * f, z = a[db][4 * j + 2] * f,
-                            w = a[db][4 * j + 3] * f;
-                if constexpr (kHalf) *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(x, y), pack_bf16x2(z, w));
-                else *reinterpret_cast<float4*>(to) = make_float4(x, y, z, w);
+                for (int j = 0; j < 4; j += 2) {
+                    uint32_t x[2][2];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const uint32_t u = pack_bf16x2(a[db][4 * j + 2 * k] * f, a[db][4 * j + 2 * k + 1] * f);
+                        const uint32_t v = pack_bf16x2(a[db][4 * j + 4 + 2 * k] * f, a[db][4 * j + 5 + 2 * k] * f);
+                        const auto r = __builtin_amdgcn_permlane32_swap(u, v, false, false);
+                        x[0][k] = r[0], x[1][k] = r[1];
+                    }
+                    *reinterpret_cast<uint4*>(o + 32 * db + 8 * (j + (lane >> 5))) =
+                        make_uint4(x[0][0], x[0][1], x[1][0], x[1][1]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<float4*>(o + 32 * db + 8 * j + 4 * (lane >> 5)) =
+                        make_float4(a[db][4 * j] * f, a[db][4 * j + 1] * f, a[db][4 * j + 2] * f, a[db][4 * j + 3] * f);
             }
+        }
     }
 };
 
