@@ -8,6 +8,12 @@
 namespace gt {
 namespace {
 
+// A block's dS to the lane's column of the table's gradient.
+__device__ __forceinline__ void add_block(float* col, const uint4& ids, int B, const f32x16_t& ds) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) hist_add(col, id_of(ids, i, B), ds[i]);
+}
+
 // Pairs: a sequence of at most 32 rows and 32 keys, all of its backward by one
 // wavefront from one reading of Q, K, V and dO: the weights P and dS of the one
 // block, D from them, dQ; then the two turned round through LDS, dV and dK.
@@ -87,8 +93,8 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave)
             for (int i = 0; i < 16; ++i) {
                 s[0][i] *= inv;
                 dp[0][i] = s[0][i] * (dp[0][i] - Dr);
-                if constexpr (BIAS) hist_add(hist + lane, id_of(ids, i, a.B), dp[0][i]);
             }
+            if constexpr (BIAS) add_block(hist + lane, ids, a.B, dp[0]);
             typename B::Cols x;
             x.load(sK, at);
             B::template apply<1>(x, dp, dq);
@@ -230,11 +236,9 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            uint32_t id = 0;
             float t;
             if constexpr (BIAS) {
-                id = id_of(ids, i, a.B);
-                t = fmaf(fmaf(s[0][i], a.scale, s_tab[hg * kTableStride + id]) - L, kLog2e, -lg);
+                t = fmaf(fmaf(s[0][i], a.scale, s_tab[hg * kTableStride + id_of(ids, i, a.B)]) - L, kLog2e, -lg);
             } else {
                 t = fmaf(s[0][i], sl2, -L);
             }
@@ -244,11 +248,12 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
             if constexpr (PASS == kStat) {
                 sum += p;
                 dsum += s[0][i];
-            } else if constexpr (BIAS) {
-                hist_add(hist, id, s[0][i]);
             }
         }
-        if constexpr (PASS == kGrad) B::template apply<1>(kt, s, acc);
+        if constexpr (PASS == kGrad) {
+            if constexpr (BIAS) add_block(hist, ids, a.B, s[0]);
+            B::template apply<1>(kt, s, acc);
+        }
     };
     uint4 ids[STAGE / 32];  // the buckets of a stage, loaded a stage ahead
     auto next_ids = [&](int kbase) {
@@ -256,7 +261,7 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
 #pragma unroll
             for (int kb = 0; kb < STAGE / 32; ++kb) ids[kb] = load_ids(id_row, kbase + 32 * kb, it.lk, lane);
     };
-    next_ids(it.s0 + set * STAGE);
+    if (it.s0 < it.s1) next_ids(it.s0 + set * STAGE);
     auto stage = [&](auto masked, int kbase, const T* cK, const T* cV, T* nK, T* nV) {
         fetch(kbase + KS * STAGE, nK, nV);
         uint4 now[STAGE / 32];

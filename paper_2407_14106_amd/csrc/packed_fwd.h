@@ -35,7 +35,7 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
     uint4 ids;
     float* tab = s_tabs + wave * (kTableStride << gs);
     if constexpr (BIAS) {
-        ids = load_ids(a.ids + it.pair + q * ids_width(it.lk), 0, it.lk, lane);
+        if (it.lk > 0) ids = load_ids(a.ids + it.pair + q * ids_width(it.lk), 0, it.lk, lane);
         load_table<kWave>(tab, a, hk, lane);
     }
     f32x16_t s[1] = {splat16(0.f)}, acc[1][D / 32];
@@ -214,7 +214,7 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
 #pragma unroll
                 for (int b = 0; b < NB; ++b) ids[kb][b] = load_ids(id_row[b], kbase + 32 * kb, it.lk, lane);
     };
-    next_ids(it.s0 + set * STAGE);
+    if (it.s0 < it.s1) next_ids(it.s0 + set * STAGE);
     auto stage = [&](auto masked, int kbase, const T* cK, const T* cV, T* nK, T* nV) {
         fetch(kbase + KS * STAGE, nK, nV);
         uint4 now[STAGE / 32][NB];

@@ -350,11 +350,11 @@ __device__ __forceinline__ void load_table(float* s, const PackedArgs& a, int hk
 }
 
 // The buckets of a lane's row and 16 partners of a block: 16 bytes, at a multiple
-// of 16 (rows of buckets are padded to that); a block behind the row's end has
-// none to read.
+// of 16 (rows of buckets are padded to that).  Behind the row's end, where every
+// pair is masked, the row's first ones are read again (lk is at least 1).
 __device__ __forceinline__ uint4 load_ids(const uint8_t* row, int key0, int lk, int lane) {
     const int k = key0 + 16 * (lane >> 5);
-    return k < lk ? *reinterpret_cast<const uint4*>(row + k) : make_uint4(~0u, ~0u, ~0u, ~0u);
+    return *reinterpret_cast<const uint4*>(row + (k < lk ? k : 0));
 }
 // Bucket i of the 16, B for any that the table does not hold.
 __device__ __forceinline__ uint32_t id_of(const uint4& ids, int i, uint32_t B) {
@@ -364,10 +364,6 @@ __device__ __forceinline__ uint32_t id_of(const uint4& ids, int i, uint32_t B) {
 }
 __device__ __forceinline__ int64_t ids_width(int lk) { return (int64_t(lk) + 15) & ~int64_t(15); }
 
-// Adds to a lane's own column of a [bucket][lane] sum in LDS: no two lanes meet,
-// so the order of additions is the program's, and a load and a store do (12 cycles
-// a wavefront's addition; ds_add_f32 takes 193, it goes lane by lane).
-__device__ __forceinline__ void hist_add(float* col, uint32_t id, float v) { col[id * kWave] += v; }
 // out[head of the group][bucket] = the sums over the lanes (whose row's head is
 // lane % g) of `waves` such columns, each B + 1 buckets.
 template <int THREADS>
