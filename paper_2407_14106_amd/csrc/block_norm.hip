@@ -17,6 +17,7 @@ using namespace gt;
 namespace {
 
 constexpr int kMaxD = 8192;
+constexpr int64_t kFarBytes = int64_t(256) << 20;  // the last-level cache
 constexpr int kSums = 5;  // dw_post, db_post, dw_pre, db_pre, dgate (vector)
 
 struct NormArgs {
@@ -29,6 +30,7 @@ struct NormArgs {
     float* stats;
     float* part;  // [blocks][kSums][D]
     uint32_t want;  // bit k: sum k is wanted
+    bool far;       // the results go past the last-level cache
 };
 
 template <int LPR>
@@ -92,7 +94,7 @@ struct Cols {
             }
         }
     }
-    __device__ __forceinline__ void store(void* p, int64_t row, const float (&o)[NV][E]) const {
+    __device__ __forceinline__ void store(void* p, int64_t row, const float (&o)[NV][E], bool far) const {
         T* r = static_cast<T*>(p) + row * D;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
@@ -105,7 +107,9 @@ struct Cols {
                 else
                     x = make_uint4(__float_as_uint(o[v][0]), __float_as_uint(o[v][1]), __float_as_uint(o[v][2]),
                                    __float_as_uint(o[v][3]));
-                *reinterpret_cast<uint4*>(r + col(v)) = x;
+                typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+                if (far) __builtin_nontemporal_store(u32x4_t{x.x, x.y, x.z, x.w}, reinterpret_cast<u32x4_t*>(r + col(v)));
+                else *reinterpret_cast<uint4*>(r + col(v)) = x;
             } else {
 #pragma unroll
                 for (int t = 0; t < E; ++t)
@@ -189,12 +193,12 @@ __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_fwd(NormArgs a) 
             }
         row_stats<LPR>(x, c, layer, a.eps, inv_d, s_sum, my, ry);
         if (own) {
-            c.store(a.y, row, x);
+            c.store(a.y, row, x, a.far);
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
                 for (int t = 0; t < E; ++t) x[v][t] = fmaf((x[v][t] - my) * ry, w2[v][t], b2[v][t]);
-            c.store(a.z, row, x);
+            c.store(a.z, row, x, a.far);
             if (c.lane == 0) *reinterpret_cast<float4*>(a.stats + 4 * row) = make_float4(mf, rf, my, ry);
         }
     }
@@ -282,9 +286,9 @@ __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_bwd(NormArgs a) 
 #pragma unroll
             for (int t = 0; t < E; ++t) f[v][t] = st.y * (dz[v][t] - n1 - f[v][t] * n2);
         if (own) {
-            c.store(a.dx, row, x);
-            c.store(a.df, row, f);
-            if (a.gate_kind >= GT_GATE_ROWS) c.store(a.dgate, row, dy);
+            c.store(a.dx, row, x, a.far);
+            c.store(a.df, row, f, a.far);
+            if (a.gate_kind >= GT_GATE_ROWS) c.store(a.dgate, row, dy, a.far);
         }
     }
     // the columns' sums over the workgroup's rows
@@ -410,6 +414,7 @@ extern "C" gt_status gt_block_norm_fwd(int64_t n, int32_t D, gt_dtype dt, int32_
     if (!x || !f || !y || !z || !stats) return fail(GT_ERR_INVALID_ARG, std::string(who) + ": null pointer");
     if (off16(stats)) return fail(GT_ERR_UNSUPPORTED, std::string(who) + ": stats must start at a multiple of 16 bytes");
     NormArgs a = {};
+    a.far = n * D * (dt == GT_BF16 ? 2 : 4) > kFarBytes;
     a.n = n, a.D = D, a.norm = norm, a.gate_kind = gate_kind, a.eps = eps, a.res_scale = res_scale;
     a.x = x, a.f = f, a.gate = gate;
     a.w_post = w_post, a.b_post = b_post, a.w_pre = w_pre, a.b_pre = b_pre;
@@ -449,6 +454,7 @@ extern "C" gt_status gt_block_norm_bwd(int64_t n, int32_t D, gt_dtype dt, int32_
     Ws w(ws);
     const int E = dt == GT_BF16 ? 8 : 4, pieces = int(cdiv(D, E)), blocks = norm_blocks(n, D, dt);
     NormArgs a = {};
+    a.far = n * D * (dt == GT_BF16 ? 2 : 4) > kFarBytes;
     a.n = n, a.D = D, a.norm = norm, a.gate_kind = gate_kind, a.res_scale = res_scale;
     a.x = x, a.f = f, a.gate = gate, a.dy = dy, a.dz = dz;
     a.w_post = w_post, a.b_post = b_post, a.w_pre = w_pre;
