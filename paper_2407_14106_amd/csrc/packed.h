@@ -121,9 +121,7 @@ gt_status packed_merge_rows(const gt_packed_plan* p, int d, gt_dtype dt, PackedA
 gt_status packed_merge_keys(const gt_packed_plan* p, int d, gt_dtype dt, PackedArgs a, hipStream_t s);
 // dtable[b, h] = the sum of the blocks' partial tables.
 struct TableParts {
-    // per launch: partial tables [n][g][B] from `at` on; heads: 0: block i belongs to kv head i % Hkv,
-    // n_items: to i / n_items
-    int64_t at[6], n[6], items[6];
+    int64_t at[6], n[6];  // per launch: n partial tables [g][B] from `at` on, the i-th of kv head i % Hkv
     int count;
 };
 gt_status packed_table_sum(const TableParts& t, PackedArgs a, float* dtable, hipStream_t s);

@@ -554,23 +554,22 @@ gt_status packed_bwd_d(const gt_packed_plan* p, PackedArgs a, float* dtable, hip
         return a.n_items > 0;
     };
     // where a launch of n blocks (or wavefronts) leaves its partial tables
-    auto part = [&](int64_t n, int64_t items) {
+    auto part = [&](int64_t n) {
         const int k = parts.count++;
         parts.at[k] = k == 0 ? 0 : parts.at[k - 1] + parts.n[k - 1] * per;
         parts.n[k] = n;
-        parts.items[k] = items;
         a.hist = BIAS ? hist + parts.at[k] : nullptr;
     };
     if (list(kPairs)) {
         constexpr int W = pair_waves(kRow);
         const int64_t blocks = BIAS ? pair_blocks(p, kRow) : cdiv(int64_t(a.n_items) * a.Hkv, W * kXcds * a.Hkv) * kXcds * a.Hkv;
-        part(blocks * W, 0);
+        part(blocks * W);
         k_pair_bwd<T, D, BIAS><<<unsigned(blocks), W * kWave, W * (tab + col), s>>>(a);
         GT_LAUNCH_CHECK("packed_bwd pairs");
     }
 #define GT_ROWS(LIST, STAGE, W, KS, SUB, PASS)                                                                  \
     if (list(LIST)) {                                                                                           \
-        if (PASS == kGrad) part(int64_t(a.n_items) * SUB * a.Hkv, W == 1 ? 0 : int64_t(a.n_items) * SUB);       \
+        if (PASS == kGrad) part(int64_t(a.n_items) * SUB * a.Hkv);                                              \
         k_packed_rows<T, D, STAGE, W, KS, SUB, BIAS, PASS><<<packed_grid(a.n_items, a.Hkv, SUB),                \
                             W * KS * kWave, tab + (PASS == kGrad ? W * KS * col : 0), s>>>(a);                  \
         GT_LAUNCH_CHECK("packed_bwd rows");                                                                     \

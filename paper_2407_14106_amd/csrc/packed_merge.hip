@@ -115,11 +115,7 @@ __global__ __launch_bounds__(kThreads) void k_table_sum(TableParts t, int H, int
     const int64_t per = int64_t(B) << gs;
     float x = 0.f;
     for (int k = 0; k < t.count; ++k) {
-        const int64_t mine = t.items[k] ? t.items[k] : t.n[k] / Hkv;  // blocks of this kv head
-        for (int64_t i = threadIdx.x; i < mine; i += kThreads) {
-            const int64_t blk = t.items[k] ? hk * t.items[k] + i : i * Hkv + hk;
-            x += hist[t.at[k] + blk * per + hg * B + b];
-        }
+        for (int64_t i = threadIdx.x; i < t.n[k] / Hkv; i += kThreads) x += hist[t.at[k] + (i * Hkv + hk) * per + hg * B + b];
     }
     __shared__ float s[kThreads / kWave];
     x = wave_sum(x);

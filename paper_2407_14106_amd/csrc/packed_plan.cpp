@@ -213,7 +213,7 @@ extern "C" gt_status gt_packed_plan_init(int64_t n_seq, const int64_t* q_ptr, co
         return fail(GT_ERR_UNSUPPORTED, std::string(who) + ": more than 2^26 partial results");
     int64_t at = 0;
     for (int l = 0; l < kPackedLists; ++l) {
-        if (count[l] * Hkv > (int64_t(1) << 31) - 64)  // one block for each item and kv head
+        if (count[l] * Hkv > (int64_t(1) << 30))  // a workgroup or two for each item and kv head
             return fail(GT_ERR_UNSUPPORTED, std::string(who) + ": more than 2^31 tiles");
         plan->layout[2 * l] = at;
         plan->layout[2 * l + 1] = count[l];

@@ -105,6 +105,7 @@ def test_sizes_where_tiles_end(gt, dtype, d, causal, B):
 def test_grouped_heads(gt, dtype, H, Hkv, causal, B):
     compare(gt, [1, 2, 17, 40, 3], [70, 2, 17, 45, 1], H, Hkv, 32, dtype, causal, B, seed=H)
     compare(gt, [130], [150], H, Hkv, 64, dtype, causal, B, seed=H + 1)
+    compare(gt, [2, 70, 30], [30, 33, 1100], H, Hkv, 128, dtype, causal, B, seed=H + 2)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -132,6 +133,59 @@ def test_long_walks_of_few_tiles_are_split(gt, dtype, B):
     compare(gt, [4500, 3], [100, 200], 1, 1, 64, dtype, False, B)
     compare(gt, [60, 5], [3000, 2], 2, 1, 128, dtype, True, B)
     compare(gt, [2500, 40], [30, 2300], 2, 2, 32, dtype, True, B)
+
+
+@pytest.mark.parametrize("dtype,d,H,causal,B", [("bf16", 32, 32, False, 0), ("bf16", 64, 32, False, 0),
+                                                ("bf16", 128, 32, False, 0), ("f32", 32, 32, False, 0),
+                                                ("f32", 128, 32, False, 0), ("bf16", 64, 32, False, 5),
+                                                ("bf16", 128, 32, False, 64), ("f32", 64, 32, False, 64),
+                                                ("bf16", 64, 32, True, 0), ("bf16", 64, 32, True, 21)])
+def test_long_sequences_of_many_heads(gt, dtype, d, H, causal, B):
+    """Enough long walks for the largest tiles; two heads against a plain implementation in 64 bits on the GPU."""
+    lens = [2333, 2304]
+    say("large", dtype, d, H, causal, B)
+    p, scale = ptrs(lens), 1.0 / np.sqrt(d)
+    q, k, v, do, table, ids = make(lens, lens, H, H, d, dtype, B, seed=d + B)
+    plan = gt.packed_plan(p, heads=H, causal=causal)
+    assert causal or plan.c.layout[2 * 4 + 1] > 0 and plan.c.layout[2 * 8 + 1] > 0  # tiles of 256 rows and keys
+    out = run(gt, lens, lens, H, H, d, dtype, causal, (q, k, v, do, table, ids), scale)
+    half, u, scale = HALF[dtype], 2.0 ** -24, float(np.float32(scale))
+    dt = torch.zeros(B, dtype=torch.float64, device="cuda"), torch.zeros(B, dtype=torch.float64, device="cuda")
+    for h in (0, H - 1):
+        for x in dt:
+            x.zero_()
+        for s, n in enumerate(lens):
+            sl = slice(int(p[s]), int(p[s + 1]))
+            Q, K, V, G = (torch.from_numpy(x[sl, h]).cuda().double() for x in (q, k, v, do))
+            sc = scale * (Q @ K.t())
+            if B:
+                id_ = torch.from_numpy(OP.pair_buckets(ids, lens, lens, s)).cuda()
+                T = torch.cat([torch.from_numpy(table[:, h]).cuda().double(),
+                               torch.full((256 - B,), -np.inf, dtype=torch.float64, device="cuda")])
+                sc = sc + T[id_]
+            if causal:
+                sc = sc.masked_fill(torch.ones_like(sc, dtype=torch.bool).triu(1), -np.inf)
+            P = torch.softmax(sc, -1)
+            dP = G @ V.t()
+            D = (P * dP).sum(-1, keepdim=True)
+            dS = P * (dP - D)
+            # scores, weights and dP in fp32 (d terms of at most 8 in all); sums of n terms; D from a bf16 O without a bias
+            w = 4 * (d + 8) * u * 8 + 2 * n * u
+            e_o = (half + w) * (P @ V.abs()) + half * (P @ V).abs()
+            e_d = (G.abs() * e_o).sum(-1, keepdim=True) if not B else w * (P * dP.abs()).sum(-1, keepdim=True)
+            e_ds = w * dS.abs() + P * (e_d + d * u * (G.abs() @ V.abs().t()))
+            refs = [("O", out[0], P @ V, e_o), ("LSE", out[1], torch.logsumexp(sc, -1), torch.full((n,), w).cuda()),
+                    ("dQ", out[2], scale * dS @ K, scale * (e_ds + (half + w) * dS.abs()) @ K.abs()),
+                    ("dK", out[3], scale * dS.t() @ Q, scale * (e_ds + (half + w) * dS.abs()).t() @ Q.abs()),
+                    ("dV", out[4], P.t() @ G, ((half + w) * P).t() @ G.abs())]
+            for name, x, r, e in refs:
+                err = (x[sl, h].double() - r).abs() - (e + 2 * half * r.abs())
+                assert float(err.max()) <= 0, f"{name} head {h} sequence {s}: outside its bound by {float(err.max()):.2e}"
+            if B:
+                dt[0].add_(torch.bincount(id_.flatten(), weights=dS.flatten(), minlength=256)[:B])
+                dt[1].add_(torch.bincount(id_.flatten(), weights=(e_ds + 4096 * u * dS.abs()).flatten(), minlength=256)[:B])
+        if B:
+            assert float(((out[5][:, h].double() - dt[0]).abs() - dt[1]).max()) <= 0
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
