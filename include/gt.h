@@ -438,8 +438,9 @@ gt_status gt_dense_attn_bwd_noalloc(int64_t n, int32_t H, int32_t d, gt_dtype dt
  * GT_F32 (products, sums and softmax in fp32) and GT_BF16 (as above: scores,
  * statistics and sums in fp32, the weights and score gradients rounded to bf16
  * where they multiply a bf16 row).
- * Q is [nq, H, d], K and V [nk, Hkv, d] with ldq, ldk, ldv elements between
- * consecutive nodes (slices of one wider array, such as a fused projection);
+ * Q is [nq, H, d], K and V [nk, Hkv, d] with ldq, ldk, ldv < 2^23 elements
+ * between consecutive nodes (slices of one wider array, such as a fused
+ * projection);
  * O, dO, dQ [nq, H, d], dK, dV [nk, Hkv, d], LSE [nq, H] fp32, all contiguous.
  * Feature arrays start at multiples of 16 bytes and their nodes lie at such
  * (GT_ERR_UNSUPPORTED otherwise).  Rows behind the last sequence are neither
@@ -452,7 +453,9 @@ gt_status gt_dense_attn_bwd_noalloc(int64_t n, int32_t H, int32_t d, gt_dtype dt
  * buffer of item_bytes, which the caller copies to the device (16-byte aligned)
  * and enters as plan->items.  q_ptr and k_ptr are host arrays int64[n_seq + 1],
  * starting at 0 (GT_ERR_OUT_OF_RANGE) and not decreasing (GT_ERR_UNSORTED);
- * q_ptr[n_seq] and k_ptr[n_seq] < 2^31.  Both calls take the same arguments. */
+ * q_ptr[n_seq] and k_ptr[n_seq] < 2^31.  Both calls take the same arguments.
+ * A batch of more tiles than a launch takes (from 2^23 sequences times kv heads
+ * on, 2^26 for sequences of at most 32 rows and keys) is GT_ERR_UNSUPPORTED. */
 typedef struct gt_packed_plan {
     int64_t n_seq;
     int64_t nq;          /* q_ptr[n_seq] */
@@ -493,7 +496,7 @@ gt_status gt_packed_attn_bwd(const gt_packed_plan* plan, int32_t d, gt_dtype dty
  * A pair whose bucket is n_buckets or more is not attended to.  Table entries
  * may be -inf (the same) or the type's lowest value (attended to with as little
  * weight as that gives).  The backward forms D_i from the scores (dtable is
- * fp32, and a bf16 O would be off by 2^-9), so O is not an input. */
+ * fp32, and a bf16 O would be off by 2^-8), so O is not an input. */
 #define GT_MAX_BUCKETS 64
 size_t gt_packed_attn_fwd_bias_workspace_size(const gt_packed_plan* plan, int32_t d, gt_dtype dtype,
                                               int32_t n_buckets);

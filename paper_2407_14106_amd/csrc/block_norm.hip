@@ -204,11 +204,46 @@ __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_fwd(NormArgs a) 
     }
 }
 
+// A lane's parameters: in registers or, one each of a kernel's four, in LDS.
+template <typename C, int LPR, int NV, bool LDS>
+struct Params {
+    static constexpr int E = C::E;
+    float v[LDS ? 1 : NV][LDS ? 1 : E];
+    float* s;
+    __device__ __forceinline__ Params(const C& c, const float* p, float none, float* lds) {
+        if constexpr (LDS) {
+            s = lds + 4 * int(threadIdx.x);
+            float x[NV][E];
+            c.param(x, p, none);
+#pragma unroll
+            for (int k = 0; k < NV * E / 4; ++k)
+                *reinterpret_cast<float4*>(s + 4 * LPR * k) = make_float4(x[4 * k / E][4 * k % E], x[4 * k / E][4 * k % E + 1],
+                                                                          x[4 * k / E][4 * k % E + 2], x[4 * k / E][4 * k % E + 3]);
+        } else {
+            c.param(v, p, none);
+        }
+    }
+    // the lane's own writes, in the order of the program
+    __device__ __forceinline__ float operator()(int k, int t) const {
+        if constexpr (LDS) return s[4 * LPR * ((k * E + t) / 4) + t % 4];
+        else return v[k][t];
+    }
+    __device__ __forceinline__ void get(float (&o)[NV][E]) const {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int t = 0; t < E; ++t) o[k][t] = (*this)(k, t);
+    }
+};
+
 // With fh = (f - mf) rf, yh = (y - my) ry and <v> a row's mean:
 //   t  = dy + ry (dz w2 - <dz w2> - yh <dz w2 yh>)      the gradient of y
 //   dx = res_scale t, dg = u t, du = g t
 //   df = rf (du w1 - <du w1> - fh <du w1 fh>)
 // (without the <dz w2> and <du w1> terms for the root mean square).
+// Rows of 512 lanes hold 16 columns a lane, whose parameters and sums do not fit the
+// registers together: the parameters lie in LDS (8,192 columns bf16: 805 us for
+// 32,768 rows against 1632 with spilled registers).
 template <typename T, int LPR, int NV, bool VEC, bool FULL>
 __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_bwd(NormArgs a) {
     using C = Cols<T, LPR, NV, VEC, FULL>;
@@ -220,11 +255,14 @@ __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_bwd(NormArgs a) 
     const C c = {a.D, int(threadIdx.x) % LPR};
     const bool layer = a.norm == GT_NORM_LAYER;
     const float inv_d = 1.f / float(a.D);
-    float w1[NV][E], b1[NV][E], w2[NV][E], g[NV][E], sum[kSums][NV][E];
-    c.param(w1, a.w_post, 1.f);
-    c.param(b1, a.b_post, 0.f);
-    c.param(w2, a.w_pre, 1.f);
-    c.param(g, a.gate_kind == GT_GATE_VECTOR ? static_cast<const float*>(a.gate) : nullptr, 1.f);
+    const float* vector = a.gate_kind == GT_GATE_VECTOR ? static_cast<const float*>(a.gate) : nullptr;
+    constexpr bool kLds = LPR == 512;
+    constexpr int kEach = LPR * NV * E;
+    __shared__ __attribute__((aligned(16))) float s_par[kLds ? 4 * kEach : 1];
+    const Params<C, LPR, NV, kLds> w1(c, a.w_post, 1.f, s_par), b1(c, a.b_post, 0.f, s_par + kEach),
+        w2(c, a.w_pre, 1.f, s_par + 2 * kEach), gv(c, vector, 1.f, s_par + 3 * kEach);
+    float g[NV][E], sum[kSums][NV][E];
+    gv.get(g);
 #pragma unroll
     for (int k = 0; k < kSums; ++k)
 #pragma unroll
@@ -239,6 +277,7 @@ __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_bwd(NormArgs a) 
         c.load(f, a.f, row);
         c.load(x, a.x, row);
         if (a.gate_kind >= GT_GATE_ROWS) c.load(g, a.gate, row);
+        else if constexpr (kLds) gv.get(g);
         c.load(dz, a.dz, row);
         c.load(dy, a.dy, row);
         float s1 = 0.f, s2 = 0.f;
@@ -248,9 +287,9 @@ __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_bwd(NormArgs a) 
             for (int t = 0; t < E; ++t) {
                 f[v][t] = c.in(v, t) ? (f[v][t] - st.x) * st.y : 0.f;  // fh
                 if (a.gate_kind == GT_GATE_SIGMOID) g[v][t] = sigmoid(g[v][t]);
-                const float u = fmaf(f[v][t], w1[v][t], b1[v][t]);
+                const float u = fmaf(f[v][t], w1(v, t), b1(v, t));
                 x[v][t] = c.in(v, t) ? (fmaf(g[v][t], u, a.res_scale * x[v][t]) - st.z) * st.w : 0.f;  // yh
-                const float d = dz[v][t] * w2[v][t];
+                const float d = dz[v][t] * w2(v, t);
                 s1 += d;
                 s2 = fmaf(d, x[v][t], s2);
                 if (own) {
@@ -265,8 +304,8 @@ __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_bwd(NormArgs a) 
         for (int v = 0; v < NV; ++v)
 #pragma unroll
             for (int t = 0; t < E; ++t) {
-                const float ty = fmaf(st.w, dz[v][t] * w2[v][t] - m1 - x[v][t] * m2, dy[v][t]);
-                const float u = fmaf(f[v][t], w1[v][t], b1[v][t]);
+                const float ty = fmaf(st.w, dz[v][t] * w2(v, t) - m1 - x[v][t] * m2, dy[v][t]);
+                const float u = fmaf(f[v][t], w1(v, t), b1(v, t));
                 const float du = g[v][t] * ty, dg = u * ty;
                 x[v][t] = a.res_scale * ty;
                 dy[v][t] = a.gate_kind == GT_GATE_SIGMOID ? dg * (g[v][t] * (1.f - g[v][t])) : dg;
@@ -275,7 +314,7 @@ __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_bwd(NormArgs a) 
                     sum[1][v][t] += du;
                     sum[4][v][t] += dg;
                 }
-                dz[v][t] = c.in(v, t) ? du * w1[v][t] : 0.f;
+                dz[v][t] = c.in(v, t) ? du * w1(v, t) : 0.f;
                 s1 += dz[v][t];
                 s2 = fmaf(dz[v][t], f[v][t], s2);
             }
@@ -340,7 +379,7 @@ __global__ __launch_bounds__(1024) void k_norm_sum(int blocks, int D, const floa
 
 // Lanes per row and pieces per lane: the fewest lanes that hold a row at one
 // piece each, and two a lane where a row would only just leave a wavefront (or
-// a workgroup).
+// a workgroup of 256 or 512).
 #define GT_NORM_SHAPE(pieces, CALL)                 \
     do {                                            \
         if ((pieces) <= 8) { CALL(8, 1); }          \
@@ -350,8 +389,10 @@ __global__ __launch_bounds__(1024) void k_norm_sum(int blocks, int D, const floa
         else if ((pieces) <= 128) { CALL(64, 2); }  \
         else if ((pieces) <= 256) { CALL(256, 1); } \
         else if ((pieces) <= 512) { CALL(256, 2); } \
-        else if ((pieces) <= 1024) { CALL(1024, 1); } \
-        else { CALL(1024, 2); }                     \
+        else if constexpr (sizeof(T) == 4) {        \
+            if ((pieces) <= 1024) { CALL(512, 2); } \
+            else { CALL(512, 4); }                  \
+        } else { CALL(512, 2); }                    \
     } while (0)
 
 int norm_rows(int pieces) { return pieces <= 8 ? 32 : pieces <= 16 ? 16 : pieces <= 32 ? 8 : pieces <= 128 ? 4 : 1; }
@@ -388,7 +429,7 @@ void run_bwd(const NormArgs& a, int pieces, int blocks, hipStream_t s) {
 }
 
 gt_status norm_check(const char* who, int64_t n, int32_t D, gt_dtype dt, int32_t norm, int32_t gate_kind,
-                     const void* gate, float res_scale) {
+                     const void* gate) {
     const std::string w(who);
     if (n < 0 || n >= (int64_t(1) << 31)) return fail(GT_ERR_INVALID_ARG, w + ": n out of range");
     if ((dt != GT_BF16 && dt != GT_F32) || D < 1 || D > kMaxD) return fail(GT_ERR_UNSUPPORTED, w + ": unsupported (dtype, D)");
@@ -396,7 +437,6 @@ gt_status norm_check(const char* who, int64_t n, int32_t D, gt_dtype dt, int32_t
     if (gate_kind < GT_GATE_NONE || gate_kind > GT_GATE_SIGMOID) return fail(GT_ERR_UNSUPPORTED, w + ": unknown gate");
     if ((gate_kind == GT_GATE_VECTOR || (gate_kind != GT_GATE_NONE && n > 0)) && !gate)
         return fail(GT_ERR_INVALID_ARG, w + ": null gate");
-    (void)res_scale;
     return GT_OK;
 }
 
@@ -407,7 +447,7 @@ extern "C" gt_status gt_block_norm_fwd(int64_t n, int32_t D, gt_dtype dt, int32_
                                        const float* w_post, const float* b_post, const float* w_pre,
                                        const float* b_pre, void* y, void* z, float* stats, hipStream_t s) {
     const char* who = "gt_block_norm_fwd";
-    const gt_status st = norm_check(who, n, D, dt, norm, gate_kind, gate, res_scale);
+    const gt_status st = norm_check(who, n, D, dt, norm, gate_kind, gate);
     if (st != GT_OK) return st;
     if (!(eps > 0.f)) return fail(GT_ERR_INVALID_ARG, std::string(who) + ": eps must be positive");
     if (n == 0) return GT_OK;
@@ -442,7 +482,7 @@ extern "C" gt_status gt_block_norm_bwd(int64_t n, int32_t D, gt_dtype dt, int32_
                                        void* dgate, float* dw_post, float* db_post, float* dw_pre, float* db_pre,
                                        void* ws, size_t ws_bytes, hipStream_t s) {
     const char* who = "gt_block_norm_bwd";
-    const gt_status st = norm_check(who, n, D, dt, norm, gate_kind, gate, res_scale);
+    const gt_status st = norm_check(who, n, D, dt, norm, gate_kind, gate);
     if (st != GT_OK) return st;
     if (n > 0 && (!x || !f || !stats || !dy || !dz || !dx || !df || (gate_kind != GT_GATE_NONE && !dgate)))
         return fail(GT_ERR_INVALID_ARG, std::string(who) + ": null pointer");

@@ -21,6 +21,7 @@ gt_status check(const char* who, const gt_packed_plan* p, int32_t d, gt_dtype dt
     const std::string w(who);
     if (!packed_plan_ok(p)) return fail(GT_ERR_INVALID_ARG, w + ": null plan, or one that gt_packed_plan_init did not make");
     if (p->item_bytes > 0 && !p->items) return fail(GT_ERR_INVALID_ARG, w + ": plan->items is null");
+    if (off16(p->items)) return fail(GT_ERR_UNSUPPORTED, w + ": plan->items must start at a multiple of 16 bytes");
     if ((dt != GT_BF16 && dt != GT_F32) || (d != 32 && d != 64 && d != 128))
         return fail(GT_ERR_UNSUPPORTED, w + ": unsupported (dtype, d)");
     if ((p->nq > 0 && !Q) || (p->nk > 0 && (!K || !V))) return fail(GT_ERR_INVALID_ARG, w + ": null pointer");

@@ -431,11 +431,12 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
         const int from = rmin - r0 - part(0, lane);  // of the lane's 16 rows the first that attends to its key
         f32x16_t s[1] = {splat16(0.f)}, dp[1];
         const int rs0 = 32 * rb + part(0, lane);  // the lane's rows in the stage's statistics
-        if constexpr (PASS != kOnlyV)
+        if constexpr (PASS != kOnlyV) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const float4 d4 = *reinterpret_cast<const float4*>(&bR[1][rs0 + 4 * x]);
-            dp[0][4 * x] = d4.x, dp[0][4 * x + 1] = d4.y, dp[0][4 * x + 2] = d4.z, dp[0][4 * x + 3] = d4.w;
+            for (int x = 0; x < 4; ++x) {
+                const float4 d4 = *reinterpret_cast<const float4*>(&bR[1][rs0 + 4 * x]);
+                dp[0][4 * x] = d4.x, dp[0][4 * x + 1] = d4.y, dp[0][4 * x + 2] = d4.z, dp[0][4 * x + 3] = d4.w;
+            }
         }
         B::template rows<1>(bQ, lds, kf, s);
         if constexpr (PASS != kOnlyV) B::template rows<1>(bG, lds, vf, dp);
@@ -461,9 +462,7 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
                 } else {
                     t = fmaf(s[0][i], sl2, -L[y]);
                 }
-                if constexpr (masked.value) {
-                    t = i < from ? -kInf : t;
-                }
+                if constexpr (masked.value) t = i < from ? -kInf : t;
                 s[0][i] = ex2(t);
                 if constexpr (PASS != kOnlyV) dp[0][i] *= s[0][i];
             }
@@ -476,7 +475,7 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
         if constexpr (PASS == kBoth) {
             __builtin_amdgcn_sched_barrier(0);
             x.load(bQ, lds);
-                B::template apply<1>(x, dp, dk);
+            B::template apply<1>(x, dp, dk);
         }
     };
     auto stage = [&](auto masked, int base, const T* cQ, const T* cG, const Stats& cR, const Buckets& cI, T* nQ, T* nG,

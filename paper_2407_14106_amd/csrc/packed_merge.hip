@@ -17,12 +17,11 @@ __device__ __forceinline__ T from_f32(float v) {
 }
 
 // Which item, kv head and row of the item this wavefront has.
-__device__ __forceinline__ bool merge_place(const PackedArgs& a, PackedItem& it, int& hk, int& r) {
+__device__ __forceinline__ void merge_place(const PackedArgs& a, PackedItem& it, int& hk, int& r) {
     const uint32_t per = kFewRows / kOut, b = blockIdx.x;
     hk = int(b / per % uint32_t(a.Hkv));
     it = a.items[b / per / uint32_t(a.Hkv)];
     r = int(b % per) * kOut + uniform(int(threadIdx.x) / kWave);
-    return true;
 }
 unsigned merge_grid(const PackedArgs& a) { return unsigned(int64_t(a.n_items) * a.Hkv * (kFewRows / kOut)); }
 

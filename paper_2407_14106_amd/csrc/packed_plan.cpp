@@ -40,6 +40,11 @@ constexpr int64_t kCus = 256;
 constexpr int64_t kMinChunk = 1024;
 constexpr int64_t kLongWalk = 2048;
 
+// A launch has fewer than 2^32 threads (with the grids' padding); the most that a kernel of a list takes for an item
+// and kv head.
+constexpr int64_t kMostThreads = (int64_t(1) << 32) - (int64_t(1) << 22);
+int64_t list_threads(int list) { return list == kPairs ? kWave : list >= kRowMerges ? 32 * kWave : 8 * kWave; }
+
 int64_t row_walk(const Seqs& s, int64_t lk, int64_t off, int64_t last) {  // keys that rows up to `last` attend to
     return s.causal ? std::max<int64_t>(0, std::min(lk, off + (last >> s.gs) + 1)) : lk;
 }
@@ -213,8 +218,8 @@ extern "C" gt_status gt_packed_plan_init(int64_t n_seq, const int64_t* q_ptr, co
         return fail(GT_ERR_UNSUPPORTED, std::string(who) + ": more than 2^26 partial results");
     int64_t at = 0;
     for (int l = 0; l < kPackedLists; ++l) {
-        if (count[l] * Hkv > (int64_t(1) << 30))  // a workgroup or two for each item and kv head
-            return fail(GT_ERR_UNSUPPORTED, std::string(who) + ": more than 2^31 tiles");
+        if (count[l] * Hkv > kMostThreads / list_threads(l))
+            return fail(GT_ERR_UNSUPPORTED, std::string(who) + ": more tiles than one launch takes");
         plan->layout[2 * l] = at;
         plan->layout[2 * l + 1] = count[l];
         at += count[l] * int64_t(sizeof(PackedItem));

@@ -883,6 +883,7 @@ def bucket_bias_bwd(bucket: torch.Tensor, dbias: torch.Tensor, n_buckets: int) -
     _need(dbias.is_cuda and dbias.dtype == torch.float32 and dbias.dim() == 2 and dbias.is_contiguous(),
           "dbias must be a contiguous fp32 GPU tensor [nnz, H]")
     nnz, H = dbias.shape
+    _need(n_buckets >= 0, "n_buckets must not be negative")
     _need(bucket.dtype == torch.uint8 and bucket.shape == (nnz,) and bucket.is_contiguous()
           and bucket.device == dbias.device, "bucket must be a contiguous uint8 tensor [nnz] on dbias's device")
     with _on(dbias.device):

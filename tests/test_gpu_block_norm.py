@@ -87,6 +87,25 @@ def test_many_rows(gt, dtype, D):
     assert all(a[k] is b[k] is None or torch.equal(a[k], b[k]) for k in a)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [512, 8192])
+def test_rows_larger_than_the_last_level_cache(gt, dtype, D):
+    # the rows' results are those of the same rows in two smaller calls
+    n = (260 << 20) // (D * (2 if dtype == torch.bfloat16 else 4))
+    g = torch.Generator(device="cuda").manual_seed(D)
+    x, f, dy, dz, gate = (torch.randn(n, D, device="cuda", generator=g).to(dtype) for _ in range(5))
+    w = torch.randn(D, device="cuda", generator=g)
+    kw = dict(w_post=w, b_post=w, w_pre=w, b_pre=w, sigmoid=True)
+    y, z, stats = gt.block_norm_fwd(x, f, gate=gate, **kw)
+    grads = gt.block_norm_bwd(x, f, stats, dy, dz, gate=gate, **kw)
+    h = n // 2
+    for part in (slice(0, h), slice(h, n)):
+        a = gt.block_norm_fwd(x[part], f[part], gate=gate[part], **kw)
+        b = gt.block_norm_bwd(x[part], f[part], a[2], dy[part], dz[part], gate=gate[part], **kw)
+        assert torch.equal(y[part], a[0]) and torch.equal(z[part], a[1]) and torch.equal(stats[part], a[2])
+        assert all(torch.equal(grads[k][part], b[k]) for k in range(3))
+
+
 def test_no_rows_and_views(gt):
     e = torch.zeros(0, 64, dtype=torch.bfloat16, device="cuda")
     w = torch.ones(64, device="cuda")

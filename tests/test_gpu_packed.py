@@ -382,6 +382,19 @@ def test_edge_bias_and_its_gradient(gt, H, nnz, B):
     assert torch.equal(dt, again)
 
 
+@pytest.mark.parametrize("H,nnz", [(16, 4_300_003), (1, 68_000_001)])
+def test_edge_bias_larger_than_the_last_level_cache(gt, H, nnz):
+    table = torch.randn(21, H, device="cuda")
+    ids = torch.randint(0, 21, (nnz,), dtype=torch.uint8, device="cuda")
+    bias = gt.bucket_bias_fwd(table, ids)
+    assert torch.equal(bias, table[ids.long()])
+    dt = gt.bucket_bias_bwd(ids, bias, 21)
+    # every value of a bucket is the table's: the sum is the count times it, chains of at most 4 nnz / 65,536 + 2^12
+    n = torch.bincount(ids.long(), minlength=21).double()[:, None]
+    ref = n * table.double()
+    assert ((dt - ref).abs() <= (4 * nnz / 65536 + 4096) * 2.0 ** -24 * ref.abs()).all()
+
+
 def test_edge_bias_on_views_that_start_anywhere(gt):
     rng = np.random.default_rng(1)
     ids = torch.from_numpy(rng.integers(0, 5, size=1003).astype(np.uint8)).cuda()[3:]

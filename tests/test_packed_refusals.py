@@ -67,6 +67,15 @@ def test_plan_null_and_changed_arguments(lib):
                                    BIG) == gt.GT_ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("lq,lk,n,H,want", [
+    (1, 40, 1 << 20, 8, gt.GT_ERR_UNSUPPORTED), (1, 40, (1 << 20) - 4096, 8, gt.GT_OK),
+    (1, 8, 1 << 18, 256, gt.GT_ERR_UNSUPPORTED), (1, 8, (1 << 18) - 4096, 256, gt.GT_OK)])
+def test_plan_refuses_more_tiles_than_a_launch_takes(lib, lq, lk, n, H, want):
+    at = np.arange(n + 1, dtype=np.int64)
+    st, _ = init(lib, at * lq, at * lk, H, H)
+    assert st == want
+
+
 @pytest.mark.parametrize("causal", [0, 1])
 @pytest.mark.parametrize("group", [1, 4])
 @pytest.mark.parametrize("many", [False, True])
@@ -150,6 +159,12 @@ def test_attention_refusals(lib, kw, want):
     assert lib.gt_packed_attn_bwd(*a, FAKE, FAKE, FAKE, 0.1, FAKE, FAKE, FAKE, FAKE, BIG, None) == want
     assert lib.gt_packed_attn_bwd_bias(*a, FAKE, 8, FAKE, FAKE, FAKE, 0.1, FAKE, FAKE, FAKE, FAKE, FAKE, BIG,
                                        None) == want
+
+
+def test_attention_refuses_a_work_list_off_its_alignment(lib):
+    st, c = init(lib, ptrs(5, 40), ptrs(6, 40))
+    c.items = 0x1008
+    assert lib.gt_packed_attn_fwd(*attn_args(c), 0.1, FAKE, FAKE, FAKE, BIG, None) == gt.GT_ERR_UNSUPPORTED
 
 
 def test_attention_refuses_missing_outputs_tables_and_workspaces(lib):
