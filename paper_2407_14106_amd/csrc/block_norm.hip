@@ -388,11 +388,12 @@ __global__ __launch_bounds__(1024) void k_norm_sum(int blocks, int D, const floa
         else if ((pieces) <= 64) { CALL(64, 1); }   \
         else if ((pieces) <= 128) { CALL(64, 2); }  \
         else if ((pieces) <= 256) { CALL(256, 1); } \
-        else if ((pieces) <= 512) { CALL(256, 2); } \
         else if constexpr (sizeof(T) == 4) {        \
-            if ((pieces) <= 1024) { CALL(512, 2); } \
+            if ((pieces) <= 512) { CALL(256, 2); }  \
+            else if ((pieces) <= 1024) { CALL(512, 2); } \
             else { CALL(512, 4); }                  \
-        } else { CALL(512, 2); }                    \
+        } else if ((pieces) <= 512) { CALL(512, 1); } \
+        else { CALL(512, 2); }                      \
     } while (0)
 
 int norm_rows(int pieces) { return pieces <= 8 ? 32 : pieces <= 16 ? 16 : pieces <= 32 ? 8 : pieces <= 128 ? 4 : 1; }
