@@ -40,7 +40,13 @@ enum PackedList {
     kPackedLists
 };
 constexpr int kRowSlotsAt = 28, kKeySlotsAt = 29;      // layout: numbers of slots
-constexpr int kRowSharedAt = 26, kKeySharedAt = 27;    // layout: two sets of wavefronts share the walks of tiles of 128
+constexpr int kRowSharedAt = 26, kKeySharedAt = 27;    // layout: whether two sets share a walk
+
+// Whether two sets of wavefronts share the walks of tiles of 128.
+template <typename T>
+bool packed_shared(const gt_packed_plan* p, int at) {
+    return p->layout[at] >= (sizeof(T) == 4 ? 1 : 2);
+}
 
 struct PackedArgs {
     const PackedItem* items;

@@ -576,7 +576,7 @@ gt_status packed_bwd_d(const gt_packed_plan* p, PackedArgs a, float* dtable, hip
     if constexpr (BIAS) {
         GT_ROWS(kRowsFew, 32, 1, few_waves(kRow), 1, kStat)
         GT_ROWS(kRows64, kStage, 2, 1, 1, kStat)
-        if (kRow <= 128 && p->layout[kRowSharedAt]) {
+        if (kRow <= 128 && packed_shared<T>(p, kRowSharedAt)) {
             GT_ROWS(kRows128, kStage, 4, (kRow <= 128 ? 2 : 1), 1, kStat)
         } else {
             GT_ROWS(kRows128, kStage, 4, 1, 1, kStat)
@@ -590,7 +590,7 @@ gt_status packed_bwd_d(const gt_packed_plan* p, PackedArgs a, float* dtable, hip
         GT_ROWS(kRowsFew, 32, 1, few_waves_hist(kRow), 1, kGrad)
         GT_ROWS(kRows64, kStage, 2, 1, 1, kGrad)
         // two sets where their columns fit beside the stages (and the sums' exchange)
-        if (kRow <= 128 && p->layout[kRowSharedAt] && 8 * (kStage * kRow + col) + tab + (16 << 10) <= (160 << 10)) {
+        if (kRow <= 128 && packed_shared<T>(p, kRowSharedAt) && 8 * (kStage * kRow + col) + tab + (16 << 10) <= (160 << 10)) {
             GT_ROWS(kRows128, kStage, 4, (kRow <= 128 ? 2 : 1), 1, kGrad)
         } else {
             GT_ROWS(kRows128, kStage, 4, 1, 1, kGrad)
@@ -599,7 +599,7 @@ gt_status packed_bwd_d(const gt_packed_plan* p, PackedArgs a, float* dtable, hip
     } else {
         GT_ROWS(kRowsFew, 32, 1, few_waves(kRow), 1, kGrad)
         GT_ROWS(kRows64, kStage, 2, 1, 1, kGrad)
-        if (kRow <= 128 && p->layout[kRowSharedAt]) {
+        if (kRow <= 128 && packed_shared<T>(p, kRowSharedAt)) {
             GT_ROWS(kRows128, kStage, 4, (kRow <= 128 ? 2 : 1), 1, kGrad)
         } else {
             GT_ROWS(kRows128, kStage, 4, 1, 1, kGrad)
@@ -624,7 +624,7 @@ gt_status packed_bwd_d(const gt_packed_plan* p, PackedArgs a, float* dtable, hip
     GT_KEYS(kKeysFew, 32, 1, few_waves(kRow), 1, kBoth)
     if constexpr (kRow <= 128) {
         GT_KEYS(kKeys64, kStage, 2, 1, 1, kBoth)
-        if (p->layout[kKeySharedAt]) {
+        if (packed_shared<T>(p, kKeySharedAt)) {
             GT_KEYS(kKeys128, kStage, 4, 2, 1, kBoth)
         } else {
             GT_KEYS(kKeys128, kStage, 4, 1, 1, kBoth)
@@ -632,7 +632,7 @@ gt_status packed_bwd_d(const gt_packed_plan* p, PackedArgs a, float* dtable, hip
         GT_KEYS(kKeys256, kStage, 8, 1, 1, kBoth)
     } else if constexpr (sizeof(T) == 2) {
         GT_KEYS(kKeys64, kStage, 2, 1, 1, kBoth)
-        if (p->layout[kKeySharedAt]) {
+        if (packed_shared<T>(p, kKeySharedAt)) {
             GT_KEYS(kKeys128, 32, 4, 2, 1, kOnlyV)
             GT_KEYS(kKeys128, 32, 4, 2, 1, kOnlyK)
         } else {

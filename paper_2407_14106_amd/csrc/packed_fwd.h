@@ -336,7 +336,7 @@ gt_status packed_fwd_d(const gt_packed_plan* p, PackedArgs a, hipStream_t s) {
     }
     GT_FWD(kRowsFew, 32, 1, 1, few_waves(kRow))
     GT_FWD(kRows64, kStage, 1, 2, 1)
-    if (p->layout[kRowSharedAt]) {
+    if (packed_shared<T>(p, kRowSharedAt)) {
         GT_FWD(kRows128, (kRow <= 128 ? kStage : 32), 1, 4, (kRow <= 256 ? 2 : 1))
     } else {
         GT_FWD(kRows128, kStage, 1, 4, 1)

@@ -24,7 +24,7 @@ struct Seqs {
 // init and fill agree.
 struct Cut {
     bool large;         // tiles of 256 where a sequence has as many
-    bool shared;        // two sets of wavefronts share the walk of a tile of 128
+    int shared;         // two sets of wavefronts share the walk of a tile of 128: 2 always, 1 in fp32
     int64_t chunk;      // longest walk of one item
     int64_t few_chunk;  // the same for tiles of 32
 };
@@ -33,7 +33,8 @@ struct Cuts {
 };
 
 // A CU works on eight wavefronts at a time (two workgroups of four): walks that are
-// longer than a CU's share of all of them are cut to half of it.
+// longer than a CU's share of all of them are cut to a third of it (to half: four
+// causal prompts' backward 307 us, a third 274, a quarter 277, a sixth 286).
 constexpr int64_t kCus = 256;
 // Walks are not split into shorter parts than this: parts cost a second launch
 // and a merge.
@@ -70,10 +71,12 @@ Cut cut_side(const Load& few, const Load& t128, const Load& t256, int64_t Hkv) {
     // long walks, where none is more than half its share (8,192 x 16 x 64: 913 against 990 us backward; 128 sequences
     // of 512: 427 against 415 for half the work).
     c.large = t256.n * Hkv >= 2 * kCus && t256.most <= share(t256, 2 * kCus) && t256.total >= kLongWalk * t256.n;
-    // Two sets on one walk where there are fewer workgroups than the chip holds.
-    c.shared = t128.n * Hkv < 2 * kCus;
+    // Two sets on one walk wait for each other (four prompts' dQ 94 -> 116 us), so only where there are fewer workgroups
+    // than CUs and walks too short to be split over all of them (2,000 x 8 heads of 64, backward 76 -> 69 us), or in
+    // fp32, whose products take so long that the wait is small, for up to four workgroups a CU (48 graphs 212 -> 199).
+    c.shared = t128.n * Hkv < kCus && t128.total * Hkv < 2 * kCus * kMinChunk ? 2 : t128.n * Hkv < 4 * kCus;
     auto chunk = [&](int64_t x) { return std::max(kMinChunk, (x + 255) & ~int64_t(255)); };
-    c.chunk = t128.most <= share(t128, kCus) ? std::max<int64_t>(t128.most, 1) : chunk(share(t128, 2 * kCus));
+    c.chunk = t128.most <= share(t128, kCus) ? std::max<int64_t>(t128.most, 1) : chunk(share(t128, 3 * kCus));
     c.few_chunk = chunk(share(few, 2 * kCus));
     return c;
 }
