@@ -32,9 +32,11 @@ struct Cuts {
     Cut rows, keys;
 };
 
-// A CU works on eight wavefronts at a time (two workgroups of four): walks that are
-// longer than a CU's share of all of them are cut to a third of it (to half: four
-// causal prompts' backward 307 us, a third 274, a quarter 277, a sixth 286).
+// A CU works on two workgroups of four wavefronts at a time: where walks are longer
+// than a workgroup's share of all of them by more than a merge costs, they are cut to
+// two thirds of it (to the share: four causal prompts' backward 307 us, two thirds
+// 274, half 277, a third 286; whole walks of up to two shares, 8,192 x 32 / 8 heads of
+// 128 causal: its key passes 1500 and 1001 us, cut 973 and 655).
 constexpr int64_t kCus = 256;
 // Walks are not split into shorter parts than this: parts cost a second launch
 // and a merge.
@@ -76,7 +78,8 @@ Cut cut_side(const Load& few, const Load& t128, const Load& t256, int64_t Hkv) {
     // fp32, whose products take so long that the wait is small, for up to four workgroups a CU (48 graphs 212 -> 199).
     c.shared = t128.n * Hkv < kCus && t128.total * Hkv < 2 * kCus * kMinChunk ? 2 : t128.n * Hkv < 4 * kCus;
     auto chunk = [&](int64_t x) { return std::max(kMinChunk, (x + 255) & ~int64_t(255)); };
-    c.chunk = t128.most <= share(t128, kCus) ? std::max<int64_t>(t128.most, 1) : chunk(share(t128, 3 * kCus));
+    const int64_t slack = t128.n * Hkv < 2 * kCus ? 0 : 2 * kMinChunk;  // what a merge costs; idle CUs cost more
+    c.chunk = t128.most <= share(t128, 2 * kCus) + slack ? std::max<int64_t>(t128.most, 1) : chunk(share(t128, 3 * kCus));
     c.few_chunk = chunk(share(few, 2 * kCus));
     return c;
 }
