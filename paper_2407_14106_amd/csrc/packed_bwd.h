@@ -355,7 +355,7 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
     // per row of a stage: LSE (exp2 domain without a bias), -D, log2 of the weights' sum
     typedef float Stats[KS][3][STAGE];
     __shared__ __attribute__((aligned(16))) Stats sR0, sR1;
-    // with a bias, the buckets of a stage's rows and a wavefront's 32 keys: loaded a row a lane, read a key a lane
+    // with a bias, the buckets of a stage's rows and a wavefront's 32 keys: loaded a row a lane, read turned round, a key a lane
     typedef uint8_t Buckets[BIAS ? W * KS : 1][BIAS ? STAGE : 1][32];
     __shared__ __attribute__((aligned(16))) Buckets sI0, sI1;
     extern __shared__ float s_tab[];
@@ -444,6 +444,8 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
         __builtin_amdgcn_sched_barrier(0);
         typename B::Cols x;
         x.load(PASS == kOnlyK ? bQ : bG, lds);
+        uint4 ids;
+        if constexpr (BIAS) ids = turned_ids(bI + 32 * 32 * rb, lane);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const float4 l4 = *reinterpret_cast<const float4*>(&bR[0][rs0 + 4 * k]);
@@ -455,9 +457,7 @@ __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
                 const int i = 4 * k + y;
                 float t;
                 if constexpr (BIAS) {
-                    const uint32_t id = bI[(32 * rb + part(i, lane)) * 32 + (lane & 31)];
-                    const float bias =
-                        s_tab[(part(i, lane) & gm) * kTableStride + (id < uint32_t(a.B) ? id : uint32_t(a.B))];
+                    const float bias = s_tab[(part(i, lane) & gm) * kTableStride + id_of(ids, i, a.B)];
                     t = fmaf(fmaf(s[0][i], a.scale, bias) - L[y], kLog2e, -lg[y]);
                 } else {
                     t = fmaf(s[0][i], sl2, -L[y]);

@@ -368,6 +368,17 @@ __device__ __forceinline__ uint32_t id_of(const uint4& ids, int i, uint32_t B) {
     const uint32_t b = (w >> (8 * (i & 3))) & 255u;
     return b < B ? b : B;
 }
+// The buckets of a lane's key (lane & 31) and rows part(0 .., lane), from 32 rows of
+// 32 keys in LDS: 16 lanes read 8 rows of 16 keys and each takes a column.
+__device__ __forceinline__ uint4 turned_ids(const uint8_t* s, int lane) {
+    typedef int i32x2_t __attribute__((ext_vector_type(2)));
+    typedef __attribute__((address_space(3))) i32x2_t* lds_t;
+    const uint8_t* p = s + (16 * (lane >> 5) + ((lane & 15) >> 1)) * 32 + 16 * ((lane >> 4) & 1) + 8 * (lane & 1);
+    const i32x2_t a = __builtin_amdgcn_ds_read_tr8_b64_v2i32(reinterpret_cast<lds_t>(reinterpret_cast<uintptr_t>(p)));
+    const i32x2_t b =
+        __builtin_amdgcn_ds_read_tr8_b64_v2i32(reinterpret_cast<lds_t>(reinterpret_cast<uintptr_t>(p + 8 * 32)));
+    return make_uint4(uint32_t(a[0]), uint32_t(a[1]), uint32_t(b[0]), uint32_t(b[1]));
+}
 __device__ __forceinline__ int64_t ids_width(int lk) { return (int64_t(lk) + 15) & ~int64_t(15); }
 
 // out[head of the group][bucket] = the sums over the lanes (whose row's head is
