@@ -11,6 +11,7 @@
 // rounded.
 #pragma once
 
+#include "lanes.h"
 #include "packed.h"
 
 namespace gt {
@@ -382,17 +383,30 @@ __device__ __forceinline__ uint4 turned_ids(const uint8_t* s, int lane) {
 __device__ __forceinline__ int64_t ids_width(int lk) { return (int64_t(lk) + 15) & ~int64_t(15); }
 
 // out[head of the group][bucket] = the sums over the lanes (whose row's head is
-// lane % g) of `waves` such columns, each B + 1 buckets.
+// lane % g) of `waves` such columns, each B + 1 buckets; a wavefront a bucket.
 template <int THREADS>
 __device__ __forceinline__ void hist_flush(const float* s, int waves, int B, int gs, float* out, int thread) {
-    const int per = kWave >> gs;
-    for (int x = thread; x < (B << gs); x += THREADS) {
-        const int head = x / B, b = x % B;
-        float t = 0.f;
-        for (int w = 0; w < waves; ++w)
-            for (int k = 0; k < per; ++k)
-                t += s[(w * (B + 1) + b) * kWave + (((k + x) & (per - 1)) << gs | head)];
-        out[x] = t;
+    // four buckets side by side: the exchanges wait for each other only inside one
+    constexpr int kSide = 4;
+    const int lane = thread % kWave;
+    for (int b0 = thread / kWave * kSide; b0 < B; b0 += THREADS / kWave * kSide) {
+        float t[kSide];
+#pragma unroll
+        for (int k = 0; k < kSide; ++k) {
+            const int b = b0 + k < B ? b0 + k : B;
+            t[k] = 0.f;
+            for (int w = 0; w < waves; ++w) t[k] += s[(w * (B + 1) + b) * kWave + lane];
+        }
+#pragma unroll
+        for (int k = 0; k < kSide; ++k) t[k] = pair_sum(t[k]);
+#pragma unroll
+        for (int o = 16; o > 0; o /= 2)
+            if (o >> gs)  // uniform
+#pragma unroll
+                for (int k = 0; k < kSide; ++k) t[k] += __int_as_float(xor_lane_pow2(__float_as_int(t[k]), o));
+#pragma unroll
+        for (int k = 0; k < kSide; ++k)
+            if (lane >> gs == 0 && b0 + k < B) out[lane * B + b0 + k] = t[k];
     }
 }
 
