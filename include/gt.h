@@ -539,7 +539,7 @@ gt_status gt_bucket_bias_bwd(int64_t nnz, int32_t H, int32_t n_buckets, const ui
  * g: GT_GATE_NONE 1; GT_GATE_VECTOR fp32[D] (a learned scale for each feature);
  * GT_GATE_ROWS [n, D] in dtype; GT_GATE_SIGMOID sigmoid of such.
  *   x, f, y, z [n, D] contiguous in dtype (no alignment needed beyond the
- *     element's; rows of whole 16-byte pieces at 16-byte addresses run faster);
+ *     element's; rows of whole 16-byte pieces run faster);
  *   w_post, b_post, w_pre, b_pre fp32[D] or NULL (ones, zeros);
  *   stats fp32 [n, 4], for the backward: mean and 1/sqrt(var + eps) of f, then
  *     of y (mean 0 for GT_NORM_RMS).

@@ -61,36 +61,68 @@ struct RowSum {
     }
 };
 
+// 16 bytes at any element's address (global accesses need no more alignment; a
+// load or store for each element instead: rows of 511 in bf16 1,460 GB/s forward
+// and 950 backward against 3,700 and 3,850).
+template <typename T>
+struct Piece {
+    typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4)));
+    typedef uint32_t word __attribute__((aligned(4)));
+};
+template <>
+struct Piece<uint16_t> {
+    typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2)));
+    typedef uint32_t word __attribute__((aligned(2)));
+};
+
 // A lane's NV pieces of one row: E consecutive features each, LPR pieces apart.
-// VEC: whole pieces at 16-byte addresses; FULL besides: the row fills its lanes.
-template <typename T, int LPR, int NV, bool VEC, bool FULL>
+// kWhole: rows are whole pieces; kFull besides: the row fills its lanes.  kRagged:
+// the row's last piece is loaded ending with the row and shifted, and stored in
+// parts.  kTiny: rows of less than a piece, an element at a time.
+enum Rows { kFull, kWhole, kRagged, kTiny };
+
+template <typename T, int LPR, int NV, Rows R>
 struct Cols {
     static constexpr int E = 16 / int(sizeof(T));
+    static constexpr bool FULL = R == kFull, VEC = R <= kWhole;
+    typedef typename Piece<T>::type piece_t;
     int D, lane;  // lane of the row
     __device__ __forceinline__ int col(int v) const { return (lane + LPR * v) * E; }
     __device__ __forceinline__ bool in(int v, int t) const { return FULL || (VEC ? col(v) < D : col(v) + t < D); }
     __device__ __forceinline__ void load(float (&o)[NV][E], const void* p, int64_t row) const {
         const T* r = static_cast<const T*>(p) + row * D;
+        if constexpr (R == kTiny) {
+#pragma unroll
+            for (int t = 0; t < E; ++t) {
+                o[0][t] = 0.f;
+                if (col(0) + t < D) {
+                    if constexpr (E == 8) o[0][t] = bf16_to_f32(r[col(0) + t]);
+                    else o[0][t] = r[col(0) + t];
+                }
+            }
+            return;
+        }
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            if constexpr (VEC) {
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (FULL || col(v) < D) x = *reinterpret_cast<const uint4*>(r + col(v));
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            piece_t x = {0, 0, 0, 0};
+            const int c = col(v);
+            const int over = VEC || c + E <= D ? 0 : c + E - D;  // elements of the piece behind the row's end
+            if (FULL || c < D) x = *reinterpret_cast<const piece_t*>(r + c - over);
+            uint32_t w[4] = {x[0], x[1], x[2], x[3]};
+            if constexpr (!VEC) {  // down by `over` elements, zeros from above
+                const int bits = over * 8 * int(sizeof(T));
+                if (bits & 64) w[0] = w[2], w[1] = w[3], w[2] = w[3] = 0;
+                if (bits & 32) w[0] = w[1], w[1] = w[2], w[2] = w[3], w[3] = 0;
+                if constexpr (E == 8) {
+                    const uint32_t by = bits & 16;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    if constexpr (E == 8) o[v][2 * t] = bf16lo(w[t]), o[v][2 * t + 1] = bf16hi(w[t]);
-                    else o[v][t] = __uint_as_float(w[t]);
+                    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_alignbit(i < 3 ? w[i + 1] : 0, w[i], by);
                 }
-            } else {
+            }
 #pragma unroll
-                for (int t = 0; t < E; ++t) {
-                    o[v][t] = 0.f;
-                    if (col(v) + t < D) {
-                        if constexpr (E == 8) o[v][t] = bf16_to_f32(r[col(v) + t]);
-                        else o[v][t] = r[col(v) + t];
-                    }
-                }
+            for (int t = 0; t < 4; ++t) {
+                if constexpr (E == 8) o[v][2 * t] = bf16lo(w[t]), o[v][2 * t + 1] = bf16hi(w[t]);
+                else o[v][t] = __uint_as_float(w[t]);
             }
         }
     }
@@ -98,25 +130,26 @@ struct Cols {
         T* r = static_cast<T*>(p) + row * D;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            if constexpr (VEC) {
-                if (!FULL && col(v) >= D) continue;
-                uint4 x;
-                if constexpr (E == 8)
-                    x = make_uint4(pack_bf16x2(o[v][0], o[v][1]), pack_bf16x2(o[v][2], o[v][3]),
-                                   pack_bf16x2(o[v][4], o[v][5]), pack_bf16x2(o[v][6], o[v][7]));
-                else
-                    x = make_uint4(__float_as_uint(o[v][0]), __float_as_uint(o[v][1]), __float_as_uint(o[v][2]),
-                                   __float_as_uint(o[v][3]));
-                typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-                if (far) __builtin_nontemporal_store(u32x4_t{x.x, x.y, x.z, x.w}, reinterpret_cast<u32x4_t*>(r + col(v)));
-                else *reinterpret_cast<uint4*>(r + col(v)) = x;
-            } else {
+            const int c = col(v);
+            if (!FULL && c >= D) continue;
+            uint32_t w[4];
 #pragma unroll
-                for (int t = 0; t < E; ++t)
-                    if (col(v) + t < D) {
-                        if constexpr (E == 8) r[col(v) + t] = f32_to_bf16(o[v][t]);
-                        else r[col(v) + t] = o[v][t];
-                    }
+            for (int t = 0; t < 4; ++t) {
+                if constexpr (E == 8) w[t] = pack_bf16x2(o[v][2 * t], o[v][2 * t + 1]);
+                else w[t] = __float_as_uint(o[v][t]);
+            }
+            if (VEC || c + E <= D) {
+                const piece_t x = {w[0], w[1], w[2], w[3]};
+                if (far) __builtin_nontemporal_store(x, reinterpret_cast<piece_t*>(r + c));
+                else *reinterpret_cast<piece_t*>(r + c) = x;
+            } else {
+                constexpr int kWord = 4 / int(sizeof(T));  // elements per 32 bits
+                const int left = D - c;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    if (left >= kWord * (t + 1)) *reinterpret_cast<typename Piece<T>::word*>(r + c + kWord * t) = w[t];
+                    else if (kWord == 2 && left > kWord * t) r[c + kWord * t] = T(w[t]);
+                }
             }
         }
     }
@@ -157,9 +190,9 @@ __device__ __forceinline__ void row_stats(const float (&v)[NV][E], const C& c, b
 
 __device__ __forceinline__ float sigmoid(float v) { return 1.f / (1.f + __expf(-v)); }
 
-template <typename T, int LPR, int NV, bool VEC, bool FULL>
+template <typename T, int LPR, int NV, Rows R>
 __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_fwd(NormArgs a) {
-    using C = Cols<T, LPR, NV, VEC, FULL>;
+    using C = Cols<T, LPR, NV, R>;
     using S = RowSum<LPR>;
     constexpr int E = C::E;
     __shared__ float s_sum[2 * S::kThreads / kWave];
@@ -244,9 +277,9 @@ struct Params {
 // Rows of 512 lanes hold 16 columns a lane, whose parameters and sums do not fit the
 // registers together: the parameters lie in LDS (8,192 columns bf16: 805 us for
 // 32,768 rows against 1632 with spilled registers).
-template <typename T, int LPR, int NV, bool VEC, bool FULL>
+template <typename T, int LPR, int NV, Rows R>
 __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_bwd(NormArgs a) {
-    using C = Cols<T, LPR, NV, VEC, FULL>;
+    using C = Cols<T, LPR, NV, R>;
     using S = RowSum<LPR>;
     constexpr int E = C::E;
     __shared__ float s_sum[2 * S::kThreads / kWave];
@@ -408,24 +441,34 @@ int norm_blocks(int64_t n, int32_t D, gt_dtype dt) {
 
 bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 
-template <typename T, bool VEC>
+template <typename T>
 void run_fwd(const NormArgs& a, int pieces, int blocks, hipStream_t s) {
-#define GT_CALL(LPR, NV)                                                                                        \
-    do {                                                                                                        \
-        if (VEC && pieces == LPR * NV) k_norm_fwd<T, LPR, NV, VEC, VEC><<<blocks, RowSum<LPR>::kThreads, 0, s>>>(a); \
-        else k_norm_fwd<T, LPR, NV, VEC, false><<<blocks, RowSum<LPR>::kThreads, 0, s>>>(a);                     \
+    constexpr int E = 16 / int(sizeof(T));
+    const bool whole = a.D % E == 0;
+#define GT_CALL(LPR, NV)                                                                                   \
+    do {                                                                                                   \
+        constexpr int kThreads = RowSum<LPR>::kThreads;                                                    \
+        if (whole && pieces == LPR * NV) k_norm_fwd<T, LPR, NV, kFull><<<blocks, kThreads, 0, s>>>(a);     \
+        else if (whole) k_norm_fwd<T, LPR, NV, kWhole><<<blocks, kThreads, 0, s>>>(a);                     \
+        else k_norm_fwd<T, LPR, NV, kRagged><<<blocks, kThreads, 0, s>>>(a);                               \
     } while (0)
-    GT_NORM_SHAPE(pieces, GT_CALL);
+    if (a.D < E) k_norm_fwd<T, 8, 1, kTiny><<<blocks, RowSum<8>::kThreads, 0, s>>>(a);
+    else GT_NORM_SHAPE(pieces, GT_CALL);
 #undef GT_CALL
 }
-template <typename T, bool VEC>
+template <typename T>
 void run_bwd(const NormArgs& a, int pieces, int blocks, hipStream_t s) {
-#define GT_CALL(LPR, NV)                                                                                        \
-    do {                                                                                                        \
-        if (VEC && pieces == LPR * NV) k_norm_bwd<T, LPR, NV, VEC, VEC><<<blocks, RowSum<LPR>::kThreads, 0, s>>>(a); \
-        else k_norm_bwd<T, LPR, NV, VEC, false><<<blocks, RowSum<LPR>::kThreads, 0, s>>>(a);                     \
+    constexpr int E = 16 / int(sizeof(T));
+    const bool whole = a.D % E == 0;
+#define GT_CALL(LPR, NV)                                                                                   \
+    do {                                                                                                   \
+        constexpr int kThreads = RowSum<LPR>::kThreads;                                                    \
+        if (whole && pieces == LPR * NV) k_norm_bwd<T, LPR, NV, kFull><<<blocks, kThreads, 0, s>>>(a);     \
+        else if (whole) k_norm_bwd<T, LPR, NV, kWhole><<<blocks, kThreads, 0, s>>>(a);                     \
+        else k_norm_bwd<T, LPR, NV, kRagged><<<blocks, kThreads, 0, s>>>(a);                               \
     } while (0)
-    GT_NORM_SHAPE(pieces, GT_CALL);
+    if (a.D < E) k_norm_bwd<T, 8, 1, kTiny><<<blocks, RowSum<8>::kThreads, 0, s>>>(a);
+    else GT_NORM_SHAPE(pieces, GT_CALL);
 #undef GT_CALL
 }
 
@@ -461,10 +504,8 @@ extern "C" gt_status gt_block_norm_fwd(int64_t n, int32_t D, gt_dtype dt, int32_
     a.w_post = w_post, a.b_post = b_post, a.w_pre = w_pre, a.b_pre = b_pre;
     a.y = y, a.z = z, a.stats = stats;
     const int E = dt == GT_BF16 ? 8 : 4, pieces = int(cdiv(D, E)), blocks = norm_blocks(n, D, dt);
-    const bool vec = D % E == 0 && !off16(x) && !off16(f) && !off16(y) && !off16(z) &&
-                     (gate_kind < GT_GATE_ROWS || !off16(gate));
-    if (dt == GT_BF16) vec ? run_fwd<uint16_t, true>(a, pieces, blocks, s) : run_fwd<uint16_t, false>(a, pieces, blocks, s);
-    else vec ? run_fwd<float, true>(a, pieces, blocks, s) : run_fwd<float, false>(a, pieces, blocks, s);
+    if (dt == GT_BF16) run_fwd<uint16_t>(a, pieces, blocks, s);
+    else run_fwd<float>(a, pieces, blocks, s);
     GT_LAUNCH_CHECK("block_norm_fwd");
     return GT_OK;
 }
@@ -507,10 +548,8 @@ extern "C" gt_status gt_block_norm_bwd(int64_t n, int32_t D, gt_dtype dt, int32_
     for (int k = 0; k < kSums; ++k)
         if (o.p[k]) a.want |= 1u << k;
     if (n > 0) {
-        const bool vec = D % E == 0 && !off16(x) && !off16(f) && !off16(dy) && !off16(dz) && !off16(dx) && !off16(df) &&
-                         (gate_kind < GT_GATE_ROWS || (!off16(gate) && !off16(dgate)));
-        if (dt == GT_BF16) vec ? run_bwd<uint16_t, true>(a, pieces, blocks, s) : run_bwd<uint16_t, false>(a, pieces, blocks, s);
-        else vec ? run_bwd<float, true>(a, pieces, blocks, s) : run_bwd<float, false>(a, pieces, blocks, s);
+        if (dt == GT_BF16) run_bwd<uint16_t>(a, pieces, blocks, s);
+        else run_bwd<float>(a, pieces, blocks, s);
         GT_LAUNCH_CHECK("block_norm_bwd");
     }
     if (a.want) {
