@@ -476,7 +476,8 @@ gt_status gt_packed_attn_fwd(const gt_packed_plan* plan, int32_t d, gt_dtype dty
                              const void* K, int64_t ldk, const void* V, int64_t ldv, float scale, void* O, float* LSE,
                              void* ws, size_t ws_bytes, hipStream_t stream);
 /* Backward from O and LSE of the forward, with the formulas of
- * gt_dense_attn_bwd (D_i = <dO_i, O_i>); dK and dV sum over the query heads
+ * gt_dense_attn_bwd (D_i = <dO_i, O_i>, or for rows of few keys, whose D_i a
+ * rounded O would spoil, from their weights); dK and dV sum over the query heads
  * that share a kv head.  No atomics: results are the same run to run. */
 size_t gt_packed_attn_bwd_workspace_size(const gt_packed_plan* plan, int32_t d, gt_dtype dtype);
 gt_status gt_packed_attn_bwd(const gt_packed_plan* plan, int32_t d, gt_dtype dtype, const void* Q, int64_t ldq,

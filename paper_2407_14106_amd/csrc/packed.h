@@ -83,9 +83,9 @@ inline const PackedItem* packed_list(const gt_packed_plan* p, int list) {
     return reinterpret_cast<const PackedItem*>(static_cast<const char*>(p->items) + p->layout[2 * list]);
 }
 
-// Wavefronts of a workgroup: kPairWaves pairs, or kFewWaves shares of a walk.
-// They follow from the LDS that a wavefront's stages take (row bytes x 32 rows x
-// 4 buffers).
+// Wavefronts of a workgroup: of the pair kernels (a pair each) and for tiles of 32
+// (shares of one walk).  They follow from the LDS that a wavefront's stages take
+// (row bytes x 32 rows x 4 buffers).
 constexpr int pair_waves(int row_bytes) { return row_bytes <= 128 ? 4 : row_bytes <= 256 ? 2 : 1; }
 constexpr int few_waves(int row_bytes) { return row_bytes <= 64 ? 8 : row_bytes <= 256 ? 4 : 2; }
 // With the table's gradient each of them needs its columns in LDS besides.
@@ -104,7 +104,8 @@ inline int64_t fwd_slot_floats(int d) { return kFewRows * (d + 2); }
 inline int64_t row_slot_floats(int d) { return kFewRows * d; }
 inline int64_t key_slot_floats(int d) { return kFewRows * 2 * d; }
 
-// Blocks of the pair kernels' and of the row kernels' table gradients.
+// Workgroups of the pair backward with a bias: each wavefront stays and goes through
+// its sequences, so a partial table is left for a wavefront, not for a sequence.
 constexpr int64_t kPairBlocks = 1024;
 inline int64_t pair_blocks(const gt_packed_plan* p, int row_bytes) {
     // whole sets of heads on each XCD: a wavefront's pairs are all of one head, and an XCD works on the neighbouring

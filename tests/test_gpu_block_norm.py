@@ -88,7 +88,7 @@ def test_many_rows(gt, dtype, D):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("D", [512, 8192])
+@pytest.mark.parametrize("D", [511, 512, 8192])
 def test_rows_larger_than_the_last_level_cache(gt, dtype, D):
     # the rows' results are those of the same rows in two smaller calls
     n = (260 << 20) // (D * (2 if dtype == torch.bfloat16 else 4))
