@@ -29,7 +29,22 @@ __device__ __forceinline__ int64_t row_at(const PackedArgs& a, const PackedItem&
     return int64_t(it.q0 + (row >> a.gs)) * a.H + (hk << a.gs) + (row & ((1 << a.gs) - 1));
 }
 
-// O = sum of w_p O_p / sum of w_p l_p, w_p = exp(m_p - max m).
+// Calls add(load(p)) for the parts in their order, four loads at a time (one after the
+// other: 16 tokens over up to 65,536 keys 17 us, now 8).
+template <typename L, typename A>
+__device__ __forceinline__ void each_part(int parts, L load, A add) {
+    for (int p0 = 0; p0 < parts; p0 += 4) {
+        decltype(load(0)) v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = load(p0 + u < parts ? p0 + u : parts - 1);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (p0 + u < parts) add(v[u]);
+    }
+}
+
+// O = sum of w_p O_p / sum of w_p l_p, w_p = exp(m_p - max m): a lane a part for the
+// weights, then a lane a feature.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_merge_fwd(PackedArgs a, int D) {
     PackedItem it;
@@ -41,14 +56,23 @@ __global__ __launch_bounds__(kThreads) void k_merge_fwd(PackedArgs a, int D) {
     const float* s = a.slots + (int64_t(it.slot) * a.Hkv + hk) * slot;
     const float to2 = a.B > 0 ? kLog2e : 1.f;  // m is in the exp2 domain without a bias
     float m = -3.402823466e38f, l = 0.f, o[2] = {0.f, 0.f};
-    for (int p = 0; p < it.s0; ++p) m = fmaxf(m, s[p * step + r]);
-    for (int p = 0; p < it.s0; ++p) {
-        const float w = ex2((s[p * step + r] - m) * to2);
-        l = fmaf(w, s[p * step + kFewRows + r], l);
-        for (int k = 0; k < 2; ++k)
-            if (lane + kWave * k < D)
-                o[k] = fmaf(w, s[p * step + 2 * kFewRows + r * D + lane + kWave * k], o[k]);
-    }
+    for (int p = lane; p < it.s0; p += kWave) m = fmaxf(m, s[p * step + r]);
+    m = wave_max(m);
+    for (int p = lane; p < it.s0; p += kWave)
+        l = fmaf(ex2((s[p * step + r] - m) * to2), s[p * step + kFewRows + r], l);
+    l = wave_sum(l);
+    const int c0 = lane < D ? lane : 0, c1 = lane + kWave < D ? lane + kWave : 0;
+    each_part(
+        it.s0,
+        [&](int p) {
+            const float* x = s + p * step;
+            return make_float3(x[r], x[2 * kFewRows + r * D + c0], x[2 * kFewRows + r * D + c1]);
+        },
+        [&](const float3& x) {
+            const float w = ex2((x.x - m) * to2);
+            o[0] = fmaf(w, x.y, o[0]);
+            o[1] = fmaf(w, x.z, o[1]);
+        });
     const int64_t at = row_at(a, it, hk, it.tile + r);
     if (lane == 0) a.LSE[at] = l == 0.f ? -__builtin_huge_valf() : fmaf(__log2f(l), kLn2, a.B > 0 ? m : m * kLn2);
     const float f = l == 0.f ? 0.f : 1.f / l;
@@ -83,7 +107,10 @@ __global__ __launch_bounds__(kThreads) void k_merge_rows(PackedArgs a, int D) {
     const int64_t at = row_at(a, it, hk, it.tile + r);
     for (int c = lane_id(); c < D; c += kWave) {
         float t = 0.f;
-        for (int p = 0; p < it.s0; ++p) t += a.slots[(((it.slot + int64_t(p) * it.s1) * a.Hkv + hk) * kFewRows + r) * D + c];
+        each_part(
+            it.s0,
+            [&](int p) { return a.slots[(((it.slot + int64_t(p) * it.s1) * a.Hkv + hk) * kFewRows + r) * D + c]; },
+            [&](float x) { t += x; });
         static_cast<T*>(a.out0)[at * D + c] = from_f32<T>(t * a.scale);
     }
 }
@@ -97,11 +124,16 @@ __global__ __launch_bounds__(kThreads) void k_merge_keys(PackedArgs a, int D) {
     const int64_t at = int64_t(it.k0 + it.tile + r) * a.Hkv + hk;
     for (int c = lane_id(); c < D; c += kWave) {
         float k = 0.f, v = 0.f;
-        for (int p = 0; p < it.s0; ++p) {
-            const float* s = a.slots + (((it.slot + int64_t(p) * it.s1) * a.Hkv + hk) * (2 * kFewRows) + r) * D + c;
-            k += s[0];
-            v += s[kFewRows * D];
-        }
+        each_part(
+            it.s0,
+            [&](int p) {
+                const float* s = a.slots + (((it.slot + int64_t(p) * it.s1) * a.Hkv + hk) * (2 * kFewRows) + r) * D + c;
+                return make_float2(s[0], s[kFewRows * D]);
+            },
+            [&](const float2& x) {
+                k += x.x;
+                v += x.y;
+            });
         static_cast<T*>(a.out1)[at * D + c] = from_f32<T>(k * a.scale);
         static_cast<T*>(a.out2)[at * D + c] = from_f32<T>(v);
     }
