@@ -18,6 +18,7 @@ struct Seqs {
     const int64_t *q, *k;
     int gs, Hkv;
     bool causal;
+    bool fold;  // small sequences in the lists of tiles of 128
 };
 
 // How the tiles of one side (rows or keys) are cut; from the whole batch, so that
@@ -55,7 +56,25 @@ int64_t first_row(const Seqs& s, int64_t rows, int64_t off, int64_t key) {  // f
     return s.causal ? std::min(rows, std::max<int64_t>(0, key - off) << s.gs) : 0;
 }
 
-bool is_pair(int64_t rows, int64_t lk) { return rows <= 32 && lk <= 32; }
+// Sequences of every size in one small batch: each list is a launch, which costs more than the lanes that small
+// sequences leave idle in tiles of 128, up to about four of those a CU (60 sequences of 10 to 100, 8 heads of 64, step
+// 50 -> 31 us, 100 of them 51 -> 33; 200 of 20 to 60, nearly eight a CU, 42 -> 49).  Not where the wavefronts of few
+// rows share a longer walk.
+constexpr int64_t kFoldWalk = 256;
+bool folds(const Seqs& s) {
+    int64_t tiles = 0;
+    bool rows_over = false, keys_over = false;
+    for (int64_t i = 0; i < s.n; ++i) {
+        const int64_t rows = (s.q[i + 1] - s.q[i]) << s.gs, lk = s.k[i + 1] - s.k[i];
+        tiles += (std::max(rows, lk) + 127) / 128;
+        rows_over |= rows > 32;
+        keys_over |= lk > 32;
+    }
+    return rows_over && keys_over && tiles * s.Hkv <= 4 * kCus;
+}
+bool is_pair(const Seqs& s, int64_t rows, int64_t lk) { return !s.fold && rows <= 32 && lk <= 32; }
+// Rows (or keys) for the list of tiles of 32, and how long their walk can be.
+bool is_few(const Seqs& s, int64_t own, int64_t walk) { return own <= 32 && !(s.fold && walk <= kFoldWalk); }
 
 // Walks of the tiles of one size.
 struct Load {
@@ -98,11 +117,11 @@ Cuts cut(const Seqs& s) {
     Load few[2], t128[2], t256[2];
     for (int64_t i = 0; i < s.n; ++i) {
         const int64_t lq = s.q[i + 1] - s.q[i], lk = s.k[i + 1] - s.k[i], rows = lq << s.gs, off = lk - lq;
-        if (is_pair(rows, lk)) continue;
-        if (rows > 0 && rows <= 32) few[0].add(row_walk(s, lk, off, rows - 1));
+        if (is_pair(s, rows, lk)) continue;
+        if (rows > 0 && is_few(s, rows, lk)) few[0].add(row_walk(s, lk, off, rows - 1));
         else row_tiles(s, rows, lk, off, 128, [&](int64_t, int64_t w) { t128[0].add(w); });
         if (rows >= 256) row_tiles(s, rows, lk, off, 256, [&](int64_t, int64_t w) { t256[0].add(w); });
-        if (lk > 0 && lk <= 32) few[1].add(rows - first_row(s, rows, off, 0));
+        if (lk > 0 && is_few(s, lk, rows)) few[1].add(rows - first_row(s, rows, off, 0));
         else key_tiles(s, rows, lk, off, 128, [&](int64_t, int64_t w) { t128[1].add(w); });
         if (lk >= 256) key_tiles(s, rows, lk, off, 256, [&](int64_t, int64_t w) { t256[1].add(w); });
     }
@@ -113,6 +132,7 @@ Cuts cut(const Seqs& s) {
 // Returns the numbers of slots (row lists, key lists).
 template <typename F>
 std::pair<int64_t, int64_t> each_item(const Seqs& s, const Cuts& c, F f) {
+    constexpr int64_t kTile[] = {32, 64, 128, 256};
     int64_t pair = 0, row_slots = 0, key_slots = 0;
     for (int64_t i = 0; i < s.n; ++i) {
         PackedItem it = {};
@@ -124,7 +144,7 @@ std::pair<int64_t, int64_t> each_item(const Seqs& s, const Cuts& c, F f) {
         pair += int64_t(it.lq) * ((int64_t(it.lk) + 15) / 16 * 16);
         const int64_t rows = int64_t(it.lq) << s.gs, lk = it.lk, off = lk - it.lq;
         it.slot = -1;
-        if (is_pair(rows, lk)) {
+        if (is_pair(s, rows, lk)) {
             if (rows > 0 || lk > 0) f(kPairs, it);
             continue;
         }
@@ -155,14 +175,20 @@ std::pair<int64_t, int64_t> each_item(const Seqs& s, const Cuts& c, F f) {
                 if (parts > 1) it.slot += int32_t(units);
             }
         };
-        const int row_list = rows <= 32 ? kRowsFew : rows <= 64 ? kRows64 : c.rows.large && rows >= 256 ? kRows256 : kRows128;
-        const int64_t row_tile = rows <= 32 ? 32 : rows <= 64 ? 64 : row_list == kRows256 ? 256 : 128;
+        const int row_list = is_few(s, rows, lk)               ? kRowsFew
+                             : rows <= 64 && !s.fold           ? kRows64
+                             : c.rows.large && rows >= 256     ? kRows256
+                                                               : kRows128;
+        const int64_t row_tile = kTile[row_list - kRowsFew];
         row_tiles(s, rows, lk, off, row_tile, [&](int64_t t, int64_t w) {
             walk(row_list, kRowMerges, row_slots, t, (std::min(rows - t, row_tile) + 31) / 32, 0, w,
                  row_list == kRowsFew ? c.rows.few_chunk : c.rows.chunk);
         });
-        const int key_list = lk <= 32 ? kKeysFew : lk <= 64 ? kKeys64 : c.keys.large && lk >= 256 ? kKeys256 : kKeys128;
-        const int64_t key_tile = lk <= 32 ? 32 : lk <= 64 ? 64 : key_list == kKeys256 ? 256 : 128;
+        const int key_list = is_few(s, lk, rows)               ? kKeysFew
+                             : lk <= 64 && !s.fold             ? kKeys64
+                             : c.keys.large && lk >= 256       ? kKeys256
+                                                               : kKeys128;
+        const int64_t key_tile = kTile[key_list - kKeysFew];
         key_tiles(s, rows, lk, off, key_tile, [&](int64_t t, int64_t w) {
             walk(key_list, kKeyMerges, key_slots, t, (std::min(lk - t, key_tile) + 31) / 32, rows - w, rows,
                  key_list == kKeysFew ? c.keys.few_chunk : c.keys.chunk);
@@ -213,11 +239,12 @@ extern "C" gt_status gt_packed_plan_init(int64_t n_seq, const int64_t* q_ptr, co
         return fail(GT_ERR_UNSUPPORTED, std::string(who) + ": H must be a multiple of Hkv, at most 256");
     const int g = H / Hkv;
     if (g > 16 || (g & (g - 1))) return fail(GT_ERR_UNSUPPORTED, std::string(who) + ": H / Hkv must be 1, 2, 4, 8 or 16");
-    const Seqs s = {n_seq, q_ptr, k_ptr, ilog2(g), Hkv, causal != 0};
+    Seqs s = {n_seq, q_ptr, k_ptr, ilog2(g), Hkv, causal != 0, false};
     int64_t pair = 0;
     gt_status st = check_seqs(who, s, &pair);
     if (st != GT_OK) return st;
     int64_t count[kPackedLists];
+    s.fold = folds(s);
     const Cuts c = cut(s);
     const auto slots = plan_lists(s, c, count);
     if (slots.first * Hkv >= (int64_t(1) << 26) || slots.second * Hkv >= (int64_t(1) << 26))
@@ -254,11 +281,12 @@ extern "C" gt_status gt_packed_plan_fill(int64_t n_seq, const int64_t* q_ptr, co
     if (n_seq != plan->n_seq) return fail(GT_ERR_INVALID_ARG, std::string(who) + ": n_seq differs from init's");
     if (bytes < size_t(plan->item_bytes)) return fail(GT_ERR_WORKSPACE, std::string(who) + ": item buffer too small");
     if (plan->item_bytes > 0 && !host_items) return fail(GT_ERR_INVALID_ARG, std::string(who) + ": null pointer");
-    const Seqs s = {n_seq, q_ptr, k_ptr, ilog2(plan->H / plan->Hkv), plan->Hkv, plan->causal != 0};
+    Seqs s = {n_seq, q_ptr, k_ptr, ilog2(plan->H / plan->Hkv), plan->Hkv, plan->causal != 0, false};
     int64_t pair = 0;
     gt_status st = check_seqs(who, s, &pair);
     if (st != GT_OK) return st;
     int64_t count[kPackedLists];
+    s.fold = folds(s);
     const Cuts c = cut(s);
     plan_lists(s, c, count);
     bool same = pair == plan->pair_bytes && q_ptr[n_seq] == plan->nq && k_ptr[n_seq] == plan->nk;

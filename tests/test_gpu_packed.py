@@ -98,6 +98,19 @@ def test_sizes_where_tiles_end(gt, dtype, d, causal, B):
         compare(gt, lq, lk, 2, 2, d, dtype, causal, B, seed=n)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("B", [0, 33])
+def test_small_sequences_alone_and_in_large_batches(gt, dtype, d, causal, B):
+    # none above 32 rows and keys: whole sequences a wavefront
+    compare(gt, [31, 32, 1, 17, 0, 8, 32, 5], [32, 31, 5, 17, 3, 0, 32, 1], 4, 4, d, dtype, causal, B, seed=d)
+    compare(gt, [7, 8, 1, 3], [32, 31, 5, 1], 8, 2, d, dtype, causal, B, seed=d + 1)
+    # every list of tiles: more tiles than a batch may have whose small sequences go with the others
+    lq, lk = [1, 30, 33, 50, 64, 65, 130, 2, 300, 20], [32, 30, 33, 70, 40, 65, 20, 100, 5, 300]
+    compare(gt, lq * 4, lk * 4, 32, 32, d, dtype, causal, B, seed=d + 2)
+
+
 @pytest.mark.parametrize("d", [32, 64, 128])
 @pytest.mark.parametrize("H,Hkv", [(2, 2), (8, 2)])
 @pytest.mark.parametrize("causal", [False, True])

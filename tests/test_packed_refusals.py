@@ -126,9 +126,11 @@ def test_plan_covers_every_row_and_key_once(lib, causal, group, many):
         for s in range(len(lq)):
             for x in range(owned(s)):
                 lo, hi = needs(s, x)
-                assert seen[s][x] == max(0, hi - lo) or (lq[s] * group <= 32 and lk[s] <= 32), (s, x)
+                assert seen[s][x] == max(0, hi - lo) or s in small, (s, x)
 
-    small = [s for s in range(len(lq)) if lq[s] * group <= 32 and lk[s] <= 32 and lq[s] + lk[s] > 0]
+    # a batch of few tiles has its small sequences in the lists of the others
+    folded = sum((max(a * group, b) + 127) // 128 for a, b in zip(lq, lk)) * 8 <= 1024
+    small = [] if folded else [s for s in range(len(lq)) if lq[s] * group <= 32 and lk[s] <= 32 and lq[s] + lk[s] > 0]
     assert sorted(by_seq[tuple(int(it[x]) for x in (0, 2, 1, 3))] for it in items[0]) == small
     off = [b - a for a, b in zip(lq, lk)]
     row_needs = lambda s, r: (0, max(0, min(lk[s], off[s] + r // group + 1)) if causal else lk[s])  # noqa: E731
