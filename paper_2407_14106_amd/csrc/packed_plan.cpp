@@ -288,8 +288,11 @@ extern "C" gt_status gt_packed_plan_fill(int64_t n_seq, const int64_t* q_ptr, co
     int64_t count[kPackedLists];
     s.fold = folds(s);
     const Cuts c = cut(s);
-    plan_lists(s, c, count);
-    bool same = pair == plan->pair_bytes && q_ptr[n_seq] == plan->nq && k_ptr[n_seq] == plan->nk;
+    const auto slots = plan_lists(s, c, count);
+    // the slots too: the workspace has as many as init counted
+    bool same = pair == plan->pair_bytes && q_ptr[n_seq] == plan->nq && k_ptr[n_seq] == plan->nk &&
+                slots.first == plan->layout[kRowSlotsAt] && slots.second == plan->layout[kKeySlotsAt] &&
+                c.rows.shared == plan->layout[kRowSharedAt] && c.keys.shared == plan->layout[kKeySharedAt];
     for (int l = 0; l < kPackedLists; ++l) same = same && count[l] == plan->layout[2 * l + 1];
     if (!same) return fail(GT_ERR_INVALID_ARG, std::string(who) + ": the sequences differ from init's");
     PackedItem* list[kPackedLists];

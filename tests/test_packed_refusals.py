@@ -67,6 +67,22 @@ def test_plan_null_and_changed_arguments(lib):
                                    BIG) == gt.GT_ERR_INVALID_ARG
 
 
+def test_plan_fill_refuses_sequences_of_more_partial_results(lib):
+    # as many queries, keys, bucket bytes, tiles, parts and merges, but one partial result more than init counted, and
+    # the workspace holds no more: blocks of 32 rows times parts, 3 x 3 + 4 x 3 + 4 x 2 against 4 x 3 + 4 x 3 + 3 x 2
+    fewer, more = ([86, 115, 99], [2336, 2896, 1664]), ([118, 109, 73], [2176, 2704, 2016])
+    assert [sum(x) for x in fewer] == [sum(x) for x in more]
+    st, c = init(lib, ptrs(*fewer[0]), ptrs(*fewer[1]), 1, 1)
+    st2, c2 = init(lib, ptrs(*more[0]), ptrs(*more[1]), 1, 1)
+    assert st == st2 == gt.GT_OK and c.item_bytes == c2.item_bytes and c.pair_bytes == c2.pair_bytes
+    assert c2.layout[28] > c.layout[28]
+    host = np.zeros(c.item_bytes, dtype=np.uint8)
+    for lens, want in ((more, gt.GT_ERR_INVALID_ARG), (fewer, gt.GT_OK)):
+        q, k = ptrs(*lens[0]), ptrs(*lens[1])
+        assert lib.gt_packed_plan_fill(3, q.ctypes.data, k.ctypes.data, ctypes.byref(c), host.ctypes.data,
+                                       c.item_bytes) == want
+
+
 @pytest.mark.parametrize("lq,lk,n,H,want", [
     (1, 40, 1 << 20, 8, gt.GT_ERR_UNSUPPORTED), (1, 40, (1 << 20) - 4096, 8, gt.GT_OK),
     (1, 8, 1 << 18, 256, gt.GT_ERR_UNSUPPORTED), (1, 8, (1 << 18) - 4096, 256, gt.GT_OK)])
