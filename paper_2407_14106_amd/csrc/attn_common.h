@@ -13,6 +13,11 @@ constexpr float kLn2 = 0.6931471805599453f;
 // exp2 as the hardware gives it (v_exp_f32: results below 2^-126 become 0).
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// A row's LSE in the exp2 domain.  A row that attends to nothing (LSE -inf) has
+// no score but -inf, and any finite number below those gives weights of zero;
+// -inf would give NaN.
+__device__ __forceinline__ float lse_exp2(float lse) { return lse == -__builtin_huge_valf() ? 0.f : lse * kLog2e; }
+
 // Lane layout of the edge kernels: each (node, head) is owned by L = D / F
 // consecutive lanes, each holding F features (32 bytes; 64 of fp32 where the
 // node's features would not fit one wavefront otherwise), which keeps the

@@ -1215,7 +1215,7 @@ __global__ __launch_bounds__(T * 2 / NB) __attribute__((amdgpu_waves_per_eu(NB >
         const int64_t q = q0 + 32 * b + (lane & 31);
         qf[b].load(Q, q, n, H, h, lane);
         gf[b].load(dO, q, n, H, h, lane);
-        lse2[b] = q < n ? LSE[q * H + h] * kLog2e : 0.f;
+        lse2[b] = q < n ? lse_exp2(LSE[q * H + h]) : 0.f;
     }
     f32x16_t accA[NB][D / 32], accB[NB][D / 32];
     float dsum[NB];
@@ -1427,7 +1427,7 @@ __global__ __launch_bounds__(T * 2 / NB) __attribute__((amdgpu_waves_per_eu(NB >
         if (wave == 0) {
             stat = make_float2(__builtin_huge_valf(), 0.f);  // queries >= n take no weight
             const int64_t qn = qbase + lane;
-            if (qn < n) stat = make_float2(LSE[qn * H + h] * kLog2e, Dv[qn * H + h]);
+            if (qn < n) stat = make_float2(lse_exp2(LSE[qn * H + h]), Dv[qn * H + h]);
         }
         Tl::template fetch<kWaves>(nQ, Q, qbase, n, H, h, wave, lane);
         Tl::template fetch<kWaves>(nG, dO, qbase, n, H, h, wave, lane);

@@ -929,7 +929,7 @@ __attribute__((amdgpu_waves_per_eu(kBias && kEdgeWaves<T, D, H> > 2 ? kEdgeWaves
     SliceOf<T, D, H> q, g;
     q.load(Q + off);
     g.load(dO + off);
-    const float lse2 = LSE[i * H + ln.h] * kLog2e;
+    const float lse2 = lse_exp2(LSE[i * H + ln.h]);
     RowSums<C::F> rs;
     auto begin = [&] {
         rs = RowSums<C::F>();
@@ -1284,7 +1284,7 @@ __global__ __launch_bounds__(kThreads) void k_bwd_rows_long_merge(LongRows lr, i
                                 fmaf(-d, b.w, a.w) * scale));
     if (4 * q % D == 0) {
         if (Dv) Dv[i * H + h] = d;
-        if (stat) stat[i * H + h] = make_float2(LSE[i * H + h] * kLog2e, d);
+        if (stat) stat[i * H + h] = make_float2(lse_exp2(LSE[i * H + h]), d);
     }
 }
 
@@ -1329,7 +1329,7 @@ __global__ __launch_bounds__(kThreads) void k_bwd_cols_long_merge(LongRows lr, i
 __global__ void k_pack_stats(int64_t m, const float* __restrict__ LSE, const float* __restrict__ Dv,
                              float2* __restrict__ out) {
     for (int64_t x = blockIdx.x * int64_t(blockDim.x) + threadIdx.x; x < m; x += int64_t(gridDim.x) * blockDim.x)
-        out[x] = make_float2(LSE[x] * kLog2e, Dv[x]);
+        out[x] = make_float2(lse_exp2(LSE[x]), Dv[x]);
 }
 
 // ------------------------------------------------------------ gather probe

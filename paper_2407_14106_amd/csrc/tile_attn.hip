@@ -398,7 +398,7 @@ __global__ __launch_bounds__(2 * TT) void k_tile_dq(int64_t n, const int64_t* __
     RowFrag<T, D> qf, gf;
     qf.load(Q + (q * H + h) * D, qok, lane);
     gf.load(dO + (q * H + h) * D, qok, lane);
-    const float lse2 = qok ? LSE[q * H + h] * kLog2e : 0.f;
+    const float lse2 = qok ? lse_exp2(LSE[q * H + h]) : 0.f;
     float Dq = 0.f;
     if (kFull) {
         RowFrag<T, D> of;
@@ -539,7 +539,7 @@ __global__ __launch_bounds__(2 * TT) void k_tile_dkdv(int64_t n, const int64_t* 
         stage<T, D, H, TT, NT>(sG, sGt, dO, qbase, n, h);
         for (int r = threadIdx.x; r < TT; r += NT) {
             const int64_t qn = qbase + r;
-            sL[r] = qn < n ? LSE[qn * H + h] * kLog2e : 0.f;
+            sL[r] = qn < n ? lse_exp2(LSE[qn * H + h]) : 0.f;
             sD[r] = qn < n ? Dv[qn * H + h] : 0.f;
         }
         if (!kFull)
