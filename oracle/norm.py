@@ -93,3 +93,24 @@ def block(x, f, *, w_post=None, b_post=None, w_pre=None, b_pre=None, gate=None, 
 def sums(err, v):
     """The bound of a column's fp32 sum: its terms', and the additions' (chains of at most 4,096)."""
     return err.sum(axis=0) + (min(v.shape[0], 4096) + 4) * 2.0 ** -24 * np.abs(v).sum(axis=0)
+
+
+# What fp32 adds to a whole row (or a parameter's gradient), in its size.  A result is six stages from the inputs (f's
+# norm, y, y's norm, t, du and df, or a product with one of them), each at most eight roundings and a row's mean of at
+# most 32 dependent additions: 40 half steps of its operands' size.  A norm's Jacobian is a projection over the spread,
+# so what a stage takes over is not enlarged but by the weights, gates and scales, which stay within a factor of four
+# for parameters around one: 6 * 40 * 4 * 2^-24 < 2^-14.
+ROW = 2.0 ** -14
+
+
+def normwise(got, ref, half):
+    """Each result's largest error over its tolerance: a row of y, z, dx, df (and of a gradient of the gate's rows)
+    against ROW and its rounding, a parameter's gradient as a whole against ROW times the root of the rows' number (a
+    sum of n terms of random sign is that much smaller than its terms).  Above 1 is outside."""
+    n = len(ref["y"])
+    out = {}
+    for name, r in ref.items():
+        x = np.asarray(got[name], dtype=np.float64)
+        tol = half + ROW if r.ndim == 2 else ROW * np.sqrt(n)
+        out[name] = float((np.linalg.norm(x - r, axis=-1) / (tol * np.linalg.norm(r, axis=-1))).max())
+    return out

@@ -106,6 +106,49 @@ def test_rows_larger_than_the_last_level_cache(gt, dtype, D):
         assert all(torch.equal(grads[k][part], b[k]) for k in range(3))
 
 
+def run(gt, x, f, dy, dz, p, dtype, kind, gate, res_scale=0.75, eps=1e-5):
+    """The results of both calls by name, None left out."""
+    dev = {k: dev_feat(v, dtype) if v.ndim == 2 else torch.from_numpy(v).cuda() for k, v in p.items()}
+    X, F, dY, dZ = (dev_feat(v, dtype) for v in (x, f, dy, dz))
+    args = dict(sigmoid=gate == "sigmoid", res_scale=res_scale, kind=kind, eps=eps, **dev)
+    y, z, stats = gt.block_norm_fwd(X, F, **args)
+    got = dict(zip(FWD + BWD, (y, z) + gt.block_norm_bwd(X, F, stats, dY, dZ, **args)))
+    torch.cuda.synchronize()
+    return {k: v for k, v in got.items() if v is not None}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("gate", ["none", "vector", "rows", "sigmoid"])
+@pytest.mark.parametrize("D", [8, 40, 64, 100, 128, 256, 511, 512, 513, 1000, 1023, 1024, 1536, 2048, 2050, 4096, 4100,
+                               8190, 8191, 8192])
+def test_results_normwise(gt, dtype, kind, gate, D):
+    # elementwise bounds of whole chains say little about gradients of wide rows: row by row in their size
+    say("normwise", D, dtype, kind, gate)
+    x, f, dy, dz, p = make(37 if D < 2048 else 9, D, dtype, gate, seed=D)
+    got = run(gt, x, f, dy, dz, p, dtype, kind, gate)
+    r, _ = ON.block(x, f, sigmoid=gate == "sigmoid", res_scale=0.75, layer=kind == "layer", eps=float(np.float32(1e-5)),
+                    dy=dy, dz=dz, **p)
+    assert set(got) == set(r)
+    over = ON.normwise({k: host(v) for k, v in got.items()}, r, HALF[dtype])
+    assert max(over.values()) <= 1, over
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,D", [(70_001, 24), (40_003, 64), (35_001, 200), (9_001, 1024), (9_001, 511), (2_100, 4096),
+                                 (2_100, 8191)])
+def test_every_row_counts_once(gt, dtype, n, D):
+    # whole numbers, whose sums are exact in any order: a row lost or added twice in many rounds of the grid shows
+    rng = np.random.default_rng(n + D)
+    dy, dz = (rng.integers(-2, 3, size=(n, D)).astype(np.float32) for _ in range(2))
+    x, f, _, _, p = make(n, D, dtype, "none", seed=D)
+    p["w_pre"][:] = 0  # dz does not reach y: the gradient of y is dy
+    got = run(gt, x, f, dy, dz, p, dtype, "layer", "none", res_scale=2.0)
+    assert np.array_equal(host(got["db_pre"]), dz.sum(axis=0, dtype=np.float64))
+    assert np.array_equal(host(got["db_post"]), dy.sum(axis=0, dtype=np.float64))
+    assert np.array_equal(host(got["dx"]), 2.0 * dy)
+
+
 def test_no_rows_and_views(gt):
     e = torch.zeros(0, 64, dtype=torch.bfloat16, device="cuda")
     w = torch.ones(64, device="cuda")
