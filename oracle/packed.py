@@ -155,3 +155,20 @@ def bucket_bias_grad(bucket, dbias, B):
     for b in range(B):
         out[b] = dbias[bucket == b].astype(np.float64).sum(axis=0)
     return out
+
+
+def normwise(got, ref, half, most):
+    """The error of O, dQ, dK and dV as whole arrays over their tolerance (above 1 is outside): the elementwise bounds
+    add a row's terms as absolute values, which for rows of hundreds of partners is a large part of the result.
+
+    A half step for the weights or score gradients where they multiply, one for the result, and one for what a rounded O
+    does to D (which moves a gradient by less than that of its size: it is multiplied by a mean of K or Q, smaller than
+    the gradient by the root of the partners' number).  In fp32 besides, over rows of at most `most` partners and d
+    features: 4 (most + d) half steps of 2^-24 for the sums and the scores."""
+    out = {}
+    for name in ("O", "dQ", "dK", "dV"):
+        if name in ref:
+            r = ref[name]
+            tol = 3 * half + 4 * (most + r.shape[2]) * 2.0 ** -24
+            out[name] = float(np.linalg.norm(np.asarray(got[name], dtype=np.float64) - r) / (tol * np.linalg.norm(r)))
+    return out

@@ -211,6 +211,64 @@ def test_long_sequences_of_many_heads(gt, dtype, d, H, causal, B):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B", [0, 9])
+@pytest.mark.parametrize("lq,lk,H,Hkv,d,causal", [
+    ([1200, 3, 800], [1200, 2500, 700], 2, 1, 64, False), ([1200, 3, 800], [1200, 2500, 700], 2, 1, 64, True),
+    ([1], [9001], 8, 8, 32, False), ([1, 2], [5003, 4096], 16, 2, 128, True), ([100, 7], [4500, 9], 1, 1, 32, False),
+    ([4500, 3], [100, 200], 1, 1, 64, False), ([700], [2500], 4, 4, 128, True), ([300] * 24, [300] * 24, 8, 8, 32, True),
+    ([45] * 200, [45] * 200, 4, 4, 64, False), ([24] * 400, [24] * 400, 4, 4, 32, False), ([60] * 150, [60] * 150, 8, 8, 32, False)])
+def test_results_normwise(gt, dtype, B, lq, lk, H, Hkv, d, causal):
+    # whole arrays in their size, over long, split, mid-sized and small sequences (the elementwise bounds add the terms of
+    # a row as absolute values)
+    say("normwise", len(lq), lq[0], lk[0], H, Hkv, d, dtype, causal, B)
+    inputs = make(lq, lk, H, Hkv, d, dtype, B, seed=d + B)
+    scale = 1.0 / np.sqrt(d)
+    out = run(gt, lq, lk, H, Hkv, d, dtype, causal, inputs, scale)
+    q, k, v, do, table, ids = inputs
+    r, _ = OP.attn(ptrs(lq), ptrs(lk), q, k, v, np.float32(scale).astype(np.float64), causal, table, ids, do, HALF[dtype])
+    got = {name: host(x) for name, x in zip(("O", "LSE", "dQ", "dK", "dV"), out)}
+    over = OP.normwise(got, r, HALF[dtype], max(max(lk), max(lq) * (H // Hkv)))
+    say("   ", over)
+    assert len(over) == 4 and max(over.values()) <= 1, over
+
+
+@pytest.mark.parametrize("dtype,d,causal,B", [("bf16", 32, False, 0), ("bf16", 64, False, 0), ("bf16", 128, False, 0),
+                                              ("f32", 32, False, 0), ("f32", 64, True, 0), ("f32", 128, False, 0),
+                                              ("bf16", 64, False, 5), ("bf16", 128, True, 64), ("f32", 64, False, 64),
+                                              ("bf16", 64, True, 0)])
+def test_long_sequences_of_many_heads_normwise(gt, dtype, d, causal, B):
+    """The largest tiles: every head's results as whole arrays, against a plain implementation in 64 bits on the GPU."""
+    lens, H = [2333, 2304], 32
+    say("large, normwise", dtype, d, causal, B)
+    p, scale = ptrs(lens), float(np.float32(1.0 / np.sqrt(d)))
+    inputs = make(lens, lens, H, H, d, dtype, B, seed=d + B)
+    out = run(gt, lens, lens, H, H, d, dtype, causal, inputs, scale)
+    table, ids = inputs[4:]
+    for h in (0, 7, H - 1):
+        ref = [torch.empty(sum(lens), d, dtype=torch.float64, device="cuda") for _ in range(4)]
+        for s, n in enumerate(lens):
+            sl = slice(int(p[s]), int(p[s + 1]))
+            Q, K, V, G = (torch.from_numpy(x[sl, h]).cuda().double() for x in inputs[:4])
+            sc = scale * (Q @ K.t())
+            if B:
+                more = torch.full((256,), -np.inf, dtype=torch.float64, device="cuda")
+                more[:B] = torch.from_numpy(table[:, h]).cuda()
+                sc = sc + more[torch.from_numpy(OP.pair_buckets(ids, lens, lens, s)).cuda()]
+            if causal:
+                sc = sc.masked_fill(torch.ones_like(sc, dtype=torch.bool).triu(1), -np.inf)
+            # a causal row's only keys may all lie beyond the table
+            P = torch.nan_to_num(torch.softmax(sc, -1))
+            dP = G @ V.t()
+            dS = P * (dP - (P * dP).sum(-1, keepdim=True))
+            for x, r in zip(ref, (P @ V, scale * dS @ K, scale * dS.t() @ Q, P.t() @ G)):
+                x[sl] = r
+        got = dict(zip(("O", "dQ", "dK", "dV"), (host(out[k])[:, h:h + 1] for k in (0, 2, 3, 4))))
+        over = OP.normwise(got, dict(zip(got, (x.cpu().numpy()[:, None] for x in ref))), HALF[dtype], max(lens))
+        say("   ", over)
+        assert max(over.values()) <= 1, (h, over)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("scale", [-0.3, 0.0, 2.5])
 def test_any_scale(gt, dtype, scale):
     compare(gt, [70], [90], 2, 2, 32, dtype, True, scale=scale)

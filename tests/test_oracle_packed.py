@@ -100,3 +100,46 @@ def test_norm_by_hand():
     o, _ = ON.block(np.array([[1.0, 1.0]]), np.array([[3.0, 4.0]]), res_scale=2.0, layer=False, eps=0.0)
     np.testing.assert_allclose(o["y"], 2 + np.array([[3.0, 4.0]]) / np.sqrt(12.5))
     np.testing.assert_allclose((o["z"] ** 2).mean(), 1.0)
+
+
+def _rounded(lq, lk, H, d, dtype, causal, no_d=False, seed=5):
+    """One pass with the roundings of the features' type (weights and score gradients where they multiply, O, results;
+    fp32 arithmetic for fp32) and D = <dO, O> of the rounded O, or none; and the oracle's."""
+    from synth.tensors import bf16_round, normal_tensor
+
+    half, t = (2.0 ** -8, np.float64) if dtype == "bf16" else (2.0 ** -24, np.float32)
+    rnd = bf16_round if dtype == "bf16" else (lambda x: x.astype(np.float32))
+    q, k, v, do = (normal_tensor((n, H, d), (seed, i), dtype).astype(t) for i, n in enumerate((lq, lk, lk, lq)))
+    scale = t(1 / np.sqrt(d))
+    ref, _ = OP.attn([0, lq], [0, lk], q, k, v, float(scale), causal, dO=do)
+    got = {n: np.zeros(ref[n].shape) for n in ("O", "dQ", "dK", "dV")}
+    far = np.arange(lk)[None, :] > np.arange(lq)[:, None] + lk - lq if causal else np.zeros((lq, lk), dtype=bool)
+    for h in range(H):
+        Q, K, V, G = (x[:, h] for x in (q, k, v, do))
+        s = np.where(far, -np.inf, scale * (Q @ K.T))
+        p = np.exp(s - s.max(1, keepdims=True))
+        p /= p.sum(1, keepdims=True)
+        O = got["O"][:, h] = rnd(rnd(p) @ V)
+        D = 0 if no_d else (G * O.astype(t)).sum(1, keepdims=True)
+        ds = rnd(p * (G @ V.T - D)).astype(t)
+        got["dQ"][:, h], got["dK"][:, h] = rnd(scale * (ds @ K)), rnd(scale * (ds.T @ Q))
+        got["dV"][:, h] = rnd(rnd(p).astype(t).T @ G)
+    return OP.normwise(got, ref, half, max(lq, lk))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lq,lk,d,causal", [(1200, 1200, 64, False), (1200, 1200, 64, True), (700, 2500, 128, True),
+                                            (300, 300, 32, False)])
+def test_a_backward_without_its_correction_is_outside(dtype, lq, lk, d, causal):
+    inside = _rounded(lq, lk, 2, d, dtype, causal)
+    assert len(inside) == 4 and max(inside.values()) < 1, inside
+    over = _rounded(lq, lk, 2, d, dtype, causal, no_d=True)
+    assert over["dQ"] > 1 and over["dK"] > 1, over
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_single_query_without_its_correction_is_outside(dtype):
+    assert max(_rounded(1, 9001, 8, 32, dtype, False).values()) < 1
+    over = _rounded(1, 9001, 8, 32, dtype, False, no_d=True)
+    # dK_j is dS_j q alone: without D it is off by the root of 1 / 9,001 of its size, 0.0105, where bf16 allows 3 * 2^-8
+    assert over["dQ"] > 1 and (over["dK"] > 1 or dtype == "bf16"), over
