@@ -475,6 +475,19 @@ def test_edge_bias_larger_than_the_last_level_cache(gt, H, nnz):
     assert ((dt - ref).abs() <= (4 * nnz / 65536 + 4096) * 2.0 ** -24 * ref.abs()).all()
 
 
+@pytest.mark.parametrize("H,nnz,B", [(16, 4_300_003, 21), (8, 9_000_001, 64), (1, 68_000_001, 21), (2, 3_000_017, 1)])
+def test_every_edge_counts_once(gt, H, nnz, B):
+    # whole numbers whose sums stay below 2^24, exact in any order: an edge lost or added twice in many rounds of the grid
+    # shows
+    g = torch.Generator(device="cuda").manual_seed(nnz)
+    ids = torch.randint(0, B + 1, (nnz,), dtype=torch.uint8, device="cuda", generator=g)  # one bucket more than the table's
+    grad = torch.randint(-2, 4, (nnz, H), device="cuda", generator=g, dtype=torch.int8)
+    dt = gt.bucket_bias_bwd(ids, grad.float(), B)
+    want = torch.stack([torch.bincount(ids, weights=grad[:, h].double(), minlength=B)[:B] for h in range(H)], 1)
+    most = torch.bincount(ids, minlength=B)[:B].max() * 3
+    assert most < 2 ** 24 and torch.equal(dt.double(), want)
+
+
 def test_edge_bias_on_views_that_start_anywhere(gt):
     rng = np.random.default_rng(1)
     ids = torch.from_numpy(rng.integers(0, 5, size=1003).astype(np.uint8)).cuda()[3:]
