@@ -482,7 +482,9 @@ gt_status gt_packed_attn_fwd(const gt_packed_plan* plan, int32_t d, gt_dtype dty
 /* Backward from O and LSE of the forward, with the formulas of
  * gt_dense_attn_bwd (D_i = <dO_i, O_i>, or for rows of few keys, whose D_i a
  * rounded O would spoil, from their weights); dK and dV sum over the query heads
- * that share a kv head.  No atomics: results are the same run to run. */
+ * that share a kv head.  O and LSE are over the sequence's own keys: small
+ * sequences and the bias calls normalise the weights again, so an LSE merged with
+ * other keys' is not taken.  No atomics: results are the same run to run. */
 size_t gt_packed_attn_bwd_workspace_size(const gt_packed_plan* plan, int32_t d, gt_dtype dtype);
 gt_status gt_packed_attn_bwd(const gt_packed_plan* plan, int32_t d, gt_dtype dtype, const void* Q, int64_t ldq,
                              const void* K, int64_t ldk, const void* V, int64_t ldv, const void* O, const void* dO,
@@ -520,7 +522,8 @@ gt_status gt_packed_attn_bwd_bias(const gt_packed_plan* plan, int32_t d, gt_dtyp
 /* The same learned bias on the edges of a sparse layer: the per-edge bias that
  * gt_sparse_attn_*_bias take, and the table's gradient from their dbias.
  *   fwd: bias[e, h] = table[bucket[e], h], -inf (the edge is not attended to)
- *        where bucket[e] >= n_buckets;
+ *        where bucket[e] >= n_buckets (an entry that is to take edges out is
+ *        -inf, see the range of a bias there);
  *   bwd: dtable[b, h] = sum of dbias[e, h] over the edges in bucket b (fixed
  *        order of additions: the same run to run).
  * bucket uint8[nnz] and bias, dbias fp32 [nnz, H] in the CSR's edge order;

@@ -276,8 +276,8 @@ struct Params {
 //   df = rf (du w1 - <du w1> - fh <du w1 fh>)
 // (without the <dz w2> and <du w1> terms for the root mean square).
 // Rows of 512 lanes hold 16 columns a lane, whose parameters and sums do not fit the
-// registers together: the parameters lie in LDS (8,192 columns bf16: 805 us for
-// 32,768 rows against 1632 with spilled registers).
+// registers together: the parameters lie in LDS (32,768 rows of 8,192 in bf16, a gate
+// vector, all parameters: 808 us against 1632 with spilled registers).
 template <typename T, int LPR, int NV, Rows R>
 __global__ __launch_bounds__(RowSum<LPR>::kThreads) void k_norm_bwd(NormArgs a) {
     using C = Cols<T, LPR, NV, R>;
@@ -411,9 +411,11 @@ __global__ __launch_bounds__(1024) void k_norm_sum(int blocks, int D, const floa
     out[x] = t;
 }
 
-// Lanes per row and pieces per lane: the fewest lanes that hold a row at one
-// piece each, and two a lane where a row would only just leave a wavefront (or
-// a workgroup of 256 or 512).
+// Lanes per row and pieces per lane: the fewest lanes, but no fewer than 8, that
+// hold a row at one piece each, and two a lane where a row would only just leave a
+// wavefront (or a workgroup of 256 or 512).  Rows of 1 to 4 pieces leave half to
+// seven eighths of their lanes without data: 2M rows of 8, 16, 32 and 64 columns in
+// bf16 take 120, 127, 140 and 208 us forward (1.1, 2.0, 3.7 and 4.9 TB/s).
 #define GT_NORM_SHAPE(pieces, CALL)                 \
     do {                                            \
         if ((pieces) <= 8) { CALL(8, 1); }          \

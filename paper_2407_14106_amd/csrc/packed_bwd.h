@@ -18,7 +18,8 @@ __device__ __forceinline__ void add_block(float* col, const uint4& ids, int B, c
 // wavefront from one reading of Q, K, V and dO: the weights P and dS of the one
 // block, D from them, dQ; then the two turned round through LDS, dV and dK.
 // With a bias a wavefront keeps to one head and goes through its sequences, its
-// part of the table's gradient in LDS.  Bound as the forward: 4,000 molecules 94 us.
+// part of the table's gradient in LDS (56 KB a workgroup at 21 buckets: two a CU, so
+// two wavefronts a SIMD, which wait 56% of their time).  4,000 molecules 94 us.
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave)
     __attribute__((amdgpu_waves_per_eu(D * int(sizeof(T)) <= 64 ? 3 : D * int(sizeof(T)) <= 128 ? 2 : 1))) void k_pair_bwd(PackedArgs a) {
@@ -159,8 +160,9 @@ enum RowPass { kStat, kGrad };
 // stage form D_i from their weights (causal sequences of up to 275, dQ's and dK's
 // error 0.0026 -> 0.0023 of their size).
 // Bound by the matrix cores: four causal prompts of up to 4,096 (16 / 4 heads of 64)
-// 95 us, 840 TFLOP/s of its three products; with a bias by the table's gradient (16
-// graphs of up to 1,000: 55 us, kStat 38).
+// 89 us, 895 TFLOP/s of its three products; with a bias by waiting (46% of the
+// wavefronts' time, at two a SIMD; the LDS instructions, most of them the table's
+// gradient's, take 9%): 16 graphs of up to 1,000 51 us, kStat 36.
 // kStat (before it, with a bias): D_i = sum_j P_ij dP_ij from the scores, since a
 // bf16 O is off by 2^-8, which moves the table's gradient (fp32) by as much,
 // and the weights' sum under the given LSE: an fp32 LSE beside a large bias
@@ -374,8 +376,8 @@ enum KeyPass { kBoth, kOnlyV, kOnlyK };
 // dK_j = scale sum_i dS_ij Q_i and dV_j = sum_i P_ij dO_i over the rows of the
 // whole group, with the wavefront owning 32 keys and the rows streaming through
 // LDS; the dP products start from the rows' -D_i.  Bound by the matrix cores and a
-// barrier a stage: four causal prompts of up to 4,096 (16 / 4 heads of 64) 146 us,
-// 730 TFLOP/s of its four products; with a bias (16 graphs of up to 1,000) 57 us.
+// barrier a stage: four causal prompts of up to 4,096 (16 / 4 heads of 64) 133 us,
+// 800 TFLOP/s of its four products; with a bias (16 graphs of up to 1,000) 52 us.
 template <typename T, int D, int STAGE, int W, int KS, int SUB, bool BIAS, KeyPass PASS>
 __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
     PASS != kBoth || D * int(sizeof(T)) <= 128 ? waves_per_simd(KS * 4 * STAGE * D * int(sizeof(T)), W* KS) : 1))) void k_packed_keys(PackedArgs a) {

@@ -10,7 +10,7 @@ namespace {
 // Pairs: a sequence of at most 32 rows and 32 keys is one block, done by one
 // wavefront with nothing shared.  Bound by reading and writing the features and by
 // the block's chain of waits, which more wavefronts hide: 4,000 molecules of 23 to 26
-// nodes, 8 heads of 32, with a bias, 45 us (133 MB).
+// nodes, 8 heads of 32, with a bias, 46 us (133 MB).
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair_fwd(PackedArgs a) {
     using B = Blk<T, D>;
@@ -86,10 +86,11 @@ __global__ __launch_bounds__(pair_waves(D * int(sizeof(T))) * kWave) void k_pair
 // natural domain (a bias of the type's lowest value times log2 e would overflow
 // to -inf).
 // Bound by the matrix cores, then the exponentials: 8,192 x 16 heads bf16 at 950
-// (64 wide) and 1,000 TFLOP/s (128), four causal prompts of up to 6,000 (16 / 4
-// heads of 128) 208 us, 910 TFLOP/s.  Few rows are bound by reading K and V: 16
-// tokens over up to 65,536 keys 290 us, 4.9 TB/s.  With a bias by its vector work
-// (16 graphs of up to 1,000, 8 heads of 64: 39 us).
+// (64 wide) and 1,025 TFLOP/s (128), four causal prompts of up to 6,000 (16 / 4
+// heads of 128) 206 us, 920 TFLOP/s.  Few rows are bound by reading K and V: 16
+// tokens over up to 65,536 keys 293 us, 4.85 TB/s.  With a bias by waiting (38% of
+// the wavefronts' time, at two a SIMD) and its vector work (30%): 16 graphs of up to
+// 1,000, 8 heads of 64, 36 us.
 template <typename T, int D, int STAGE, int NB, int W, int KS, bool BIAS>
 __global__ __launch_bounds__(W * KS * kWave) __attribute__((amdgpu_waves_per_eu(
     waves_per_simd(KS * 4 * STAGE * D * int(sizeof(T)), W* KS)))) void k_packed_fwd(PackedArgs a) {

@@ -807,7 +807,7 @@ def packed_attn_fwd(plan: PackedPlan, Q: torch.Tensor, K: torch.Tensor, V: torch
 
 
 def packed_attn_bwd(plan: PackedPlan, Q, K, V, O, dO, LSE, scale: float | None = None):
-    """(dQ, dK, dV) of softmax attention inside each packed sequence."""
+    """(dQ, dK, dV) of softmax attention inside each packed sequence, from the O and LSE that packed_attn_fwd gave."""
     lib = load_library()
     d, dt, ldq, ldk, ldv = _check_packed(plan, Q, K, V)
     _check_contiguous(O, Q.shape, Q.dtype, Q.device, "O")
