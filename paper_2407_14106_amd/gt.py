@@ -695,10 +695,17 @@ class PackedPlan:
         self.c, self.items = c, items
         # what every call asks for, as plain values: a call over short sequences is bound by this binding
         self.ref, self.device, self._ws = ctypes.byref(c), items.device, {}
+        # the streams that items' memory is kept for: its own, and those that calls ran on
+        self._streams = {_stream(self.device)} if items.is_cuda else set()
         self.nq, self.nk, self.heads, self.kv_heads, self.pair_bytes = c.nq, c.nk, c.H, c.Hkv, c.pair_bytes
 
     def workspace(self, size, *args) -> torch.Tensor:
-        """A workspace for the call whose size query `size` takes (plan, *args)."""
+        """A workspace for the call whose size query `size` takes (plan, *args) on the current stream; the work list
+        stays allocated until that stream has gone through the call, also where the plan is dropped before."""
+        stream = _stream(self.device)
+        if stream not in self._streams:
+            self.items.record_stream(torch.cuda.current_stream(self.device))
+            self._streams.add(stream)
         key = (size.__name__, args)
         n = self._ws.get(key)
         if n is None:

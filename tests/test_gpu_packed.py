@@ -417,6 +417,50 @@ def test_same_results_again_and_on_another_stream(gt):
             assert all(torch.equal(x, y) for x, y in zip(a, b))
 
 
+@pytest.mark.parametrize("mode", ["forward", "backward", "bias forward", "bias backward"])
+def test_a_plan_dropped_while_another_stream_reads_it(gt, mode):
+    # the memory of a plan's work list is not handed out again while a call on another stream than the plan's may read it
+    lq = [70, 5, 200]
+    q, k, v, do, table, ids = make(lq, lq, 2, 2, 32, "bf16", 4)
+    Q, K, V, dO = (dev_feat(x, "bf16") for x in (q, k, v, do))
+    T, I = torch.from_numpy(table).cuda(), torch.from_numpy(ids).cuda()
+    plan = gt.packed_plan(ptrs(lq), heads=2)
+    O, L = gt.packed_attn_fwd(plan, Q, K, V)
+    Ob, Lb = gt.packed_attn_fwd_bias(plan, Q, K, V, T, I)
+    call = {"forward": lambda p: gt.packed_attn_fwd(p, Q, K, V),
+            "backward": lambda p: gt.packed_attn_bwd(p, Q, K, V, O, dO, L),
+            "bias forward": lambda p: gt.packed_attn_fwd_bias(p, Q, K, V, T, I),
+            "bias backward": lambda p: gt.packed_attn_bwd_bias(p, Q, K, V, T, I, dO, Lb)}[mode]
+    want = call(plan)
+    busy = torch.zeros(8192, 8192, dtype=torch.bfloat16, device="cuda")
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        busy @ busy
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(300):
+            busy @ busy
+        got = call(plan)
+    at, n = plan.items.data_ptr(), plan.items.numel()
+    del plan
+    blocks = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    assert not side.query(), "the stream ran empty: this says nothing"
+    assert all(x.data_ptr() != at for x in blocks)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("B", [0, 9])
+def test_sequences_without_keys_or_queries_beside_others(gt, dtype, d, causal, B):
+    # more rows (or keys) than a small sequence's, in every list of tiles, with nothing to walk
+    compare(gt, [100, 0, 70, 300, 0, 40, 1], [0, 100, 50, 0, 300, 0, 0], 2, 2, d, dtype, causal, B, seed=d)
+    compare(gt, [20, 0, 70, 300, 50] * 40, [0, 40, 50, 0, 60] * 40, 16, 4, d, dtype, causal, B, seed=d + 1)
+    compare(gt, [3000, 0], [0, 2600], 1, 1, d, dtype, causal, B, seed=d + 2)
+
+
 def test_captured_step_replays(gt):
     lq, H, d, B = [150, 30, 33], 4, 32, 6
     q, k, v, do, table, ids = make(lq, lq, H, 2, d, "bf16", B)
