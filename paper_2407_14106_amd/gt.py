@@ -724,7 +724,8 @@ def packed_plan(q_ptr, k_ptr=None, *, heads: int, kv_heads: int | None = None, c
                 device=None) -> PackedPlan:
     """Plan of attention over packed sequences: sequence s holds the queries q_ptr[s] to q_ptr[s + 1] - 1 and the
     keys k_ptr[s] to k_ptr[s + 1] - 1 (the same when k_ptr is not given).  The pointers may be lists or tensors
-    (one on the GPU is read back, which waits for it).  Built once per batch and kept for every layer."""
+    (one on the GPU is read back, which waits for it).  Built once per batch and kept for every layer, and as long as
+    a captured graph whose calls took it."""
     lib = load_library()
     if device is None:
         device = q_ptr.device if isinstance(q_ptr, torch.Tensor) and q_ptr.is_cuda else "cuda"
