@@ -360,7 +360,7 @@ gt_status gt_sparse_attn_bwd_cols(const gt_tiles* plan, int32_t H, int32_t d, gt
  * e the position of edge (i, j) in the input CSR the plan was built from, on
  * remainder edges and dense-tile edges alike; bias and dbias are fp32 [nnz, H]
  * device arrays (nnz = nnz_sparse + the dense tiles' edges, < 2^31).  An edge
- * whose bias is -inf (or below -2.3e38, whose product with log2 e is) is not
+ * whose bias is -inf (or below -2.36e38, whose product with log2 e is) is not
  * attended to and has no gradient; a row left with none gives O = 0 and
  * LSE = -inf.  The weights of the backward are off by about |LSE| 2^-23, so a
  * mask is -inf, not a large finite value on all of a row's edges.  The
