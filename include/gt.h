@@ -575,6 +575,72 @@ gt_status gt_block_norm_bwd(int64_t n, int32_t D, gt_dtype dtype, int32_t norm, 
                             const void* dz, void* dx, void* df, void* dgate, float* dw_post, float* db_post,
                             float* dw_pre, float* db_pre, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ------------------------------------------------------------------------ */
+/* The ends of a model and what its training adds: embedding, dropout, loss. */
+/* ------------------------------------------------------------------------ */
+/* ids and labels are int32 or int64 arrays. */
+typedef int32_t gt_itype;
+#define GT_I32 0
+#define GT_I64 1
+#define GT_MAX_WIDTH 65536 /* of the rows of the calls below */
+
+/* A model's input: the scaled sum of one row of a learned table for each of the F
+ * ids of a token or node (a vocabulary; a node's categorical features and the
+ * encodings of its degrees, as ranges of one table, §2.1),
+ *   out_i = scale * sum_f table[ids[i, f]],
+ * and the table's gradient dtable[r] = scale * (sum of dout_i over the (i, f) with
+ * ids[i, f] = r).  An id outside [0, R) adds nothing and has no gradient.
+ *   ids [n, F] in itype; table, dtable [R, D], out, dout [n, D] contiguous in dtype
+ *     (no alignment needed beyond the element's).
+ * Sums in fp32, rounded once; the gradient goes by the sorted ids, a row's terms
+ * added in an order that the ids alone give (the same run to run), and every row of
+ * dtable is written.  1 <= D <= GT_MAX_WIDTH, 1 <= R < 2^31, 0 <= n, n F < 2^31. */
+gt_status gt_embed_fwd(int64_t n, int32_t F, int64_t R, int32_t D, gt_dtype dtype, gt_itype itype, const void* ids,
+                       const void* table, float scale, void* out, hipStream_t stream);
+size_t gt_embed_bwd_workspace_size(int64_t n, int32_t F, int64_t R, int32_t D, gt_dtype dtype);
+gt_status gt_embed_bwd(int64_t n, int32_t F, int64_t R, int32_t D, gt_dtype dtype, gt_itype itype, const void* ids,
+                       const void* dout, float scale, void* dtable, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Dropout of n elements from a counter-based generator, whose mask is never stored,
+ *   y_i = (add_i +) (w_i >= T ? x_i / (1 - p) : 0),  T = round(p 2^32),
+ * w_i word i % 4 of Philox4x32-10 with key rng[0] at counter rng[1] + i / 4 (mod 2^64,
+ * the counter's high 64 bits zero).  The same call on dy (without add) is the backward.
+ *   rng uint64[2] on the device: read when the call runs, so a captured call takes new
+ *     numbers from what lies there at its replay; a caller's next call that is to draw
+ *     others moves rng[1] on by at least (n + 3) / 4;
+ *   x, add, y in dtype (no alignment needed beyond the element's); add may be NULL;
+ *     y may be x or add.
+ * 0 <= p < 1 (a p whose T is 2^32 is refused), 0 <= n < 2^48. */
+gt_status gt_dropout(int64_t n, gt_dtype dtype, double p, const uint64_t* rng, const void* x, const void* add, void* y,
+                     hipStream_t stream);
+
+/* Softmax cross entropy over V classes (node or graph classes, a vocabulary) from the
+ * last features X [n, D] and the class weights W [V, D], without keeping the logits
+ * s_iv = <X_i, W_v>:
+ *   lse_i = log sum_v exp(s_iv),  loss_i = lse_i - s_i,y(i);
+ * and for the gradient dloss_i of each row's loss (a mean over m rows: 1 / m)
+ *   dL_iv = dloss_i (exp(s_iv - lse_i) - [v = y(i)]),
+ *   dX_i = sum_v dL_iv W_v,  dW_v = sum_i dL_iv X_i.
+ * A row whose label lies outside [0, V) (an unlabelled node, a prompt's token) takes no
+ * part: loss 0, lse 0, dX 0, and its products are not formed.
+ *   labels [n] in itype; loss, lse, dloss fp32 [n]; dX [n, D], dW [V, D] contiguous in
+ *     dtype, either may be NULL (not wanted);
+ *   X and W start at multiples of 16 bytes (GT_ERR_UNSUPPORTED otherwise) with any
+ *     strides ldx, ldw >= D elements between rows; rows whose stride or width is no
+ *     multiple of 16 or 128 bytes are laid out once in the workspace.
+ * GT_F32 multiplies and adds in fp32.  GT_BF16: logits, statistics and sums in fp32;
+ * dL is rounded to bf16 where it multiplies a bf16 row (a relative error of at most
+ * 2^-8 a term), dX and dW once at the end.  Sums in a fixed order.  Features are finite.
+ * 0 <= n < 2^31, 1 <= V < 2^31, 1 <= D <= GT_MAX_WIDTH. */
+size_t gt_class_loss_fwd_workspace_size(int64_t n, int64_t V, int32_t D, gt_dtype dtype, int64_t ldx, int64_t ldw);
+gt_status gt_class_loss_fwd(int64_t n, int64_t V, int32_t D, gt_dtype dtype, gt_itype itype, const void* X, int64_t ldx,
+                            const void* W, int64_t ldw, const void* labels, float* loss, float* lse, void* ws,
+                            size_t ws_bytes, hipStream_t stream);
+size_t gt_class_loss_bwd_workspace_size(int64_t n, int64_t V, int32_t D, gt_dtype dtype, int64_t ldx, int64_t ldw);
+gt_status gt_class_loss_bwd(int64_t n, int64_t V, int32_t D, gt_dtype dtype, gt_itype itype, const void* X, int64_t ldx,
+                            const void* W, int64_t ldw, const void* labels, const float* lse, const float* dloss,
+                            void* dX, void* dW, void* ws, size_t ws_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -34,6 +34,8 @@ GT_LONG_ROW = 256
 GT_MAX_BUCKETS = 64
 GT_NORM_LAYER, GT_NORM_RMS = 0, 1
 GT_GATE_NONE, GT_GATE_VECTOR, GT_GATE_ROWS, GT_GATE_SIGMOID = 0, 1, 2, 3
+GT_I32, GT_I64 = 0, 1
+GT_MAX_WIDTH = 65536
 
 _i32, _i64, _u32, _u64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint64
 _vp, _sz, _f32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float
@@ -153,6 +155,15 @@ SIGNATURES = {
     "gt_block_norm_bwd_workspace_size": (_sz, [_i64, _i32, _i32]),
     "gt_block_norm_bwd": (_i32, [_i64, _i32, _i32, _i32, _vp, _f32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                  _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "gt_embed_fwd": (_i32, [_i64, _i32, _i64, _i32, _i32, _i32, _vp, _vp, _f32, _vp, _vp]),
+    "gt_embed_bwd_workspace_size": (_sz, [_i64, _i32, _i64, _i32, _i32]),
+    "gt_embed_bwd": (_i32, [_i64, _i32, _i64, _i32, _i32, _i32, _vp, _vp, _f32, _vp, _vp, _sz, _vp]),
+    "gt_dropout": (_i32, [_i64, _i32, _f64, _vp, _vp, _vp, _vp, _vp]),
+    "gt_class_loss_fwd_workspace_size": (_sz, [_i64, _i64, _i32, _i32, _i64, _i64]),
+    "gt_class_loss_fwd": (_i32, [_i64, _i64, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "gt_class_loss_bwd_workspace_size": (_sz, [_i64, _i64, _i32, _i32, _i64, _i64]),
+    "gt_class_loss_bwd": (_i32, [_i64, _i64, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _sz,
+                                 _vp]),
 }
 
 _LIB = None
@@ -966,3 +977,116 @@ def block_norm_bwd(x, f, stats, dy, dz, *, w_post=None, b_post=None, w_pre=None,
                                      _ptr(dz), _ptr(dx), _ptr(df), _ptr(dgate), *map(_ptr, grads), _ptr(ws),
                                      ws.numel(), _stream(x.device)), "gt_block_norm_bwd")
     return (dx, df, dgate, *grads)
+
+
+# ------------------------------------------------- embedding, dropout, loss
+
+_ITYPE_CODES = {torch.int32: GT_I32, torch.int64: GT_I64}
+
+
+def _itype_code(t: torch.Tensor, name: str) -> int:
+    code = _ITYPE_CODES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be int32 or int64")
+    return code
+
+
+def _check_ids(ids: torch.Tensor):
+    _need(ids.is_cuda and ids.dim() in (1, 2) and ids.is_contiguous(),
+          "ids must be a contiguous GPU tensor [n] or [n, F]")
+    n, F = (ids.shape[0], 1) if ids.dim() == 1 else ids.shape
+    _need(F >= 1, "ids must have at least one field")
+    return n, F, _itype_code(ids, "ids")
+
+
+def embed_fwd(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0) -> torch.Tensor:
+    """out [n, D] with out_i = scale * (sum over the fields f of table[ids[i, f]]); table [R, D], ids int32 or int64
+    [n] or [n, F].  An id outside [0, R) adds nothing."""
+    lib = load_library()
+    _need(table.is_cuda and table.dim() == 2 and table.is_contiguous(), "table must be a contiguous GPU tensor [R, D]")
+    n, F, it = _check_ids(ids)
+    _need(ids.device == table.device, "ids must be on the table's device")
+    R, D = table.shape
+    with _on(table.device):
+        out = torch.empty((n, D), dtype=table.dtype, device=table.device)
+        _check(lib.gt_embed_fwd(n, F, R, D, _dtype_code(table), it, _ptr(ids), _ptr(table), float(scale), _ptr(out),
+                                _stream(table.device)), "gt_embed_fwd")
+    return out
+
+
+def embed_bwd(ids: torch.Tensor, dout: torch.Tensor, n_rows: int, scale: float = 1.0) -> torch.Tensor:
+    """The table's gradient [n_rows, D] from dout [n, D] and the ids that embed_fwd took (zeros in rows that no id
+    names)."""
+    lib = load_library()
+    n, F, it = _check_ids(ids)
+    _need(dout.is_cuda and dout.dim() == 2 and dout.shape[0] == n and dout.is_contiguous() and dout.device == ids.device,
+          "dout must be a contiguous tensor [n, D] on the ids' device")
+    R, D, dt = int(n_rows), dout.shape[1], _dtype_code(dout)
+    _need(R >= 1, "n_rows must be positive")
+    with _on(dout.device):
+        dtable = torch.empty((R, D), dtype=dout.dtype, device=dout.device)
+        ws = _workspace(lib.gt_embed_bwd_workspace_size(n, F, R, D, dt), dout.device)
+        _check(lib.gt_embed_bwd(n, F, R, D, dt, it, _ptr(ids), _ptr(dout), float(scale), _ptr(dtable), _ptr(ws),
+                                ws.numel(), _stream(dout.device)), "gt_embed_bwd")
+    return dtable
+
+
+def dropout(x: torch.Tensor, p: float, rng: torch.Tensor, add: torch.Tensor | None = None) -> torch.Tensor:
+    """(add +) dropout of x, kept elements divided by 1 - p.  rng: int64 (or uint64) [2] on the GPU, the generator's
+    key and its first counter; the same rng draws the same numbers, so the call on the gradient (without add) is the
+    backward.  Move rng[1] on by (x.numel() + 3) // 4 or more before numbers that are to be others."""
+    lib = load_library()
+    _need(x.is_cuda and x.is_contiguous(), "x must be a contiguous GPU tensor")
+    _need(rng.dtype in (torch.int64, torch.uint64) and rng.shape == (2,) and rng.is_contiguous()
+          and rng.device == x.device, "rng must be a contiguous int64 or uint64 tensor [2] on x's device")
+    if add is not None:
+        _check_contiguous(add, x.shape, x.dtype, x.device, "add")
+    with _on(x.device):
+        y = torch.empty_like(x)
+        _check(lib.gt_dropout(x.numel(), _dtype_code(x), float(p), _ptr(rng), _ptr(x), _ptr(add), _ptr(y),
+                              _stream(x.device)), "gt_dropout")
+    return y
+
+
+def _check_loss(X, W, labels):
+    _need(X.is_cuda and X.dim() == 2 and W.dim() == 2 and X.shape[1] == W.shape[1] and X.dtype is W.dtype
+          and X.device == W.device, "X [n, D] and W [V, D] must be GPU tensors of one dtype and device")
+    n, D = X.shape
+    lds = []
+    for t in (X, W):
+        s = t.stride()
+        _need((D == 1 or s[1] == 1) and (t.shape[0] <= 1 or s[0] >= D), "the features of a row of X and W must be contiguous")
+        lds.append(s[0] if t.shape[0] > 1 else D)
+    _need(labels.shape == (n,) and labels.is_contiguous() and labels.device == X.device,
+          "labels must be a contiguous tensor [n] on the features' device")
+    return n, W.shape[0], D, _dtype_code(X), _itype_code(labels, "labels"), lds[0], lds[1]
+
+
+def class_loss_fwd(X: torch.Tensor, W: torch.Tensor, labels: torch.Tensor):
+    """(loss, lse), fp32 [n], of softmax cross entropy over the V classes whose logits are X W^T: X [n, D], W [V, D],
+    labels int32 or int64 [n].  A row whose label is outside [0, V) has loss 0 and lse 0."""
+    lib = load_library()
+    n, V, D, dt, it, ldx, ldw = _check_loss(X, W, labels)
+    with _on(X.device):
+        out = torch.empty((2, n), dtype=torch.float32, device=X.device)
+        loss, lse = out[0], out[1]
+        ws = _workspace(lib.gt_class_loss_fwd_workspace_size(n, V, D, dt, ldx, ldw), X.device)
+        _check(lib.gt_class_loss_fwd(n, V, D, dt, it, _ptr(X), ldx, _ptr(W), ldw, _ptr(labels), _ptr(loss), _ptr(lse),
+                                     _ptr(ws), ws.numel(), _stream(X.device)), "gt_class_loss_fwd")
+    return loss, lse
+
+
+def class_loss_bwd(X, W, labels, lse, dloss, want_dx: bool = True, want_dw: bool = True):
+    """(dX, dW) from the lse that class_loss_fwd gave and the gradient dloss (fp32 [n]) of each row's loss; None for
+    what is not wanted."""
+    lib = load_library()
+    n, V, D, dt, it, ldx, ldw = _check_loss(X, W, labels)
+    _check_contiguous(lse, (n,), torch.float32, X.device, "lse")
+    _check_contiguous(dloss, (n,), torch.float32, X.device, "dloss")
+    with _on(X.device):
+        dX = torch.empty((n, D), dtype=X.dtype, device=X.device) if want_dx else None
+        dW = torch.empty((V, D), dtype=X.dtype, device=X.device) if want_dw else None
+        ws = _workspace(lib.gt_class_loss_bwd_workspace_size(n, V, D, dt, ldx, ldw), X.device)
+        _check(lib.gt_class_loss_bwd(n, V, D, dt, it, _ptr(X), ldx, _ptr(W), ldw, _ptr(labels), _ptr(lse), _ptr(dloss),
+                                     _ptr(dX), _ptr(dW), _ptr(ws), ws.numel(), _stream(X.device)), "gt_class_loss_bwd")
+    return dX, dW
