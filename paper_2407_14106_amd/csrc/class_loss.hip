@@ -211,7 +211,7 @@ __device__ __forceinline__ void store4(T* p, float a, float b, float c, float d,
 template <typename T, int WHAT, int WM, int WN, int TM, int TN>
 __global__ __launch_bounds__(WM * WN * 64) void k_product(LossArgs a) {
     using G = GemmNT<T, WM, WN, TM, TN>;
-    __shared__ __attribute__((aligned(1024))) char s_buf[G::kLds];
+    __shared__ __attribute__((aligned(1024))) char s_buf[G::kStage], s_buf2[G::kStage];
     const int64_t N = a.n_count ? *a.n_count : a.N;
     int64_t bm, bn;
     if (!block_of(cdiv(a.M, G::BM), cdiv(N, G::BN), bm, bn)) return;
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_product(LossArgs a) {
     if (a.k_count) steps = cdiv(int64_t(*a.k_count) * int64_t(sizeof(T)), kStepBytes);
     const int64_t each = cdiv(steps, a.splits), s0 = int64_t(blockIdx.y) * each;
     G g;
-    g.run(s_buf, a.A, a.lda, m0, a.M, a.B, a.ldb, n0, N, a.rows, s0, s0 + each < steps ? s0 + each : steps);
+    g.run(s_buf, s_buf2, a.A, a.lda, m0, a.M, a.B, a.ldb, n0, N, a.rows, s0, s0 + each < steps ? s0 + each : steps);
 
     const int lane = lane_id(), wave = threadIdx.x / kWave, wm = wave % WM, wn = wave / WM;
     const int64_t mw = m0 + wm * TM * 32 + 4 * (lane >> 5);       // + 32 i + 8 (e / 4) + e % 4
