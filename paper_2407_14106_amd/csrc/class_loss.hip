@@ -4,8 +4,9 @@
 //   s_iv = <X_i, W_v>,  lse_i = log sum_v exp s_iv,  loss_i = lse_i - s_i,y(i),
 //   dL_iv = dloss_i (exp(s_iv - lse_i) - [v = y(i)]),  dX = dL W,  dW = dL^T X.
 //
-// Rows without a label take no part: the labelled rows are listed first (on the
-// device, in order), and every product runs over the list.
+// Rows without a label take no part: where there are more rows than a block takes, the
+// labelled ones are listed first (on the device, in order), and every product runs over
+// the list.
 //
 // Forward: the product s with the classes as its rows, so that a lane holds one
 // token and a block's classes: the block leaves (max, sum of exp) for each of its
@@ -17,6 +18,7 @@
 // Where a product has few blocks its sum is split over the grid and the parts are
 // added in order.  No atomics: results are the same run to run.
 #include "gemm_nt.h"
+#include "lanes.h"
 #include "rows.h"
 
 using namespace gt;
@@ -27,6 +29,11 @@ constexpr int kListThreads = 1024, kListRounds = 8, kListRows = kListThreads * k
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // of dL, one way round: the last-level cache
 constexpr int64_t kMinPiece = 1024;                  // classes
 constexpr int kSplitBlocks = 256;                    // blocks that fill the chip
+constexpr int64_t kGatherClasses = 2048;             // above, X's listed rows are laid out once: every block of
+                                                     // classes would read them through the list (3% of its time)
+constexpr int64_t kListed = 256;                     // up to so many rows none is left out: they are one block
+constexpr int64_t kOff = 64;                         // elements behind a row of a turned or dL array: rows whose
+                                                     // stride is a large power of two meet in few channels
 constexpr int kSplitSteps = 8;                       // of a split sum, at least
 
 constexpr float kNegInf = -__builtin_huge_valf();
@@ -106,7 +113,13 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_zero_rows(int64_t n, int D, int64_t V, bool wide, const void* labels, T* dx) {
     for (int64_t i = int64_t(blockIdx.x) * 4 + threadIdx.x / kWave; i < n; i += int64_t(gridDim.x) * 4) {
         if (load_id(labels, wide, i, V) >= 0) continue;
-        for (int c = lane_id(); c < D; c += kWave) dx[i * D + c] = T(0);
+        constexpr int E = Piece<T>::E;
+        if (D < E) {
+            if (lane_id() < D) dx[i * D + lane_id()] = T(0);
+            continue;
+        }
+        const float zero[E] = {};
+        for (int c = lane_id() * E; c < D; c += kWave * E) store_piece(dx + i * D + (c + E <= D ? c : D - E), zero, false);
     }
 }
 template <typename T>
@@ -116,33 +129,74 @@ __global__ __launch_bounds__(256) void k_zero(int64_t n, T* p) {
 
 // ------------------------------------------------------------------ layouts
 
-// dst[r][0 .. ldd) = src[r][0 .. C), zeros behind
+// dst[r][0 .. ldd) = src[r][0 .. C), zeros behind; rows through the list, if there is
+// one, count of them.  whole: both are whole 16-byte pieces.
 template <typename T>
-__global__ __launch_bounds__(256) void k_pad(int64_t R, int C, const T* src, int64_t lds, T* dst, int ldd) {
-    for (int64_t r = int64_t(blockIdx.x) * 4 + threadIdx.x / kWave; r < R; r += int64_t(gridDim.x) * 4)
-        for (int c = lane_id(); c < ldd; c += kWave) dst[r * ldd + c] = c < C ? src[r * lds + c] : T(0);
+__global__ __launch_bounds__(256) void k_pad(int64_t R, const int32_t* list, const int32_t* count, int C, const T* src,
+                                              int64_t lds, T* dst, int ldd, bool whole) {
+    constexpr int E = Piece<T>::E;
+    if (count) R = *count;
+    for (int64_t r = int64_t(blockIdx.x) * 4 + threadIdx.x / kWave; r < R; r += int64_t(gridDim.x) * 4) {
+        const T* from = src + (list ? int64_t(list[r]) : r) * lds;
+        if (whole)
+            for (int c = lane_id() * E; c < ldd; c += kWave * E)
+                *reinterpret_cast<uint4*>(dst + r * ldd + c) = *reinterpret_cast<const uint4*>(from + c);
+        else
+            for (int c = lane_id(); c < ldd; c += kWave) dst[r * ldd + c] = c < C ? from[c] : T(0);
+    }
 }
 
-// dst[c][r] = src[r][c], for r < R; zeros for R <= r < R rounded up to 64
+// dst[c][r] = src[r][c] for the rows r < R, zeros for R <= r < R rounded up to 64.
+// Rows through a list, or all of them, those without a label as zeros.  Source rows
+// are whole 16-byte pieces (zeros behind column C).
+struct Turn {
+    int64_t R;
+    const int32_t *count, *list;
+    const void* labels;  // or null
+    bool wide;
+    int64_t V;
+    const void* src;
+    int64_t lds;
+    void* dst;
+    int64_t ldd;
+};
+struct Turns {
+    Turn t[2];
+};
 template <typename T>
-__global__ __launch_bounds__(256) void k_turn(int64_t R, const int32_t* count, const int32_t* list, int C,
-                                               const T* src, int64_t lds, T* dst, int64_t ldd) {
-    __shared__ T s[64][65 + (sizeof(T) == 2)];
-    if (count) R = *count;
-    const int64_t r0 = int64_t(blockIdx.x) * 64;
+__global__ __launch_bounds__(256) void k_turn(Turns both, int C) {
+    constexpr int E = 16 / int(sizeof(T)), P = 64 / E;  // pieces of 64 elements
+    __shared__ T s[64][64 + 4 / sizeof(T)];
+    const Turn& a = both.t[blockIdx.z];
+    const int64_t R = a.count ? int64_t(*a.count) : a.R, r0 = int64_t(blockIdx.x) * 64;
     if (r0 >= R) return;
-    const int c0 = blockIdx.y * 64, x = threadIdx.x % 64, y = threadIdx.x / 64;
+    const int c0 = blockIdx.y * 64;
 #pragma unroll
-    for (int k = 0; k < 64; k += 4) {
-        const int64_t r = r0 + k + y;
-        T v = T(0);
-        if (r < R && c0 + x < C) v = src[(list ? int64_t(list[r]) : r) * lds + c0 + x];
-        s[k + y][x] = v;
+    for (int k = 0; k < 64 * P / 256; ++k) {
+        const int y = (k * 256 + int(threadIdx.x)) / P, c = int(threadIdx.x) % P * E;
+        const int64_t r = r0 + y;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (r < R && c0 + c < C) {
+            const int64_t row = a.list ? int64_t(a.list[r]) : r;
+            if (!a.labels || load_id(a.labels, a.wide, row, a.V) >= 0)
+                v = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.src) + row * a.lds + c0 + c);
+        }
+        uint32_t* o = reinterpret_cast<uint32_t*>(&s[y][c]);
+        o[0] = v.x, o[1] = v.y, o[2] = v.z, o[3] = v.w;
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 64; k += 4)
-        if (c0 + k + y < C) dst[int64_t(c0 + k + y) * ldd + r0 + x] = s[x][k + y];
+    for (int k = 0; k < 64 * P / 256; ++k) {
+        const int c = (k * 256 + int(threadIdx.x)) / P, y = int(threadIdx.x) % P * E;
+        if (c0 + c >= C) continue;
+        union {
+            T e[E];
+            uint4 v;
+        } x;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x.e[e] = s[y + e][c];
+        *reinterpret_cast<uint4*>(static_cast<T*>(a.dst) + int64_t(c0 + c) * a.ldd + r0 + y) = x.v;
+    }
 }
 
 // ----------------------------------------------------------------- products
@@ -154,19 +208,20 @@ struct LossArgs {
     int64_t lda, ldb;       // bytes
     int64_t M, N;
     const int32_t* n_count;  // N on the device, or null
-    const int32_t* rows;     // B's rows through the list, or null
     int64_t steps;           // of the sum
     const int32_t* k_count;  // the sum's length in elements on the device, or null
     int splits;
-    // kStats, kGrad
+    // kStats, kGrad: B's rows are tokens, listed if there is a list
     int64_t v0, V;  // class of A's first row; classes
     const int32_t* list;
+    bool gather;  // B's rows too go through the list (they do not lie in its order already)
     const void* labels;
     bool wide;
-    float *part, *hit;  // kStats: part[block][token] of two floats
+    float *part, *hit;  // kStats: part[block][token] of two floats; with one block of classes, null and
+    float *loss, *lse;  // the results themselves
     int64_t part_ld;
-    const float *lse, *dloss;  // kGrad
-    void *dl, *dlt;            // [token][dl_ld], [class][dlt_ld] or null
+    const float *lse_in, *dloss;  // kGrad
+    void *dl, *dlt;               // [token][dl_ld], [class][dlt_ld], either may be null
     int64_t dl_ld, dlt_ld;
     // kStore: out[split][row][M], or the result itself
     float* slots;
@@ -176,91 +231,192 @@ struct LossArgs {
     const int32_t* out_rows;
 };
 
-// The block of C that a workgroup forms: consecutive blocks of an XCD are close to
-// each other in both directions.  False: none.
-__device__ __forceinline__ bool block_of(int64_t mt, int64_t nt, int64_t& m, int64_t& n) {
-    const int64_t total = mt * nt, per = cdiv(total, kXcds), i = int64_t(blockIdx.x) / kXcds;
-    const int64_t t = int64_t(blockIdx.x) % kXcds * per + i;
-    if (i >= per || t >= total) return false;
-    constexpr int64_t G = 4;
-    const int64_t g = t / (G * mt), w = nt - g * G < G ? nt - g * G : G, at = t - g * G * mt;
-    m = at / w;
-    n = g * G + at % w;
-    return true;
+// The block of C, or of a part of a split sum, that a workgroup forms.  Each XCD takes
+// a contiguous share of the blocks, those that are formed together close to each other
+// in both directions.
+struct Block {
+    uint32_t m, n, split;
+    // false: none
+    __device__ __forceinline__ bool at(int64_t mt_, int64_t nt_, int splits) {
+        const uint32_t mt = uint32_t(mt_), nt = uint32_t(nt_), each = mt * nt, total = each * uint32_t(splits);
+        const uint32_t per = (total + kXcds - 1) / kXcds, i = blockIdx.x / kXcds;
+        uint32_t t = blockIdx.x % kXcds * per + i;
+        if (i >= per || t >= total) return false;
+        split = t / each;
+        t -= split * each;
+        constexpr uint32_t G = 4;
+        const uint32_t g = t / (G * mt), w = nt - g * G < G ? nt - g * G : G, r = t - g * G * mt;
+        m = r / w;
+        n = g * G + r % w;
+        return true;
+    }
+};
+
+// A lane's four values (consecutive columns of its row) of each lane of a quad, turned:
+// lane k of the quad gets column k of the quad's rows, as two packed words.
+__device__ __forceinline__ uint2 turn_quad(uint32_t lo, uint32_t hi, int lane) {
+    const uint32_t lo1 = uint32_t(xor_lane<1>(int(lo))), hi1 = uint32_t(xor_lane<1>(int(hi)));
+    // columns 0 and 2 of a pair of rows in its even lane, 1 and 3 in its odd one
+    const bool odd = lane & 1;
+    const uint32_t sel = odd ? 0x07060302u : 0x05040100u;
+    const uint32_t x = __builtin_amdgcn_perm(odd ? lo : lo1, odd ? lo1 : lo, sel);
+    const uint32_t y = __builtin_amdgcn_perm(odd ? hi : hi1, odd ? hi1 : hi, sel);
+    const uint32_t got = uint32_t(xor_lane<2>(int(lane & 2 ? x : y)));
+    return lane & 2 ? make_uint2(got, y) : make_uint2(x, got);
 }
 
-template <typename T>
-__device__ __forceinline__ void store4(T* p, float a, float b, float c, float d, int64_t room) {
-    if (room >= 4) {
-        if constexpr (sizeof(T) == 2) {
-            typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
-            const u2 x = {pack_bf16x2(a, b), pack_bf16x2(c, d)};
-            *reinterpret_cast<u2*>(p) = x;
-        } else {
-            typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
-            const f4 x = {a, b, c, d};
-            *reinterpret_cast<f4*>(p) = x;
+// 32 rows of C of one wavefront (its blocks j), through LDS, so that stores to memory
+// are whole runs of a row.  put(i, q, v): the lane's four values of block i, columns
+// 8 q + 4 (lane / 32) + 0..3; out(row of the 32, first column, 16 bytes' values).
+template <typename O, int TM>
+struct Rows32 {
+    static constexpr int E = 16 / int(sizeof(O));
+    static constexpr int kBlocks = sizeof(O) == 2 && TM > 1 ? 2 : 1;  // at a time: rows of at most 128 bytes
+    static constexpr int kRow = kBlocks * 32 * int(sizeof(O)), kPieces = kRow / 16;
+    static constexpr int kRounds = TM / kBlocks;
+
+    // a row's pieces are permuted by its number, as in a stage
+    __device__ __forceinline__ static char* place(char* lds, int row, int piece) {
+        return lds + row * kRow + (piece ^ ((kPieces == 8 ? row >> 1 : row >> 2) & (kPieces - 1))) * 16;
+    }
+    template <typename Get, typename Out>
+    __device__ __forceinline__ static void run(char* lds, int lane, const Get& get, const Out& out) {
+        const int row = lane & 31, half = lane >> 5;
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float v[4];
+                    get(r * kBlocks + i, q, v);
+                    if constexpr (sizeof(O) == 2)
+                        *reinterpret_cast<uint2*>(place(lds, row, 4 * i + q) + 8 * half) =
+                            make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+                    else
+                        *reinterpret_cast<float4*>(place(lds, row, 8 * i + 2 * q + half)) =
+                            make_float4(v[0], v[1], v[2], v[3]);
+                }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_wave_barrier();
+            constexpr int rows = kWave / kPieces;
+#pragma unroll
+            for (int k = 0; k < 32; k += rows) {
+                const int at = k + lane / kPieces, p = lane % kPieces;
+                const uint4 x = *reinterpret_cast<const uint4*>(place(lds, at, p));
+                out(at, r * kBlocks * 32 + p * E, x);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_wave_barrier();
         }
+    }
+};
+constexpr int kRowsBytes = 4096;  // of LDS for a wavefront's rows
+
+// 16 bytes of a row of which `room` elements are left, at any alignment
+template <typename O>
+__device__ __forceinline__ void store_room(O* p, const uint4& x, int64_t room) {
+    typedef typename Piece<O>::type piece_t;
+    constexpr int E = Piece<O>::E;
+    if (room >= E) {
+        const piece_t v = {x.x, x.y, x.z, x.w};
+        *reinterpret_cast<piece_t*>(p) = v;
     } else {
-        if (room > 0) store_one(p, a);
-        if (room > 1) store_one(p + 1, b);
-        if (room > 2) store_one(p + 2, c);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e < room) {
+                if constexpr (sizeof(O) == 2) p[e] = O(w[e / 2] >> 16 * (e % 2));
+                else p[e] = __uint_as_float(w[e]);
+            }
     }
 }
 
 template <typename T, int WHAT, int WM, int WN, int TM, int TN>
 __global__ __launch_bounds__(WM * WN * 64) void k_product(LossArgs a) {
     using G = GemmNT<T, WM, WN, TM, TN>;
-    __shared__ __attribute__((aligned(1024))) char s_buf[G::kStage], s_buf2[G::kStage];
+    // two objects: the compiler makes a read of one wait for loads into the same object
+    __shared__ __attribute__((aligned(1024))) char s_0[G::kStage], s_1[G::kStage];
+    static_assert(WM * WN * kRowsBytes <= G::kStage, "the wavefronts' rows fit");
+    char* const s_out = s_0;
     const int64_t N = a.n_count ? *a.n_count : a.N;
-    int64_t bm, bn;
-    if (!block_of(cdiv(a.M, G::BM), cdiv(N, G::BN), bm, bn)) return;
-    const int64_t m0 = bm * G::BM, n0 = bn * G::BN;
     int64_t steps = a.steps;
     if (a.k_count) steps = cdiv(int64_t(*a.k_count) * int64_t(sizeof(T)), kStepBytes);
-    const int64_t each = cdiv(steps, a.splits), s0 = int64_t(blockIdx.y) * each;
+    const int64_t each = cdiv(steps, a.splits);
+    const int lane = lane_id(), wave = uniform(threadIdx.x / kWave), wm = wave % WM, wn = wave / WM;
+    Block blk;
+    if (!blk.at(cdiv(a.M, G::BM), cdiv(N, G::BN), a.splits)) return;
+    const int64_t bm = blk.m, split = blk.split, m0 = bm * G::BM, n0 = int64_t(blk.n) * G::BN, s0 = split * each;
+    const int64_t mw = m0 + wm * TM * 32, nw = n0 + wn * TN * 32;  // of the wavefront
+    const int mh = 4 * (lane >> 5);  // the lane's classes: mw + mh + 32 i + 8 (e / 4) + e % 4
+    const bool last = m0 + G::BM > a.M;
     G g;
-    g.run(s_buf, s_buf2, a.A, a.lda, m0, a.M, a.B, a.ldb, n0, N, a.rows, s0, s0 + each < steps ? s0 + each : steps);
-
-    const int lane = lane_id(), wave = threadIdx.x / kWave, wm = wave % WM, wn = wave / WM;
-    const int64_t mw = m0 + wm * TM * 32 + 4 * (lane >> 5);       // + 32 i + 8 (e / 4) + e % 4
-    const int64_t nw = n0 + wn * TN * 32 + (lane & 31);           // + 32 j
-    if constexpr (WHAT == kStats) {
-        __syncthreads();
-        float2* s_part = reinterpret_cast<float2*>(s_buf);  // [WM][BN]
-        const bool last = m0 + G::BM > a.M;
+    g.source(wave, lane, a.A, a.lda, m0, a.M, a.B, a.ldb, n0, N, a.gather ? a.list : nullptr, s0,
+             s0 + each < steps ? s0 + each : steps);
+    g.start(s_0, s_1, wave);
+    // What the lane's tokens bring along, read beside the first steps' loads: the label's place
+    // behind the wavefront's first class (-1 if it is not among its classes), whether
+    // there is one at all, and the backward's statistics.
+    int place[TN];
+    bool labelled[TN];
+    float lse[TN], up[TN];
+    if constexpr (WHAT != kStore) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-            const int64_t t = nw + 32 * j;
+            const int64_t t = nw + 32 * j + (lane & 31);
+            const int64_t row = t < N ? (a.list ? int64_t(a.list[t]) : t) : -1;
+            const int64_t id = row >= 0 ? load_id(a.labels, a.wide, row, a.V) : -1, at = id - a.v0 - mw;
+            labelled[j] = id >= 0;
+            place[j] = id >= 0 && at >= 0 && at < TM * 32 ? int(at) : -1;
+            if constexpr (WHAT == kGrad) {
+                lse[j] = id >= 0 ? a.lse_in[row] : 0.f;
+                up[j] = id >= 0 ? a.dloss[row] : 0.f;
+            }
+        }
+    }
+    g.run(s_0, s_1, wave, lane);
+    lds_barrier();  // the stages have been read
+    if constexpr (WHAT == kStats) {
+        // statistics in the exp2 domain: the largest product times log2 e, and the sum of 2 to the power of what lies
+        // below it
+        float2* s_part = reinterpret_cast<float2*>(s_out);                // [WM][BN]
+        float* s_hit = reinterpret_cast<float*>(s_out + WM * G::BN * 8);  // [BN], of one block of classes
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int c = wn * TN * 32 + 32 * j + (lane & 31);
+            if (ballot(place[j] >= 0)) {  // few wavefronts hold any
+                float hit = 0.f;
+                bool mine = false;
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (place[j] == mh + 32 * i + 8 * (e / 4) + e % 4) hit = g.acc[i][j][e], mine = true;
+                if (mine) (a.loss ? s_hit + c : a.hit + n0 + c)[0] = hit;
+            }
             float top = kNegInf;
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    if (last && mw + 32 * i + 8 * (e / 4) + e % 4 >= a.M) g.acc[i][j][e] = kNegInf;
+                    if (last && mw + mh + 32 * i + 8 * (e / 4) + e % 4 >= a.M) g.acc[i][j][e] = kNegInf;
                     top = fmaxf(top, g.acc[i][j][e]);
                 }
-            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            top = fmaxf(top, __shfl_xor(top, 32, kWave)) * kLog2e;
             const float ref = top == kNegInf ? 0.f : top;
-            float sum = 0.f;
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sum += ex2((g.acc[i][j][e] - ref) * kLog2e);
-            sum += __shfl_xor(sum, 32, kWave);
-            if (lane < 32) s_part[wm * G::BN + wn * TN * 32 + 32 * j + lane] = make_float2(top, sum);
-            if (t < N) {
-                const int64_t y = load_id(a.labels, a.wide, a.list[t], a.V) - mw;  // the label's place among the lane's classes
-#pragma unroll
-                for (int i = 0; i < TM; ++i)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (y == 32 * i + 8 * (e / 4) + e % 4) a.hit[t] = g.acc[i][j][e];
-            }
+                for (int e = 0; e < 16; ++e) sum[e % 4] += ex2(fmaf(g.acc[i][j][e], kLog2e, -ref));
+            float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            all += __shfl_xor(all, 32, kWave);
+            if (lane < 32) s_part[wm * G::BN + c] = make_float2(top, all);
         }
-        __syncthreads();
+        lds_barrier();
         for (int c = threadIdx.x; c < G::BN; c += G::kThreads) {
-            if (n0 + c >= N) break;
+            const int64_t t = n0 + c;
+            if (t >= N) break;
             float top = kNegInf, sum = 0.f;
 #pragma unroll
             for (int w = 0; w < WM; ++w) top = fmaxf(top, s_part[w * G::BN + c].x);
@@ -268,109 +424,212 @@ __global__ __launch_bounds__(WM * WN * 64) void k_product(LossArgs a) {
 #pragma unroll
             for (int w = 0; w < WM; ++w) {
                 const float2 p = s_part[w * G::BN + c];
-                sum += p.y * ex2((p.x - ref) * kLog2e);
+                sum += p.y * ex2(p.x - ref);
             }
-            reinterpret_cast<float2*>(a.part)[bm * a.part_ld + n0 + c] = make_float2(top, sum);
-        }
-    } else if constexpr (WHAT == kGrad) {
-        T* dl = static_cast<T*>(a.dl);
-        T* dlt = static_cast<T*>(a.dlt);
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const int64_t t = nw + 32 * j;
-            const bool in = t < N;
-            const int64_t row = in ? a.list[t] : 0;
-            const float lse = in ? a.lse[row] : 0.f, up = in ? a.dloss[row] : 0.f;
-            const int64_t y = in ? load_id(a.labels, a.wide, row, a.V) - a.v0 - mw : -1;
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int k = 32 * i + 8 * q + e;
-                        const float p = ex2((g.acc[i][j][4 * q + e] - lse) * kLog2e);
-                        v[e] = in && mw + k < a.M ? up * (y == k ? p - 1.f : p) : 0.f;
-                    }
-                    const int64_t m = mw + 32 * i + 8 * q;
-                    store4(dl + t * a.dl_ld + m, v[0], v[1], v[2], v[3], 4);
-                    if (dlt) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) store_one(dlt + (m + e) * a.dlt_ld + t, v[e]);
-                    }
-                }
+            if (a.loss) {
+                const int64_t row = a.list ? int64_t(a.list[t]) : t;
+                const bool has = load_id(a.labels, a.wide, row, a.V) >= 0;
+                const float l = (ref + log2f(sum)) * kLn2;
+                a.lse[row] = has ? l : 0.f;
+                a.loss[row] = has ? l - s_hit[c] : 0.f;
+            } else {
+                reinterpret_cast<float2*>(a.part)[bm * a.part_ld + t] = make_float2(top, sum);
+            }
         }
     } else {
+        char* const lds = s_out + wave * kRowsBytes;
+        if constexpr (WHAT == kGrad) {
+            using R = Rows32<T, TM>;
+            T* dl = static_cast<T*>(a.dl);
+            T* dlt = static_cast<T*>(a.dlt);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const int64_t n = nw + 32 * j;
-            if (n >= N) continue;
-            float* o = a.slots ? a.slots + (int64_t(blockIdx.y) * a.slot_rows + n) * a.M : nullptr;
-            T* r = a.slots ? nullptr : static_cast<T*>(a.out) + (a.out_rows ? int64_t(a.out_rows[n]) : n) * a.M;
+            for (int j = 0; j < TN; ++j) {
+                const int64_t t0 = nw + 32 * j;
+                const bool label = ballot(place[j] >= 0);  // few wavefronts hold any
+                const auto value = [&](int i, int q, float(&v)[4]) {
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int64_t m = mw + 32 * i + 8 * q, room = a.M - m;
-                    float v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = g.acc[i][j][4 * q + e];
-                    if (o) {
-                        if (a.add) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (e < room) v[e] += o[m + e];
-                        }
-                        store4(o + m, v[0], v[1], v[2], v[3], room);
-                    } else {
-                        store4(r + m, v[0], v[1], v[2], v[3], room);
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = ex2((g.acc[i][j][4 * q + e] - lse[j]) * kLog2e);
+                        v[e] = labelled[j] ? p : 0.f;
                     }
+                    if (label) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (place[j] == mh + 32 * i + 8 * q + e) v[e] -= 1.f;
+                    }
+                    if (last) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (mw + mh + 32 * i + 8 * q + e >= a.M) v[e] = 0.f;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] *= up[j];
+                    if (dlt) {
+                        T* o = dlt + (mw + mh + 32 * i + 8 * q) * a.dlt_ld + t0;
+                        if constexpr (sizeof(T) == 2) {
+                            const uint2 x = turn_quad(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), lane);
+                            *reinterpret_cast<uint2*>(o + (lane & 3) * a.dlt_ld + (lane & 28)) = x;
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[e * a.dlt_ld + (lane & 31)] = v[e];
+                        }
+                    }
+                };
+                R::run(lds, lane, value, [&](int at, int m, const uint4& x) {
+                    if (dl) *reinterpret_cast<uint4*>(dl + (t0 + at) * a.dl_ld + mw + m) = x;
+                });
+            }
+        } else {
+            const auto rows = [&](auto o, int j, const auto& out) {
+                using R = Rows32<decltype(o), TM>;
+                    R::run(
+                    lds, lane,
+                    [&](int i, int q, float(&v)[4]) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = g.acc[i][j][4 * q + e];
+                    },
+                    out);
+            };
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int64_t t0 = nw + 32 * j;
+                if (a.slots) {
+                    float* o = a.slots + split * a.slot_rows * a.M;
+                    rows(float(), j, [&](int at, int m, uint4 x) {
+                        const int64_t n = t0 + at, room = a.M - mw - m;
+                        if (n >= N || room <= 0) return;
+                        float* p = o + n * a.M + mw + m;
+                        if (a.add) {
+                            float v[4] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w)};
+                            if (room >= 4) {
+                                float w[4];
+                                load_piece(w, p);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) v[e] += w[e];
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    if (e < room) v[e] += p[e];
+                            }
+                            x = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+                        }
+                        store_room(p, x, room);
+                    });
+                } else {
+                    rows(T(), j, [&](int at, int m, const uint4& x) {
+                        const int64_t n = t0 + at, room = a.M - mw - m;
+                        if (n >= N || room <= 0) return;
+                        const int64_t r = a.out_rows ? int64_t(a.out_rows[n]) : n;
+                        store_room(static_cast<T*>(a.out) + r * a.M + mw + m, x, room);
+                    });
                 }
+            }
         }
     }
 }
 
-// The parts of a token's statistics, joined: a token's blocks go by over 32 lanes.
-__global__ __launch_bounds__(256) void k_loss(int64_t blocks, const float2* part, int64_t ld, const float* hit,
-                                               const int32_t* list, const int32_t* count, float* loss, float* lse) {
-    constexpr int P = 32;  // tokens of a workgroup
-    __shared__ float2 s[256 / P][P];
+// The parts of a token's statistics, joined: 64 lanes take a token's blocks in turn.
+__global__ __launch_bounds__(1024) void k_loss(int64_t blocks, const float2* part, int64_t ld, const float* hit,
+                                                const void* labels, bool wide, int64_t V, const int32_t* list,
+                                                const int32_t* count, int64_t n, float* loss, float* lse) {
+    constexpr int P = 16, G = 1024 / P;  // tokens of a workgroup
+    __shared__ float2 s[G][P + 1];
     const int x = threadIdx.x % P, y = threadIdx.x / P;
-    const int64_t t = int64_t(blockIdx.x) * P + x, n = *count;
+    const int64_t t = int64_t(blockIdx.x) * P + x;
+    if (count) n = *count;
     if (int64_t(blockIdx.x) * P >= n) return;
     float top = kNegInf, sum = 0.f;
     if (t < n)
-        for (int64_t b = y; b < blocks; b += 256 / P) {
+        for (int64_t b = y; b < blocks; b += G) {
             const float2 p = part[b * ld + t];
             const float m = fmaxf(top, p.x), ref = m == kNegInf ? 0.f : m;
-            sum = sum * ex2((top - ref) * kLog2e) + p.y * ex2((p.x - ref) * kLog2e);
+            sum = sum * ex2(top - ref) + p.y * ex2(p.x - ref);
             top = m;
         }
     s[y][x] = make_float2(top, sum);
     __syncthreads();
-    if (y || t >= n) return;
-    top = kNegInf, sum = 0.f;
-    for (int k = 0; k < 256 / P; ++k) top = fmaxf(top, s[k][x].x);
+    if (y >= P) return;
+    // the lanes turned: a wavefront's 16 lanes of a token take its 64 sums
+    const int tok = y, l = x;
+    const int64_t tt = int64_t(blockIdx.x) * P + tok;
+    top = kNegInf;
+    float2 p[G / P];
+#pragma unroll
+    for (int k = 0; k < G / P; ++k) p[k] = s[l + P * k][tok], top = fmaxf(top, p[k].x);
+#pragma unroll
+    for (int o = 1; o < P; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
     const float ref = top == kNegInf ? 0.f : top;
-    for (int k = 0; k < 256 / P; ++k) sum += s[k][x].y * ex2((s[k][x].x - ref) * kLog2e);
-    const float l = ref + logf(sum);
-    const int64_t i = list[t];
-    lse[i] = l;
-    loss[i] = l - hit[t];
+    sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < G / P; ++k) sum += p[k].y * ex2(p[k].x - ref);
+#pragma unroll
+    for (int o = 1; o < P; o <<= 1) sum += __shfl_xor(sum, o, kWave);
+    if (l || tt >= n) return;
+    const int64_t i = list ? int64_t(list[tt]) : tt;
+    const bool has = load_id(labels, wide, i, V) >= 0;
+    const float all = (ref + log2f(sum)) * kLn2;
+    lse[i] = has ? all : 0.f;
+    loss[i] = has ? all - hit[tt] : 0.f;
 }
 
-// out[row][c] = the sum of the slots
-template <typename T>
+// out[row][c] = the sum of the slots, four columns a lane where rows are whole such;
+// the slots go by over L lanes.
+template <typename T, int L>
 __global__ __launch_bounds__(256) void k_sum_slots(int splits, int64_t slot_rows, int64_t R, const int32_t* count,
                                                     int64_t C, const float* slots, const int32_t* rows, T* out) {
+    constexpr int P = 256 / L;
+    __shared__ float4 s[L][P];
     if (count) R = *count;
-    const int64_t total = R * C;
-    for (int64_t i = blockIdx.x * int64_t(256) + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
-        float v = 0.f;
-        for (int k = 0; k < splits; ++k) v += slots[int64_t(k) * slot_rows * C + i];
+    const int64_t total = R * C, each = slot_rows * C;
+    const int x = threadIdx.x % P, y = threadIdx.x / P;
+    for (int64_t i0 = int64_t(blockIdx.x) * P * 4; i0 < total; i0 += int64_t(gridDim.x) * P * 4) {
+        const int64_t i = i0 + 4 * x, room = total - i;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        if (room >= 4) {
+#pragma unroll 4
+            for (int k = y; k < splits; k += L) {
+                float w[4];
+                load_piece(w, slots + k * each + i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += w[e];
+            }
+        } else if (room > 0) {
+            for (int k = y; k < splits; k += L)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < room) v[e] += slots[k * each + i + e];
+        }
+        if constexpr (L > 1) {
+            s[y][x] = make_float4(v[0], v[1], v[2], v[3]);
+            __syncthreads();
+            if (y == 0) {
+#pragma unroll
+                for (int k = 1; k < L; ++k) {
+                    const float4 w = s[k][x];
+                    v[0] += w.x, v[1] += w.y, v[2] += w.z, v[3] += w.w;
+                }
+            }
+            __syncthreads();
+        }
+        if (y) continue;
         const int64_t r = i / C;
-        store_one(out + (rows ? int64_t(rows[r]) * C + (i - r * C) : i), v);
+        if (room >= 4 && (i + 3) / C == r) {
+            T* o = rows ? out + int64_t(rows[r]) * C + (i - r * C) : out + i;
+            if constexpr (sizeof(T) == 2) {
+                typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
+                const u2 p = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                *reinterpret_cast<u2*>(o) = p;
+            } else {
+                store_piece(o, v, false);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < room) {
+                    const int64_t re = (i + e) / C;
+                    store_one(rows ? out + int64_t(rows[re]) * C + (i + e - re * C) : out + i + e, v[e]);
+                }
+        }
     }
 }
 
@@ -379,8 +638,8 @@ gt_status product(const LossArgs& a, hipStream_t s) {
 #define GT_CALL(WM, WN, TM, TN)                                                                            \
     do {                                                                                                   \
         using G = GemmNT<T, WM, WN, TM, TN>;                                                               \
-        const dim3 grid(xcd_grid(cdiv(a.M, G::BM) * cdiv(a.N, G::BN)), unsigned(a.splits));                \
-        k_product<T, WHAT, WM, WN, TM, TN><<<grid, G::kThreads, 0, s>>>(a);                                \
+        const unsigned blocks = xcd_grid(cdiv(a.M, G::BM) * cdiv(a.N, G::BN) * a.splits);                  \
+        k_product<T, WHAT, WM, WN, TM, TN><<<blocks, G::kThreads, 0, s>>>(a);                              \
     } while (0)
     if (a.M <= 64) {
         if (a.N <= 64) GT_CALL(2, 2, 1, 1);
@@ -408,10 +667,11 @@ int splits_of(int64_t M, int64_t N, int64_t steps) {
 struct Shape {
     int64_t n, V, ldx, ldw;
     int D, size;
-    bool pad_x, pad_w;
+    bool whole_x, copy_x, copy_w;
     int64_t row;   // bytes of a padded row
     int64_t mp;    // tokens, whole blocks
-    int64_t piece;  // classes a piece
+    int64_t ldt;   // row stride of the arrays along the tokens
+    int64_t piece, ldp;  // classes a piece, row stride of the arrays along them
     int sx, sw;     // splits of dX and dW
     bool slots_x;
 };
@@ -422,13 +682,16 @@ Shape shape_of(int64_t n, int64_t V, int32_t D, gt_dtype dt, int64_t ldx, int64_
     h.size = dt == GT_BF16 ? 2 : 4;
     h.row = cdiv(int64_t(D) * h.size, kStepBytes) * kStepBytes;
     const bool whole = h.row == int64_t(D) * h.size;
-    h.pad_x = !whole || ldx * h.size % 16 != 0;
-    h.pad_w = !whole || ldw * h.size % 16 != 0;
+    h.whole_x = whole && ldx * h.size % 16 == 0;
+    h.copy_w = !whole || ldw * h.size % 16 != 0;
+    h.copy_x = !h.whole_x || (n > kListed && V > kGatherClasses);
     h.mp = cdiv(n, 256) * 256;
+    h.ldt = h.mp + kOff;
     const int64_t all = cdiv(V, 256) * 256;
     int64_t piece = kPieceBytes / (h.mp * h.size) / 256 * 256;
     if (piece < kMinPiece) piece = kMinPiece;
     h.piece = piece < all ? piece : all;
+    h.ldp = h.piece + kOff;
     h.sx = splits_of(D, n, h.piece * h.size / kStepBytes);
     h.sw = splits_of(D, h.piece < V ? h.piece : V, h.mp * h.size / kStepBytes);
     h.slots_x = h.sx > 1 || h.piece < V;
@@ -454,8 +717,8 @@ struct FwdWs {
 FwdWs fwd_ws(Ws& w, const Shape& h) {
     FwdWs f;
     f.l = list_ws(w, h.n);
-    f.x = h.pad_x ? w.take<char>(size_t(h.n * h.row)) : nullptr;
-    f.w = h.pad_w ? w.take<char>(size_t(h.V * h.row)) : nullptr;
+    f.x = h.copy_x ? w.take<char>(size_t(h.n * h.row)) : nullptr;
+    f.w = h.copy_w ? w.take<char>(size_t(h.V * h.row)) : nullptr;
     f.part = w.take<float>(size_t(2 * h.mp * cdiv(h.V, block_rows(h.V))));
     f.hit = w.take<float>(size_t(h.n));
     return f;
@@ -469,19 +732,22 @@ struct BwdWs {
 BwdWs bwd_ws(Ws& w, const Shape& h) {
     BwdWs b;
     b.l = list_ws(w, h.n);
-    b.x = h.pad_x ? w.take<char>(size_t(h.n * h.row)) : nullptr;
-    b.w = h.pad_w ? w.take<char>(size_t(h.V * h.row)) : nullptr;
-    b.xt = w.take<char>(size_t(h.D) * size_t(h.mp * h.size));
-    b.wt = w.take<char>(size_t(h.D) * size_t(h.piece * h.size));
-    b.dl = w.take<char>(size_t(h.mp * h.piece * h.size));
-    b.dlt = w.take<char>(size_t(h.mp * h.piece * h.size));
+    b.x = h.copy_x ? w.take<char>(size_t(h.n * h.row)) : nullptr;
+    b.w = h.copy_w ? w.take<char>(size_t(h.V * h.row)) : nullptr;
+    b.xt = w.take<char>(size_t(h.D) * size_t(h.ldt * h.size));
+    b.wt = w.take<char>(size_t(h.D) * size_t(h.ldp * h.size));
+    b.dl = w.take<char>(size_t(h.mp) * size_t(h.ldp * h.size));
+    b.dlt = w.take<char>(size_t(h.piece) * size_t(h.ldt * h.size));
     b.slots_x = h.slots_x ? w.take<float>(size_t(h.sx) * size_t(h.n) * h.D) : nullptr;
     b.slots_w = h.sw > 1 ? w.take<float>(size_t(h.sw) * size_t(h.piece) * h.D) : nullptr;
     return b;
 }
 
-gt_status make_list(const Shape& h, bool wide, const void* labels, const List& l, float* loss, float* lse,
-                    hipStream_t s) {
+gt_status make_list(const Shape& h, bool wide, const void* labels, List& l, float* loss, float* lse, hipStream_t s) {
+    if (h.n <= kListed) {
+        l.list = l.count = nullptr;
+        return GT_OK;
+    }
     const unsigned blocks = unsigned(cdiv(h.n, kListRows));
     if (blocks > 1) {
         k_list_count<<<blocks, kListThreads, 0, s>>>(h.n, h.V, wide, labels, l.cnt);
@@ -492,21 +758,21 @@ gt_status make_list(const Shape& h, bool wide, const void* labels, const List& l
     return GT_OK;
 }
 
-// X and W as the products take them
+// X and W as the products take them; a copy of X has the listed rows alone, in order
 template <typename T>
-gt_status make_rows(const Shape& h, const void*& X, int64_t& ldx, char* x, const void*& W, int64_t& ldw, char* w,
-                    hipStream_t s) {
+gt_status make_rows(const Shape& h, const List& l, const void*& X, int64_t& ldx, char* x, const void*& W, int64_t& ldw,
+                    char* w, hipStream_t s) {
     const int ldd = int(h.row / h.size);
-    if (h.pad_x) {
-        k_pad<T><<<grid_for(h.n, 4, 1 << 16), 256, 0, s>>>(h.n, h.D, static_cast<const T*>(X), ldx,
-                                                           reinterpret_cast<T*>(x), ldd);
-        GT_LAUNCH_CHECK("class_loss pad");
+    if (h.copy_x) {
+        k_pad<T><<<grid_for(h.n, 4, 1 << 16), 256, 0, s>>>(h.n, l.list, l.count, h.D, static_cast<const T*>(X), ldx,
+                                                           reinterpret_cast<T*>(x), ldd, h.whole_x);
+        GT_LAUNCH_CHECK("class_loss rows");
         X = x, ldx = ldd;
     }
-    if (h.pad_w) {
-        k_pad<T><<<grid_for(h.V, 4, 1 << 16), 256, 0, s>>>(h.V, h.D, static_cast<const T*>(W), ldw,
-                                                           reinterpret_cast<T*>(w), ldd);
-        GT_LAUNCH_CHECK("class_loss pad");
+    if (h.copy_w) {
+        k_pad<T><<<grid_for(h.V, 4, 1 << 16), 256, 0, s>>>(h.V, nullptr, nullptr, h.D, static_cast<const T*>(W), ldw,
+                                                           reinterpret_cast<T*>(w), ldd, false);
+        GT_LAUNCH_CHECK("class_loss rows");
         W = w, ldw = ldd;
     }
     return GT_OK;
@@ -514,30 +780,43 @@ gt_status make_rows(const Shape& h, const void*& X, int64_t& ldx, char* x, const
 
 template <typename T>
 gt_status run_fwd(const Shape& h, const void* X, const void* W, bool wide, const void* labels, float* loss, float* lse,
-                  const FwdWs& f, hipStream_t s) {
+                  FwdWs f, hipStream_t s) {
     gt_status st = make_list(h, wide, labels, f.l, loss, lse, s);
     if (st != GT_OK) return st;
     int64_t ldx = h.ldx, ldw = h.ldw;
-    st = make_rows<T>(h, X, ldx, f.x, W, ldw, f.w, s);
+    st = make_rows<T>(h, f.l, X, ldx, f.x, W, ldw, f.w, s);
     if (st != GT_OK) return st;
+    const int64_t blocks = cdiv(h.V, block_rows(h.V));
     LossArgs a = {};
     a.A = static_cast<const char*>(W), a.lda = ldw * h.size, a.M = h.V;
     a.B = static_cast<const char*>(X), a.ldb = ldx * h.size, a.N = h.n;
-    a.n_count = f.l.count, a.rows = f.l.list, a.list = f.l.list;
+    a.n_count = f.l.count, a.list = f.l.list, a.gather = !h.copy_x;
     a.steps = h.row / kStepBytes, a.splits = 1;
     a.V = h.V, a.labels = labels, a.wide = wide;
-    a.part = f.part, a.part_ld = h.mp, a.hit = f.hit;
+    if (blocks == 1) a.loss = loss, a.lse = lse;
+    else a.part = f.part, a.part_ld = h.mp, a.hit = f.hit;
     st = product<T, kStats>(a, s);
-    if (st != GT_OK) return st;
-    k_loss<<<unsigned(cdiv(h.n, 32)), 256, 0, s>>>(cdiv(h.V, block_rows(h.V)), reinterpret_cast<float2*>(f.part), h.mp,
-                                                   f.hit, f.l.list, f.l.count, loss, lse);
+    if (st != GT_OK || blocks == 1) return st;
+    k_loss<<<unsigned(cdiv(h.n, 16)), 1024, 0, s>>>(blocks, reinterpret_cast<float2*>(f.part), h.mp, f.hit, labels, wide,
+                                                    h.V, f.l.list, f.l.count, h.n, loss, lse);
     GT_LAUNCH_CHECK("class_loss join");
     return GT_OK;
 }
 
 template <typename T>
-gt_status run_bwd(const Shape& h, const void* X0, const void* W0, bool wide, const void* labels, const float* lse,
-                  const float* dloss, void* dX, void* dW, const BwdWs& b, hipStream_t s) {
+gt_status sum_slots(int splits, int64_t slot_rows, int64_t R, const int32_t* count, int64_t C, const float* slots,
+                    const int32_t* rows, T* out, hipStream_t s) {
+    if (splits > 1)
+        k_sum_slots<T, 8><<<grid_for(R * C, 128, 1 << 16), 256, 0, s>>>(splits, slot_rows, R, count, C, slots, rows, out);
+    else
+        k_sum_slots<T, 1><<<grid_for(R * C, 1024, 1 << 16), 256, 0, s>>>(splits, slot_rows, R, count, C, slots, rows, out);
+    GT_LAUNCH_CHECK("class_loss sum");
+    return GT_OK;
+}
+
+template <typename T>
+gt_status run_bwd(const Shape& h, const void* X, const void* W, bool wide, const void* labels, const float* lse,
+                  const float* dloss, void* dX, void* dW, BwdWs b, hipStream_t s) {
     if (h.n == 0) {
         k_zero<T><<<grid_for(h.V * h.D, 256, 1 << 16), 256, 0, s>>>(h.V * h.D, static_cast<T*>(dW));
         GT_LAUNCH_CHECK("class_loss zero");
@@ -545,40 +824,46 @@ gt_status run_bwd(const Shape& h, const void* X0, const void* W0, bool wide, con
     }
     gt_status st = make_list(h, wide, labels, b.l, nullptr, nullptr, s);
     if (st != GT_OK) return st;
-    const void *X = X0, *W = W0;
     int64_t ldx = h.ldx, ldw = h.ldw;
-    st = make_rows<T>(h, X, ldx, b.x, W, ldw, b.w, s);
+    st = make_rows<T>(h, b.l, X, ldx, b.x, W, ldw, b.w, s);
     if (st != GT_OK) return st;
-    if (dX) {
+    if (dX && b.l.list) {
         k_zero_rows<T><<<grid_for(h.n, 4, 1 << 16), 256, 0, s>>>(h.n, h.D, h.V, wide, labels, static_cast<T*>(dX));
         GT_LAUNCH_CHECK("class_loss zero rows");
-    }
-    const unsigned turns = unsigned(cdiv(h.D, 64));
-    if (dW) {
-        k_turn<T><<<dim3(unsigned(cdiv(h.n, 64)), turns), 256, 0, s>>>(
-            h.n, b.l.count, b.l.list, h.D, static_cast<const T*>(X), ldx, reinterpret_cast<T*>(b.xt), h.mp);
-        GT_LAUNCH_CHECK("class_loss turn");
     }
     for (int64_t v0 = 0; v0 < h.V; v0 += h.piece) {
         const int64_t vn = h.V - v0 < h.piece ? h.V - v0 : h.piece;
         const char* w = static_cast<const char*>(W) + v0 * ldw * h.size;
+        Turns turns = {};
+        int jobs = 0;
+        int64_t most = 0;
+        if (dX) {
+            turns.t[jobs++] = {vn, nullptr, nullptr, nullptr, false, 0, w, ldw, b.wt, h.ldp};
+            most = vn;
+        }
+        if (dW && v0 == 0) {
+            turns.t[jobs++] = {h.n, b.l.count, h.copy_x ? nullptr : b.l.list, b.l.list ? nullptr : labels,
+                               wide, h.V, X, ldx, b.xt, h.ldt};
+            most = most > h.n ? most : h.n;
+        }
+        if (jobs) {
+            k_turn<T><<<dim3(unsigned(cdiv(most, 64)), unsigned(cdiv(h.D, 64)), unsigned(jobs)), 256, 0, s>>>(turns, h.D);
+            GT_LAUNCH_CHECK("class_loss turn");
+        }
         LossArgs a = {};
         a.A = w, a.lda = ldw * h.size, a.M = vn;
         a.B = static_cast<const char*>(X), a.ldb = ldx * h.size, a.N = h.n;
-        a.n_count = b.l.count, a.rows = b.l.list, a.list = b.l.list;
+        a.n_count = b.l.count, a.list = b.l.list, a.gather = !h.copy_x;
         a.steps = h.row / kStepBytes, a.splits = 1;
-        a.v0 = v0, a.V = h.V, a.labels = labels, a.wide = wide, a.lse = lse, a.dloss = dloss;
-        a.dl = b.dl, a.dl_ld = h.piece;
-        a.dlt = dW ? b.dlt : nullptr, a.dlt_ld = h.mp;
+        a.v0 = v0, a.V = h.V, a.labels = labels, a.wide = wide, a.lse_in = lse, a.dloss = dloss;
+        a.dl = dX ? b.dl : nullptr, a.dl_ld = h.ldp;
+        a.dlt = dW ? b.dlt : nullptr, a.dlt_ld = h.ldt;
         st = product<T, kGrad>(a, s);
         if (st != GT_OK) return st;
         if (dX) {
-            k_turn<T><<<dim3(unsigned(cdiv(vn, 64)), turns), 256, 0, s>>>(
-                vn, nullptr, nullptr, h.D, reinterpret_cast<const T*>(w), ldw, reinterpret_cast<T*>(b.wt), h.piece);
-            GT_LAUNCH_CHECK("class_loss turn");
             LossArgs x = {};
-            x.A = b.wt, x.lda = h.piece * h.size, x.M = h.D;
-            x.B = b.dl, x.ldb = h.piece * h.size, x.N = h.n, x.n_count = b.l.count;
+            x.A = b.wt, x.lda = h.ldp * h.size, x.M = h.D;
+            x.B = b.dl, x.ldb = h.ldp * h.size, x.N = h.n, x.n_count = b.l.count;
             x.steps = cdiv(vn * h.size, kStepBytes), x.splits = h.sx;
             x.slots = b.slots_x, x.slot_rows = h.n, x.add = v0 > 0;
             x.out = dX, x.out_rows = b.l.list;
@@ -587,33 +872,28 @@ gt_status run_bwd(const Shape& h, const void* X0, const void* W0, bool wide, con
         }
         if (dW) {
             LossArgs x = {};
-            x.A = b.xt, x.lda = h.mp * h.size, x.M = h.D;
-            x.B = b.dlt, x.ldb = h.mp * h.size, x.N = vn;
-            x.k_count = b.l.count, x.splits = h.sw;
+            x.A = b.xt, x.lda = h.ldt * h.size, x.M = h.D;
+            x.B = b.dlt, x.ldb = h.ldt * h.size, x.N = vn;
+            x.steps = cdiv(h.n * h.size, kStepBytes), x.k_count = b.l.count, x.splits = h.sw;
             x.slots = b.slots_w, x.slot_rows = h.piece;
             T* out = static_cast<T*>(dW) + v0 * h.D;
             x.out = out;
             st = product<T, kStore>(x, s);
+            if (st == GT_OK && b.slots_w)
+                st = sum_slots<T>(h.sw, h.piece, vn, nullptr, h.D, b.slots_w, nullptr, out, s);
             if (st != GT_OK) return st;
-            if (b.slots_w) {
-                k_sum_slots<T><<<grid_for(vn * h.D, 256, 1 << 16), 256, 0, s>>>(h.sw, h.piece, vn, nullptr, h.D,
-                                                                                b.slots_w, nullptr, out);
-                GT_LAUNCH_CHECK("class_loss sum");
-            }
         }
     }
-    if (dX && b.slots_x) {
-        k_sum_slots<T><<<grid_for(h.n * h.D, 256, 1 << 16), 256, 0, s>>>(h.sx, h.n, h.n, b.l.count, h.D, b.slots_x,
-                                                                         b.l.list, static_cast<T*>(dX));
-        GT_LAUNCH_CHECK("class_loss sum");
-    }
+    if (dX && b.slots_x)
+        return sum_slots<T>(h.sx, h.n, h.n, b.l.count, h.D, b.slots_x, b.l.list, static_cast<T*>(dX), s);
     return GT_OK;
 }
 
 bool loss_sizes(int64_t n, int64_t V, int32_t D, gt_dtype dt, int64_t ldx, int64_t ldw) {
     const int64_t most = int64_t(1) << 31;
     return (dt == GT_BF16 || dt == GT_F32) && n >= 0 && n < most && V >= 1 && V < most && D >= 1 && D <= GT_MAX_WIDTH &&
-           ldx >= D && ldw >= D && ldx < most && ldw < most;
+           ldx >= D && ldw >= D && ldx < most && ldw < most &&
+           cdiv(n, 64) * cdiv(V, 64) < (int64_t(1) << 30);  // blocks are counted in 32 bits
 }
 gt_status loss_check(const char* who, int64_t n, int64_t V, int32_t D, gt_dtype dt, gt_itype it, const void* X,
                      int64_t ldx, const void* W, int64_t ldw, const void* labels) {

@@ -20,15 +20,16 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kStepBytes = 128;  // of every row, a step
 
-__device__ __forceinline__ void mma_piece(uint16_t, const uint4& a, const uint4& b, f32x16_t& c) {
+// One matrix instruction of a 16-byte piece of each operand: bf16 takes the pieces
+// whole, fp32 an element e of each.
+__device__ __forceinline__ void mma_part(uint16_t, const uint4& a, const uint4& b, f32x16_t& c, int) {
     c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0,
                                                 0, 0);
 }
-__device__ __forceinline__ void mma_piece(float, const uint4& a, const uint4& b, f32x16_t& c) {
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
+__device__ __forceinline__ void mma_part(float, const uint4& a, const uint4& b, f32x16_t& c, int e) {
+    const uint32_t x = e == 0 ? a.x : e == 1 ? a.y : e == 2 ? a.z : a.w;
+    const uint32_t y = e == 0 ? b.x : e == 1 ? b.y : e == 2 ? b.z : b.w;
+    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x), __uint_as_float(y), c, 0, 0, 0);
 }
 
 __device__ __forceinline__ void copy_to_lds(char* lds, const char* src) {
@@ -37,11 +38,18 @@ __device__ __forceinline__ void copy_to_lds(char* lds, const char* src) {
         reinterpret_cast<__attribute__((address_space(3))) uint32_t*>(reinterpret_cast<uintptr_t>(lds)), 16, 0, 0);
 }
 
-// What orders the compiler's memory accesses around a barrier that waits for no more
-// than is needed.
+// A barrier that waits for no more than is needed (and what orders the compiler's
+// memory accesses around it): all but the last LOADS loads of the wavefront have landed
+// and its reads of LDS are done.
 template <int LOADS>
-__device__ __forceinline__ void wait_loads() {  // all but the last LOADS loads of the wavefront have landed
+__device__ __forceinline__ void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+// The same for accesses to LDS alone.
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
@@ -53,56 +61,68 @@ struct GemmNT {
     static constexpr int BM = WM * TM * 32, BN = WN * TN * 32;
     static constexpr int kStage = (BM + BN) * kStepBytes;
     static constexpr int kLoads = kStage / 1024 / (WM * WN);  // 1 KiB loads of a wavefront, a step
+    static constexpr int kParts = sizeof(T) == 2 ? 1 : 4;     // matrix instructions of a piece
     static_assert(kStage % (1024 * WM * WN) == 0, "whole loads a wavefront");
-
-    f32x16_t acc[TM][TN];
 
     struct Frag {
         uint4 a[TM], b[TN];
     };
+    f32x16_t acc[TM][TN];
+    const char* src[kLoads];  // where a lane's loads of the next step come from
+    int64_t left;             // steps of the block
 
+    // The steps [s0, s1) of kStepBytes of the rows m0.. of A and n0.. of B (B's through the
+    // list, if there is one); rows at or above M and N repeat the last one.  A stage holds
+    // BM rows of A, then BN of B; eight rows, a load of a wavefront, are of one of the two.
+    __device__ __forceinline__ void source(int wave, int lane, const char* A, int64_t lda, int64_t m0, int64_t M,
+                                           const char* B, int64_t ldb, int64_t n0, int64_t N, const int32_t* list,
+                                           int64_t s0, int64_t s1) {
+        left = s0 < s1 ? s1 - s0 : 0;
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            const int at = (wave * kLoads + l) * 8, r = at + lane / 8, piece = (lane % 8) ^ turn(r);
+            const bool b = at >= BM;
+            const int64_t limit = b ? N : M, c = (b ? n0 - BM : m0) + r;
+            int64_t row = c < limit ? c : limit - 1;
+            if (list && b) row = list[row];
+            src[l] = (b ? B : A) + row * (b ? ldb : lda) + piece * 16 + s0 * kStepBytes;
+        }
+    }
+
+    __device__ __forceinline__ void fetch(char* lds, int wave) {
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            copy_to_lds(lds + (wave * kLoads + l) * 1024, src[l]);
+            src[l] += kStepBytes;
+        }
+    }
+
+    // The loads of the first two steps; nothing reads or writes the stages before run().
     // lds0, lds1: two arrays of kStage bytes (two objects: the compiler makes a read of
-    // one wait for loads into the same object).  Rows m0.. of A and n0.. of B (rows at
-    // or above M and N repeat the last one; B's rows through the list, if there is
-    // one), steps [s0, s1) of kStepBytes.
-    //
-    // A step's four quarters (two pieces of each row) are read a quarter ahead of their
-    // products, the next step's first quarter too: the one barrier of a step stands
-    // before its last products, whose operands are in registers, and behind it the
-    // buffer just read takes the loads of the step after the next.
-    __device__ __forceinline__ void run(char* lds0, char* lds1, const char* A, int64_t lda, int64_t m0, int64_t M,
-                                        const char* B, int64_t ldb, int64_t n0, int64_t N, const int32_t* rows,
-                                        int64_t s0, int64_t s1) {
-        const int tid = threadIdx.x, wave = uniform(tid / kWave), lane = tid % kWave;
-        const int wm = wave % WM, wn = wave / WM;
+    // one wait for loads into the same object).
+    __device__ __forceinline__ void start(char* lds0, char* lds1, int wave) {
+        if (left & 1) {
+            fetch(lds1, wave);
+            if (left > 1) fetch(lds0, wave);
+        } else if (left) {
+            fetch(lds0, wave);
+            fetch(lds1, wave);
+        }
+    }
+
+    // The products.  A step's four quarters (two pieces of each row) are read a quarter
+    // ahead of their products, the next step's first quarter too: the one barrier of a
+    // step stands before its last products, whose operands are in registers, and behind
+    // it the buffer just read takes the loads of the step after the next.
+    __device__ __forceinline__ void run(char* lds0, char* lds1, int wave, int lane) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-        if (s0 >= s1) return;
-        const char* src[kLoads];
-#pragma unroll
-        for (int l = 0; l < kLoads; ++l) {
-            const int r = (wave * kLoads + l) * 8 + lane / 8;  // row of the stage: BM of A, then BN of B
-            const int piece = (lane % 8) ^ turn(r);
-            if (r < BM) {
-                const int64_t m = m0 + r < M ? m0 + r : M - 1;
-                src[l] = A + m * lda + piece * 16 + s0 * kStepBytes;
-            } else {
-                int64_t n = n0 + (r - BM) < N ? n0 + (r - BM) : N - 1;
-                if (rows) n = rows[n];
-                src[l] = B + n * ldb + piece * 16 + s0 * kStepBytes;
-            }
-        }
-        const auto fetch = [&](char* lds) {
-#pragma unroll
-            for (int l = 0; l < kLoads; ++l) {
-                copy_to_lds(lds + (wave * kLoads + l) * 1024, src[l]);
-                src[l] += kStepBytes;
-            }
-        };
+        if (left == 0) return;
+        const int wm = wave % WM, wn = wave / WM;
         uint32_t at_a[4], at_b[4];  // a lane's places in a stage, by quarter
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -120,9 +140,11 @@ struct GemmNT {
         };
         const auto mul = [&](const Frag& f) {
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+            for (int e = 0; e < kParts; ++e)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) mma_piece(T(), f.a[i], f.b[j], acc[i][j]);
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) mma_part(T(), f.a[i], f.b[j], acc[i][j], e);
         };
         Frag f0, f1;
         const auto step = [&](char* cur, const char* nxt, bool more) {
@@ -136,33 +158,26 @@ struct GemmNT {
             mul(f0);
             mix();
             wait_loads<0>();
-            if (more) fetch(cur);
+            if (more) fetch(cur, wave);
             read(f0, nxt, 0);  // behind the last step what lies there, multiplied by nothing
             mul(f1);
             mix();
         };
-        int64_t left = s1 - s0;
-        fetch(left & 1 ? lds1 : lds0);
+        if (left > 1) wait_loads<kLoads>();
+        else wait_loads<0>();
         if (left & 1) {  // one step by itself, the others go in pairs
-            if (left > 1) {
-                fetch(lds0);
-                wait_loads<kLoads>();
-            } else {
-                wait_loads<0>();
-            }
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 read(f0, lds1, c);
                 mul(f0);
             }
-            wait_loads<kLoads>();  // lds1 has been read
-            --left;
+            lds_barrier();  // lds1 has been read
+            if (--left) {
+                fetch(lds1, wave);
+                wait_loads<kLoads>();
+            }
         }
-        if (left) {
-            fetch(lds1);
-            wait_loads<kLoads>();
-            read(f0, lds0, 0);
-        }
+        if (left) read(f0, lds0, 0);
         for (; left; left -= 2) {
             step(lds0, lds1, left > 2);
             step(lds1, lds0, left > 2);
@@ -175,7 +190,7 @@ private:
 
     // reads between the products
     __device__ __forceinline__ static void mix() {
-        constexpr int reads = TM + TN, products = TM * TN * (sizeof(T) == 2 ? 1 : 4);
+        constexpr int reads = TM + TN, products = TM * TN * kParts;
 #pragma unroll
         for (int k = 0; k < reads; ++k) {
             __builtin_amdgcn_sched_group_barrier(0x008, products / reads, 0);

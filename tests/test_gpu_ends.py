@@ -242,8 +242,9 @@ def test_loss_labels_that_leave_nothing(gt, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_loss_rows_without_a_label_are_not_read_into_results(gt, dtype):
-    x, w, y, up = loss_inputs(500, 200, 64, dtype, "i64", 0.5, 6)
+@pytest.mark.parametrize("n", [60, 256, 257, 500])
+def test_loss_rows_without_a_label_are_not_read_into_results(gt, n, dtype):
+    x, w, y, up = loss_inputs(n, 200, 64, dtype, "i64", 0.5, 6)
     off = (y < 0) | (y >= 200)
     want = gt.class_loss_fwd(x, w, y)
     grad = gt.class_loss_bwd(x, w, y, want[1], up)
