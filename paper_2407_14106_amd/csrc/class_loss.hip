@@ -108,18 +108,28 @@ __global__ __launch_bounds__(kListThreads) void k_list_place(int64_t n, int64_t 
     }
 }
 
-// Rows without a label have no gradient.
+// Rows without a label have no gradient: a wavefront looks at 64 labels, then groups of
+// its lanes clear the rows without one, a 16-byte piece a lane (the last one ending with
+// the row).
 template <typename T>
-__global__ __launch_bounds__(256) void k_zero_rows(int64_t n, int D, int64_t V, bool wide, const void* labels, T* dx) {
-    for (int64_t i = int64_t(blockIdx.x) * 4 + threadIdx.x / kWave; i < n; i += int64_t(gridDim.x) * 4) {
-        if (load_id(labels, wide, i, V) >= 0) continue;
-        constexpr int E = Piece<T>::E;
-        if (D < E) {
-            if (lane_id() < D) dx[i * D + lane_id()] = T(0);
-            continue;
+__global__ __launch_bounds__(256) void k_zero_rows(int64_t n, int D, int64_t V, bool wide, const void* labels, T* dx,
+                                                    int shift, bool far) {
+    constexpr int E = Piece<T>::E;
+    const float zero[E] = {};
+    const int lane = lane_id(), lanes = 1 << shift, groups = kWave >> shift, x = lane & (lanes - 1);
+    const int pieces = int(cdiv(D, E));
+    for (int64_t i0 = (int64_t(blockIdx.x) * 4 + threadIdx.x / kWave) * kWave; i0 < n;
+         i0 += int64_t(gridDim.x) * 4 * kWave) {
+        uint64_t none = ballot(i0 + lane < n && load_id(labels, wide, i0 + lane, V) < 0);
+        for (int r = lane >> shift; r < kWave; r += groups) {
+            if (!((none >> r) & 1u)) continue;
+            T* row = dx + (i0 + r) * D;
+            if (D < E) {
+                for (int c = x; c < D; c += lanes) row[c] = T(0);
+            } else {
+                for (int p = x; p < pieces; p += lanes) store_piece(row + (p * E + E <= D ? p * E : D - E), zero, far);
+            }
         }
-        const float zero[E] = {};
-        for (int c = lane_id() * E; c < D; c += kWave * E) store_piece(dx + i * D + (c + E <= D ? c : D - E), zero, false);
     }
 }
 template <typename T>
@@ -828,7 +838,10 @@ gt_status run_bwd(const Shape& h, const void* X, const void* W, bool wide, const
     st = make_rows<T>(h, b.l, X, ldx, b.x, W, ldw, b.w, s);
     if (st != GT_OK) return st;
     if (dX && b.l.list) {
-        k_zero_rows<T><<<grid_for(h.n, 4, 1 << 16), 256, 0, s>>>(h.n, h.D, h.V, wide, labels, static_cast<T*>(dX));
+        int shift = 0;
+        while (shift < 6 && (Piece<T>::E << shift) < h.D) ++shift;
+        k_zero_rows<T><<<grid_for(h.n, 256, 1 << 16), 256, 0, s>>>(h.n, h.D, h.V, wide, labels, static_cast<T*>(dX), shift,
+                                                                   h.n * h.D * h.size > kFarBytes);
         GT_LAUNCH_CHECK("class_loss zero rows");
     }
     for (int64_t v0 = 0; v0 < h.V; v0 += h.piece) {
