@@ -629,9 +629,11 @@ gt_status gt_dropout(int64_t n, gt_dtype dtype, double p, const uint64_t* rng, c
  *     strides ldx, ldw >= D elements between rows; rows whose stride or width is no
  *     multiple of 16 or 128 bytes are laid out once in the workspace.
  * GT_F32 multiplies and adds in fp32.  GT_BF16: logits, statistics and sums in fp32;
- * dL is rounded to bf16 where it multiplies a bf16 row (a relative error of at most
- * 2^-8 a term), dX and dW once at the end.  Sums in a fixed order.  Features are finite.
- * 0 <= n < 2^31, 1 <= V < 2^31, 1 <= D <= GT_MAX_WIDTH. */
+ * exp(s - lse) - [v = y] is rounded to bf16 where it multiplies a row of W, and times
+ * dloss_i / max |dloss| where it multiplies a row of X (a relative error of at most 2^-8
+ * a term each; dloss and its maximum join in fp32 at the end), dX and dW once more.
+ * Sums in a fixed order.  The labelled rows' features, W and dloss are finite.
+ * 0 <= n < 2^28, 1 <= V < 2^31, 1 <= D <= GT_MAX_WIDTH. */
 size_t gt_class_loss_fwd_workspace_size(int64_t n, int64_t V, int32_t D, gt_dtype dtype, int64_t ldx, int64_t ldw);
 gt_status gt_class_loss_fwd(int64_t n, int64_t V, int32_t D, gt_dtype dtype, gt_itype itype, const void* X, int64_t ldx,
                             const void* W, int64_t ldw, const void* labels, float* loss, float* lse, void* ws,

@@ -111,8 +111,9 @@ def class_loss(x, w, labels, dloss, half):
     g = p
     g[at, y] -= 1.0
     g = g * up
-    # of dL: p's, the subtraction's and the product's roundings, then the rounding to the features' type
-    dg = up.abs() * (dp + U) + 2 * U * g.abs() + half * g.abs()
+    # of dL: p's and the subtraction's roundings, four more of factors (dloss over its largest, the product, the largest
+    # again at the end), then the rounding to the features' type
+    dg = up.abs() * (dp + U) + 5 * U * g.abs() + half * g.abs()
     del s, ds, p, dp
     dx, dw = g @ w, g.t().contiguous() @ x
     out["dx"] = dx, dg @ w.abs() + 2 * U * V * (g.abs() @ w.abs()) + half * dx.abs()

@@ -29,6 +29,7 @@ constexpr int kListThreads = 1024, kListRounds = 8, kListRows = kListThreads * k
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // of dL, one way round: the last-level cache
 constexpr int64_t kMinPiece = 1024;                  // classes
 constexpr int kSplitBlocks = 256;                    // blocks that fill the chip
+constexpr int64_t kLaunchBlocks = int64_t(1) << 22;  // of a launch (its threads are counted in 32 bits)
 constexpr int64_t kGatherClasses = 2048;             // above, X's listed rows are laid out once: every block of
                                                      // classes would read them through the list (3% of its time)
 constexpr int64_t kListed = 256;                     // up to so many rows none is left out: they are one block
@@ -53,8 +54,9 @@ __device__ __forceinline__ uint32_t labelled(const void* labels, bool wide, int6
 }
 
 __global__ __launch_bounds__(kListThreads) void k_list_count(int64_t n, int64_t V, bool wide, const void* labels,
-                                                              int32_t* cnt) {
+                                                              int32_t* cnt, uint32_t* top) {
     __shared__ int s_n[kListThreads / kWave];
+    if (top && blockIdx.x == 0 && threadIdx.x == 0) *top = 0;
     const int c = wave_sum(__popc(labelled(labels, wide, n, V)));
     if (lane_id() == 0) s_n[threadIdx.x / kWave] = c;
     __syncthreads();
@@ -65,12 +67,18 @@ __global__ __launch_bounds__(kListThreads) void k_list_count(int64_t n, int64_t 
     }
 }
 
-// The list, and what a row without a label has in the forward's results.
+// Bits of |x|, which compare as |x| does.
+__device__ __forceinline__ uint32_t size_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+// The list; for the forward, what a row without a label has in its results; for the
+// backward, the largest |dloss| of a listed row (top, as bits).
 __global__ __launch_bounds__(kListThreads) void k_list_place(int64_t n, int64_t V, bool wide, const void* labels,
                                                               const int32_t* cnt, int32_t* list, int32_t* count,
-                                                              float* loss, float* lse) {
+                                                              float* loss, float* lse, const float* dloss,
+                                                              uint32_t* top) {
     constexpr int W = kListThreads / kWave;
     __shared__ int s_n[kListRounds * W], s_before[W];
+    __shared__ uint32_t s_top[W];
     const int wave = threadIdx.x / kWave, lane = lane_id();
     const uint32_t m = labelled(labels, wide, n, V);
     int rank[kListRounds];
@@ -83,11 +91,28 @@ __global__ __launch_bounds__(kListThreads) void k_list_place(int64_t n, int64_t 
     int before = 0;
     for (int64_t b = threadIdx.x; b < int64_t(blockIdx.x); b += kListThreads) before += cnt[b];
     before = wave_sum(before);
-    if (lane == 0) s_before[wave] = before;
+    uint32_t most = 0;
+    if (top) {
+#pragma unroll
+        for (int r = 0; r < kListRounds; ++r)
+            if ((m >> r) & 1u) {
+                const uint32_t b = size_bits(dloss[int64_t(blockIdx.x) * kListRows + r * kListThreads + threadIdx.x]);
+                most = most > b ? most : b;
+            }
+        most = wave_max(most);
+    }
+    if (lane == 0) s_before[wave] = before, s_top[wave] = most;
     __syncthreads();
     if (threadIdx.x == 0) {
         int t = 0;
-        for (int w = 0; w < W; ++w) t += s_before[w];
+        for (int w = 0; w < W; ++w) {
+            t += s_before[w];
+            most = most > s_top[w] ? most : s_top[w];
+        }
+        if (top) {
+            if (gridDim.x == 1) *top = most;
+            else atomicMax(top, most);
+        }
         for (int k = 0; k < kListRounds * W; ++k) {
             const int c = s_n[k];
             s_n[k] = t;
@@ -108,20 +133,20 @@ __global__ __launch_bounds__(kListThreads) void k_list_place(int64_t n, int64_t 
     }
 }
 
-// Rows without a label have no gradient: a wavefront looks at 64 labels, then groups of
-// its lanes clear the rows without one, a 16-byte piece a lane (the last one ending with
+// Rows without a label have no gradient: a wavefront looks at `span` labels (64, or fewer
+// where rows are few), then groups of its lanes clear the rows without one, a 16-byte piece a lane (the last one ending with
 // the row).
 template <typename T>
 __global__ __launch_bounds__(256) void k_zero_rows(int64_t n, int D, int64_t V, bool wide, const void* labels, T* dx,
-                                                    int shift, bool far) {
+                                                    int shift, int span, bool far) {
     constexpr int E = Piece<T>::E;
     const float zero[E] = {};
     const int lane = lane_id(), lanes = 1 << shift, groups = kWave >> shift, x = lane & (lanes - 1);
     const int pieces = int(cdiv(D, E));
-    for (int64_t i0 = (int64_t(blockIdx.x) * 4 + threadIdx.x / kWave) * kWave; i0 < n;
-         i0 += int64_t(gridDim.x) * 4 * kWave) {
-        uint64_t none = ballot(i0 + lane < n && load_id(labels, wide, i0 + lane, V) < 0);
-        for (int r = lane >> shift; r < kWave; r += groups) {
+    for (int64_t i0 = (int64_t(blockIdx.x) * 4 + threadIdx.x / kWave) * span; i0 < n;
+         i0 += int64_t(gridDim.x) * 4 * span) {
+        const uint64_t none = ballot(lane < span && i0 + lane < n && load_id(labels, wide, i0 + lane, V) < 0);
+        for (int r = lane >> shift; r < span; r += groups) {
             if (!((none >> r) & 1u)) continue;
             T* row = dx + (i0 + r) * D;
             if (D < E) {
@@ -172,12 +197,27 @@ struct Turn {
 };
 struct Turns {
     Turn t[2];
+    // of a call without a list, by the way: the largest |dloss| of a row with a label
+    const float* dloss;
+    uint32_t* top;
 };
 template <typename T>
 __global__ __launch_bounds__(256) void k_turn(Turns both, int C) {
     constexpr int E = 16 / int(sizeof(T)), P = 64 / E;  // pieces of 64 elements
     __shared__ T s[64][64 + 4 / sizeof(T)];
     const Turn& a = both.t[blockIdx.z];
+    if (both.top && a.labels && blockIdx.x == 0 && blockIdx.y == 0) {
+        __shared__ uint32_t s_top[4];
+        const int i = threadIdx.x;  // there are no more rows than threads
+        uint32_t most = i < a.R && load_id(a.labels, a.wide, i, a.V) >= 0 ? size_bits(both.dloss[i]) : 0u;
+        most = wave_max(most);
+        if (lane_id() == 0) s_top[i / kWave] = most;
+        __syncthreads();
+        if (i == 0) {
+            for (int w = 1; w < 4; ++w) most = most > s_top[w] ? most : s_top[w];
+            *both.top = most;
+        }
+    }
     const int64_t R = a.count ? int64_t(*a.count) : a.R, r0 = int64_t(blockIdx.x) * 64;
     if (r0 >= R) return;
     const int c0 = blockIdx.y * 64;
@@ -230,8 +270,9 @@ struct LossArgs {
     float *part, *hit;  // kStats: part[block][token] of two floats; with one block of classes, null and
     float *loss, *lse;  // the results themselves
     int64_t part_ld;
-    const float *lse_in, *dloss;  // kGrad
-    void *dl, *dlt;               // [token][dl_ld], [class][dlt_ld], either may be null
+    const float *lse_in, *dloss;  // kGrad; kStore: dloss, the rows' factors, or null
+    const uint32_t* top;          // kGrad: what dlt is relative to; kStore: a factor, or null
+    void *dl, *dlt;               // kGrad: dL without dloss [token][dl_ld], and with it [class][dlt_ld], or null
     int64_t dl_ld, dlt_ld;
     // kStore: out[split][row][M], or the result itself
     float* slots;
@@ -240,6 +281,23 @@ struct LossArgs {
     void* out;
     const int32_t* out_rows;
 };
+
+// The size that dL^T is relative to: the largest |dloss|.  In a mean all rows' dloss are
+// the same number, and dloss (p - 1) of the many labels with a small p would all be off
+// by the rounding of that one number (0.3% of dW at 1 / 6963); relative to it they are
+// -1.  dX takes its row's dloss at the end, in fp32.
+__device__ __forceinline__ float whole_size(const uint32_t* top) {
+    const float u = __uint_as_float(*top);
+    return u > 0.f ? u : 1.f;
+}
+
+// What a row of a stored result is multiplied by.
+__device__ __forceinline__ float factor_of(const float* dloss, const void* labels, bool wide, int64_t V,
+                                           const uint32_t* top, int64_t row) {
+    float f = top ? whole_size(top) : 1.f;
+    if (dloss) f = row >= 0 && (!labels || load_id(labels, wide, row, V) >= 0) ? f * dloss[row] : 0.f;
+    return f;
+}
 
 // The block of C, or of a part of a split sum, that a workgroup forms.  Each XCD takes
 // a contiguous share of the blocks, those that are formed together close to each other
@@ -380,7 +438,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_product(LossArgs a) {
             place[j] = id >= 0 && at >= 0 && at < TM * 32 ? int(at) : -1;
             if constexpr (WHAT == kGrad) {
                 lse[j] = id >= 0 ? a.lse_in[row] : 0.f;
-                up[j] = id >= 0 ? a.dloss[row] : 0.f;
+                up[j] = id >= 0 && a.dlt ? a.dloss[row] / whole_size(a.top) : 0.f;
             }
         }
     }
@@ -472,16 +530,15 @@ __global__ __launch_bounds__(WM * WN * 64) void k_product(LossArgs a) {
                         for (int e = 0; e < 4; ++e)
                             if (mw + mh + 32 * i + 8 * q + e >= a.M) v[e] = 0.f;
                     }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] *= up[j];
                     if (dlt) {
                         T* o = dlt + (mw + mh + 32 * i + 8 * q) * a.dlt_ld + t0;
                         if constexpr (sizeof(T) == 2) {
-                            const uint2 x = turn_quad(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), lane);
+                            const uint2 x = turn_quad(pack_bf16x2(v[0] * up[j], v[1] * up[j]),
+                                                      pack_bf16x2(v[2] * up[j], v[3] * up[j]), lane);
                             *reinterpret_cast<uint2*>(o + (lane & 3) * a.dlt_ld + (lane & 28)) = x;
                         } else {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) o[e * a.dlt_ld + (lane & 31)] = v[e];
+                            for (int e = 0; e < 4; ++e) o[e * a.dlt_ld + (lane & 31)] = v[e] * up[j];
                         }
                     }
                 };
@@ -490,13 +547,12 @@ __global__ __launch_bounds__(WM * WN * 64) void k_product(LossArgs a) {
                 });
             }
         } else {
-            const auto rows = [&](auto o, int j, const auto& out) {
-                using R = Rows32<decltype(o), TM>;
-                    R::run(
+            const auto rows = [&](auto o, int j, float factor, const auto& out) {
+                Rows32<decltype(o), TM>::run(
                     lds, lane,
                     [&](int i, int q, float(&v)[4]) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = g.acc[i][j][4 * q + e];
+                        for (int e = 0; e < 4; ++e) v[e] = g.acc[i][j][4 * q + e] * factor;
                     },
                     out);
             };
@@ -505,7 +561,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_product(LossArgs a) {
                 const int64_t t0 = nw + 32 * j;
                 if (a.slots) {
                     float* o = a.slots + split * a.slot_rows * a.M;
-                    rows(float(), j, [&](int at, int m, uint4 x) {
+                    rows(float(), j, 1.f, [&](int at, int m, uint4 x) {
                         const int64_t n = t0 + at, room = a.M - mw - m;
                         if (n >= N || room <= 0) return;
                         float* p = o + n * a.M + mw + m;
@@ -526,7 +582,10 @@ __global__ __launch_bounds__(WM * WN * 64) void k_product(LossArgs a) {
                         store_room(p, x, room);
                     });
                 } else {
-                    rows(T(), j, [&](int at, int m, const uint4& x) {
+                    const int64_t n = t0 + (lane & 31);
+                    const float factor = factor_of(a.dloss, a.labels, a.wide, a.V, a.top,
+                                                   n < N ? (a.out_rows ? int64_t(a.out_rows[n]) : n) : -1);
+                    rows(T(), j, factor, [&](int at, int m, const uint4& x) {
                         const int64_t n = t0 + at, room = a.M - mw - m;
                         if (n >= N || room <= 0) return;
                         const int64_t r = a.out_rows ? int64_t(a.out_rows[n]) : n;
@@ -545,48 +604,57 @@ __global__ __launch_bounds__(1024) void k_loss(int64_t blocks, const float2* par
     constexpr int P = 16, G = 1024 / P;  // tokens of a workgroup
     __shared__ float2 s[G][P + 1];
     const int x = threadIdx.x % P, y = threadIdx.x / P;
-    const int64_t t = int64_t(blockIdx.x) * P + x;
     if (count) n = *count;
-    if (int64_t(blockIdx.x) * P >= n) return;
-    float top = kNegInf, sum = 0.f;
-    if (t < n)
-        for (int64_t b = y; b < blocks; b += G) {
-            const float2 p = part[b * ld + t];
-            const float m = fmaxf(top, p.x), ref = m == kNegInf ? 0.f : m;
-            sum = sum * ex2(top - ref) + p.y * ex2(p.x - ref);
-            top = m;
+    for (int64_t t0 = int64_t(blockIdx.x) * P; t0 < n; t0 += int64_t(gridDim.x) * P) {
+        float top = kNegInf, sum = 0.f;
+        if (t0 + x < n)
+            for (int64_t b = y; b < blocks; b += G) {
+                const float2 p = part[b * ld + t0 + x];
+                const float m = fmaxf(top, p.x), ref = m == kNegInf ? 0.f : m;
+                sum = sum * ex2(top - ref) + p.y * ex2(p.x - ref);
+                top = m;
+            }
+        s[y][x] = make_float2(top, sum);
+        __syncthreads();
+        if (y < P) {  // turned: a wavefront's 16 lanes of a token take its 64 sums
+            top = kNegInf;
+            float2 p[G / P];
+#pragma unroll
+            for (int k = 0; k < G / P; ++k) p[k] = s[x + P * k][y], top = fmaxf(top, p[k].x);
+#pragma unroll
+            for (int o = 1; o < P; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+            const float ref = top == kNegInf ? 0.f : top;
+            sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < G / P; ++k) sum += p[k].y * ex2(p[k].x - ref);
+#pragma unroll
+            for (int o = 1; o < P; o <<= 1) sum += __shfl_xor(sum, o, kWave);
+            const int64_t t = t0 + y;
+            if (x == 0 && t < n) {
+                const int64_t i = list ? int64_t(list[t]) : t;
+                const bool has = load_id(labels, wide, i, V) >= 0;
+                const float all = (ref + log2f(sum)) * kLn2;
+                lse[i] = has ? all : 0.f;
+                loss[i] = has ? all - hit[t] : 0.f;
+            }
         }
-    s[y][x] = make_float2(top, sum);
-    __syncthreads();
-    if (y >= P) return;
-    // the lanes turned: a wavefront's 16 lanes of a token take its 64 sums
-    const int tok = y, l = x;
-    const int64_t tt = int64_t(blockIdx.x) * P + tok;
-    top = kNegInf;
-    float2 p[G / P];
-#pragma unroll
-    for (int k = 0; k < G / P; ++k) p[k] = s[l + P * k][tok], top = fmaxf(top, p[k].x);
-#pragma unroll
-    for (int o = 1; o < P; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
-    const float ref = top == kNegInf ? 0.f : top;
-    sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < G / P; ++k) sum += p[k].y * ex2(p[k].x - ref);
-#pragma unroll
-    for (int o = 1; o < P; o <<= 1) sum += __shfl_xor(sum, o, kWave);
-    if (l || tt >= n) return;
-    const int64_t i = list ? int64_t(list[tt]) : tt;
-    const bool has = load_id(labels, wide, i, V) >= 0;
-    const float all = (ref + log2f(sum)) * kLn2;
-    lse[i] = has ? all : 0.f;
-    loss[i] = has ? all - hit[tt] : 0.f;
+        __syncthreads();
+    }
 }
 
 // out[row][c] = the sum of the slots, four columns a lane where rows are whole such;
 // the slots go by over L lanes.
+struct Factors {
+    const float* dloss;
+    const void* labels;
+    bool wide;
+    int64_t V;
+    const uint32_t* top;
+    __device__ __forceinline__ float of(int64_t row) const { return factor_of(dloss, labels, wide, V, top, row); }
+};
 template <typename T, int L>
 __global__ __launch_bounds__(256) void k_sum_slots(int splits, int64_t slot_rows, int64_t R, const int32_t* count,
-                                                    int64_t C, const float* slots, const int32_t* rows, T* out) {
+                                                    int64_t C, const float* slots, const int32_t* rows, T* out, Factors f) {
     constexpr int P = 256 / L;
     __shared__ float4 s[L][P];
     if (count) R = *count;
@@ -624,6 +692,9 @@ __global__ __launch_bounds__(256) void k_sum_slots(int splits, int64_t slot_rows
         if (y) continue;
         const int64_t r = i / C;
         if (room >= 4 && (i + 3) / C == r) {
+            const float by = f.of(rows ? int64_t(rows[r]) : r);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] *= by;
             T* o = rows ? out + int64_t(rows[r]) * C + (i - r * C) : out + i;
             if constexpr (sizeof(T) == 2) {
                 typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
@@ -637,7 +708,8 @@ __global__ __launch_bounds__(256) void k_sum_slots(int splits, int64_t slot_rows
             for (int e = 0; e < 4; ++e)
                 if (e < room) {
                     const int64_t re = (i + e) / C;
-                    store_one(rows ? out + int64_t(rows[re]) * C + (i + e - re * C) : out + i + e, v[e]);
+                    const int64_t row = rows ? int64_t(rows[re]) : re;
+                    store_one(out + row * C + (i + e - re * C), v[e] * f.of(row));
                 }
         }
     }
@@ -710,12 +782,14 @@ Shape shape_of(int64_t n, int64_t V, int32_t D, gt_dtype dt, int64_t ldx, int64_
 
 struct List {
     int32_t *list, *count, *cnt;
+    uint32_t* top;  // the largest |dloss|
 };
 List list_ws(Ws& w, int64_t n) {
     List l;
     l.list = w.take<int32_t>(size_t(n));
     l.count = w.take<int32_t>(1);
     l.cnt = w.take<int32_t>(size_t(cdiv(n, kListRows)));
+    l.top = w.take<uint32_t>(1);
     return l;
 }
 
@@ -753,17 +827,19 @@ BwdWs bwd_ws(Ws& w, const Shape& h) {
     return b;
 }
 
-gt_status make_list(const Shape& h, bool wide, const void* labels, List& l, float* loss, float* lse, hipStream_t s) {
+gt_status make_list(const Shape& h, bool wide, const void* labels, List& l, float* loss, float* lse, const float* dloss,
+                    hipStream_t s) {
     if (h.n <= kListed) {
         l.list = l.count = nullptr;
         return GT_OK;
     }
     const unsigned blocks = unsigned(cdiv(h.n, kListRows));
     if (blocks > 1) {
-        k_list_count<<<blocks, kListThreads, 0, s>>>(h.n, h.V, wide, labels, l.cnt);
+        k_list_count<<<blocks, kListThreads, 0, s>>>(h.n, h.V, wide, labels, l.cnt, dloss ? l.top : nullptr);
         GT_LAUNCH_CHECK("class_loss count");
     }
-    k_list_place<<<blocks, kListThreads, 0, s>>>(h.n, h.V, wide, labels, l.cnt, l.list, l.count, loss, lse);
+    k_list_place<<<blocks, kListThreads, 0, s>>>(h.n, h.V, wide, labels, l.cnt, l.list, l.count, loss, lse, dloss,
+                                                   dloss ? l.top : nullptr);
     GT_LAUNCH_CHECK("class_loss list");
     return GT_OK;
 }
@@ -791,35 +867,45 @@ gt_status make_rows(const Shape& h, const List& l, const void*& X, int64_t& ldx,
 template <typename T>
 gt_status run_fwd(const Shape& h, const void* X, const void* W, bool wide, const void* labels, float* loss, float* lse,
                   FwdWs f, hipStream_t s) {
-    gt_status st = make_list(h, wide, labels, f.l, loss, lse, s);
+    gt_status st = make_list(h, wide, labels, f.l, loss, lse, nullptr, s);
     if (st != GT_OK) return st;
     int64_t ldx = h.ldx, ldw = h.ldw;
     st = make_rows<T>(h, f.l, X, ldx, f.x, W, ldw, f.w, s);
     if (st != GT_OK) return st;
-    const int64_t blocks = cdiv(h.V, block_rows(h.V));
+    const int64_t side = block_rows(h.V), blocks = cdiv(h.V, side);
     LossArgs a = {};
-    a.A = static_cast<const char*>(W), a.lda = ldw * h.size, a.M = h.V;
+    a.lda = ldw * h.size;
     a.B = static_cast<const char*>(X), a.ldb = ldx * h.size, a.N = h.n;
     a.n_count = f.l.count, a.list = f.l.list, a.gather = !h.copy_x;
     a.steps = h.row / kStepBytes, a.splits = 1;
     a.V = h.V, a.labels = labels, a.wide = wide;
     if (blocks == 1) a.loss = loss, a.lse = lse;
-    else a.part = f.part, a.part_ld = h.mp, a.hit = f.hit;
-    st = product<T, kStats>(a, s);
-    if (st != GT_OK || blocks == 1) return st;
-    k_loss<<<unsigned(cdiv(h.n, 16)), 1024, 0, s>>>(blocks, reinterpret_cast<float2*>(f.part), h.mp, f.hit, labels, wide,
-                                                    h.V, f.l.list, f.l.count, h.n, loss, lse);
+    else a.part_ld = h.mp, a.hit = f.hit;
+    // as many classes as a launch takes
+    const int64_t piece = side * (kLaunchBlocks / cdiv(h.n, block_rows(h.n)));
+    for (int64_t v0 = 0; v0 < h.V; v0 += piece) {
+        a.A = static_cast<const char*>(W) + v0 * a.lda;
+        a.M = h.V - v0 < piece ? h.V - v0 : piece;
+        a.v0 = v0;
+        a.part = f.part + 2 * (v0 / side) * h.mp;
+        st = product<T, kStats>(a, s);
+        if (st != GT_OK) return st;
+    }
+    if (blocks == 1) return GT_OK;
+    k_loss<<<grid_for(h.n, 16, 1 << 16), 1024, 0, s>>>(blocks, reinterpret_cast<float2*>(f.part), h.mp, f.hit, labels, wide,
+                                                       h.V, f.l.list, f.l.count, h.n, loss, lse);
     GT_LAUNCH_CHECK("class_loss join");
     return GT_OK;
 }
 
 template <typename T>
 gt_status sum_slots(int splits, int64_t slot_rows, int64_t R, const int32_t* count, int64_t C, const float* slots,
-                    const int32_t* rows, T* out, hipStream_t s) {
+                    const int32_t* rows, T* out, const LossArgs& a, hipStream_t s) {
+    const Factors f = {a.dloss, a.labels, a.wide, a.V, a.top};
     if (splits > 1)
-        k_sum_slots<T, 8><<<grid_for(R * C, 128, 1 << 16), 256, 0, s>>>(splits, slot_rows, R, count, C, slots, rows, out);
+        k_sum_slots<T, 8><<<grid_for(R * C, 128, 1 << 16), 256, 0, s>>>(splits, slot_rows, R, count, C, slots, rows, out, f);
     else
-        k_sum_slots<T, 1><<<grid_for(R * C, 1024, 1 << 16), 256, 0, s>>>(splits, slot_rows, R, count, C, slots, rows, out);
+        k_sum_slots<T, 1><<<grid_for(R * C, 1024, 1 << 16), 256, 0, s>>>(splits, slot_rows, R, count, C, slots, rows, out, f);
     GT_LAUNCH_CHECK("class_loss sum");
     return GT_OK;
 }
@@ -832,7 +918,7 @@ gt_status run_bwd(const Shape& h, const void* X, const void* W, bool wide, const
         GT_LAUNCH_CHECK("class_loss zero");
         return GT_OK;
     }
-    gt_status st = make_list(h, wide, labels, b.l, nullptr, nullptr, s);
+    gt_status st = make_list(h, wide, labels, b.l, nullptr, nullptr, dW ? dloss : nullptr, s);
     if (st != GT_OK) return st;
     int64_t ldx = h.ldx, ldw = h.ldw;
     st = make_rows<T>(h, b.l, X, ldx, b.x, W, ldw, b.w, s);
@@ -840,10 +926,12 @@ gt_status run_bwd(const Shape& h, const void* X, const void* W, bool wide, const
     if (dX && b.l.list) {
         int shift = 0;
         while (shift < 6 && (Piece<T>::E << shift) < h.D) ++shift;
-        k_zero_rows<T><<<grid_for(h.n, 256, 1 << 16), 256, 0, s>>>(h.n, h.D, h.V, wide, labels, static_cast<T*>(dX), shift,
-                                                                   h.n * h.D * h.size > kFarBytes);
+        const int span = h.n >= 65536 ? 64 : 8;
+        k_zero_rows<T><<<grid_for(h.n, 4 * span, 1 << 16), 256, 0, s>>>(h.n, h.D, h.V, wide, labels, static_cast<T*>(dX),
+                                                                        shift, span, h.n * h.D * h.size > kFarBytes);
         GT_LAUNCH_CHECK("class_loss zero rows");
     }
+    LossArgs last_x = {};
     for (int64_t v0 = 0; v0 < h.V; v0 += h.piece) {
         const int64_t vn = h.V - v0 < h.piece ? h.V - v0 : h.piece;
         const char* w = static_cast<const char*>(W) + v0 * ldw * h.size;
@@ -855,6 +943,7 @@ gt_status run_bwd(const Shape& h, const void* X, const void* W, bool wide, const
             most = vn;
         }
         if (dW && v0 == 0) {
+            if (!b.l.list) turns.dloss = dloss, turns.top = b.l.top;
             turns.t[jobs++] = {h.n, b.l.count, h.copy_x ? nullptr : b.l.list, b.l.list ? nullptr : labels,
                                wide, h.V, X, ldx, b.xt, h.ldt};
             most = most > h.n ? most : h.n;
@@ -870,7 +959,7 @@ gt_status run_bwd(const Shape& h, const void* X, const void* W, bool wide, const
         a.steps = h.row / kStepBytes, a.splits = 1;
         a.v0 = v0, a.V = h.V, a.labels = labels, a.wide = wide, a.lse_in = lse, a.dloss = dloss;
         a.dl = dX ? b.dl : nullptr, a.dl_ld = h.ldp;
-        a.dlt = dW ? b.dlt : nullptr, a.dlt_ld = h.ldt;
+        a.dlt = dW ? b.dlt : nullptr, a.dlt_ld = h.ldt, a.top = b.l.top;
         st = product<T, kGrad>(a, s);
         if (st != GT_OK) return st;
         if (dX) {
@@ -880,6 +969,8 @@ gt_status run_bwd(const Shape& h, const void* X, const void* W, bool wide, const
             x.steps = cdiv(vn * h.size, kStepBytes), x.splits = h.sx;
             x.slots = b.slots_x, x.slot_rows = h.n, x.add = v0 > 0;
             x.out = dX, x.out_rows = b.l.list;
+            x.dloss = dloss, x.labels = b.l.list ? nullptr : labels, x.wide = wide, x.V = h.V;
+            last_x = x;
             st = product<T, kStore>(x, s);
             if (st != GT_OK) return st;
         }
@@ -890,23 +981,22 @@ gt_status run_bwd(const Shape& h, const void* X, const void* W, bool wide, const
             x.steps = cdiv(h.n * h.size, kStepBytes), x.k_count = b.l.count, x.splits = h.sw;
             x.slots = b.slots_w, x.slot_rows = h.piece;
             T* out = static_cast<T*>(dW) + v0 * h.D;
-            x.out = out;
+            x.out = out, x.top = b.l.top;
             st = product<T, kStore>(x, s);
             if (st == GT_OK && b.slots_w)
-                st = sum_slots<T>(h.sw, h.piece, vn, nullptr, h.D, b.slots_w, nullptr, out, s);
+                st = sum_slots<T>(h.sw, h.piece, vn, nullptr, h.D, b.slots_w, nullptr, out, x, s);
             if (st != GT_OK) return st;
         }
     }
     if (dX && b.slots_x)
-        return sum_slots<T>(h.sx, h.n, h.n, b.l.count, h.D, b.slots_x, b.l.list, static_cast<T*>(dX), s);
+        return sum_slots<T>(h.sx, h.n, h.n, b.l.count, h.D, b.slots_x, b.l.list, static_cast<T*>(dX), last_x, s);
     return GT_OK;
 }
 
 bool loss_sizes(int64_t n, int64_t V, int32_t D, gt_dtype dt, int64_t ldx, int64_t ldw) {
     const int64_t most = int64_t(1) << 31;
-    return (dt == GT_BF16 || dt == GT_F32) && n >= 0 && n < most && V >= 1 && V < most && D >= 1 && D <= GT_MAX_WIDTH &&
-           ldx >= D && ldw >= D && ldx < most && ldw < most &&
-           cdiv(n, 64) * cdiv(V, 64) < (int64_t(1) << 30);  // blocks are counted in 32 bits
+    return (dt == GT_BF16 || dt == GT_F32) && n >= 0 && n < most / 8 && V >= 1 && V < most && D >= 1 && D <= GT_MAX_WIDTH &&
+           ldx >= D && ldw >= D && ldx < most && ldw < most;
 }
 gt_status loss_check(const char* who, int64_t n, int64_t V, int32_t D, gt_dtype dt, gt_itype it, const void* X,
                      int64_t ldx, const void* W, int64_t ldw, const void* labels) {

@@ -62,7 +62,7 @@ def test_dropout_arguments(lib):
 
 
 @pytest.mark.parametrize("n,V,D,dt,it,ldx,ldw,want", [
-    (-1, 10, 8, BF, I32, 8, 8, ARG), (1 << 31, 10, 8, BF, I32, 8, 8, ARG), (5, 0, 8, BF, I32, 8, 8, ARG),
+    (-1, 10, 8, BF, I32, 8, 8, ARG), (1 << 28, 10, 8, BF, I32, 8, 8, ARG), (5, 0, 8, BF, I32, 8, 8, ARG),
     (5, 1 << 31, 8, BF, I32, 8, 8, ARG), (5, 10, 0, BF, I32, 8, 8, ARG), (5, 10, 8, BF, I32, 7, 8, ARG),
     (5, 10, 8, BF, I32, 8, 7, ARG), (5, 10, 8, BF, I32, 1 << 31, 8, ARG),
     (5, 10, gt.GT_MAX_WIDTH + 1, BF, I32, 1 << 20, 1 << 20, ARG), (5, 10, 8, 2, I32, 8, 8, UNS),

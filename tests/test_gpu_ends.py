@@ -95,6 +95,40 @@ def test_embed_whole_numbers(gt):
         assert torch.equal(got.double(), want[:-1])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_embed_tables_of_few_rows(gt, dtype):
+    # rows held in LDS: 16 or 8 pieces of 16 bytes, whole ones and a last one that ends with the row; and the limits
+    D16, D8 = (256, 150) if dtype == "bf16" else (128, 77)
+    for n, F, R, D in ((4000, 9, 173, D16), (5000, 4, 256, D8), (9000, 3, 257, D16), (12_000, 5, 512, D8 + 3),
+                       (12_000, 5, 513, D16), (700, 2, 20, 64), (701, 2, 1, 129), (3000, 12, 31, 1000)):
+        embed_case(gt, n, F, R, D, dtype, "i64" if n % 2 else "i32", seed=n + R)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_embed_shared_rows_taken_together(gt, dtype):
+    # more rows than the L2 caches hold, several fields each: the chunks go by the rows they read
+    D = 256 if dtype == "bf16" else 128
+    embed_case(gt, 70_000, 3, 900, D, dtype, "i32", seed=1)
+    embed_case(gt, 70_000, 2, 100_000, D + 1, dtype, "i64", seed=2)
+
+
+@pytest.mark.parametrize("pairs", [8191, 8192, 8193])
+def test_embed_sorts_at_their_limits(gt, pairs):
+    # one workgroup's sort and the device-wide one, keys of one to four digits
+    for R in (200, 255, 256, 40_000, 70_000, 20_000_000):
+        embed_case(gt, pairs, 1, R, 3, "f32", "i64", seed=R % 1000)
+
+
+def test_embed_same_id_in_two_fields(gt):
+    ids = torch.randint(0, 7, (300, 1), generator=torch.Generator().manual_seed(0)).cuda().repeat(1, 3).contiguous()
+    embed_case(gt, 300, 3, 7, 40, "bf16", "i64", ids=ids)
+
+
+def test_embed_results_beyond_the_caches(gt):
+    embed_case(gt, 150_000, 1, 140_000, 1024, "bf16", "i64", seed=3)
+    embed_case(gt, 80_000, 2, 90_000, 1001, "f32", "i32", seed=4)
+
+
 def test_embed_nothing_and_far_ids(gt):
     table = normal((10, 16), 0, "f32")
     none = torch.empty((0, 3), dtype=torch.int32, device="cuda")
@@ -285,6 +319,33 @@ def test_loss_pieces_and_split_sums(gt, dtype):
     # many rows and more classes than a piece holds; few rows and a long sum for dX; few classes and a long one for dW
     for n, V, D, lab in ((70_000, 3000, 64, 0.9), (100, 40_000, 64, 1.0), (60_000, 30, 64, 0.5), (9000, 300, 128, 0.1)):
         loss_case(gt, n, V, D, dtype, labelled=lab, seed=n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_loss_equal_upstream_gradients_are_exact_factors(gt, dtype):
+    # a mean: what is rounded to bf16 does not depend on 1 / m, so another m scales every gradient by the ratio alone
+    x, w, y, _ = loss_inputs(300, 500, 64, dtype, "i64", 0.7, 11)
+    lse = gt.class_loss_fwd(x, w, y)[1]
+    a = gt.class_loss_bwd(x, w, y, lse, torch.full((300,), 1.0, device="cuda"))
+    b = gt.class_loss_bwd(x, w, y, lse, torch.full((300,), 1.0 / 6963, device="cuda"))
+    for p, q in zip(a, b):
+        # two roundings to the features' type, and a few of fp32
+        assert ((p.double() / 6963 - q.double()).abs() <= (2 * HALF[dtype] + 8 * 2.0 ** -24) * q.double().abs()).all()
+    zero = gt.class_loss_bwd(x, w, y, lse, torch.zeros(300, device="cuda"))
+    assert not zero[0].any() and not zero[1].any()
+    tiny = torch.full((300,), 1e-36, device="cuda")
+    big = torch.full((300,), 1e30, device="cuda")
+    for up in (tiny, big):
+        for p, q in zip(a, gt.class_loss_bwd(x, w, y, lse, up)):
+            f = float(up[0])
+            # fp32 has no finer numbers than 2^-149, and bf16 none below 2^-133
+            assert ((p.double() * f - q.double()).abs() <= (2 * HALF[dtype] + 2.0 ** -20) * q.double().abs() + 2.0 ** -132).all()
+
+
+@pytest.mark.parametrize("n", [255, 256, 257, 8192, 8193])
+def test_loss_listed_rows_at_their_limits(gt, n):
+    loss_case(gt, n, 70, 64, "bf16", labelled=0.5, seed=n)
+    loss_case(gt, n, 2049, 32, "f32", labelled=0.9, seed=n)  # X's rows laid out once
 
 
 # ----------------------------------------------------------------------------- streams, graphs, together
