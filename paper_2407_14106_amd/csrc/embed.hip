@@ -233,14 +233,122 @@ void run_fwd(FwdArgs g, hipStream_t s) {
     else k_embed_fwd<T, 4><<<grid, 256, 0, s>>>(g);
 }
 
-__global__ __launch_bounds__(256) void k_embed_keys(int64_t pairs, int F, int64_t R, bool wide, const void* ids,
-                                                     uint32_t* key, uint32_t* row, uint32_t* count) {
-    const int64_t k = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (k < kCounts) count[k] = 0;
-    if (k >= pairs) return;
-    const int64_t id = load_id(ids, wide, k, R);
-    key[k] = uint32_t(id >= 0 ? id : R);  // behind the table: added to nothing
-    row[k] = uint32_t(k / F);
+// The pairs' stable sort by key, up to 9 bits a pass, least significant first (a table of
+// up to 511 rows takes one pass, of 262,143 two; in 11 bits, three million pairs of 1,501
+// keys took one pass of 139 us instead of two of 40: the digits' counts are as many as
+// the pairs, and neighbours go to places far apart).  A workgroup has a tile of pairs,
+// wavefront after wavefront in rounds of 64; it counts the tile's digits, the counts of
+// all tiles are scanned digit by digit, and a pair goes to its digit's place in its tile
+// by (wavefront, round, lane).  The first pass takes the ids themselves.
+constexpr int kSortThreads = 256, kSortWaves = kSortThreads / kWave, kSortRounds = 8;
+constexpr int kSortTile = kSortThreads * kSortRounds, kMostBits = 9;
+
+struct SortArgs {
+    int64_t pairs, tiles, R;
+    int F, shift, bits;  // 2^bits digits at `shift`
+    bool wide;
+    const void* ids;            // first pass
+    const uint32_t *key, *row;  // the others
+    uint32_t* hist;             // [digit][tile]
+    const int64_t* place;       // its scan
+    uint32_t *key_out, *row_out, *count;
+};
+
+// Digits of a wavefront's rounds; behind the last pair 2^bits.
+template <bool FIRST>
+__device__ __forceinline__ void load_pairs(const SortArgs& a, int64_t base, uint32_t (&key)[kSortRounds],
+                                           uint32_t (&row)[kSortRounds], bool rows) {
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r) {
+        const int64_t i = base + r * kWave;
+        key[r] = row[r] = 0;
+        if (i >= a.pairs) continue;
+        if constexpr (FIRST) {
+            const int64_t id = load_id(a.ids, a.wide, i, a.R);
+            key[r] = uint32_t(id >= 0 ? id : a.R);  // behind the table: added to nothing
+            row[r] = uint32_t(i) / uint32_t(a.F);
+        } else {
+            key[r] = a.key[i];
+            if (rows) row[r] = a.row[i];
+        }
+    }
+}
+
+template <bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void k_embed_sort_count(SortArgs a) {
+    __shared__ uint32_t s_n[1 << kMostBits];
+    const int digits = 1 << a.bits, tid = threadIdx.x;
+    for (int d = tid; d < digits; d += kSortThreads) s_n[d] = 0;
+    if constexpr (FIRST)
+        if (blockIdx.x == 0)
+            for (int k = tid; k < kCounts; k += kSortThreads) a.count[k] = 0;
+    uint32_t key[kSortRounds], row[kSortRounds];
+    const int64_t base = int64_t(blockIdx.x) * kSortTile + tid / kWave * (kSortRounds * kWave) + tid % kWave;
+    load_pairs<FIRST>(a, base, key, row, false);
+    __syncthreads();
+    const uint64_t lt = lanemask_lt();
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r) {
+        const bool valid = base + r * kWave < a.pairs;
+        const uint32_t d = (key[r] >> a.shift) & uint32_t(digits - 1);
+        // frequent digits: the wavefront's pairs of its first pair's digit in one addition
+        const uint32_t lead = uint32_t(__builtin_amdgcn_readfirstlane(int(d)));
+        const uint64_t same = ballot(valid && d == lead);
+        if (valid) {
+            if (d != lead) atomicAdd(&s_n[d], 1u);
+            else if ((same & lt) == 0) atomicAdd(&s_n[d], uint32_t(__popcll(same)));
+        }
+    }
+    __syncthreads();
+    for (int d = tid; d < digits; d += kSortThreads) a.hist[int64_t(d) * a.tiles + blockIdx.x] = s_n[d];
+}
+
+template <bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void k_embed_sort_place(SortArgs a) {
+    __shared__ uint32_t s_n[kSortWaves][1 << kMostBits];  // counts, then where a wavefront's pairs of a digit go
+    const int digits = 1 << a.bits, tid = threadIdx.x, w = tid / kWave;
+    for (int d = tid; d < digits; d += kSortThreads)
+#pragma unroll
+        for (int q = 0; q < kSortWaves; ++q) s_n[q][d] = 0;
+    uint32_t key[kSortRounds], row[kSortRounds], rank[kSortRounds];
+    const int64_t base = int64_t(blockIdx.x) * kSortTile + w * (kSortRounds * kWave) + tid % kWave;
+    load_pairs<FIRST>(a, base, key, row, true);
+    __syncthreads();
+    const uint64_t lt = lanemask_lt();
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r) {
+        const bool valid = base + r * kWave < a.pairs;
+        const uint32_t d = (key[r] >> a.shift) & uint32_t(digits - 1);
+        uint64_t peers = ballot(valid);
+        for (int b = 0; b < a.bits; ++b) {
+            const bool bit = (d >> b) & 1u;
+            const uint64_t bm = ballot(bit);
+            peers &= bit ? bm : ~bm;
+        }
+        // the wavefront's pairs of the digit so far: read by all of them, then moved on
+        // by the first (a wavefront's LDS accesses complete in order)
+        const uint32_t mine = uint32_t(__popcll(peers & lt)), before = valid ? s_n[w][d] : 0u;
+        if (valid && mine == 0) s_n[w][d] = before + uint32_t(__popcll(peers));
+        rank[r] = before + mine;
+    }
+    __syncthreads();
+    for (int d = tid; d < digits; d += kSortThreads) {
+        uint32_t at = uint32_t(a.place[int64_t(d) * a.tiles + blockIdx.x]);  // fewer than 2^31 pairs
+#pragma unroll
+        for (int q = 0; q < kSortWaves; ++q) {
+            const uint32_t c = s_n[q][d];
+            s_n[q][d] = at;
+            at += c;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r)
+        if (base + r * kWave < a.pairs) {
+            const uint32_t p = s_n[w][(key[r] >> a.shift) & uint32_t(digits - 1)] + rank[r];
+            a.key_out[p] = key[r];
+            a.row_out[p] = row[r];
+        }
 }
 
 // The first of the sorted pairs whose key is at or above r.
@@ -552,9 +660,10 @@ __global__ __launch_bounds__(256) void k_embed_merge(int D, const int32_t* start
 }
 
 struct BwdWs {
-    uint32_t *key, *row, *count, *order;
+    uint32_t *key, *row, *key2, *row2, *hist, *count, *order;
+    int64_t* place;
+    ScanTmp scan;
     int32_t *start, *list;
-    SortTmp sort;
     float* part;
 };
 
@@ -562,12 +671,56 @@ struct BwdWs {
 // more than the L2 caches hold anyway.
 bool ordered(int64_t n, int32_t F, int32_t D, int size) { return F > 1 && n * D * size > kL2Bytes; }
 
+// Passes over keys 0 to R, and the bits that each takes.
+struct SortPasses {
+    int passes, bits;
+    explicit SortPasses(int64_t R) {
+        const int all = bits_for(R + 1);
+        passes = int(cdiv(all, kMostBits));
+        bits = int(cdiv(all, passes));
+    }
+};
+
+// Sorts the pairs into b.key and b.row.
+gt_status sort_pairs(int64_t pairs, int32_t F, int64_t R, bool wide, const void* ids, const BwdWs& b, hipStream_t s) {
+    const SortPasses p(R);
+    SortArgs a = {};
+    a.pairs = pairs, a.tiles = cdiv(pairs, kSortTile), a.R = R, a.F = F, a.bits = p.bits, a.wide = wide, a.ids = ids;
+    a.hist = b.hist, a.place = b.place, a.count = b.count;
+    const unsigned grid = unsigned(a.tiles);
+    for (int k = 0; k < p.passes; ++k, a.shift += p.bits) {
+        // the last pass ends in key and row
+        const bool main = (p.passes - 1 - k) % 2 == 0;
+        a.key = main ? b.key2 : b.key, a.row = main ? b.row2 : b.row;
+        a.key_out = main ? b.key : b.key2, a.row_out = main ? b.row : b.row2;
+        if (k == 0) k_embed_sort_count<true><<<grid, kSortThreads, 0, s>>>(a);
+        else k_embed_sort_count<false><<<grid, kSortThreads, 0, s>>>(a);
+        GT_LAUNCH_CHECK("embed_bwd count");
+        const gt_status st = exclusive_scan_u32(b.hist, a.tiles << p.bits, b.place, b.scan, s);
+        if (st != GT_OK) return st;
+        if (k == 0) k_embed_sort_place<true><<<grid, kSortThreads, 0, s>>>(a);
+        else k_embed_sort_place<false><<<grid, kSortThreads, 0, s>>>(a);
+        GT_LAUNCH_CHECK("embed_bwd place");
+    }
+    return GT_OK;
+}
+
 BwdWs bwd_ws(Ws& w, int64_t n, int32_t F, int64_t R, int32_t D, int size) {
     const int64_t pairs = n * F, chunks = cdiv(pairs, kRun);
     BwdWs b = {};
     b.key = w.take<uint32_t>(size_t(pairs));
     b.row = w.take<uint32_t>(size_t(pairs));
-    if (pairs > kSmallPairs) b.sort = sort_tmp(w, pairs, 4, true);
+    if (pairs > kSmallPairs) {
+        const SortPasses p(R);
+        const int64_t entries = cdiv(pairs, kSortTile) << p.bits;
+        if (p.passes > 1) {
+            b.key2 = w.take<uint32_t>(size_t(pairs));
+            b.row2 = w.take<uint32_t>(size_t(pairs));
+        }
+        b.hist = w.take<uint32_t>(size_t(entries));
+        b.place = w.take<int64_t>(size_t(entries + 1));
+        b.scan.block_sums = w.take<int64_t>(size_t(scan_tmp_elems(entries)));
+    }
     b.start = w.take<int32_t>(size_t(R + 1));
     b.count = w.take<uint32_t>(kCounts);
     b.list = w.take<int32_t>(size_t(pairs / kRun + 1));
@@ -586,9 +739,7 @@ gt_status run_bwd(int64_t n, int32_t F, int64_t R, int32_t D, bool wide, const v
                                                        b.count);
         GT_LAUNCH_CHECK("embed_bwd sort");
     } else {
-        k_embed_keys<<<unsigned(cdiv(pairs, 256)), 256, 0, s>>>(pairs, F, R, wide, ids, b.key, b.row, b.count);
-        GT_LAUNCH_CHECK("embed_bwd keys");
-        const gt_status st = radix_sort_u32(b.key, b.row, pairs, bits_for(R + 1), b.sort, s);
+        const gt_status st = sort_pairs(pairs, F, R, wide, ids, b, s);
         if (st != GT_OK) return st;
     }
     k_embed_starts<<<unsigned(cdiv(R + 1, 256)), 256, 0, s>>>(pairs, R, b.key, b.start, b.list, b.count);
