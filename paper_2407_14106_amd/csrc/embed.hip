@@ -82,6 +82,16 @@ template <typename T, int FB>
 __device__ __forceinline__ void embed_piece(const FwdArgs& g, int64_t i, const uint32_t (&first)[FB],
                                             const T* const (&row)[FB], int c, T* out) {
     constexpr int E = Piece<T>::E;
+    if constexpr (FB == 1) {
+        if (g.scale == 1.f) {  // one row as it is
+            typedef typename Piece<T>::type piece_t;
+            piece_t x = {0, 0, 0, 0};
+            if (first[0] != kNoId) x = *reinterpret_cast<const piece_t*>(row[0] + c);
+            if (g.far) __builtin_nontemporal_store(x, reinterpret_cast<piece_t*>(out + c));
+            else *reinterpret_cast<piece_t*>(out + c) = x;
+            return;
+        }
+    }
     float acc[E];
 #pragma unroll
     for (int t = 0; t < E; ++t) acc[t] = 0.f;
