@@ -23,6 +23,8 @@ Modules:
 * ``packed`` - softmax attention inside packed sequences, with the learned
   bias by buckets and its gradient.
 * ``norm`` - the norms, gate and scaled residual between two blocks.
+* ``ends`` - embedding and its gradient, dropout, softmax cross entropy over
+  classes, each result with a bound on fp32 arithmetic.
 """
 
-from . import attention, ecr, interleave, norm, packed, plan, reorder  # noqa: F401
+from . import attention, ecr, ends, interleave, norm, packed, plan, reorder  # noqa: F401

@@ -16,7 +16,16 @@
 // piece's dW and its part of dX, which is summed in fp32 over the pieces.  W and X
 // are laid out the other way round for these, so that one product serves for all.
 // Where a product has few blocks its sum is split over the grid and the parts are
-// added in order.  No atomics: results are the same run to run.
+// added in order.  No atomics on a sum: results are the same run to run.
+//
+// Bound by the matrix cores from some thousand tokens and classes on: 6,963 labelled of
+// 8,192 tokens x 2,048 over 128,000 classes in bf16 3.2 ms forward (1,120 TFLOP/s, of
+// 1,080 to 1,300 that a library's large products reach), 10.4 backward (a piece of 16,384
+// classes: dL 465 us, of which its stores take about 60, dX 410, dW 395); in fp32, 2,048 x
+// 512 over 32,000, 0.53 and 1.6 ms (127 TFLOP/s).  By the class weights for a few tokens
+// (16 x 2,048 over 128,000: 4.2 TB/s), by memory and the chain of small kernels for few
+// classes (200,000 nodes x 256, three in ten labelled, 172 classes: 160 us, where the
+// features, dL, its turn and the results are 0.3 GB).
 #include "gemm_nt.h"
 #include "lanes.h"
 #include "rows.h"
@@ -133,7 +142,7 @@ __global__ __launch_bounds__(kListThreads) void k_list_place(int64_t n, int64_t 
     }
 }
 
-// Rows without a label have no gradient: a wavefront looks at `span` labels (64, or fewer
+// Rows without a label have no gradient (140,000 rows of 256 bf16 14 us): a wavefront looks at `span` labels (64, or fewer
 // where rows are few), then groups of its lanes clear the rows without one, a 16-byte piece a lane (the last one ending with
 // the row).
 template <typename T>
@@ -251,6 +260,7 @@ __global__ __launch_bounds__(256) void k_turn(Turns both, int C) {
 
 // ----------------------------------------------------------------- products
 
+// kStats: the forward's statistics; kGrad: dL, both ways round; kStore: dX or dW.
 enum What { kStats, kGrad, kStore };
 
 struct LossArgs {

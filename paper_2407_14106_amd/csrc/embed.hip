@@ -11,6 +11,12 @@
 // grid, each leaves the sums of the (at most two) long runs that it holds, and one
 // workgroup a run and 64 columns adds those.  No atomics touch a sum: results are the
 // same run to run.
+//
+// 16,384 tokens x 2,048 of 128,000 rows in bf16: forward 29 us (4.6 TB/s), the gradient's
+// sort 46 and sums 143 (524 MB written, 4.1 TB/s).  A million nodes x 256, three fields of
+// 1,500 rows: forward 165 us (512 MB written, 1.5 GB gathered from L2), sort 80, sums 234
+// (1.5 GB of dout's rows gathered, 0.65 of them from memory), their merge 30.  100,000 x
+// 256 in fp32, nine fields of 173 rows: forward 41 us from LDS (70 from L2), backward 110.
 #include "prim.h"
 #include "rows.h"
 
@@ -18,15 +24,16 @@ using namespace gt;
 
 namespace {
 
-constexpr int kRun = 64;         // terms one group of lanes adds alone
+constexpr int kRun = 64;         // terms one group of lanes adds alone (128: 100,000 x 9 fields' sums 76 us, not 47)
 constexpr int kMergeCols = 64;   // columns of a workgroup that adds partial sums
 constexpr unsigned kMergeBlocks = 1024;
 constexpr unsigned kMostBlocks = 1 << 20;
 constexpr int64_t kL2Bytes = int64_t(32) << 20;  // of all XCDs
 
 constexpr int kFwdBlocks = 256 * 8;  // workgroups of 256 that the chip holds
-constexpr int kHeldBlocks = 256 * 2, kHeldReads = 64;
-constexpr int64_t kSmallPairs = 8192;  // one workgroup sorts
+constexpr int kHeldBlocks = 256 * 2;
+constexpr int64_t kHeldGathers = int64_t(128) << 20;  // bytes
+constexpr int64_t kSmallPairs = 8192;  // one workgroup sorts them in 36 us where the grid's six kernels take 46
 constexpr int kCounts = 1 + 256 + 256;  // long runs; chunks of a class, and how many of them have been placed
 
 // Lanes that share a row: a power of two from 8 to 256.
@@ -168,7 +175,8 @@ __global__ __launch_bounds__(256) void k_embed_fwd(FwdArgs g) {
 }
 
 // The same from LDS, for tables of few rows: a workgroup holds P pieces of every table
-// row and forms those pieces of many output rows.
+// row and forms those pieces of many output rows (100,000 x 256 fp32, nine fields of 173
+// rows: 41 us; gathered from L2 70).
 constexpr int kHeldBytes = 64 * 1024, kHeldThreads = 1024;  // two workgroups a CU
 template <typename T, int P>
 __global__ __launch_bounds__(kHeldThreads) void k_embed_held(FwdArgs g) {
@@ -225,9 +233,13 @@ __global__ __launch_bounds__(kHeldThreads) void k_embed_held(FwdArgs g) {
 template <typename T>
 void run_fwd(FwdArgs g, hipStream_t s) {
     const int64_t pieces = cdiv(g.D, Piece<T>::E);
-    // a table row's pieces in LDS where several fields read them often enough
-    for (int P = 16; P >= 8; P /= 2)
-        if (g.F > 1 && g.D >= Piece<T>::E && pieces >= P && g.R * P * 16 <= kHeldBytes && g.n * g.F >= kHeldReads * g.R) {
+    // Table rows' pieces in LDS where many gathers repay their copies to the workgroups:
+    // four fields or more (100,000 x 256 to 1,024, fields 1 / 2 / 4 / 9: 0.8 to 0.95, 0.8
+    // to 0.92, 1.1 to 1.46, 1.3 to 1.8 times as fast as from L2) of 128 MB together (10,000
+    // x 9 x 256 fp32, 92 MB: 0.9; 10,000 x 9 x 1,024 bf16, 184 MB: 1.2).
+    const bool many = g.F >= 4 && g.n * g.F * g.D * int64_t(sizeof(T)) >= kHeldGathers;
+    for (int P = 16; many && P >= 8; P /= 2)
+        if (pieces >= P && g.R * P * 16 <= kHeldBytes) {
             const int64_t slices = cdiv(pieces, P), blocks = cdiv(g.n, kHeldThreads / P), most = cdiv(kHeldBlocks, slices);
             const dim3 grid(unsigned(blocks < most ? blocks : most), unsigned(slices));
             if (P == 16) k_embed_held<T, 16><<<grid, kHeldThreads, 0, s>>>(g);
@@ -678,7 +690,8 @@ struct BwdWs {
 };
 
 // Rows that several fields read are taken together (kept in the caches) where they are
-// more than the L2 caches hold anyway.
+// more than the L2 caches hold anyway (nine fields of 100,000 x 256 fp32: sums 124 -> 49
+// us, three of a million x 256 bf16 314 -> 217, for 13 of ordering).
 bool ordered(int64_t n, int32_t F, int32_t D, int size) { return F > 1 && n * D * size > kL2Bytes; }
 
 // Passes over keys 0 to R, and the bits that each takes.
