@@ -38,6 +38,10 @@ constexpr int kListThreads = 1024, kListRounds = 8, kListRows = kListThreads * k
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // of dL, one way round: the last-level cache
 constexpr int64_t kMinPiece = 1024;                  // classes
 constexpr int kSplitBlocks = 256;                    // blocks that fill the chip
+constexpr int64_t kCutBlocks = int64_t(1) << 20;     // of a product whose blocks' shape is chosen
+constexpr int64_t kFewBlocks = 8;                    // of classes, that one lane joins
+constexpr double kParts = 2.4e5;                     // of the tokens' statistics, joined in a microsecond
+constexpr double kSlotBytes = 1.2e6;                 // of a split sum's parts, joined in a microsecond
 constexpr int64_t kLaunchBlocks = int64_t(1) << 22;  // of a launch (its threads are counted in 32 bits)
 constexpr int64_t kGatherClasses = 2048;             // above, X's listed rows are laid out once: every block of
                                                      // classes would read them through the list (3% of its time)
@@ -607,10 +611,52 @@ __global__ __launch_bounds__(WM * WN * 64) void k_product(LossArgs a) {
     }
 }
 
-// The parts of a token's statistics, joined: 64 lanes take a token's blocks in turn.
-__global__ __launch_bounds__(1024) void k_loss(int64_t blocks, const float2* part, int64_t ld, const float* hit,
-                                                const void* labels, bool wide, int64_t V, const int32_t* list,
-                                                const int32_t* count, int64_t n, float* loss, float* lse) {
+// A token's statistics, taken on by U more parts.
+template <int U>
+__device__ __forceinline__ void join(float& top, float& sum, const float2 (&p)[U]) {
+    float m = top;
+#pragma unroll
+    for (int k = 0; k < U; ++k) m = fmaxf(m, p[k].x);
+    const float ref = m == kNegInf ? 0.f : m;
+    sum *= ex2(top - ref);
+#pragma unroll
+    for (int k = 0; k < U; ++k) sum += p[k].y * ex2(p[k].x - ref);
+    top = m;
+}
+struct Joined {
+    const float* hit;
+    const void* labels;
+    bool wide;
+    int64_t V;
+    const int32_t* list;
+    float *loss, *lse;
+    __device__ __forceinline__ void put(int64_t t, float top, float sum) const {
+        const int64_t i = list ? int64_t(list[t]) : t;
+        const bool has = load_id(labels, wide, i, V) >= 0;
+        const float all = ((top == kNegInf ? 0.f : top) + log2f(sum)) * kLn2;
+        lse[i] = has ? all : 0.f;
+        loss[i] = has ? all - hit[t] : 0.f;
+    }
+};
+
+// The parts of a token's statistics, joined.  Of a few blocks of classes: a lane a token
+// (60,000 tokens of three blocks 5 us, by 64 lanes each 24).
+__global__ __launch_bounds__(256) void k_loss_few(int blocks, const float2* part, int64_t ld, const int32_t* count,
+                                                  int64_t n, Joined j) {
+    if (count) n = *count;
+    for (int64_t t = int64_t(blockIdx.x) * 256 + threadIdx.x; t < n; t += int64_t(gridDim.x) * 256) {
+        float top = kNegInf, sum = 0.f;
+        for (int b = 0; b < blocks; ++b) {
+            const float2 p[1] = {part[b * ld + t]};
+            join(top, sum, p);
+        }
+        j.put(t, top, sum);
+    }
+}
+
+// Of more: 64 lanes take a token's blocks in turn, four at a time.
+__global__ __launch_bounds__(1024) void k_loss(int64_t blocks, const float2* part, int64_t ld, const int32_t* count,
+                                                int64_t n, Joined j) {
     constexpr int P = 16, G = 1024 / P;  // tokens of a workgroup
     __shared__ float2 s[G][P + 1];
     const int x = threadIdx.x % P, y = threadIdx.x / P;
@@ -618,11 +664,12 @@ __global__ __launch_bounds__(1024) void k_loss(int64_t blocks, const float2* par
     for (int64_t t0 = int64_t(blockIdx.x) * P; t0 < n; t0 += int64_t(gridDim.x) * P) {
         float top = kNegInf, sum = 0.f;
         if (t0 + x < n)
-            for (int64_t b = y; b < blocks; b += G) {
-                const float2 p = part[b * ld + t0 + x];
-                const float m = fmaxf(top, p.x), ref = m == kNegInf ? 0.f : m;
-                sum = sum * ex2(top - ref) + p.y * ex2(p.x - ref);
-                top = m;
+            for (int64_t b = y; b < blocks; b += 4 * G) {
+                float2 p[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    p[k] = b + k * G < blocks ? part[(b + k * G) * ld + t0 + x] : make_float2(kNegInf, 0.f);
+                join(top, sum, p);
             }
         s[y][x] = make_float2(top, sum);
         __syncthreads();
@@ -639,14 +686,7 @@ __global__ __launch_bounds__(1024) void k_loss(int64_t blocks, const float2* par
             for (int k = 0; k < G / P; ++k) sum += p[k].y * ex2(p[k].x - ref);
 #pragma unroll
             for (int o = 1; o < P; o <<= 1) sum += __shfl_xor(sum, o, kWave);
-            const int64_t t = t0 + y;
-            if (x == 0 && t < n) {
-                const int64_t i = list ? int64_t(list[t]) : t;
-                const bool has = load_id(labels, wide, i, V) >= 0;
-                const float all = (ref + log2f(sum)) * kLn2;
-                lse[i] = has ? all : 0.f;
-                loss[i] = has ? all - hit[t] : 0.f;
-            }
+            if (x == 0 && t0 + y < n) j.put(t0 + y, top, sum);
         }
         __syncthreads();
     }
@@ -725,33 +765,81 @@ __global__ __launch_bounds__(256) void k_sum_slots(int splits, int64_t slot_rows
     }
 }
 
+// How a product is cut: rows of A and of B a block, and parts of the sum.
+struct Cut {
+    int m, n, splits;
+};
+
 template <typename T, int WHAT>
-gt_status product(const LossArgs& a, hipStream_t s) {
-#define GT_CALL(WM, WN, TM, TN)                                                                            \
-    do {                                                                                                   \
-        using G = GemmNT<T, WM, WN, TM, TN>;                                                               \
-        const unsigned blocks = xcd_grid(cdiv(a.M, G::BM) * cdiv(a.N, G::BN) * a.splits);                  \
-        k_product<T, WHAT, WM, WN, TM, TN><<<blocks, G::kThreads, 0, s>>>(a);                              \
+gt_status product(const LossArgs& a, const Cut& cut, hipStream_t s) {
+#define GT_CALL(WM, WN, TM, TN)                                                                       \
+    do {                                                                                              \
+        using G = GemmNT<T, WM, WN, TM, TN>;                                                          \
+        const unsigned blocks = xcd_grid(cdiv(a.M, G::BM) * cdiv(a.N, G::BN) * a.splits);             \
+        k_product<T, WHAT, WM, WN, TM, TN><<<blocks, G::kThreads, 0, s>>>(a);                         \
     } while (0)
-    if (a.M <= 64) {
-        if (a.N <= 64) GT_CALL(2, 2, 1, 1);
+    if (cut.m == 64) {
+        if (cut.n == 64) GT_CALL(2, 2, 1, 1);
         else GT_CALL(2, 4, 1, 2);
+    } else if (cut.m == 128) {
+        GT_CALL(2, 2, 2, 2);
     } else {
-        if (a.N <= 64) GT_CALL(4, 1, 2, 2);
+        if (cut.n == 64) GT_CALL(4, 1, 2, 2);
         else GT_CALL(2, 4, 4, 2);
     }
 #undef GT_CALL
     GT_LAUNCH_CHECK("class_loss product");
     return GT_OK;
 }
-// the block sides that product() takes
-int64_t block_rows(int64_t x) { return x <= 64 ? 64 : 256; }
 
-int splits_of(int64_t M, int64_t N, int64_t steps) {
-    const int64_t blocks = cdiv(M, block_rows(M)) * cdiv(N, block_rows(N));
-    int64_t s = kSplitBlocks / blocks;
-    if (s > steps / kSplitSteps) s = steps / kSplitSteps;
-    return int(s < 1 ? 1 : s);
+// A block shape's microseconds, as measured (products of 200 to 8,192 rows, classes and
+// features): what a block takes beside its steps, a step of a block that has its CU to
+// itself and of one that shares it with as many as fit, in bf16 and fp32.  The sums over
+// classes and tokens, whose operands come from beyond L2, take up to twice that a step;
+// a table of their own for them, or the time of a third of the rows beside that of all
+// (how many have a label is known on the device alone), chose no better (200 sizes).
+struct Side {
+    int m, n, fit;
+    float fixed, lone[2], full[2];
+};
+constexpr Side kSides[] = {
+    {256, 256, 1, 10.6f, {1.09f, 7.17f}, {1.62f, 7.34f}},
+    {128, 128, 2, 6.7f, {0.43f, 1.86f}, {0.44f, 1.88f}},
+    {256, 64, 2, 6.3f, {0.48f, 1.93f}, {0.52f, 1.94f}},
+    {64, 256, 2, 4.8f, {0.43f, 1.79f}, {0.57f, 1.89f}},
+    {64, 64, 5, 4.2f, {0.21f, 0.48f}, {0.17f, 0.52f}},
+};
+
+// The shape of the least time by that table, and for a product that may be split the
+// parts: as many as fill the chip once, or as many as its CUs hold.  A product of few large
+// blocks would leave CUs idle: fp32 logits of 3,447 x 214 classes x 924, 14 blocks of
+// 256 x 256, 218 us, in blocks of 64 x 64 19; 1,118 x 1,596 x 960 227 and 37; 8,192 x 8,192
+// x 1,024 970 and 1,119, in bf16 147 and 226.  Logits of up to 64 tokens are bound by the
+// class weights' loads, of which small blocks have more on the way (16 x 1,024 over
+// 128,000 classes in bf16 68 us, 256 x 64 77).
+Cut cut_of(What what, int64_t M, int64_t N, int64_t steps, int size) {
+    const bool split = what == kStore;
+    Cut best = {M <= 64 ? 64 : 256, N <= 64 ? 64 : 256, 1};
+    if (!split && N <= 64) return {64, 64, 1};
+    const int f = size == 2 ? 0 : 1;
+    double least = 1e30;
+    for (const Side& c : kSides) {
+        const int64_t blocks = cdiv(M, c.m) * cdiv(N, c.n);
+        if (blocks > kCutBlocks) continue;
+        for (int full = 0; full <= (split && c.fit > 1 ? 1 : 0); ++full) {
+            int64_t s = split ? kSplitBlocks * (full ? c.fit : 1) / blocks : 1;
+            if (s > steps / kSplitSteps) s = steps / kSplitSteps;
+            if (s < 1) s = 1;
+            const double k = double(cdiv(blocks * s, kSplitBlocks)), n = double(cdiv(steps, s));
+            const double lone = double(cdiv(int64_t(k), c.fit)) * (c.fixed + n * c.lone[f]);
+            const double shared = k * (c.fixed / c.fit + n * c.full[f]);
+            double time = lone > shared ? lone : shared;
+            if (what == kStats && M > c.m) time += 4 + double(cdiv(M, c.m)) * double(N) / kParts;  // the join
+            if (s > 1) time += 4 + double(s) * double(M) * double(N) * 4 / kSlotBytes;  // the parts' sum
+            if (time < least) least = time, best = {c.m, c.n, int(s)};
+        }
+    }
+    return best;
 }
 
 // ----------------------------------------------------------------- workspace
@@ -764,7 +852,7 @@ struct Shape {
     int64_t mp;    // tokens, whole blocks
     int64_t ldt;   // row stride of the arrays along the tokens
     int64_t piece, ldp;  // classes a piece, row stride of the arrays along them
-    int sx, sw;     // splits of dX and dW
+    Cut logits, grad, dx, dw;
     bool slots_x;
 };
 
@@ -784,9 +872,12 @@ Shape shape_of(int64_t n, int64_t V, int32_t D, gt_dtype dt, int64_t ldx, int64_
     if (piece < kMinPiece) piece = kMinPiece;
     h.piece = piece < all ? piece : all;
     h.ldp = h.piece + kOff;
-    h.sx = splits_of(D, n, h.piece * h.size / kStepBytes);
-    h.sw = splits_of(D, h.piece < V ? h.piece : V, h.mp * h.size / kStepBytes);
-    h.slots_x = h.sx > 1 || h.piece < V;
+    const int64_t classes = h.piece < V ? h.piece : V;
+    h.logits = cut_of(kStats, V, n, h.row / kStepBytes, h.size);
+    h.grad = cut_of(kGrad, classes, n, h.row / kStepBytes, h.size);
+    h.dx = cut_of(kStore, D, n, cdiv(classes * h.size, kStepBytes), h.size);
+    h.dw = cut_of(kStore, D, classes, h.mp * h.size / kStepBytes, h.size);
+    h.slots_x = h.dx.splits > 1 || h.piece < V;
     return h;
 }
 
@@ -813,7 +904,7 @@ FwdWs fwd_ws(Ws& w, const Shape& h) {
     f.l = list_ws(w, h.n);
     f.x = h.copy_x ? w.take<char>(size_t(h.n * h.row)) : nullptr;
     f.w = h.copy_w ? w.take<char>(size_t(h.V * h.row)) : nullptr;
-    f.part = w.take<float>(size_t(2 * h.mp * cdiv(h.V, block_rows(h.V))));
+    f.part = w.take<float>(size_t(2 * h.mp * cdiv(h.V, h.logits.m)));
     f.hit = w.take<float>(size_t(h.n));
     return f;
 }
@@ -832,8 +923,8 @@ BwdWs bwd_ws(Ws& w, const Shape& h) {
     b.wt = w.take<char>(size_t(h.D) * size_t(h.ldp * h.size));
     b.dl = w.take<char>(size_t(h.mp) * size_t(h.ldp * h.size));
     b.dlt = w.take<char>(size_t(h.piece) * size_t(h.ldt * h.size));
-    b.slots_x = h.slots_x ? w.take<float>(size_t(h.sx) * size_t(h.n) * h.D) : nullptr;
-    b.slots_w = h.sw > 1 ? w.take<float>(size_t(h.sw) * size_t(h.piece) * h.D) : nullptr;
+    b.slots_x = h.slots_x ? w.take<float>(size_t(h.dx.splits) * size_t(h.n) * h.D) : nullptr;
+    b.slots_w = h.dw.splits > 1 ? w.take<float>(size_t(h.dw.splits) * size_t(h.piece) * h.D) : nullptr;
     return b;
 }
 
@@ -882,7 +973,7 @@ gt_status run_fwd(const Shape& h, const void* X, const void* W, bool wide, const
     int64_t ldx = h.ldx, ldw = h.ldw;
     st = make_rows<T>(h, f.l, X, ldx, f.x, W, ldw, f.w, s);
     if (st != GT_OK) return st;
-    const int64_t side = block_rows(h.V), blocks = cdiv(h.V, side);
+    const int64_t side = h.logits.m, blocks = cdiv(h.V, side);
     LossArgs a = {};
     a.lda = ldw * h.size;
     a.B = static_cast<const char*>(X), a.ldb = ldx * h.size, a.N = h.n;
@@ -892,18 +983,22 @@ gt_status run_fwd(const Shape& h, const void* X, const void* W, bool wide, const
     if (blocks == 1) a.loss = loss, a.lse = lse;
     else a.part_ld = h.mp, a.hit = f.hit;
     // as many classes as a launch takes
-    const int64_t piece = side * (kLaunchBlocks / cdiv(h.n, block_rows(h.n)));
+    const int64_t piece = side * (kLaunchBlocks / cdiv(h.n, h.logits.n));
     for (int64_t v0 = 0; v0 < h.V; v0 += piece) {
         a.A = static_cast<const char*>(W) + v0 * a.lda;
         a.M = h.V - v0 < piece ? h.V - v0 : piece;
         a.v0 = v0;
         a.part = f.part + 2 * (v0 / side) * h.mp;
-        st = product<T, kStats>(a, s);
+        st = product<T, kStats>(a, h.logits, s);
         if (st != GT_OK) return st;
     }
     if (blocks == 1) return GT_OK;
-    k_loss<<<grid_for(h.n, 16, 1 << 16), 1024, 0, s>>>(blocks, reinterpret_cast<float2*>(f.part), h.mp, f.hit, labels, wide,
-                                                       h.V, f.l.list, f.l.count, h.n, loss, lse);
+    const Joined j = {f.hit, labels, wide, h.V, f.l.list, loss, lse};
+    const float2* part = reinterpret_cast<float2*>(f.part);
+    if (blocks <= kFewBlocks)
+        k_loss_few<<<grid_for(h.n, 256, 1 << 16), 256, 0, s>>>(int(blocks), part, h.mp, f.l.count, h.n, j);
+    else
+        k_loss<<<grid_for(h.n, 16, 1 << 16), 1024, 0, s>>>(blocks, part, h.mp, f.l.count, h.n, j);
     GT_LAUNCH_CHECK("class_loss join");
     return GT_OK;
 }
@@ -912,7 +1007,7 @@ template <typename T>
 gt_status sum_slots(int splits, int64_t slot_rows, int64_t R, const int32_t* count, int64_t C, const float* slots,
                     const int32_t* rows, T* out, const LossArgs& a, hipStream_t s) {
     const Factors f = {a.dloss, a.labels, a.wide, a.V, a.top};
-    if (splits > 1)
+    if (splits > 4)
         k_sum_slots<T, 8><<<grid_for(R * C, 128, 1 << 16), 256, 0, s>>>(splits, slot_rows, R, count, C, slots, rows, out, f);
     else
         k_sum_slots<T, 1><<<grid_for(R * C, 1024, 1 << 16), 256, 0, s>>>(splits, slot_rows, R, count, C, slots, rows, out, f);
@@ -970,36 +1065,36 @@ gt_status run_bwd(const Shape& h, const void* X, const void* W, bool wide, const
         a.v0 = v0, a.V = h.V, a.labels = labels, a.wide = wide, a.lse_in = lse, a.dloss = dloss;
         a.dl = dX ? b.dl : nullptr, a.dl_ld = h.ldp;
         a.dlt = dW ? b.dlt : nullptr, a.dlt_ld = h.ldt, a.top = b.l.top;
-        st = product<T, kGrad>(a, s);
+        st = product<T, kGrad>(a, h.grad, s);
         if (st != GT_OK) return st;
         if (dX) {
             LossArgs x = {};
             x.A = b.wt, x.lda = h.ldp * h.size, x.M = h.D;
             x.B = b.dl, x.ldb = h.ldp * h.size, x.N = h.n, x.n_count = b.l.count;
-            x.steps = cdiv(vn * h.size, kStepBytes), x.splits = h.sx;
+            x.steps = cdiv(vn * h.size, kStepBytes), x.splits = h.dx.splits;
             x.slots = b.slots_x, x.slot_rows = h.n, x.add = v0 > 0;
             x.out = dX, x.out_rows = b.l.list;
             x.dloss = dloss, x.labels = b.l.list ? nullptr : labels, x.wide = wide, x.V = h.V;
             last_x = x;
-            st = product<T, kStore>(x, s);
+            st = product<T, kStore>(x, h.dx, s);
             if (st != GT_OK) return st;
         }
         if (dW) {
             LossArgs x = {};
             x.A = b.xt, x.lda = h.ldt * h.size, x.M = h.D;
             x.B = b.dlt, x.ldb = h.ldt * h.size, x.N = vn;
-            x.steps = cdiv(h.n * h.size, kStepBytes), x.k_count = b.l.count, x.splits = h.sw;
+            x.steps = cdiv(h.n * h.size, kStepBytes), x.k_count = b.l.count, x.splits = h.dw.splits;
             x.slots = b.slots_w, x.slot_rows = h.piece;
             T* out = static_cast<T*>(dW) + v0 * h.D;
             x.out = out, x.top = b.l.top;
-            st = product<T, kStore>(x, s);
+            st = product<T, kStore>(x, h.dw, s);
             if (st == GT_OK && b.slots_w)
-                st = sum_slots<T>(h.sw, h.piece, vn, nullptr, h.D, b.slots_w, nullptr, out, x, s);
+                st = sum_slots<T>(h.dw.splits, h.piece, vn, nullptr, h.D, b.slots_w, nullptr, out, x, s);
             if (st != GT_OK) return st;
         }
     }
     if (dX && b.slots_x)
-        return sum_slots<T>(h.sx, h.n, h.n, b.l.count, h.D, b.slots_x, b.l.list, static_cast<T*>(dX), last_x, s);
+        return sum_slots<T>(h.dx.splits, h.n, h.n, b.l.count, h.D, b.slots_x, b.l.list, static_cast<T*>(dX), last_x, s);
     return GT_OK;
 }
 

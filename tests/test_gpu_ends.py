@@ -250,6 +250,16 @@ def test_loss(gt, n, V, D, dtype):
     loss_case(gt, n, V, D, dtype, itype="i32" if n % 2 else "i64", labelled=1.0 if n < 4 else 0.7, seed=n + V + D)
 
 
+# every shape of block that the logits, dX and dW are formed in at middle sizes, whole and in split sums, with rows
+# without a label: the device has fewer rows than the shapes were chosen for
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V,D", [(300, 3000, 1100), (1100, 3000, 1100), (2100, 1500, 130), (2100, 3000, 130),
+                                   (5000, 6000, 70), (9000, 300, 1100), (9000, 6000, 70), (9000, 1500, 130),
+                                   (20_000, 70, 600), (20_000, 300, 600), (20_000, 700, 300), (20_000, 3000, 70)])
+def test_loss_in_blocks_of_every_shape(gt, n, V, D, dtype):
+    loss_case(gt, n, V, D, dtype, labelled=0.7, seed=n + V + D)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_loss_one_side_at_a_time(gt, dtype):
     x, w, y, up = loss_inputs(300, 500, 128, dtype, "i64", 0.6, 3)
