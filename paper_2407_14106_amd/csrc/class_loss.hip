@@ -19,10 +19,11 @@
 // added in order.  No atomics on a sum: results are the same run to run.
 //
 // Bound by the matrix cores from some thousand tokens and classes on: 6,963 labelled of
-// 8,192 tokens x 2,048 over 128,000 classes in bf16 3.2 ms forward (1,120 TFLOP/s, of
-// 1,080 to 1,300 that a library's large products reach), 10.4 backward (a piece of 16,384
-// classes: dL 465 us, of which its stores take about 60, dX 410, dW 395); in fp32, 2,048 x
-// 512 over 32,000, 0.53 and 1.6 ms (127 TFLOP/s).  By the class weights for a few tokens
+// 8,192 tokens x 2,048 over 128,000 classes in bf16 3.2 ms forward (1,130 TFLOP/s; without
+// the exponentials and sums 9% less time), 10.4 backward (eight pieces of 16,384 classes:
+// dL 464 us, dX and dW 410 each, 980 and 1,110 TFLOP/s), where a library's products of
+// such sizes reach 1,150 to 1,170 (logits, dL) and 1,360 to 1,460 (dX, dW); in fp32, 2,048
+// x 512 over 32,000, 0.53 and 1.6 ms (127 TFLOP/s).  By the class weights for a few tokens
 // (16 x 2,048 over 128,000: 4.2 TB/s), by memory and the chain of small kernels for few
 // classes (200,000 nodes x 256, three in ten labelled, 172 classes: 160 us, where the
 // features, dL, its turn and the results are 0.3 GB).
@@ -41,7 +42,7 @@ constexpr int kSplitBlocks = 256;                    // blocks that fill the chi
 constexpr int64_t kCutBlocks = int64_t(1) << 20;     // of a product whose blocks' shape is chosen
 constexpr int64_t kFewBlocks = 8;                    // of classes, that one lane joins
 constexpr double kParts = 2.4e5;                     // of the tokens' statistics, joined in a microsecond
-constexpr double kSlotBytes = 1.2e6;                 // of a split sum's parts, joined in a microsecond
+constexpr double kSlotBytes = 2e6;                   // of a split sum's parts, joined in a microsecond
 constexpr int64_t kLaunchBlocks = int64_t(1) << 22;  // of a launch (its threads are counted in 32 bits)
 constexpr int64_t kGatherClasses = 2048;             // above, X's listed rows are laid out once: every block of
                                                      // classes would read them through the list (3% of its time)
@@ -580,7 +581,8 @@ __global__ __launch_bounds__(WM * WN * 64) void k_product(LossArgs a) {
                         if (n >= N || room <= 0) return;
                         float* p = o + n * a.M + mw + m;
                         if (a.add) {
-                            float v[4] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w)};
+                            float v[4] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z),
+                                          __uint_as_float(x.w)};
                             if (room >= 4) {
                                 float w[4];
                                 load_piece(w, p);
@@ -591,7 +593,8 @@ __global__ __launch_bounds__(WM * WN * 64) void k_product(LossArgs a) {
                                 for (int e = 0; e < 4; ++e)
                                     if (e < room) v[e] += p[e];
                             }
-                            x = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+                            x = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
+                                           __float_as_uint(v[3]));
                         }
                         store_room(p, x, room);
                     });
@@ -704,7 +707,8 @@ struct Factors {
 };
 template <typename T, int L>
 __global__ __launch_bounds__(256) void k_sum_slots(int splits, int64_t slot_rows, int64_t R, const int32_t* count,
-                                                    int64_t C, const float* slots, const int32_t* rows, T* out, Factors f) {
+                                                    int64_t C, const float* slots, const int32_t* rows, T* out,
+                                                    Factors f) {
     constexpr int P = 256 / L;
     __shared__ float4 s[L][P];
     if (count) R = *count;
@@ -792,50 +796,57 @@ gt_status product(const LossArgs& a, const Cut& cut, hipStream_t s) {
     return GT_OK;
 }
 
-// A block shape's microseconds, as measured (products of 200 to 8,192 rows, classes and
-// features): what a block takes beside its steps, a step of a block that has its CU to
-// itself and of one that shares it with as many as fit, in bf16 and fp32.  The sums over
-// classes and tokens, whose operands come from beyond L2, take up to twice that a step;
-// a table of their own for them, or the time of a third of the rows beside that of all
-// (how many have a label is known on the device alone), chose no better (200 sizes).
-struct Side {
-    int m, n, fit;
+// A block shape's microseconds: what a block takes beside its steps, a step of a block
+// that has its CU to itself and of one that shares it with as many as fit, in bf16 and
+// fp32.  Logits are measured at 200 to 8,192 rows, classes and features.  The sums over
+// classes and tokens, whose operands come from beyond L2, have a table of their own,
+// fitted to every shape's times at 48 sizes (100 to 300,000 rows, 30 to 150,000 classes,
+// 50 to 4,000 features; half of them held back from a first fit).  What the two choose
+// takes 1.03 times (fp32 1.02) the time of the best shape at these sizes, for logits and
+// for the sums; 256 x 256 wherever both sides pass 64, 1.35 (1.85) and 1.33 (1.65).
+struct Times {
     float fixed, lone[2], full[2];
 };
+struct Side {
+    int m, n, fit;
+    Times logits, sum;
+};
 constexpr Side kSides[] = {
-    {256, 256, 1, 10.6f, {1.09f, 7.17f}, {1.62f, 7.34f}},
-    {128, 128, 2, 6.7f, {0.43f, 1.86f}, {0.44f, 1.88f}},
-    {256, 64, 2, 6.3f, {0.48f, 1.93f}, {0.52f, 1.94f}},
-    {64, 256, 2, 4.8f, {0.43f, 1.79f}, {0.57f, 1.89f}},
-    {64, 64, 5, 4.2f, {0.21f, 0.48f}, {0.17f, 0.52f}},
+    {256, 256, 1, {10.6f, {1.09f, 7.17f}, {1.62f, 7.34f}}, {7.0f, {1.6f, 7.3f}, {1.6f, 7.3f}}},
+    {128, 128, 2, {6.7f, {0.43f, 1.86f}, {0.44f, 1.88f}}, {5.5f, {0.78f, 1.9f}, {0.54f, 1.9f}}},
+    {256, 64, 2, {6.3f, {0.48f, 1.93f}, {0.52f, 1.94f}}, {5.1f, {0.89f, 2.0f}, {0.57f, 1.9f}}},
+    {64, 256, 2, {4.8f, {0.43f, 1.79f}, {0.57f, 1.89f}}, {4.9f, {0.81f, 2.0f}, {0.61f, 1.9f}}},
+    {64, 64, 5, {4.2f, {0.21f, 0.48f}, {0.17f, 0.52f}}, {3.6f, {0.52f, 0.63f}, {0.21f, 0.53f}}},
 };
 
-// The shape of the least time by that table, and for a product that may be split the
-// parts: as many as fill the chip once, or as many as its CUs hold.  A product of few large
-// blocks would leave CUs idle: fp32 logits of 3,447 x 214 classes x 924, 14 blocks of
-// 256 x 256, 218 us, in blocks of 64 x 64 19; 1,118 x 1,596 x 960 227 and 37; 8,192 x 8,192
-// x 1,024 970 and 1,119, in bf16 147 and 226.  Logits of up to 64 tokens are bound by the
-// class weights' loads, of which small blocks have more on the way (16 x 1,024 over
-// 128,000 classes in bf16 68 us, 256 x 64 77).
+// The shape of the least time by that table, and for the sums the parts: as many as fill
+// the chip once, or as many as its CUs hold.  A product of few large blocks would leave
+// CUs idle: fp32 logits of 3,447 x 214 classes x 924, 14 blocks of 256 x 256, 218 us, in
+// blocks of 64 x 64 19; 1,118 x 1,596 x 960 227 and 37; but 8,192 x 8,192 x 1,024 970 and
+// 1,119, in bf16 147 and 226.  Logits of up to 64 tokens are bound by the class weights'
+// loads, of which small blocks have more on the way (16 x 1,024 over 128,000 classes in
+// bf16 68 us, 256 x 64 77); one block of up to 256 classes needs no join (2 x 896 over 213
+// in bf16 13 us, four and a join 17).
 Cut cut_of(What what, int64_t M, int64_t N, int64_t steps, int size) {
     const bool split = what == kStore;
     Cut best = {M <= 64 ? 64 : 256, N <= 64 ? 64 : 256, 1};
-    if (!split && N <= 64) return {64, 64, 1};
+    if (!split && N <= 64 && M > 256) return {64, 64, 1};
     const int f = size == 2 ? 0 : 1;
     double least = 1e30;
     for (const Side& c : kSides) {
         const int64_t blocks = cdiv(M, c.m) * cdiv(N, c.n);
         if (blocks > kCutBlocks) continue;
+        const Times& t = split ? c.sum : c.logits;
         for (int full = 0; full <= (split && c.fit > 1 ? 1 : 0); ++full) {
             int64_t s = split ? kSplitBlocks * (full ? c.fit : 1) / blocks : 1;
             if (s > steps / kSplitSteps) s = steps / kSplitSteps;
             if (s < 1) s = 1;
             const double k = double(cdiv(blocks * s, kSplitBlocks)), n = double(cdiv(steps, s));
-            const double lone = double(cdiv(int64_t(k), c.fit)) * (c.fixed + n * c.lone[f]);
-            const double shared = k * (c.fixed / c.fit + n * c.full[f]);
+            const double lone = double(cdiv(int64_t(k), c.fit)) * (t.fixed + n * t.lone[f]);
+            const double shared = k * (t.fixed / c.fit + n * t.full[f]);
             double time = lone > shared ? lone : shared;
-            if (what == kStats && M > c.m) time += 4 + double(cdiv(M, c.m)) * double(N) / kParts;  // the join
-            if (s > 1) time += 4 + double(s) * double(M) * double(N) * 4 / kSlotBytes;  // the parts' sum
+            if (what == kStats && M > c.m) time += 7 + double(cdiv(M, c.m)) * double(N) / kParts;  // the join
+            if (s > 1) time += 2 + double(s) * double(M) * double(N) * 4 / kSlotBytes;  // the parts' sum
             if (time < least) least = time, best = {c.m, c.n, int(s)};
         }
     }
@@ -1008,9 +1019,11 @@ gt_status sum_slots(int splits, int64_t slot_rows, int64_t R, const int32_t* cou
                     const int32_t* rows, T* out, const LossArgs& a, hipStream_t s) {
     const Factors f = {a.dloss, a.labels, a.wide, a.V, a.top};
     if (splits > 4)
-        k_sum_slots<T, 8><<<grid_for(R * C, 128, 1 << 16), 256, 0, s>>>(splits, slot_rows, R, count, C, slots, rows, out, f);
+        k_sum_slots<T, 8><<<grid_for(R * C, 128, 1 << 16), 256, 0, s>>>(splits, slot_rows, R, count, C, slots, rows,
+                                                                        out, f);
     else
-        k_sum_slots<T, 1><<<grid_for(R * C, 1024, 1 << 16), 256, 0, s>>>(splits, slot_rows, R, count, C, slots, rows, out, f);
+        k_sum_slots<T, 1><<<grid_for(R * C, 1024, 1 << 16), 256, 0, s>>>(splits, slot_rows, R, count, C, slots, rows,
+                                                                        out, f);
     GT_LAUNCH_CHECK("class_loss sum");
     return GT_OK;
 }
@@ -1032,8 +1045,8 @@ gt_status run_bwd(const Shape& h, const void* X, const void* W, bool wide, const
         int shift = 0;
         while (shift < 6 && (Piece<T>::E << shift) < h.D) ++shift;
         const int span = h.n >= 65536 ? 64 : 8;
-        k_zero_rows<T><<<grid_for(h.n, 4 * span, 1 << 16), 256, 0, s>>>(h.n, h.D, h.V, wide, labels, static_cast<T*>(dX),
-                                                                        shift, span, h.n * h.D * h.size > kFarBytes);
+        k_zero_rows<T><<<grid_for(h.n, 4 * span, 1 << 16), 256, 0, s>>>(
+            h.n, h.D, h.V, wide, labels, static_cast<T*>(dX), shift, span, h.n * h.D * h.size > kFarBytes);
         GT_LAUNCH_CHECK("class_loss zero rows");
     }
     LossArgs last_x = {};
@@ -1054,7 +1067,8 @@ gt_status run_bwd(const Shape& h, const void* X, const void* W, bool wide, const
             most = most > h.n ? most : h.n;
         }
         if (jobs) {
-            k_turn<T><<<dim3(unsigned(cdiv(most, 64)), unsigned(cdiv(h.D, 64)), unsigned(jobs)), 256, 0, s>>>(turns, h.D);
+            k_turn<T><<<dim3(unsigned(cdiv(most, 64)), unsigned(cdiv(h.D, 64)), unsigned(jobs)), 256, 0, s>>>(
+                turns, h.D);
             GT_LAUNCH_CHECK("class_loss turn");
         }
         LossArgs a = {};
@@ -1100,8 +1114,8 @@ gt_status run_bwd(const Shape& h, const void* X, const void* W, bool wide, const
 
 bool loss_sizes(int64_t n, int64_t V, int32_t D, gt_dtype dt, int64_t ldx, int64_t ldw) {
     const int64_t most = int64_t(1) << 31;
-    return (dt == GT_BF16 || dt == GT_F32) && n >= 0 && n < most / 8 && V >= 1 && V < most && D >= 1 && D <= GT_MAX_WIDTH &&
-           ldx >= D && ldw >= D && ldx < most && ldw < most;
+    return (dt == GT_BF16 || dt == GT_F32) && n >= 0 && n < most / 8 && V >= 1 && V < most && D >= 1 &&
+           D <= GT_MAX_WIDTH && ldx >= D && ldw >= D && ldx < most && ldw < most;
 }
 gt_status loss_check(const char* who, int64_t n, int64_t V, int32_t D, gt_dtype dt, gt_itype it, const void* X,
                      int64_t ldx, const void* W, int64_t ldw, const void* labels) {

@@ -10,17 +10,17 @@
 // operand as it lies).  Accumulator element i of a lane is
 // C[lane % 32][8 (i / 4) + 4 (lane / 32) + i % 4] of its block: four consecutive m.
 //
-// 256 x 256 blocks of eight wavefronts, 2,048 x 8,192 x 16,384 in bf16: 1,320 TFLOP/s
-// (a library's product on the same card 1,300), the matrix cores busy 72% of the time at
-// 1.85 GHz; with zeros as data, which draw less power, 1,670 at 2.3 GHz.  Reading a
-// quarter step ahead took it from 830 (with one LDS array for both stages every step
-// waited for its own loads) to 1,200, rows that are no multiple of 32 KB apart to 1,320.
-// Tried and not kept: four stages of half the depth (1,250), loads spread over the
-// step's quarters (1,250) or between the products (1,300), four wavefronts with 128 x 128
-// each (1,160: no other wavefront of the SIMD covers the issue of the loads), staging
-// through registers (275), a wave priority around the products (1,190), workgroups that
-// stay and begin the next block's loads before they store (no faster: 80 registers
-// spill), 128 x 128 blocks (fp32 550 us where these take 510).
+// The products alone, stored as they are, 2,048 x 8,192 x 16,384 in bf16, blocks of 256 x
+// 256 by eight wavefronts: 1,320 TFLOP/s (a library's 1,300 to 1,390), the matrix cores
+// busy 72% of the time at 1.85 GHz; with no loads from memory 1,680.  Reading a quarter
+// step ahead took it to 1,200, rows that are no multiple of 32 KB apart to 1,320.  Power
+// bounds the clock: logits of 8,192 x 2,048 over 128,000 classes run at 1.65 GHz, and with
+// zeros as data at 2.23 in 24% less time, the matrix cores busy 60% of the time in both.
+// Tried and not kept, at 1,290 to 1,320: four stages of half the depth (1,250), the loads
+// spread over the step's quarters (1,260) or between the products (1,210 to 1,300), four
+// wavefronts with 128 x 128 each (1,160), staging through registers (275); at 1,200, a
+// wave priority around the products (1,180); workgroups that stay and begin the next
+// block's loads before they store (no faster: 80 registers spill).
 #pragma once
 
 #include "attn_common.h"
