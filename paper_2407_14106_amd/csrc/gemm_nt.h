@@ -15,7 +15,7 @@
 // busy 72% of the time at 1.85 GHz; with no loads from memory 1,680.  Reading a quarter
 // step ahead took it to 1,200, rows that are no multiple of 32 KB apart to 1,320.  Power
 // bounds the clock: logits of 8,192 x 2,048 over 128,000 classes run at 1.65 GHz, and with
-// zeros as data at 2.23 in 24% less time, the matrix cores busy 60% of the time in both.
+// zeros as data at 2.24 in 23% less time, the matrix cores busy 60% of the time in both.
 // Tried and not kept, at 1,290 to 1,320: four stages of half the depth (1,250), the loads
 // spread over the step's quarters (1,260) or between the products (1,210 to 1,300), four
 // wavefronts with 128 x 128 each (1,160), staging through registers (275); at 1,200, a
