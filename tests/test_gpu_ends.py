@@ -121,6 +121,20 @@ def test_embed_sorts_at_their_limits(gt, pairs):
         embed_case(gt, pairs, 1, R, 3, "f32", "i64", seed=R % 1000)
 
 
+# ids of 9, 10, 19, 20 and 29 bits: one to four passes of the sort over the grid, into either array at its end
+@pytest.mark.parametrize("R,D", [(511, 40), (512, 40), (300_000, 24), (1 << 20, 8), ((1 << 28) + 3, 1)])
+def test_embed_sorts_of_every_number_of_passes(gt, R, D):
+    embed_case(gt, 9001, 2, R, D, "bf16", "i64" if R % 2 else "i32", seed=R % 1000)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_embed_widest_rows_and_many_fields(gt, dtype):
+    embed_case(gt, 150, 1, 20, gt.GT_MAX_WIDTH, dtype, "i32", seed=1)
+    embed_case(gt, 40, 2, 3, gt.GT_MAX_WIDTH - 1, dtype, "i64", seed=2)
+    embed_case(gt, 300, 100, 50, 36, dtype, "i32", seed=3)
+    embed_case(gt, 2, 5000, 9, 20, dtype, "i64", seed=4)
+
+
 def test_embed_same_id_in_two_fields(gt):
     ids = torch.randint(0, 7, (300, 1), generator=torch.Generator().manual_seed(0)).cuda().repeat(1, 3).contiguous()
     embed_case(gt, 300, 3, 7, 40, "bf16", "i64", ids=ids)
@@ -258,6 +272,12 @@ def test_loss(gt, n, V, D, dtype):
                                    (20_000, 70, 600), (20_000, 300, 600), (20_000, 700, 300), (20_000, 3000, 70)])
 def test_loss_in_blocks_of_every_shape(gt, n, V, D, dtype):
     loss_case(gt, n, V, D, dtype, labelled=0.7, seed=n + V + D)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_loss_widest_rows(gt, dtype):
+    loss_case(gt, 70, 130, gt.GT_MAX_WIDTH, dtype, seed=1)
+    loss_case(gt, 300, 20, gt.GT_MAX_WIDTH - 1, dtype, labelled=0.5, seed=2)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -404,6 +424,42 @@ def test_other_stream_and_captured_replays(gt):
         torch.cuda.synchronize()
         kept = [t.clone() for t in got]
         for a, b in zip(kept, step()):
+            assert torch.equal(a, b), k
+
+
+def test_two_captured_steps_that_share_memory(gt):
+    """Two graphs of one pool, replayed in turn with eager work between them, at sizes where every kernel of a large call
+    runs: the sort over the grid, long runs, rows taken together, listed and laid-out rows, joined statistics."""
+    cases = []
+    for k, (n, R, D, V) in enumerate([(20_000, 1000, 1024, 3000), (30_000, 700, 640, 300)]):
+        ids, w = skewed_ids(n, 2, R, k, "i32"), normal((V, D), 10 + k, "bf16", 0.05)
+        labels = torch.randint(-V // 4, V, (n,), device="cuda")
+        x, up = normal((n, D), 20 + k, "bf16"), torch.full((n,), 1.0 / n, device="cuda")
+        cases.append((x, w, labels, up, ids, torch.tensor([k, 3], device="cuda"), R))
+
+    def step(x, w, labels, up, ids, rng, R):
+        h = gt.dropout(x, 0.3, rng)
+        loss, lse = gt.class_loss_fwd(h, w, labels)
+        dh, dw = gt.class_loss_bwd(h, w, labels, lse, up)
+        return loss, lse, dh, dw, gt.embed_bwd(ids, dh, R)
+
+    for c in cases:
+        step(*c)
+    torch.cuda.synchronize()
+    graphs, got = [], []
+    for c in cases:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], pool=graphs[0].pool() if len(graphs) > 1 else None):
+            got.append(step(*c))
+    for k in (0, 1, 1, 0, 1, 0):
+        c = cases[k]
+        c[0].copy_(normal(c[0].shape, 100 + k, "bf16"))
+        c[2].copy_(c[2].roll(17))
+        c[5][1] += 10_000_000
+        graphs[k].replay()
+        torch.cuda.synchronize()
+        kept = [t.clone() for t in got[k]]
+        for a, b in zip(kept, step(*c)):
             assert torch.equal(a, b), k
 
 
