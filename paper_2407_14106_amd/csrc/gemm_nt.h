@@ -50,9 +50,16 @@ __device__ __forceinline__ void copy_to_lds(char* lds, const char* src) {
         reinterpret_cast<__attribute__((address_space(3))) uint32_t*>(reinterpret_cast<uintptr_t>(lds)), 16, 0, 0);
 }
 
+// Loads before it are issued before loads behind it; no instruction.
+__device__ __forceinline__ void issue_order() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // A barrier that waits for no more than is needed (and what orders the compiler's
 // memory accesses around it): all but the last LOADS loads of the wavefront have landed
-// and its reads of LDS are done.
+// and its reads of LDS are done.  That a stage has landed when LOADS are on their way
+// needs as many loads behind its own: issue_order() between one stage's and the next's.
 template <int LOADS>
 __device__ __forceinline__ void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS) : "memory");
@@ -115,9 +122,11 @@ struct GemmNT {
     __device__ __forceinline__ void start(char* lds0, char* lds1, int wave) {
         if (left & 1) {
             fetch(lds1, wave);
+            issue_order();
             if (left > 1) fetch(lds0, wave);
         } else if (left) {
             fetch(lds0, wave);
+            issue_order();
             fetch(lds1, wave);
         }
     }
