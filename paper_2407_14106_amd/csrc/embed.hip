@@ -276,6 +276,14 @@ struct SortArgs {
     uint32_t *key_out, *row_out, *count;
 };
 
+// Between two accesses by which lanes of one wavefront exchange values in LDS: the
+// hardware completes them in order, this keeps the compiler from moving or merging them
+// (no instruction).
+__device__ __forceinline__ void lanes_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Digits of a wavefront's rounds; behind the last pair 2^bits.
 template <bool FIRST>
 __device__ __forceinline__ void load_pairs(const SortArgs& a, int64_t base, uint32_t (&key)[kSortRounds],
@@ -350,7 +358,9 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort_place(SortArgs a) {
         // the wavefront's pairs of the digit so far: read by all of them, then moved on
         // by the first (a wavefront's LDS accesses complete in order)
         const uint32_t mine = uint32_t(__popcll(peers & lt)), before = valid ? s_n[w][d] : 0u;
+        lanes_fence();
         if (valid && mine == 0) s_n[w][d] = before + uint32_t(__popcll(peers));
+        lanes_fence();
         rank[r] = before + mine;
     }
     __syncthreads();
@@ -466,7 +476,9 @@ __global__ __launch_bounds__(kSmallThreads) void k_embed_sort_small(int pairs, i
             const int mine = __popcll(peers & lt);
             const uint32_t at = valid ? s_n[w][d] : 0u;
             if (valid) s_v[from ^ 1][at + mine] = v;
+            lanes_fence();
             if (valid && mine == 0) s_n[w][d] = at + uint32_t(__popcll(peers));
+            lanes_fence();
         }
         __syncthreads();
     }
