@@ -617,7 +617,9 @@ gt_status gt_dropout(int64_t n, gt_dtype dtype, double p, const uint64_t* rng, c
 /* Softmax cross entropy over V classes (node or graph classes, a vocabulary) from the
  * last features X [n, D] and the class weights W [V, D], without keeping the logits
  * s_iv = <X_i, W_v>:
- *   lse_i = log sum_v exp(s_iv),  loss_i = lse_i - s_i,y(i);
+ *   lse_i = log sum_v exp(s_iv),  loss_i = lse_i - s_i,y(i)
+ * (formed as (max_v s_iv - s_i,y) + log sum_v exp(s_iv - max): never below 0, and 0 to within the sum's rounding for a
+ * label that is sure, whatever the logits' size);
  * and for the gradient dloss_i of each row's loss (a mean over m rows: 1 / m)
  *   dL_iv = dloss_i (exp(s_iv - lse_i) - [v = y(i)]),
  *   dX_i = sum_v dL_iv W_v,  dW_v = sum_i dL_iv X_i.

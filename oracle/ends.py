@@ -96,16 +96,18 @@ def class_loss(x, w, labels, dloss, half):
     top = s.amax(1, keepdim=True)
     lse = top + torch.log(torch.exp(s - top).sum(1, keepdim=True))
     p = torch.exp(s - lse)
-    # of lse: the logits', the exponents' (a difference and a product rounded), exp's own, the sums' (a lane's 64
-    # classes, then the blocks' results, each scaled once), the logarithm's and the last sum's
+    # of lse: the logits', the exponents' (a difference, a rounded constant and a product), exp's own, the sums' (a
+    # lane's 64 classes, then the blocks' results, each scaled once), the logarithm's and the last sum's; the loss is
+    # the largest logit's distance from the label's and the same logarithm, and no rounding of lse's size
     blocks = -(-V // 64)
-    dlse = (1.01 * (p * ds).sum(1, keepdim=True) + 4 * U * (p * (top - s)).sum(1, keepdim=True)
-            + U * (90 + 3 * blocks) + 4 * U * (1 + lse.abs() + top.abs()))
+    dsum = (1.01 * (p * ds).sum(1, keepdim=True) + 4 * U * (p * (top - s)).sum(1, keepdim=True)
+            + U * (90 + 3 * blocks) + 4 * U * (lse - top))
+    dlse = dsum + 2 * U * lse.abs()
     at = torch.arange(n, device=x.device)
     sy, dsy = s[at, y], ds[at, y]
     loss = lse[:, 0] - sy
     out = {"lse": (torch.where(has, lse[:, 0], 0.0), dlse[:, 0]),
-           "loss": (torch.where(has, loss, 0.0), dlse[:, 0] + dsy + 2 * U * (loss.abs() + lse[:, 0].abs() + sy.abs()))}
+           "loss": (torch.where(has, loss, 0.0), dsum[:, 0] + dsy + 2 * U * (loss + top[:, 0] - sy))}
     up = torch.where(has, dloss.double(), 0.0)[:, None]
     dp = 1.01 * p * (ds + dlse + 4 * U * (s - lse).abs() + 4 * U)
     g = p

@@ -4,7 +4,7 @@ products of every number of steps, losses of rows that are sure of their label."
 import pytest
 import torch
 
-from tests.test_gpu_ends import loss_case, say
+from tests.test_gpu_ends import DT, loss_case, say
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +53,88 @@ def test_loss_products_of_every_number_of_steps(gt, dtype, steps):
     k = steps * (64 if dtype == "bf16" else 32)
     for n, V, D in ((33, 40, k), (300, 300, k), (1100, 3000, k), (40, k, 96), (k, 70, 64), (250, k, 700)):
         loss_case(gt, n, V, D, dtype, labelled=1.0 if n <= 256 else 0.7, seed=n + V + D)
+
+# one block of classes, a few blocks (joined by a lane a token) and many (by 64 lanes), listed rows and not
+SIZES = [(33, 200), (300, 200), (40, 1500), (700, 2000), (50, 5000), (400, 9000)]
+
+
+def whole_logits(n, V, D, dtype, scale, seed):
+    """Features and weights of small whole numbers and multiples of `scale`, a power of two: every logit is exact."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randint(-4, 5, (n, D), generator=g, device="cuda").to(DT[dtype]) * scale
+    w = torch.randint(-4, 5, (V, D), generator=g, device="cuda").to(DT[dtype])
+    return x, w, x.double() @ w.double().t().contiguous()
+
+
+def rest_of(s, y):
+    """The other classes' sum relative to class y's term, log of it and one, and sum of p |s - s_y|."""
+    d = s - s.gather(1, y[:, None])
+    other = torch.exp(d).scatter_(1, y[:, None], 0.0)
+    p = other / (1 + other.sum(1, keepdim=True))
+    return other.sum(1), torch.log1p(other.sum(1)), (p * d.abs()).sum(1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", SIZES)
+def test_loss_of_rows_sure_of_their_label(gt, dtype, n, V):
+    # the label's logit is the largest: the loss is what the other classes add to the sum, however large the logits are.
+    # Its error: the sum's additions (a lane's 64 classes, then the blocks: at most 90 + 3 V / 64), each off by at most
+    # half a step of the sum and by no more than what is added; the exponents' (a difference, a rounded constant, a
+    # product, exp's own); the logarithm's, a rounded constant and a product
+    say("loss sure", n, V, dtype)
+    for scale in (1.0 / 32, 0.25, 1.0, 8.0):
+        x, w, s = whole_logits(n, V, 64, dtype, scale, n + V)
+        y = s.argmax(1)
+        loss, lse = gt.class_loss_fwd(x, w, y)
+        other, want, size = rest_of(s, y)
+        u, adds = 2.0 ** -24, 90 + 3 * (V // 64)
+        bound = adds * torch.minimum(u * (1 + other), other) + 4 * u * size + 4 * u * want + 2 * u * want
+        assert (loss >= 0).all()
+        assert ((loss.double() - want).abs() <= bound).all(), (scale, float((loss.double() - want).abs().max()))
+        top = s.amax(1)
+        assert ((lse.double() - (top + want)).abs() <= bound + u * (top + want).abs()).all()
+        sure = other < 2.0 ** -30  # no sum in fp32 shows the others
+        assert scale < 1 or sure.any()
+        assert (lse[sure].double() == top[sure]).all() and (loss[sure].double() <= bound[sure]).all()
+        # and the label's own gradient is the others' sum, not the rounding of lse
+        up = torch.where(sure, 1.0, 0.0)
+        dx, dw = gt.class_loss_bwd(x, w, y, lse, up)
+        most = 2.0 ** -30 * 4 * max(1.0, 4 * scale) * 2
+        assert dx.abs().max() <= most and dw.abs().max() <= n * most
+        # at another label it is the distance too
+        z = (y + 1) % V
+        far = gt.class_loss_fwd(x, w, z)[0].double()
+        gap = (top - s.gather(1, z[:, None])[:, 0])
+        assert ((far - (gap + want)).abs() <= bound + 2 * u * (gap + want)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 60, 500])
+def test_loss_of_one_class_is_nothing(gt, dtype, n):
+    for scale in (0.125, 1.0, 16.0):
+        x, w, s = whole_logits(n, 1, 100, dtype, scale, n)
+        y = torch.zeros(n, dtype=torch.int64, device="cuda")
+        loss, lse = gt.class_loss_fwd(x, w, y)
+        assert not loss.any() and torch.equal(lse.double(), s[:, 0])
+        dx, dw = gt.class_loss_bwd(x, w, y, lse, torch.ones(n, device="cuda"))
+        assert not dx.any() and not dw.any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", SIZES)
+def test_loss_of_near_rows_is_not_negative(gt, dtype, n, V):
+    # weights of any value, the features along a class's own
+    g = torch.Generator(device="cuda").manual_seed(n)
+    w = torch.randn(V, 64, generator=g, device="cuda").to(DT[dtype])
+    y = torch.randint(0, V, (n,), generator=g, device="cuda")
+    for scale in (0.3, 1.0, 3.0, 15.0):
+        x = (w[y].float() * scale).to(DT[dtype])
+        s = x.double() @ w.double().t().contiguous()
+        at = s.argmax(1)
+        loss, lse = gt.class_loss_fwd(x, w, at)
+        other, want, _ = rest_of(s, at)
+        # two logits' errors (64 terms, in size up to 64 of the label's) move a term of the sum
+        ds = 2 * 64 * 2 * 2.0 ** -24 * (x.double().abs() @ w.double().abs().t().contiguous()).amax(1)
+        assert (loss >= 0).all()
+        assert (loss.double() <= (1.01 + 2 * ds) * want + (90 + 3 * (V // 64)) * torch.minimum(2.0 ** -24 * (1 + other),
+                                                                                             other)).all()
