@@ -634,6 +634,9 @@ gt_status gt_dropout(int64_t n, gt_dtype dtype, double p, const uint64_t* rng, c
  * exp(s - lse) - [v = y] is rounded to bf16 where it multiplies a row of W, and times
  * dloss_i / max |dloss| where it multiplies a row of X (a relative error of at most 2^-8
  * a term each; dloss and its maximum join in fp32 at the end), dX and dW once more.
+ * The backward's workspace: dL, both ways round, of 256 MB of classes at a time and all rows, or of 1,024 classes (or all
+ * of fewer) and rows of up to 1 GB; X and that piece of W the other way round; fp32 sums of dX if there is more than one
+ * piece of classes.
  * Sums in a fixed order.  The labelled rows' features, W and dloss are finite.
  * 0 <= n < 2^28, 1 <= V < 2^31, 1 <= D <= GT_MAX_WIDTH. */
 size_t gt_class_loss_fwd_workspace_size(int64_t n, int64_t V, int32_t D, gt_dtype dtype, int64_t ldx, int64_t ldw);

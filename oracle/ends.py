@@ -84,8 +84,9 @@ def dropout(x, add, keep, p, half):
 
 # --------------------------------------------------------------------------------------------------- loss
 
-def class_loss(x, w, labels, dloss, half):
-    """{name: (result, bound)} of loss, lse [n], dx [n, D], dw [V, D]."""
+def class_loss(x, w, labels, dloss, half, rows=None):
+    """{name: (result, bound)} of loss, lse [n], dx [n, D], dw [V, D].  rows: of dW's sum, where these are a part of them
+    (the parts' results and bounds then add up, but for the last rounding)."""
     x, w, n, (V, D) = x.double(), w.double(), x.shape[0], w.shape
     y = labels.long()
     has = (y >= 0) & (y < V)
@@ -120,5 +121,5 @@ def class_loss(x, w, labels, dloss, half):
     dx, dw = g @ w, g.t().contiguous() @ x
     out["dx"] = dx, dg @ w.abs() + 2 * U * V * (g.abs() @ w.abs()) + half * dx.abs()
     gt, dgt = g.abs().t().contiguous(), dg.t().contiguous()
-    out["dw"] = dw, dgt @ x.abs() + 2 * U * n * (gt @ x.abs()) + half * dw.abs()
+    out["dw"] = dw, dgt @ x.abs() + 2 * U * (rows or n) * (gt @ x.abs()) + half * dw.abs()
     return out

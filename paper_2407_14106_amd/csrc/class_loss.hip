@@ -11,10 +11,11 @@
 // Forward: the product s with the classes as its rows, so that a lane holds one
 // token and a block's classes: the block leaves (max, sum of exp) for each of its
 // tokens, and one small kernel joins the blocks of a token.
-// Backward: the classes go by in pieces.  A piece's s is formed again, dL is rounded
-// to the features' type and written both ways round, and two products give the
-// piece's dW and its part of dX, which is summed in fp32 over the pieces.  W and X
-// are laid out the other way round for these, so that one product serves for all.
+// Backward: the classes go by in pieces, and where there are many rows these too.  A
+// piece's s is formed again, dL is rounded to the features' type and written both ways
+// round, and two products give its part of dW and of dX, which are summed in fp32 over
+// the pieces.  W and X are laid out the other way round for these, so that one product
+// serves for all.
 // Where a product has few blocks its sum is split over the grid and the parts are
 // added in order.  No atomics on a sum: results are the same run to run.
 //
@@ -36,8 +37,11 @@ using namespace gt;
 namespace {
 
 constexpr int kListThreads = 1024, kListRounds = 8, kListRows = kListThreads * kListRounds;
-constexpr int64_t kPieceBytes = int64_t(256) << 20;  // of dL, one way round: the last-level cache
-constexpr int64_t kMinPiece = 1024;                  // classes
+constexpr int64_t kPieceBytes = int64_t(256) << 20;  // of a piece's dL, one way round: the last-level cache
+constexpr int64_t kMinPiece = 1024;                  // classes of a piece
+constexpr int64_t kPartBytes = int64_t(1) << 30;     // of dL, one way round, where a piece has that few classes or all:
+                                                     // more rows go by in parts (parts of 256 MB: 400,000 x 64 over
+                                                     // 1,000 11% slower, a million rows 14%; of 512 MB 7 and 7; 2% of 1 GB)
 constexpr int kSplitBlocks = 256;                    // blocks that fill the chip
 constexpr int64_t kCutBlocks = int64_t(1) << 20;     // of a product whose blocks' shape is chosen
 constexpr int64_t kFewBlocks = 8;                    // of classes, that one lane joins
@@ -49,6 +53,8 @@ constexpr int64_t kGatherClasses = 2048;             // above, X's listed rows a
 constexpr int64_t kListed = 256;                     // up to so many rows none is left out: they are one block
 constexpr int64_t kOff = 64;                         // elements behind a row of a turned or dL array: rows whose
                                                      // stride is a large power of two meet in few channels
+constexpr int64_t kOffBytes = 4096;                  // of such a row of dL along few classes, which has none (its stride
+                                                     // with or without: 0.99 to 1.01 times as fast)
 constexpr int kSplitSteps = 8;                       // of a split sum, at least
 
 constexpr float kNegInf = -__builtin_huge_valf();
@@ -272,9 +278,10 @@ struct LossArgs {
     const char *A, *B;      // rows of A: classes or features; rows of B: tokens or classes
     int64_t lda, ldb;       // bytes
     int64_t M, N;
-    const int32_t* n_count;  // N on the device, or null
+    const int32_t* n_count;  // rows of the list (on the device; N at most of them count), or null
     int64_t steps;           // of the sum
-    const int32_t* k_count;  // the sum's length in elements on the device, or null
+    const int32_t* k_count;  // the same of the sum's elements (steps at most), or null
+    int64_t first;           // of the list's rows, those before this part
     int splits;
     // kStats, kGrad: B's rows are tokens, listed if there is a list
     int64_t v0, V;  // class of A's first row; classes
@@ -433,6 +440,12 @@ __device__ __forceinline__ void store_room(O* p, const uint4& x, int64_t room) {
     }
 }
 
+// Of the list's rows those from `first` on, `most` at most.
+__device__ __forceinline__ int64_t left_of(const int32_t* count, int64_t first, int64_t most) {
+    const int64_t n = int64_t(*count) - first;
+    return n < 0 ? 0 : n < most ? n : most;
+}
+
 template <typename T, int WHAT, int WM, int WN, int TM, int TN>
 __global__ __launch_bounds__(WM * WN * 64) void k_product(LossArgs a) {
     using G = GemmNT<T, WM, WN, TM, TN>;
@@ -440,9 +453,10 @@ __global__ __launch_bounds__(WM * WN * 64) void k_product(LossArgs a) {
     __shared__ __attribute__((aligned(1024))) char s_0[G::kStage], s_1[G::kStage];
     static_assert(WM * WN * kRowsBytes <= G::kStage, "the wavefronts' rows fit");
     char* const s_out = s_0;
-    const int64_t N = a.n_count ? *a.n_count : a.N;
-    int64_t steps = a.steps;
-    if (a.k_count) steps = cdiv(int64_t(*a.k_count) * int64_t(sizeof(T)), kStepBytes);
+    const int64_t N = !a.n_count ? a.N : WHAT == kStats ? int64_t(*a.n_count) : left_of(a.n_count, a.first, a.N);
+    constexpr int64_t kStep = kStepBytes / int64_t(sizeof(T));  // elements
+    const int64_t steps =
+        WHAT == kStore && a.k_count ? cdiv(left_of(a.k_count, a.first, a.steps * kStep), kStep) : a.steps;
     const int64_t each = cdiv(steps, a.splits);
     const int lane = lane_id(), wave = uniform(threadIdx.x / kWave), wm = wave % WM, wn = wave / WM;
     Block blk;
@@ -879,10 +893,12 @@ struct Shape {
     bool whole_x, copy_x, copy_w;
     int64_t row;   // bytes of a padded row
     int64_t mp;    // tokens, whole blocks
-    int64_t ldt;   // row stride of the arrays along the tokens
+    int64_t ldt;   // row stride of X laid out along the tokens
     int64_t piece, ldp;  // classes a piece, row stride of the arrays along them
+    int64_t held;        // classes of a piece in whole blocks
+    int64_t rows, ldr;   // tokens a piece (whole blocks), row stride of dL along them
     Cut logits, grad, dx, dw;
-    bool slots_x;
+    bool slots_x, slots_w;
 };
 
 Shape shape_of(int64_t n, int64_t V, int32_t D, gt_dtype dt, int64_t ldx, int64_t ldw) {
@@ -896,17 +912,22 @@ Shape shape_of(int64_t n, int64_t V, int32_t D, gt_dtype dt, int64_t ldx, int64_
     h.copy_x = !h.whole_x || (n > kListed && V > kGatherClasses);
     h.mp = cdiv(n, 256) * 256;
     h.ldt = h.mp + kOff;
-    const int64_t all = cdiv(V, 256) * 256;
     int64_t piece = kPieceBytes / (h.mp * h.size) / 256 * 256;
     if (piece < kMinPiece) piece = kMinPiece;
-    h.piece = piece < all ? piece : all;
-    h.ldp = h.piece + kOff;
-    const int64_t classes = h.piece < V ? h.piece : V;
+    h.piece = piece < V ? piece : V;
+    // rows of a piece: all that fit, or equal parts
+    const int64_t most = kPartBytes / (cdiv(h.piece, 64) * 64 * h.size);
+    h.rows = h.mp <= most ? h.mp : cdiv(cdiv(n, cdiv(n, most)), 256) * 256;
+    h.ldr = h.rows + kOff;
+    const int64_t rows = h.rows < n ? h.rows : n;
     h.logits = cut_of(kStats, V, n, h.row / kStepBytes, h.size);
-    h.grad = cut_of(kGrad, classes, n, h.row / kStepBytes, h.size);
-    h.dx = cut_of(kStore, D, n, cdiv(classes * h.size, kStepBytes), h.size);
-    h.dw = cut_of(kStore, D, classes, h.mp * h.size / kStepBytes, h.size);
+    h.grad = cut_of(kGrad, h.piece, rows, h.row / kStepBytes, h.size);
+    h.dx = cut_of(kStore, D, rows, cdiv(h.piece * h.size, kStepBytes), h.size);
+    h.dw = cut_of(kStore, D, h.piece, h.rows * h.size / kStepBytes, h.size);
+    h.held = cdiv(h.piece, h.grad.m) * h.grad.m;
+    h.ldp = h.held + (h.held * h.size < kOffBytes ? 0 : kOff);
     h.slots_x = h.dx.splits > 1 || h.piece < V;
+    h.slots_w = h.dw.splits > 1 || h.rows < n;
     return h;
 }
 
@@ -950,10 +971,10 @@ BwdWs bwd_ws(Ws& w, const Shape& h) {
     b.w = h.copy_w ? w.take<char>(size_t(h.V * h.row)) : nullptr;
     b.xt = w.take<char>(size_t(h.D) * size_t(h.ldt * h.size));
     b.wt = w.take<char>(size_t(h.D) * size_t(h.ldp * h.size));
-    b.dl = w.take<char>(size_t(h.mp) * size_t(h.ldp * h.size));
-    b.dlt = w.take<char>(size_t(h.piece) * size_t(h.ldt * h.size));
+    b.dl = w.take<char>(size_t(h.rows) * size_t(h.ldp * h.size));
+    b.dlt = w.take<char>(size_t(h.held) * size_t(h.ldr * h.size));
     b.slots_x = h.slots_x ? w.take<float>(size_t(h.dx.splits) * size_t(h.n) * h.D) : nullptr;
-    b.slots_w = h.dw.splits > 1 ? w.take<float>(size_t(h.dw.splits) * size_t(h.piece) * h.D) : nullptr;
+    b.slots_w = h.slots_w ? w.take<float>(size_t(h.dw.splits) * size_t(h.piece) * h.D) : nullptr;
     return b;
 }
 
@@ -1089,39 +1110,47 @@ gt_status run_bwd(const Shape& h, const void* X, const void* W, bool wide, const
                 turns, h.D);
             GT_LAUNCH_CHECK("class_loss turn");
         }
-        LossArgs a = {};
-        a.A = w, a.lda = ldw * h.size, a.M = vn;
-        a.B = static_cast<const char*>(X), a.ldb = ldx * h.size, a.N = h.n;
-        a.n_count = b.l.count, a.list = b.l.list, a.gather = !h.copy_x;
-        a.steps = h.row / kStepBytes, a.splits = 1;
-        a.v0 = v0, a.V = h.V, a.labels = labels, a.wide = wide, a.lse_in = lse, a.dloss = dloss;
-        a.dl = dX ? b.dl : nullptr, a.dl_ld = h.ldp;
-        a.dlt = dW ? b.dlt : nullptr, a.dlt_ld = h.ldt, a.top = b.l.top;
-        st = product<T, kGrad>(a, h.grad, s);
-        if (st != GT_OK) return st;
-        if (dX) {
-            LossArgs x = {};
-            x.A = b.wt, x.lda = h.ldp * h.size, x.M = h.D;
-            x.B = b.dl, x.ldb = h.ldp * h.size, x.N = h.n, x.n_count = b.l.count;
-            x.steps = cdiv(vn * h.size, kStepBytes), x.splits = h.dx.splits;
-            x.slots = b.slots_x, x.slot_rows = h.n, x.add = v0 > 0;
-            x.out = dX, x.out_rows = b.l.list;
-            x.dloss = dloss, x.labels = b.l.list ? nullptr : labels, x.wide = wide, x.V = h.V;
-            last_x = x;
-            st = product<T, kStore>(x, h.dx, s);
+        LossArgs last_w = {};
+        T* out = dW ? static_cast<T*>(dW) + v0 * h.D : nullptr;
+        for (int64_t r0 = 0; r0 < h.n; r0 += h.rows) {
+            const int64_t rn = h.n - r0 < h.rows ? h.n - r0 : h.rows;
+            const int32_t* list = b.l.list ? b.l.list + r0 : nullptr;
+            LossArgs a = {};
+            a.A = w, a.lda = ldw * h.size, a.M = vn;
+            a.B = static_cast<const char*>(X) + (h.copy_x ? r0 * ldx * h.size : 0), a.ldb = ldx * h.size, a.N = rn;
+            a.n_count = b.l.count, a.first = r0, a.list = list, a.gather = !h.copy_x;
+            a.steps = h.row / kStepBytes, a.splits = 1;
+            a.v0 = v0, a.V = h.V, a.labels = labels, a.wide = wide, a.lse_in = lse, a.dloss = dloss;
+            a.dl = dX ? b.dl : nullptr, a.dl_ld = h.ldp;
+            a.dlt = dW ? b.dlt : nullptr, a.dlt_ld = h.ldr, a.top = b.l.top;
+            st = product<T, kGrad>(a, h.grad, s);
             if (st != GT_OK) return st;
+            if (dX) {
+                LossArgs x = {};
+                x.A = b.wt, x.lda = h.ldp * h.size, x.M = h.D;
+                x.B = b.dl, x.ldb = h.ldp * h.size, x.N = rn, x.n_count = b.l.count, x.first = r0;
+                x.steps = cdiv(vn * h.size, kStepBytes), x.splits = h.dx.splits;
+                x.slots = b.slots_x ? b.slots_x + r0 * h.D : nullptr, x.slot_rows = h.n, x.add = v0 > 0;
+                x.out = dX, x.out_rows = list;
+                x.dloss = dloss, x.labels = list ? nullptr : labels, x.wide = wide, x.V = h.V;
+                last_x = x;
+                st = product<T, kStore>(x, h.dx, s);
+                if (st != GT_OK) return st;
+            }
+            if (dW) {
+                LossArgs x = {};
+                x.A = b.xt + r0 * h.size, x.lda = h.ldt * h.size, x.M = h.D;
+                x.B = b.dlt, x.ldb = h.ldr * h.size, x.N = vn;
+                x.steps = cdiv(rn * h.size, kStepBytes), x.k_count = b.l.count, x.first = r0, x.splits = h.dw.splits;
+                x.slots = b.slots_w, x.slot_rows = h.piece, x.add = r0 > 0;
+                x.out = out, x.top = b.l.top;
+                last_w = x;
+                st = product<T, kStore>(x, h.dw, s);
+                if (st != GT_OK) return st;
+            }
         }
-        if (dW) {
-            LossArgs x = {};
-            x.A = b.xt, x.lda = h.ldt * h.size, x.M = h.D;
-            x.B = b.dlt, x.ldb = h.ldt * h.size, x.N = vn;
-            x.steps = cdiv(h.n * h.size, kStepBytes), x.k_count = b.l.count, x.splits = h.dw.splits;
-            x.slots = b.slots_w, x.slot_rows = h.piece;
-            T* out = static_cast<T*>(dW) + v0 * h.D;
-            x.out = out, x.top = b.l.top;
-            st = product<T, kStore>(x, h.dw, s);
-            if (st == GT_OK && b.slots_w)
-                st = sum_slots<T>(h.dw.splits, h.piece, vn, nullptr, h.D, b.slots_w, nullptr, out, x, s);
+        if (dW && b.slots_w) {
+            st = sum_slots<T>(h.dw.splits, h.piece, vn, nullptr, h.D, b.slots_w, nullptr, out, last_w, s);
             if (st != GT_OK) return st;
         }
     }

@@ -4,7 +4,8 @@ products of every number of steps, losses of rows that are sure of their label."
 import pytest
 import torch
 
-from tests.test_gpu_ends import DT, loss_case, say
+from oracle import ends as OE
+from tests.test_gpu_ends import DT, HALF, check, loss_case, loss_inputs, say
 
 pytestmark = pytest.mark.gpu
 
@@ -138,3 +139,32 @@ def test_loss_of_near_rows_is_not_negative(gt, dtype, n, V):
         assert (loss >= 0).all()
         assert (loss.double() <= (1.01 + 2 * ds) * want + (90 + 3 * (V // 64)) * torch.minimum(2.0 ** -24 * (1 + other),
                                                                                              other)).all()
+
+
+# dL of all rows over 1,024 classes, or over all of fewer, beyond 1 GB: the rows too go by in parts, of which the last
+# ones may hold no labelled row
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V,D,labelled", [(600_000, 1030, 40, 0.9), (560_000, 2100, 24, 1.0), (900_000, 640, 72, 0.2),
+                                            (1_100_000, 1000, 256, 0.95), (2_900_000, 200, 24, 0.5)])
+def test_loss_rows_in_parts(gt, n, V, D, labelled, dtype):
+    x, w, y, up = loss_inputs(n, V, D, dtype, "i64", labelled, n + V)
+    loss, lse = gt.class_loss_fwd(x, w, y)
+    dx, dw = gt.class_loss_bwd(x, w, y, lse, up)
+    say("loss parts", n, V, D, dtype, labelled)
+    # the oracle in parts of its own
+    at = torch.arange(0, n, 97, device="cuda")
+    ref = OE.class_loss(x[at], w, y[at], up[at], HALF[dtype])
+    for name, v in dict(loss=loss[at], lse=lse[at], dx=dx[at]).items():
+        check(name, v, ref[name])
+    r, b = torch.zeros(V, D, dtype=torch.float64, device="cuda"), torch.zeros(V, D, dtype=torch.float64, device="cuda")
+    for k in range(0, n, 35_000):
+        p, q = OE.class_loss(x[k:k + 35_000], w, y[k:k + 35_000], up[k:k + 35_000], HALF[dtype], rows=n)["dw"]
+        r += p
+        b += q - HALF[dtype] * p.abs()
+    check("dw", dw, (r, b + HALF[dtype] * r.abs()))
+    # and as a whole: two roundings of half a step; in fp32 additions to sums that grow as the root of their terms
+    assert (dw.double() - r).norm() <= (2.0 ** -7 if dtype == "bf16" else 2.0 ** -24 * (n ** 0.5 + 100)) * r.norm()
+    off = (y < 0) | (y >= V)
+    assert not loss[off].any() and not lse[off].any() and not dx[off].any()
+    only = gt.class_loss_bwd(x, w, y, lse, up, want_dx=False)[1]
+    assert torch.equal(only, dw) and torch.equal(gt.class_loss_bwd(x, w, y, lse, up, want_dw=False)[0], dx)
