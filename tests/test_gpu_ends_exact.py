@@ -168,3 +168,17 @@ def test_loss_rows_in_parts(gt, n, V, D, labelled, dtype):
     assert not loss[off].any() and not lse[off].any() and not dx[off].any()
     only = gt.class_loss_bwd(x, w, y, lse, up, want_dx=False)[1]
     assert torch.equal(only, dw) and torch.equal(gt.class_loss_bwd(x, w, y, lse, up, want_dw=False)[0], dx)
+
+
+@pytest.mark.parametrize("n,V,D", [(300, 257, 128), (2000, 172, 256), (1500, 5000, 192), (256, 40, 64)])
+def test_loss_gradients_in_norm(gt, n, V, D):
+    # bf16, upstream gradients over four powers of ten: two roundings, of dL and of the result.  A rounding is off by at
+    # most 2^-8 of its value and evenly spread below that: 2^-8 / sqrt 3 in the mean square, two of them 0.82 x 2^-8 where
+    # they are independent.  2^-8 leaves room for no third
+    x, w, y, up = loss_inputs(n, V, D, "bf16", "i64", 0.8, n + V)
+    up = up * 10.0 ** torch.linspace(-4, 0, n, device="cuda")[torch.randperm(n, device="cuda")]
+    lse = gt.class_loss_fwd(x, w, y)[1]
+    ref = OE.class_loss(x, w, y, up, HALF["bf16"])
+    for name, v in zip(("dx", "dw"), gt.class_loss_bwd(x, w, y, lse, up)):
+        check(name, v, ref[name])
+        assert (v.double() - ref[name][0]).norm() <= 2.0 ** -8 * ref[name][0].norm(), name
