@@ -115,6 +115,14 @@ __device__ __forceinline__ uint64_t lanemask_lt() {
     return l == 0 ? 0ull : (~0ull >> (64 - l));
 }
 
+// Between two accesses by which lanes of one wavefront exchange values in LDS: the
+// hardware completes them in order, this keeps the compiler from moving or merging them
+// (no instruction).
+__device__ __forceinline__ void lanes_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 template <typename T>
 __device__ __forceinline__ T uniform(T v) {
     return static_cast<T>(__builtin_amdgcn_readfirstlane(static_cast<int>(v)));

@@ -276,14 +276,6 @@ struct SortArgs {
     uint32_t *key_out, *row_out, *count;
 };
 
-// Between two accesses by which lanes of one wavefront exchange values in LDS: the
-// hardware completes them in order, this keeps the compiler from moving or merging them
-// (no instruction).
-__device__ __forceinline__ void lanes_fence() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // Digits of a wavefront's rounds; behind the last pair 2^bits.
 template <bool FIRST>
 __device__ __forceinline__ void load_pairs(const SortArgs& a, int64_t base, uint32_t (&key)[kSortRounds],

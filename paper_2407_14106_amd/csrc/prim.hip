@@ -377,7 +377,9 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_scatter(const K* keys, co
         // digit, then advanced by its first lane (a wavefront's LDS accesses
         // complete in order)
         const int before = valid ? s_wc[w][d] : 0;
+        lanes_fence();
         if (valid && rank == 0) s_wc[w][d] = before + __popcll(peers);
+        lanes_fence();
         rk[r] = before + rank;
     }
     __syncthreads();
