@@ -624,7 +624,8 @@ gt_status gt_dropout(int64_t n, gt_dtype dtype, double p, const uint64_t* rng, c
  *   dL_iv = dloss_i (exp(s_iv - lse_i) - [v = y(i)]),
  *   dX_i = sum_v dL_iv W_v,  dW_v = sum_i dL_iv X_i.
  * A row whose label lies outside [0, V) (an unlabelled node, a prompt's token) takes no
- * part: loss 0, lse 0, dX 0, and its products are not formed.
+ * part in any result: loss 0, lse 0, dX 0, whatever its features hold.  Of more than 256
+ * rows the others are listed first, and its products are not formed.
  *   labels [n] in itype; loss, lse, dloss fp32 [n]; dX [n, D], dW [V, D] contiguous in
  *     dtype, either may be NULL (not wanted);
  *   X and W start at multiples of 16 bytes (GT_ERR_UNSUPPORTED otherwise) with any

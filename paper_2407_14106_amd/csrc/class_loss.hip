@@ -20,11 +20,11 @@
 // added in order.  No atomics on a sum: results are the same run to run.
 //
 // Bound by the matrix cores from some thousand tokens and classes on: 6,963 labelled of
-// 8,192 tokens x 2,048 over 128,000 classes in bf16 3.2 ms forward (1,130 TFLOP/s; without
+// 8,192 tokens x 2,048 over 128,000 classes in bf16 3.3 ms forward (1,115 TFLOP/s; without
 // the exponentials and sums 9% less time), 10.4 backward (eight pieces of 16,384 classes:
-// dL 464 us, dX and dW 410 each, 980 and 1,110 TFLOP/s), where a library's products of
+// dL 466 us, dX 447, dW 374: 980, 1,020 and 1,220 TFLOP/s), where a library's products of
 // such sizes reach 1,150 to 1,170 (logits, dL) and 1,360 to 1,460 (dX, dW); in fp32, 2,048
-// x 512 over 32,000, 0.53 and 1.6 ms (127 TFLOP/s).  By the class weights for a few tokens
+// x 512 over 32,000, 0.52 and 1.6 ms (127 TFLOP/s).  By the class weights for a few tokens
 // (16 x 2,048 over 128,000: 4.2 TB/s), by memory and the chain of small kernels for few
 // classes (200,000 nodes x 256, three in ten labelled, 172 classes: 160 us, where the
 // features, dL, its turn and the results are 0.3 GB).
@@ -446,6 +446,9 @@ __device__ __forceinline__ int64_t left_of(const int32_t* count, int64_t first, 
     return n < 0 ? 0 : n < most ? n : most;
 }
 
+// The largest blocks hold 212 (bf16 logits) to 230 registers and none lies in scratch; the
+// logits' keep 236 scalars in vector lanes (dL 60, dX and dW 14 at most): the masks of the
+// labels' search and of the last block's classes, beside the exponentials.
 template <typename T, int WHAT, int WM, int WN, int TM, int TN>
 __global__ __launch_bounds__(WM * WN * 64) void k_product(LossArgs a) {
     using G = GemmNT<T, WM, WN, TM, TN>;
