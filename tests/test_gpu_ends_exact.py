@@ -176,7 +176,7 @@ def test_loss_gradients_in_norm(gt, n, V, D):
     # most 2^-8 of its value and evenly spread below that: 2^-8 / sqrt 3 in the mean square, two of them 0.82 x 2^-8 where
     # they are independent.  2^-8 leaves room for no third
     x, w, y, up = loss_inputs(n, V, D, "bf16", "i64", 0.8, n + V)
-    up = up * 10.0 ** torch.linspace(-4, 0, n, device="cuda")[torch.randperm(n, device="cuda")]
+    up = up * 10.0 ** torch.linspace(-4, 0, n)[torch.randperm(n, generator=torch.Generator().manual_seed(n))].cuda()
     lse = gt.class_loss_fwd(x, w, y)[1]
     ref = OE.class_loss(x, w, y, up, HALF["bf16"])
     for name, v in zip(("dx", "dw"), gt.class_loss_bwd(x, w, y, lse, up)):
